@@ -357,7 +357,7 @@ def _plan(s):
 
 def _attn(s, layer, q, o, lse):
     if own:
-        s["nsd"].nsd_chunk_attn(s["plan"], s["max_rows"], s["pool"], q, o, lse, s["kv_indptr"], s["kv_indices"], layer=layer,
+        s["nsd"].nsd_chunk_attn(s["plan"], s["max_rows"], s["pool"], q, o, lse, s["kv_indices"], layer=layer,
                                 softcap=s["case"]["softcap"], alibi_slopes=s["slopes"])
     else:
         for g in s["groups"]:

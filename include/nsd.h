@@ -472,6 +472,146 @@ nsd_status nsd_schedule_batch(const nsd_sched_params* prm, int32_t n, const uint
                               const int32_t* blocks, const int32_t* tokens, int32_t* batch_out,
                               int32_t* batch_size, double* batch_start);
 
+/*
+ * ---- Chunks of new tokens: prompts and single tokens over the same pool -----------------
+ * What a worker does beside verification: bring a prompt, or the next piece of one, into the
+ * pool, and decode single tokens.  Request r holds ctx_len[r] committed entries and brings
+ * n_r = q_indptr[r+1] - q_indptr[r] new tokens (any number from 0 up; no bound by max_gamma),
+ * at positions ctx_len[r] .. ctx_len[r] + n_r - 1.  Everything that depends on the lengths is
+ * worked out on the device, so a step needs no host copy of them and can be captured into a
+ * CUDA graph once and replayed with other lengths:
+ *   nsd_block_tables   tables, slots and positions from the lengths
+ *   nsd_chunk_plan     visible keys of every row and the split of the work, once per step
+ *   per layer: nsd_rope_append   rotate q and k, store k and v
+ *              nsd_chunk_attn    attention of the new rows over the request's entries
+ * max_rows is the host's upper bound of q_indptr[batch] (the rows the buffers hold); rows
+ * behind the last request's are left as they are.  Of nsd_config these calls use the pool's
+ * geometry and max_batch.  They run on the context's device, whichever device is current.
+ */
+
+/*
+ * Block tables and slot maps from request lengths ("KV cache organization", Section 3; the
+ * bank's free list, Appendix E.2).  Request r needs ceil((ctx_len+new_len)/block_size) blocks
+ * and holds n_held[r] of them (at least ceil(ctx_len/block_size); it may hold more, kept from
+ * rejected drafts); what it lacks comes from the free list, in request order.
+ *   ctx_len, new_len  int32 [batch]
+ *   held         int32 [batch][held_stride], in/out: the first n_held[r] entries of row r are
+ *                the request's blocks in position order; newly taken ones are written behind
+ *   n_held       int32 [batch];  n_held_new  int32 [batch]: blocks held after the call (must
+ *                not be n_held itself)
+ *   free_blocks  int32 [n_free]: ids of free blocks; entries below *free_begin (device int64,
+ *                null = 0) are taken already.  *free_end (device int64, not free_begin) = the
+ *                new first free entry
+ *   kv_indptr    int64 [batch+1], kv_indices int32 [max_entries]: the batch's tables end to
+ *                end; entries from kv_indptr[batch] on are left as they are
+ *   q_indptr     int64 [batch+1]: prefix sums of new_len
+ *   slot_map     nullable int64 [max_rows]: block * block_size + slot of every new row, -1 for
+ *                padding rows (behind q_indptr[batch])
+ *   positions    nullable int32 [max_rows]: ctx_len + i, 0 for padding rows
+ *   row_req      nullable int32 [max_rows]: owner of the row, -1 for padding rows
+ * Reported by nsd_get_status as DEVICE_FAULT (with the request's index): a negative length, a
+ * request that outgrows held_stride or holds too few blocks for ctx_len (it counts as one
+ * without entries and rows); a free list that runs out and block ids outside the pool (table
+ * entry -1 or as it is, slot -1); tables or rows beyond max_entries / max_rows (not written).
+ * Errors: INVALID_ARG, OUT_OF_RANGE (batch > max_batch, max_entries or max_rows beyond 2^31 - 1024),
+ * CAPACITY (batch > 16384).
+ */
+nsd_status nsd_block_tables(nsd_ctx* ctx, int32_t batch, const int32_t* ctx_len, const int32_t* new_len, int32_t* held,
+                            int64_t held_stride, const int32_t* n_held, const int32_t* free_blocks, int64_t n_free,
+                            const int64_t* free_begin, int64_t max_entries, int64_t max_rows, int64_t* kv_indptr,
+                            int32_t* kv_indices, int64_t* q_indptr, int64_t* slot_map, int32_t* positions,
+                            int32_t* row_req, int32_t* n_held_new, int64_t* free_end, void* stream);
+
+/*
+ * Rotary positions, and the append of the rotated keys and the values, for one layer.  Pair p
+ * of a head turns by the angle positions[axis(p)][row] * inv_freq[p]: (a, b) becomes
+ * (a cos - b sin, b cos + a sin).  Angles are formed and reduced in 64 bits, the rotation is
+ * computed in 32 and rounded once.
+ *   q            nullable [n_rows][num_q_heads][head_dim], rows q_stride elements apart
+ *   k, v         nullable (both or none) [n_rows][num_kv_heads][head_dim], rows k_stride /
+ *                v_stride apart (slices of one projection's output need no copy)
+ *   in_dtype     0 = fp32, 1 = bf16, of q, k and v
+ *   q_out        bf16, rows q_out_stride apart; may be q itself (bf16, same stride).  k and v
+ *                go to the pool
+ *   positions    int32 [n_axes][n_rows]
+ *   n_axes       1..4 (text: 1; images and video: time, height, width)
+ *   h_sections   HOST int32 [n_axes]: pairs of each axis; their sum S is the number of pairs
+ *                that turn, 1 <= S <= head_dim/2, dims from 2S on are copied
+ *   inv_freq     fp32 [S]
+ *   flags        NSD_ROPE_ADJACENT: pair p = dims (2p, 2p+1), else (p, p+S).  NSD_ROPE_CYCLED:
+ *                pair p belongs to axis p % n_axes while p / n_axes < h_sections[that axis],
+ *                else to axis 0 (such sections have to fit: INVALID_ARG), instead of the axes'
+ *                pairs one after another
+ *   slot_map     int64 [n_rows] as nsd_block_tables writes it.  A row with a negative slot is
+ *                padding: nothing of it is read or written.  A slot beyond the pool is reported
+ *                as DEVICE_FAULT (first bad index = row) and its k and v are dropped.  Null:
+ *                every row turns, allowed without k and v only
+ * Two rows must not share a slot.  Errors: INVALID_ARG (nulls, strides below a row, in-place
+ * with fp32), OUT_OF_RANGE (layer, n_axes, sections), UNSUPPORTED (dtype).
+ */
+enum { NSD_ROPE_ADJACENT = 1 << 0, NSD_ROPE_CYCLED = 1 << 1 };
+nsd_status nsd_rope_append(nsd_ctx* ctx, void* kv_pool, int32_t layer, int64_t n_rows, int32_t in_dtype, const void* q,
+                           int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                           void* q_out, int64_t q_out_stride, const int32_t* positions, int32_t n_axes,
+                           const int32_t* h_sections, const float* inv_freq, int32_t flags, const int64_t* slot_map,
+                           void* stream);
+
+/*
+ * The plan of a step's attention: which keys every row sees, and the split of the work over
+ * the SMs.  Row i of request r, at position t = ctx_len[r] + i, sees the keys [first, stop):
+ *   stop   t + 1; with prefix_len (nullable int32 [batch]) max(t + 1, min(prefix_len[r],
+ *          ctx_len[r] + n_r)): the first prefix_len tokens see one another both ways
+ *   first  0; with window > 0 at least t + 1 - window; with row_first (nullable int32
+ *          [max_rows]) at least row_first[row]: the position where the row's document starts,
+ *          in a request that packs several
+ * A row may see nothing (first >= stop): its output is 0 and its lse -inf.
+ * `plan` is the caller's device buffer (256-byte aligned, nsd_chunk_plan_bytes(ctx, max_rows)
+ * bytes, no initial contents).  It also holds the partial results of nsd_chunk_attn, so calls
+ * that use one plan must not overlap on the GPU; calls with plans of their own may.  A plan
+ * serves any number of layers whose tables have the same kv_indptr.  q_indptr and kv_indptr
+ * must not decrease, q_indptr stay within max_rows, ctx_len not be negative: else DEVICE_FAULT
+ * is reported and the plan is empty (nsd_chunk_attn then writes nothing).  Errors: INVALID_ARG, OUT_OF_RANGE, CAPACITY (plan_bytes too small),
+ * UNSUPPORTED (more than 128 q heads per kv head).  nsd_chunk_plan_bytes returns 0 for bad arguments.
+ */
+typedef struct {
+    int32_t window;               /* 0 = none */
+    int32_t reserved;             /* 0 */
+    const int32_t* prefix_len;    /* nullable */
+    const int32_t* row_first;     /* nullable */
+} nsd_chunk_masks;
+
+size_t nsd_chunk_plan_bytes(const nsd_ctx* ctx, int64_t max_rows);
+nsd_status nsd_chunk_plan(nsd_ctx* ctx, void* plan, size_t plan_bytes, int32_t batch, int64_t max_rows,
+                          const int64_t* q_indptr, const int32_t* ctx_len, const int64_t* kv_indptr,
+                          const nsd_chunk_masks* masks, void* stream);
+
+/*
+ * Attention of the planned rows for one layer: with s = scale * q.k,
+ *     s' = softcap * tanh(s / softcap)     (softcap > 0)
+ *     s'' = s' + alibi_slopes[h] * (key position - t)   (alibi_slopes given)
+ *     o = softmax(s'') V over the row's visible keys, q head h reading kv head
+ *         h / (num_q_heads/num_kv_heads)
+ * The new tokens' K and V must be in the pool already (nsd_rope_append, nsd_kv_prepare).
+ *   q          bf16 [max_rows][num_q_heads][head_dim], rows q_stride elements apart (a multiple
+ *              of 8; q 16-byte aligned)
+ *   o          bf16 [max_rows][num_q_heads][head_dim]; 16-byte aligned
+ *   lse        nullable fp32 [max_rows][num_q_heads]: natural logarithm of the sum of exp(s'')
+ *   kv_indices the tables, at the offsets the plan was given; a bad block id or a table that is
+ *              too short reads as zeros and is reported as DEVICE_FAULT.  Entries no row of the
+ *              request can see (before the window, after the last token) may hold anything
+ *   scale      0 = 1/sqrt(head_dim), else > 0;  softcap  0 = none, else > 0
+ *   alibi_slopes  nullable fp32 [num_q_heads]
+ * Slots that hold no visible token may hold anything, NaN included.  A non-finite value of a
+ * key that one row of a request sees may reach the request's other rows of the same chunk.
+ * max_rows and plan_bytes as given to nsd_chunk_plan; a buffer that holds no such plan
+ * is reported as DEVICE_FAULT and nothing is written.  bf16 inputs, fp32 accumulation and
+ * softmax statistics; the weights are rounded to bf16 for the product with V.
+ * Errors: INVALID_ARG, OUT_OF_RANGE, CAPACITY, UNSUPPORTED.
+ */
+nsd_status nsd_chunk_attn(nsd_ctx* ctx, void* plan, size_t plan_bytes, const void* kv_pool, const void* q,
+                          int64_t q_stride, void* o, float* lse, int64_t max_rows, const int32_t* kv_indices,
+                          int32_t layer, float scale, float softcap, const float* alibi_slopes, void* stream);
+
 /* Number of kernels this library has launched through `ctx` since creation. */
 int64_t nsd_launch_count(const nsd_ctx* ctx);
 

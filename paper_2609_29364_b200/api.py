@@ -62,6 +62,15 @@ class RoundArgs(ctypes.Structure):
     ]
 
 
+class ChunkMasks(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int32), ("reserved", ctypes.c_int32), ("prefix_len", _vp), ("row_first", _vp)]
+
+
+# nsd_rope_append flags (include/nsd.h)
+NSD_ROPE_ADJACENT = 1 << 0
+NSD_ROPE_CYCLED = 1 << 1
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -111,6 +120,16 @@ def load_library():
     lib.nsd_schedule_batch.restype = i32
     lib.nsd_schedule_batch.argtypes = [ctypes.POINTER(SchedParams), i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                        ctypes.POINTER(i32), ctypes.POINTER(ctypes.c_double)]
+    lib.nsd_block_tables.restype = i32
+    lib.nsd_block_tables.argtypes = [_vp, i32, _vp, _vp, _vp, i64, _vp, _vp, i64, _vp, i64, i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+    lib.nsd_rope_append.restype = i32
+    lib.nsd_rope_append.argtypes = [_vp, _vp, i32, i64, i32, _vp, i64, _vp, i64, _vp, i64, _vp, i64, _vp, i32, _vp, _vp, i32, _vp, _vp]
+    lib.nsd_chunk_plan_bytes.restype = sz
+    lib.nsd_chunk_plan_bytes.argtypes = [_vp, i64]
+    lib.nsd_chunk_plan.restype = i32
+    lib.nsd_chunk_plan.argtypes = [_vp, _vp, sz, i32, i64, _vp, _vp, _vp, ctypes.POINTER(ChunkMasks), _vp]
+    lib.nsd_chunk_attn.restype = i32
+    lib.nsd_chunk_attn.argtypes = [_vp, _vp, sz, _vp, _vp, i64, _vp, _vp, i64, _vp, i32, ctypes.c_float, ctypes.c_float, _vp, _vp]
     lib.nsd_launch_count.restype = i64
     lib.nsd_launch_count.argtypes = [_vp]
     lib.nsd_get_status.restype = i32
@@ -132,6 +151,33 @@ def _ptr(t) -> Optional[int]:
         assert t.flags["C_CONTIGUOUS"]
         return t.ctypes.data
     raise TypeError(type(t))
+
+
+def _tensor(t, dtype, what, shape=None):
+    """Address of a contiguous torch tensor of the given dtype name (and at least the given number of elements)."""
+    if t is None:
+        return None
+    if str(t.dtype) != dtype:
+        raise TypeError(f"{what}: {dtype} is wanted, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what} has to be contiguous")
+    if shape is not None and t.numel() < shape:
+        raise ValueError(f"{what}: {shape} elements are wanted, got {t.numel()}")
+    return t.data_ptr()
+
+
+def _rows(t, width, what):
+    """Address and row stride of a tensor [rows][...] whose rows are `width` contiguous elements."""
+    if t.dim() == 2:
+        inner = t.shape[1] == width and (t.stride(1) == 1 or width == 1)
+    else:
+        inner = t.dim() == 3 and t.shape[1] * t.shape[2] == width and t.stride(2) == 1 and t.stride(1) == t.shape[2]
+    if not inner:
+        raise ValueError(f"{what}: rows of {width} contiguous elements are wanted, got shape {tuple(t.shape)}, strides {t.stride()}")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else width)
+
+
+_DTYPE_CODE = {"torch.float32": 0, "torch.bfloat16": 1}
 
 
 def _stream_handle(stream) -> Optional[int]:
@@ -266,6 +312,92 @@ class VerifyContext:
                                                     _ptr(draft_tok), _ptr(u_acc), _ptr(u_smp), batch, gamma, vocab,
                                                     _ptr(gamma_r), _ptr(ctx_len), _ptr(acc_len), _ptr(out_tok),
                                                     _ptr(new_ctx_len), _stream_handle(stream)), "nsd_spec_accept_logits")
+
+    # -- chunks of new tokens
+    def _stream(self, stream):
+        """The given stream, or the current one of the context's device (whichever device is current)."""
+        if stream is None:
+            import torch
+
+            return torch.cuda.current_stream(self.device).cuda_stream
+        return stream if isinstance(stream, int) else stream.cuda_stream
+
+    def nsd_block_tables(self, ctx_len, new_len, held, n_held, free_blocks, free_begin, kv_indptr, kv_indices, q_indptr,
+                         slot_map, positions, row_req, n_held_new, free_end, stream=None):
+        """Sizes come from the tensors: batch = len(ctx_len), held [batch][stride], capacities of kv_indices and of the
+        row outputs (slot_map, positions, row_req: nullable, of one length)."""
+        batch = ctx_len.numel()
+        i32, i64 = "torch.int32", "torch.int64"
+        rows = [t.numel() for t in (slot_map, positions, row_req) if t is not None]
+        if rows and min(rows) != max(rows):
+            raise ValueError("slot_map, positions and row_req have to have one length")
+        if held.dim() != 2 or held.shape[0] < batch:
+            raise ValueError("held: [batch][stride] is wanted")
+        self._check(self.lib.nsd_block_tables(
+            self._h, batch, _tensor(ctx_len, i32, "ctx_len"), _tensor(new_len, i32, "new_len", batch), _tensor(held, i32, "held"),
+            held.shape[1], _tensor(n_held, i32, "n_held", batch), _tensor(free_blocks, i32, "free_blocks"), free_blocks.numel(),
+            _tensor(free_begin, i64, "free_begin", 1), kv_indices.numel(), rows[0] if rows else 0,
+            _tensor(kv_indptr, i64, "kv_indptr", batch + 1), _tensor(kv_indices, i32, "kv_indices"),
+            _tensor(q_indptr, i64, "q_indptr", batch + 1), _tensor(slot_map, i64, "slot_map"), _tensor(positions, i32, "positions"),
+            _tensor(row_req, i32, "row_req"), _tensor(n_held_new, i32, "n_held_new", batch), _tensor(free_end, i64, "free_end", 1),
+            self._stream(stream)), "nsd_block_tables")
+
+    def nsd_rope_append(self, kv_pool, layer, q, k, v, q_out, positions, sections, inv_freq, slot_map=None, adjacent=False,
+                        cycled=False, stream=None):
+        """q, k, v: [rows][heads * head_dim] or [rows][heads][head_dim], rows any stride apart (slices of one projection),
+        fp32 or bf16; q_out bf16; positions int32 [axes][rows]; sections: pairs of each axis."""
+        D, some = self.cfg.head_dim, q if q is not None else k
+        if some is None or (k is None) != (v is None):
+            raise ValueError("q, or k and v, or all three are wanted")
+        n, code = some.shape[0], _DTYPE_CODE.get(str(some.dtype), -1)
+        for t in (q, k, v):
+            if t is not None and (t.shape[0] != n or t.dtype != some.dtype):
+                raise ValueError("q, k and v have to have the same rows and dtype")
+        qp = kp = vp = op = None
+        qs = ks = vs = os_ = 0
+        if q is not None:
+            qp, qs = _rows(q, self.cfg.num_q_heads * D, "q")
+            if q_out is None or str(q_out.dtype) != "torch.bfloat16" or q_out.shape[0] < n:
+                raise TypeError("q_out: bfloat16 with q's rows is wanted")
+            op, os_ = _rows(q_out, self.cfg.num_q_heads * D, "q_out")
+        if k is not None:
+            kp, ks = _rows(k, self.cfg.num_kv_heads * D, "k")
+            vp, vs = _rows(v, self.cfg.num_kv_heads * D, "v")
+        if positions.dim() != 2 or positions.shape[1] != n:
+            raise ValueError("positions: [axes][rows] is wanted")
+        if len(sections) != positions.shape[0]:
+            raise ValueError("sections: one number per axis of positions is wanted")
+        self._check(self.lib.nsd_rope_append(
+            self._h, _ptr(kv_pool), layer, n, code, qp, qs, kp, ks, vp, vs, op, os_, _tensor(positions, "torch.int32", "positions"),
+            positions.shape[0], (ctypes.c_int32 * len(sections))(*sections),
+            _tensor(inv_freq, "torch.float32", "inv_freq", sum(sections)),
+            (NSD_ROPE_ADJACENT if adjacent else 0) | (NSD_ROPE_CYCLED if cycled else 0),
+            _tensor(slot_map, "torch.int64", "slot_map", n), self._stream(stream)), "nsd_rope_append")
+
+    def nsd_chunk_plan_bytes(self, max_rows: int) -> int:
+        return int(self.lib.nsd_chunk_plan_bytes(self._h, max_rows))
+
+    def nsd_chunk_plan(self, plan, max_rows, q_indptr, ctx_len, kv_indptr, window=0, prefix_len=None, row_first=None, stream=None):
+        batch = ctx_len.numel()
+        i32, i64 = "torch.int32", "torch.int64"
+        masks = ChunkMasks(window, 0, _tensor(prefix_len, i32, "prefix_len", batch), _tensor(row_first, i32, "row_first", max_rows))
+        self._check(self.lib.nsd_chunk_plan(
+            self._h, _ptr(plan), plan.numel() * plan.element_size(), batch, max_rows, _tensor(q_indptr, i64, "q_indptr", batch + 1),
+            _tensor(ctx_len, i32, "ctx_len"), _tensor(kv_indptr, i64, "kv_indptr", batch + 1), ctypes.byref(masks),
+            self._stream(stream)), "nsd_chunk_plan")
+
+    def nsd_chunk_attn(self, plan, max_rows, kv_pool, q, o, lse, kv_indices, layer=0, scale=0.0, softcap=0.0, alibi_slopes=None,
+                       stream=None):
+        """q: [rows][q heads * head_dim] or [rows][q heads][head_dim], rows any multiple of 8 elements apart; o contiguous."""
+        width = self.cfg.num_q_heads * self.cfg.head_dim
+        if str(q.dtype) != "torch.bfloat16" or q.shape[0] < max_rows:
+            raise TypeError("q: bfloat16 with max_rows rows is wanted")
+        qp, qs = _rows(q, width, "q")
+        self._check(self.lib.nsd_chunk_attn(
+            self._h, _ptr(plan), plan.numel() * plan.element_size(), _ptr(kv_pool), qp, qs,
+            _tensor(o, "torch.bfloat16", "o", max_rows * width), _tensor(lse, "torch.float32", "lse", max_rows * self.cfg.num_q_heads),
+            max_rows, _tensor(kv_indices, "torch.int32", "kv_indices"), layer, scale, softcap,
+            _tensor(alibi_slopes, "torch.float32", "alibi_slopes", self.cfg.num_q_heads), self._stream(stream)), "nsd_chunk_attn")
 
     @staticmethod
     def round_args(**kw) -> RoundArgs:

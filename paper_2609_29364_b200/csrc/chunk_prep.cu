@@ -1,0 +1,381 @@
+// What precedes the attention of a chunk of new tokens: block tables and slot maps from request
+// lengths, and rotary positions fused with the append into the paged pool (Section 3, "KV cache
+// organization"; the free list of a bank, Appendix E.2).
+#include <cuda_bf16.h>
+
+#include "nsd_internal.h"
+
+namespace nsd {
+namespace {
+
+// ---- block tables ---------------------------------------------------------------------------
+// Every output position is computed on its own: the flat entry e of kv_indices (or the flat row i
+// of slot_map) finds its request by a search in the prefix sums and reads the one block id it
+// needs.  So the work is spread evenly however unequal the requests are (one prompt of 100 000
+// tokens beside 500 single tokens), and no CTA waits for another: each forms the prefix sums of
+// the whole batch for itself in shared memory (12 bytes per request read from L2), which costs
+// less than a second launch.
+constexpr int kTablesThreads = 256;
+constexpr int kTablesPerCta = 1024;               // flat positions per CTA, four per thread
+constexpr int kBsT = 16;
+
+struct TablesArgs {
+    int32_t batch, num_blocks;
+    const int32_t *ctx_len, *new_len, *n_held, *free_blocks;
+    int32_t* held;
+    int64_t held_stride, n_free;
+    const int64_t* free_begin;
+    int64_t max_entries, max_rows;
+    int64_t *kv_indptr, *q_indptr, *free_end;
+    int32_t* kv_indices;
+    int64_t* slot_map;
+    int32_t *positions, *row_req, *n_held_new, *status;
+};
+
+struct Need {
+    int32_t entries, rows, take;
+    bool ok;
+};
+__device__ __forceinline__ Need need_of(const TablesArgs& a, int r) {
+    const int64_t c = a.ctx_len[r], n = a.new_len[r], h = a.n_held[r];
+    const int64_t need = (c + n + kBsT - 1) / kBsT;
+    const bool ok = c >= 0 && n >= 0 && c + n <= 0x7fffffffll - kBsT && need <= a.held_stride && h >= (c + kBsT - 1) / kBsT && h <= a.held_stride;
+    return ok ? Need{(int32_t)need, (int32_t)n, (int32_t)(need > h ? need - h : 0), true} : Need{0, 0, 0, false};
+}
+__device__ __forceinline__ void report(int32_t* status, int32_t bit, int r) {
+    atomicOr(status, bit);
+    atomicCAS(status + 1, 0, r + 1);
+}
+// The request that owns flat position x: the last r with p[r] <= x (requests without positions are skipped).
+__device__ __forceinline__ int owner_of(const int32_t* p, int batch, int32_t x) {
+    int lo = 0, hi = batch;                        // p[lo] <= x < p[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (p[mid] <= x) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+__global__ void __launch_bounds__(kTablesThreads)
+block_tables_kernel(const TablesArgs a) {
+    extern __shared__ int32_t pre[];               // three prefix sums of batch + 1 entries: table entries, rows, blocks taken
+    __shared__ int64_t warp_sum[3][kTablesThreads / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int32_t *kvp = pre, *qp = pre + a.batch + 1, *tp = qp + a.batch + 1;
+    const int per = (a.batch + kTablesThreads - 1) / kTablesThreads;
+    const int r0 = min(tid * per, a.batch), r1 = min(r0 + per, a.batch);
+    int64_t mine[3] = {0, 0, 0};
+    for (int r = r0; r < r1; ++r) {
+        const Need d = need_of(a, r);
+        mine[0] += d.entries, mine[1] += d.rows, mine[2] += d.take;
+        if (!d.ok && blockIdx.x == 0) report(a.status, STATUS_BAD_TOKEN, r);
+    }
+    int64_t inc[3] = {mine[0], mine[1], mine[2]};
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            const int64_t v = __shfl_up_sync(0xffffffffu, inc[k], s);
+            if (lane >= s) inc[k] += v;
+        }
+    if (lane == 31)
+        for (int k = 0; k < 3; ++k) warp_sum[k][warp] = inc[k];
+    __syncthreads();
+    int64_t at[3], total[3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        int64_t before = 0, all = 0;
+        for (int w = 0; w < kTablesThreads / 32; ++w) {
+            if (w < warp) before += warp_sum[k][w];
+            all += warp_sum[k][w];
+        }
+        at[k] = before + inc[k] - mine[k];
+        total[k] = all;
+    }
+    // positions past 2^31 are past every buffer: the sums may saturate there
+    auto sat = [](int64_t v) { return (int32_t)(v > 0x7fffffffll ? 0x7fffffffll : v); };
+    for (int r = r0; r < r1; ++r) {
+        const Need d = need_of(a, r);
+        kvp[r] = sat(at[0]), qp[r] = sat(at[1]), tp[r] = sat(at[2]);
+        at[0] += d.entries, at[1] += d.rows, at[2] += d.take;
+    }
+    if (tid == 0) kvp[a.batch] = sat(total[0]), qp[a.batch] = sat(total[1]), tp[a.batch] = sat(total[2]);
+    __syncthreads();
+
+    int64_t fb = a.free_begin ? *a.free_begin : 0;
+    if (fb < 0 || fb > a.n_free) {
+        if (blockIdx.x == 0 && tid == 0) report(a.status, STATUS_BAD_BLOCK, -1);
+        fb = a.n_free;
+    }
+    // block k of request r's table; a block that is missing or outside the pool is the request's fault to report
+    auto block_of = [&](int r, int k, int held) -> int32_t {
+        if (k < held) return a.held[(int64_t)r * a.held_stride + k];
+        const int64_t f = fb + tp[r] + (k - held);
+        return f < a.n_free ? a.free_blocks[f] : -1;
+    };
+    const int64_t x0 = (int64_t)blockIdx.x * kTablesPerCta;
+#pragma unroll
+    for (int u = 0; u < kTablesPerCta / kTablesThreads; ++u) {
+        const int64_t e = x0 + u * kTablesThreads + tid;
+        if (e < kvp[a.batch] && e < a.max_entries) {
+            const int r = owner_of(kvp, a.batch, (int32_t)e), k = (int)e - kvp[r], held = a.n_held[r];
+            const int32_t id = block_of(r, k, held);
+            a.kv_indices[e] = id;
+            if ((uint32_t)id >= (uint32_t)a.num_blocks) report(a.status, STATUS_BAD_BLOCK, r);
+            else if (k >= held) a.held[(int64_t)r * a.held_stride + k] = id;
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kTablesPerCta / kTablesThreads; ++u) {
+        const int64_t i = x0 + u * kTablesThreads + tid;
+        if (i >= a.max_rows) break;
+        int64_t slot = -1;
+        int32_t pos = 0, req = -1;
+        if (i < qp[a.batch]) {
+            req = owner_of(qp, a.batch, (int32_t)i);
+            pos = a.ctx_len[req] + (int32_t)i - qp[req];
+            const int32_t id = block_of(req, pos / kBsT, a.n_held[req]);
+            if ((uint32_t)id < (uint32_t)a.num_blocks) slot = (int64_t)id * kBsT + pos % kBsT;
+        }
+        if (a.slot_map) a.slot_map[i] = slot;
+        if (a.positions) a.positions[i] = pos;
+        if (a.row_req) a.row_req[i] = req;
+    }
+    // the per-request outputs, shared out over the CTAs
+    for (int r = blockIdx.x * kTablesThreads + tid; r <= a.batch; r += gridDim.x * kTablesThreads) {
+        a.kv_indptr[r] = kvp[r];
+        a.q_indptr[r] = qp[r];
+        if (r == a.batch) {
+            const int64_t end = fb + tp[r];
+            *a.free_end = end < a.n_free ? end : a.n_free;
+            if (kvp[r] > a.max_entries || (qp[r] > a.max_rows && (a.slot_map || a.positions || a.row_req))) report(a.status, STATUS_BAD_TOKEN, -1);
+        } else {
+            const int64_t left = a.n_free - fb - tp[r], take = tp[r + 1] - tp[r];
+            a.n_held_new[r] = a.n_held[r] + (int32_t)(left < 0 ? 0 : (left < take ? left : take));
+        }
+    }
+}
+
+// ---- rotary positions + append ----------------------------------------------------------------
+// (a, b) -> (a cos - b sin, b cos + a sin) for the pairs of every q and k head of a row, q to its
+// buffer, k and v to the pool: each value is read once and written once, so the bound is HBM.
+// The angle is position * frequency with a position up to millions and a result needed modulo
+// 2 pi: it is formed in turns and reduced in 64 bits, then sincospi in 32.
+// A warp owns a row (or a share of its heads, when there are few rows: the sines are then formed
+// again, which costs less than idle SMs).  A lane keeps 16 dims of a head -- two 16-byte pieces,
+// both members of eight pairs -- and meets the same eight pairs in every head it visits, so
+// sines and cosines stay in registers: they are formed once per row, two pairs per lane, and
+// handed round by shuffles.
+struct RopeArgs {
+    int64_t n_rows;
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride, qo_stride;
+    uint16_t* q_out;
+    uint16_t* slab;
+    const int32_t* positions;
+    const float* inv_freq;
+    const int64_t* slot_map;
+    int32_t* status;
+    int32_t Hq, Hkv, num_blocks, pairs, adjacent, parts;
+    int32_t hq0;                                   // first head of the walk: 0, or Hq when there is no q
+    int32_t heads;                                 // one past its last: Hq + 2 Hkv, or Hq without k and v
+    uint8_t axis[64];
+};
+
+template <typename T> struct In;
+template <> struct In<float> {
+    static __device__ __forceinline__ void load8(const float* p, float* x) {
+        const float4 u = __ldg(reinterpret_cast<const float4*>(p)), v = __ldg(reinterpret_cast<const float4*>(p) + 1);
+        x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
+    }
+    static __device__ __forceinline__ float load1(const float* p) { return *p; }
+};
+template <> struct In<__nv_bfloat16> {
+    static __device__ __forceinline__ void load8(const __nv_bfloat16* p, float* x) {
+        const uint4 u = *reinterpret_cast<const uint4*>(p);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+    static __device__ __forceinline__ float load1(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+};
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ void store8(uint16_t* p, const float* x) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
+}
+
+// VEC: every row of q, k, v and q_out starts on 16 bytes and the members of a pair sit at the same place of two pieces
+// (adjacent pairs, or pairs a multiple of eight apart): 16-byte loads and stores.  Otherwise pair by pair.
+template <typename T, int D, bool VEC>
+__global__ void __launch_bounds__(256)
+rope_append_kernel(const __grid_constant__ RopeArgs a) {
+    constexpr int kUnits = D / 16;                 // a head in units of two 16-byte pieces
+    constexpr int kHeads = 32 / kUnits;            // heads a warp has under way
+    const int lane = threadIdx.x & 31;
+    const int64_t w = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
+    const int64_t row = w / a.parts;
+    const int part = (int)(w - row * a.parts);
+    if (row >= a.n_rows) return;
+    const int64_t slot = a.slot_map ? a.slot_map[row] : 0;
+    if (slot < 0) return;                          // a padding row
+    const bool stored = slot < (int64_t)a.num_blocks * kBsT;
+    if (!stored && lane == 0 && part == 0) report(a.status, STATUS_BAD_BLOCK, (int)row);
+    // two pairs per lane (one where a head has 32): 2 lane, 2 lane + 1
+    constexpr int kMine = D / 64;
+    float cs[kMine], sn[kMine];
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        const int p = lane * kMine + i;
+        cs[i] = 1.f, sn[i] = 0.f;
+        if (p < a.pairs) {
+            const double turns = (double)a.positions[(int64_t)a.axis[p] * a.n_rows + row] * ((double)a.inv_freq[p] * 0.15915494309189533577);
+            sincospif((float)(2.0 * (turns - rint(turns))), &sn[i], &cs[i]);
+        }
+    }
+    const int Hk0 = a.Hq, Hv0 = a.Hq + a.Hkv;
+    const int per = (a.heads - a.hq0 + a.parts - 1) / a.parts;
+    const int h_end = min(a.hq0 + (part + 1) * per, a.heads);
+    auto source = [&](int h) -> const T* {
+        if (h < Hk0) return static_cast<const T*>(a.q) + row * a.q_stride + h * D;
+        if (h < Hv0) return static_cast<const T*>(a.k) + row * a.k_stride + (h - Hk0) * D;
+        return static_cast<const T*>(a.v) + row * a.v_stride + (h - Hv0) * D;
+    };
+    auto target = [&](int h) -> uint16_t* {
+        if (h < Hk0) return a.q_out + row * a.qo_stride + h * D;
+        if (!stored) return nullptr;
+        // tile of (block, K|V, kv head): block * 2 Hkv + K|V * Hkv + head = block * 2 Hkv + (h - Hq)
+        return a.slab + (((slot / kBsT) * 2 * a.Hkv + (h - Hk0)) * kBsT + slot % kBsT) * D;
+    };
+    if constexpr (VEC) {
+        const int u = lane % kUnits;
+        float c[8], s[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int p = u * 8 + i;               // sits with lane p / kMine
+            c[i] = __shfl_sync(0xffffffffu, cs[i % kMine], p / kMine);
+            s[i] = __shfl_sync(0xffffffffu, sn[i % kMine], p / kMine);
+        }
+        // adjacent: the unit's 16 dims are its eight pairs.  Apart: dims p and p + pairs for the units that turn, and
+        // the dims from 2 pairs on, 16 at a time, for the rest.
+        const int d0 = a.adjacent ? u * 16 : (u * 8 < a.pairs ? u * 8 : 2 * a.pairs + (u - a.pairs / 8) * 16);
+        const int d1 = a.adjacent || u * 8 >= a.pairs ? d0 + 8 : d0 + a.pairs;
+        constexpr int kAhead = 4;                  // heads per lane whose loads are in flight together
+        for (int h0 = a.hq0 + part * per + lane / kUnits; h0 < h_end; h0 += kHeads * kAhead) {
+            float x[kAhead][16];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                const int h = h0 + j * kHeads;
+                if (h < h_end) {
+                    const T* src = source(h);
+                    In<T>::load8(src + d0, x[j]);
+                    In<T>::load8(src + d1, x[j] + 8);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                const int h = h0 + j * kHeads;
+                if (h >= h_end) break;
+                uint16_t* dst = target(h);
+                if (!dst) continue;
+                if (h < Hv0) {
+                    if (a.adjacent) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            if (u * 8 + i >= a.pairs) continue;            // dims that do not turn stay bit for bit
+                            const float p = x[j][2 * i], q = x[j][2 * i + 1];
+                            x[j][2 * i] = p * c[i] - q * s[i];
+                            x[j][2 * i + 1] = q * c[i] + p * s[i];
+                        }
+                    } else if (u * 8 < a.pairs) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float p = x[j][i], q = x[j][8 + i];
+                            x[j][i] = p * c[i] - q * s[i];
+                            x[j][8 + i] = q * c[i] + p * s[i];
+                        }
+                    }
+                }
+                store8(dst + d0, x[j]);
+                store8(dst + d1, x[j] + 8);
+            }
+        }
+    } else {
+        // a lane keeps its own pairs and walks the heads; dims that do not turn are copied two by two
+        for (int h = a.hq0 + part * per; h < h_end; ++h) {
+            const T* src = source(h);
+            uint16_t* dst = target(h);
+            if (!dst) continue;
+            const bool turns = h < Hv0;
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+                const int p = lane * kMine + i;
+                const bool mine = p < a.pairs;
+                const int d0 = mine && !a.adjacent ? p : 2 * p, d1 = mine && !a.adjacent ? p + a.pairs : 2 * p + 1;
+                const float x = In<T>::load1(src + d0), y = In<T>::load1(src + d1);
+                const uint32_t out = mine && turns ? pack2(x * cs[i] - y * sn[i], y * cs[i] + x * sn[i]) : pack2(x, y);
+                dst[d0] = (uint16_t)out, dst[d1] = (uint16_t)(out >> 16);
+            }
+        }
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_block_tables(int32_t batch, int32_t num_blocks, const int32_t* ctx_len, const int32_t* new_len, int32_t* held,
+                                int64_t held_stride, const int32_t* n_held, const int32_t* free_blocks, int64_t n_free,
+                                const int64_t* free_begin, int64_t max_entries, int64_t max_rows, int64_t* kv_indptr,
+                                int32_t* kv_indices, int64_t* q_indptr, int64_t* slot_map, int32_t* positions, int32_t* row_req,
+                                int32_t* n_held_new, int64_t* free_end, int32_t* status, cudaStream_t stream) {
+    const TablesArgs a{batch, num_blocks, ctx_len, new_len, n_held, free_blocks, held, held_stride, n_free, free_begin, max_entries,
+                       max_rows, kv_indptr, q_indptr, free_end, kv_indices, slot_map, positions, row_req, n_held_new, status};
+    const int64_t most = max_entries > max_rows ? max_entries : max_rows;
+    const int64_t grid = most > 0 ? (most + kTablesPerCta - 1) / kTablesPerCta : 1;
+    block_tables_kernel<<<(unsigned)grid, kTablesThreads, 3 * (size_t)(batch + 1) * sizeof(int32_t), stream>>>(a);
+    return cudaGetLastError();
+}
+
+cudaError_t tables_init() {
+    return cudaFuncSetAttribute(block_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * (kMaxTableBatch + 1) * (int)sizeof(int32_t));
+}
+
+cudaError_t launch_rope_append(const RopeLaunch& l, cudaStream_t stream) {
+    RopeArgs a{};
+    a.n_rows = l.n_rows;
+    a.q = l.q, a.k = l.k, a.v = l.v;
+    a.q_stride = l.q_stride, a.k_stride = l.k_stride, a.v_stride = l.v_stride, a.qo_stride = l.q_out_stride;
+    a.q_out = l.q_out;
+    a.slab = l.slab;
+    a.positions = l.positions;
+    a.inv_freq = l.inv_freq;
+    a.slot_map = l.slot_map;
+    a.status = l.status;
+    a.Hq = l.shape.Hq, a.Hkv = l.shape.Hkv, a.num_blocks = l.shape.num_blocks;
+    a.pairs = l.pairs, a.adjacent = l.adjacent;
+    a.hq0 = l.q ? 0 : a.Hq;
+    a.heads = l.k ? a.Hq + 2 * a.Hkv : a.Hq;
+    for (int p = 0; p < l.pairs; ++p) a.axis[p] = l.axis[p];
+    const int elem = l.in_bf16 ? 2 : 4;
+    auto aligned = [](const void* p, int64_t stride_bytes) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride_bytes % 16 == 0; };
+    const bool vec = (l.adjacent || l.pairs % 8 == 0) && (!l.q || (aligned(l.q, l.q_stride * elem) && aligned(l.q_out, l.q_out_stride * 2))) &&
+                     (!l.k || (aligned(l.k, l.k_stride * elem) && aligned(l.v, l.v_stride * elem)));
+    // Few rows: a row's heads go to several warps, until the machine has some eight warps per SM.
+    a.parts = 1;
+    while (a.parts < 8 && l.n_rows * a.parts < 8LL * l.n_sms && (a.heads - a.hq0) / (2 * a.parts) >= 4) a.parts *= 2;
+    const int64_t warps = l.n_rows * a.parts;
+    const unsigned grid = (unsigned)((warps * 32 + 255) / 256);
+#define NSD_ROPE(T, D, V) rope_append_kernel<T, D, V><<<grid, 256, 0, stream>>>(a)
+    if (l.in_bf16) {
+        if (l.shape.D == 128) vec ? NSD_ROPE(__nv_bfloat16, 128, true) : NSD_ROPE(__nv_bfloat16, 128, false);
+        else vec ? NSD_ROPE(__nv_bfloat16, 64, true) : NSD_ROPE(__nv_bfloat16, 64, false);
+    } else {
+        if (l.shape.D == 128) vec ? NSD_ROPE(float, 128, true) : NSD_ROPE(float, 128, false);
+        else vec ? NSD_ROPE(float, 64, true) : NSD_ROPE(float, 64, false);
+    }
+#undef NSD_ROPE
+    return cudaGetLastError();
+}
+
+}  // namespace nsd

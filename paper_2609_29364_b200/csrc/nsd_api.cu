@@ -3,6 +3,7 @@
 // preparation of state overlaps model execution; Eq. (F.3): a batch runs only
 // once its KV state is ready).  See include/nsd.h for the contract.
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -255,6 +256,8 @@ static nsd_status create_impl(const nsd_config* cfg, void* d_workspace, size_t w
     }
     if ((e = attn_init()) != cudaSuccess) return fail(e, "cudaFuncSetAttribute(attention)");
     if ((e = gather_init()) != cudaSuccess) return fail(e, "cudaFuncSetAttribute(gather)");
+    if ((e = tables_init()) != cudaSuccess) return fail(e, "cudaFuncSetAttribute(block tables)");
+    if ((e = chunk_attn_init()) != cudaSuccess) return fail(e, "cudaFuncSetAttribute(chunk attention)");
     if ((e = attn_umma_init()) != cudaSuccess) return fail(e, "cudaFuncSetAttribute(tcgen05 attention)");
     ctx->tmaps.resize(cfg->num_slabs);
     ctx->tmaps3.resize(cfg->num_slabs);
@@ -921,6 +924,166 @@ nsd_status nsd_verify_round_host(nsd_ctx* ctx, const nsd_round_args* h, const ns
 }
 
 int64_t nsd_launch_count(const nsd_ctx* ctx) { return ctx ? ctx->launches : 0; }
+
+// ---- chunks of new tokens ---------------------------------------------------------------------
+namespace {
+// These calls launch on the context's device, whichever is current.
+struct OnDevice {
+    int before = -1;
+    cudaError_t err = cudaSuccess;
+    explicit OnDevice(int device) {
+        int cur = device;
+        err = cudaGetDevice(&cur);
+        if (err == cudaSuccess && cur != device) {
+            err = cudaSetDevice(device);
+            before = cur;
+        }
+    }
+    ~OnDevice() { if (before >= 0) cudaSetDevice(before); }
+};
+constexpr int64_t kMaxFlat = 0x7fffffffll - 1024;       // rows and table entries a step may have
+bool misaligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
+}  // namespace
+
+nsd_status nsd_block_tables(nsd_ctx* ctx, int32_t batch, const int32_t* ctx_len, const int32_t* new_len, int32_t* held,
+                            int64_t held_stride, const int32_t* n_held, const int32_t* free_blocks, int64_t n_free,
+                            const int64_t* free_begin, int64_t max_entries, int64_t max_rows, int64_t* kv_indptr,
+                            int32_t* kv_indices, int64_t* q_indptr, int64_t* slot_map, int32_t* positions,
+                            int32_t* row_req, int32_t* n_held_new, int64_t* free_end, void* stream) {
+    if (!ctx) return NSD_ERR_INVALID_ARG;
+    if (batch < 0 || batch > ctx->cfg.max_batch) return NSD_ERR_OUT_OF_RANGE;
+    if (max_entries > kMaxFlat || max_rows > kMaxFlat) return NSD_ERR_OUT_OF_RANGE;
+    if (max_entries < 0 || max_rows < 0 || n_free < 0 || held_stride < 0) return NSD_ERR_INVALID_ARG;
+    if (batch > kMaxTableBatch) return NSD_ERR_CAPACITY;
+    if (!kv_indptr || !q_indptr || !free_end || free_end == free_begin) return NSD_ERR_INVALID_ARG;
+    if (batch > 0 && (!ctx_len || !new_len || !n_held || !n_held_new || n_held == n_held_new)) return NSD_ERR_INVALID_ARG;
+    if (batch > 0 && held_stride > 0 && !held) return NSD_ERR_INVALID_ARG;
+    if ((n_free > 0 && !free_blocks) || (max_entries > 0 && !kv_indices)) return NSD_ERR_INVALID_ARG;
+    const OnDevice on(ctx->device);
+    NSD_CUDA(ctx, on.err);
+    NSD_CUDA(ctx, launch_block_tables(batch, ctx->cfg.num_blocks, ctx_len, new_len, held, held_stride, n_held, free_blocks, n_free,
+                                      free_begin, max_entries, max_rows, kv_indptr, kv_indices, q_indptr, slot_map, positions,
+                                      row_req, n_held_new, free_end, ctx->d_status, static_cast<cudaStream_t>(stream)));
+    ctx->launches++;
+    return NSD_OK;
+}
+
+nsd_status nsd_rope_append(nsd_ctx* ctx, void* kv_pool, int32_t layer, int64_t n_rows, int32_t in_dtype, const void* q,
+                           int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                           void* q_out, int64_t q_out_stride, const int32_t* positions, int32_t n_axes,
+                           const int32_t* h_sections, const float* inv_freq, int32_t flags, const int64_t* slot_map,
+                           void* stream) {
+    if (!ctx || n_rows < 0) return NSD_ERR_INVALID_ARG;
+    if (n_rows > kMaxFlat || layer < 0 || layer >= ctx->cfg.num_layers) return NSD_ERR_OUT_OF_RANGE;
+    if (in_dtype != 0 && in_dtype != 1) return NSD_ERR_UNSUPPORTED;
+    if (n_axes < 1 || n_axes > 4) return NSD_ERR_OUT_OF_RANGE;
+    if (!h_sections || (flags & ~(NSD_ROPE_ADJACENT | NSD_ROPE_CYCLED))) return NSD_ERR_INVALID_ARG;
+    int64_t pairs = 0;
+    for (int a = 0; a < n_axes; ++a) {
+        if (h_sections[a] < 0) return NSD_ERR_OUT_OF_RANGE;
+        pairs += h_sections[a];
+    }
+    if (pairs < 1 || pairs > ctx->cfg.head_dim / 2) return NSD_ERR_OUT_OF_RANGE;
+    RopeLaunch l{};
+    if (flags & NSD_ROPE_CYCLED) {
+        for (int a = 1; a < n_axes; ++a)                    // the axis' last pair, counted in turns of n_axes, has to exist
+            if (h_sections[a] > 0 && (int64_t)(h_sections[a] - 1) * n_axes + a >= pairs) return NSD_ERR_INVALID_ARG;
+        for (int p = 0; p < pairs; ++p) l.axis[p] = (uint8_t)(p / n_axes < h_sections[p % n_axes] ? p % n_axes : 0);
+    } else {
+        for (int a = 0, p = 0; a < n_axes; ++a)
+            for (int i = 0; i < h_sections[a]; ++i) l.axis[p++] = (uint8_t)a;
+    }
+    if ((k != nullptr) != (v != nullptr) || (!q && !k)) return NSD_ERR_INVALID_ARG;
+    if (n_rows == 0) return NSD_OK;
+    if (!positions || !inv_freq) return NSD_ERR_INVALID_ARG;
+    const int64_t wq = (int64_t)ctx->cfg.num_q_heads * ctx->cfg.head_dim, wk = (int64_t)ctx->cfg.num_kv_heads * ctx->cfg.head_dim;
+    if (q && (!q_out || q_stride < wq || q_out_stride < wq)) return NSD_ERR_INVALID_ARG;
+    if (q && q == q_out && (in_dtype != 1 || q_stride != q_out_stride)) return NSD_ERR_INVALID_ARG;
+    if (k && (!kv_pool || !slot_map || k_stride < wk || v_stride < wk)) return NSD_ERR_INVALID_ARG;
+    if (misaligned(kv_pool, 16)) return NSD_ERR_INVALID_ARG;
+    l.shape = ctx->shape;
+    l.slab = k ? slab_ptr(ctx, kv_pool, layer) : nullptr;
+    l.n_rows = n_rows;
+    l.in_bf16 = in_dtype;
+    l.q = q, l.k = k, l.v = v;
+    l.q_stride = q_stride, l.k_stride = k_stride, l.v_stride = v_stride, l.q_out_stride = q_out_stride;
+    l.q_out = static_cast<uint16_t*>(q_out);
+    l.positions = positions;
+    l.inv_freq = inv_freq;
+    l.slot_map = slot_map;
+    l.pairs = (int32_t)pairs;
+    l.adjacent = (flags & NSD_ROPE_ADJACENT) ? 1 : 0;
+    l.n_sms = ctx->n_sms;
+    l.status = ctx->d_status;
+    const OnDevice on(ctx->device);
+    NSD_CUDA(ctx, on.err);
+    NSD_CUDA(ctx, launch_rope_append(l, static_cast<cudaStream_t>(stream)));
+    ctx->launches++;
+    return NSD_OK;
+}
+
+size_t nsd_chunk_plan_bytes(const nsd_ctx* ctx, int64_t max_rows) {
+    if (!ctx || max_rows < 0 || max_rows > kMaxFlat || ctx->cfg.num_q_heads / ctx->cfg.num_kv_heads > 128) return 0;
+    return chunk_plan_layout(nullptr, nullptr, ctx->shape, ctx->cfg.max_batch, max_rows, ctx->n_sms);
+}
+
+static nsd_status chunk_plan_of(const nsd_ctx* ctx, ChunkPlan* p, void* plan, size_t plan_bytes, int64_t max_rows) {
+    if (max_rows < 0 || !plan || misaligned(plan, 256)) return NSD_ERR_INVALID_ARG;
+    if (max_rows > kMaxFlat) return NSD_ERR_OUT_OF_RANGE;
+    if (ctx->cfg.num_q_heads / ctx->cfg.num_kv_heads > 128) return NSD_ERR_UNSUPPORTED;
+    if (plan_bytes < chunk_plan_layout(p, plan, ctx->shape, ctx->cfg.max_batch, max_rows, ctx->n_sms)) return NSD_ERR_CAPACITY;
+    return NSD_OK;
+}
+
+nsd_status nsd_chunk_plan(nsd_ctx* ctx, void* plan, size_t plan_bytes, int32_t batch, int64_t max_rows,
+                          const int64_t* q_indptr, const int32_t* ctx_len, const int64_t* kv_indptr,
+                          const nsd_chunk_masks* masks, void* stream) {
+    if (!ctx) return NSD_ERR_INVALID_ARG;
+    if (batch < 0 || batch > ctx->cfg.max_batch) return NSD_ERR_OUT_OF_RANGE;
+    const nsd_chunk_masks m = masks ? *masks : nsd_chunk_masks{};
+    if (m.window < 0 || m.reserved != 0) return NSD_ERR_INVALID_ARG;
+    if (batch > 0 && (!q_indptr || !ctx_len || !kv_indptr)) return NSD_ERR_INVALID_ARG;
+    ChunkPlan p;
+    if (const nsd_status s = chunk_plan_of(ctx, &p, plan, plan_bytes, max_rows)) return s;
+    const OnDevice on(ctx->device);
+    NSD_CUDA(ctx, on.err);
+    NSD_CUDA(ctx, launch_chunk_plan(p, ctx->shape, batch, q_indptr, ctx_len, kv_indptr, m, ctx->d_status, static_cast<cudaStream_t>(stream)));
+    ctx->launches += batch > 0 ? 2 : 1;
+    return NSD_OK;
+}
+
+nsd_status nsd_chunk_attn(nsd_ctx* ctx, void* plan, size_t plan_bytes, const void* kv_pool, const void* q,
+                          int64_t q_stride, void* o, float* lse, int64_t max_rows, const int32_t* kv_indices,
+                          int32_t layer, float scale, float softcap, const float* alibi_slopes, void* stream) {
+    if (!ctx) return NSD_ERR_INVALID_ARG;
+    if (layer < 0 || layer >= ctx->cfg.num_layers) return NSD_ERR_OUT_OF_RANGE;
+    if (!(scale >= 0.f) || !(softcap >= 0.f) || scale > 3e38f || softcap > 3e38f) return NSD_ERR_INVALID_ARG;      // NaN too
+    ChunkPlan p;
+    if (const nsd_status s = chunk_plan_of(ctx, &p, plan, plan_bytes, max_rows)) return s;
+    if (max_rows == 0) return NSD_OK;
+    if (!kv_pool || !q || !o || !kv_indices) return NSD_ERR_INVALID_ARG;
+    if (q_stride < (int64_t)ctx->cfg.num_q_heads * ctx->cfg.head_dim || q_stride % 8) return NSD_ERR_INVALID_ARG;
+    if (misaligned(q, 16) || misaligned(o, 16) || misaligned(kv_pool, 16)) return NSD_ERR_INVALID_ARG;
+    ChunkAttnLaunch l{};
+    l.shape = ctx->shape;
+    l.slab = slab_ptr(ctx, const_cast<void*>(kv_pool), layer);
+    l.q = static_cast<const uint16_t*>(q);
+    l.q_stride = q_stride;
+    l.o = static_cast<uint16_t*>(o);
+    l.lse = lse;
+    l.kv_indices = kv_indices;
+    l.scale = scale > 0.f ? scale : 1.f / sqrtf((float)ctx->cfg.head_dim);
+    l.softcap = softcap;
+    l.slopes = alibi_slopes;
+    l.status = ctx->d_status;
+    l.wait_budget = ctx->wait_budget;
+    const OnDevice on(ctx->device);
+    NSD_CUDA(ctx, on.err);
+    int launched = 0;
+    NSD_CUDA(ctx, launch_chunk_attn(p, l, static_cast<cudaStream_t>(stream), &launched));
+    ctx->launches += launched;
+    return NSD_OK;
+}
 
 nsd_status nsd_get_status(nsd_ctx* ctx, void* stream, int32_t* first_bad_request) {
     if (!ctx) return NSD_ERR_INVALID_ARG;

@@ -139,4 +139,83 @@ cudaError_t launch_accept_logits(const void* logits, int32_t logits_bf16, float 
                                  int32_t n_sms, int32_t feed /* 0 = direct loads, 1 = shared-memory ring where aligned */,
                                  int32_t* tickets /* two words, zero between launches */, cudaStream_t stream);
 
+// ---- chunks of new tokens (chunk_prep.cu, chunk_attn.cu) ----------------------------------------
+constexpr int kMaxTableBatch = 16384;        // requests whose prefix sums one CTA holds in shared memory
+cudaError_t tables_init();
+cudaError_t launch_block_tables(int32_t batch, int32_t num_blocks, const int32_t* ctx_len, const int32_t* new_len, int32_t* held,
+                                int64_t held_stride, const int32_t* n_held, const int32_t* free_blocks, int64_t n_free,
+                                const int64_t* free_begin, int64_t max_entries, int64_t max_rows, int64_t* kv_indptr,
+                                int32_t* kv_indices, int64_t* q_indptr, int64_t* slot_map, int32_t* positions, int32_t* row_req,
+                                int32_t* n_held_new, int64_t* free_end, int32_t* status, cudaStream_t stream);
+
+struct RopeLaunch {
+    Shape shape;
+    uint16_t* slab;
+    int64_t n_rows;
+    int32_t in_bf16;
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride, q_out_stride;
+    uint16_t* q_out;
+    const int32_t* positions;
+    const float* inv_freq;
+    const int64_t* slot_map;
+    int32_t pairs, adjacent, n_sms;
+    uint8_t axis[64];                        // position axis of each pair
+    int32_t* status;
+};
+cudaError_t launch_rope_append(const RopeLaunch& l, cudaStream_t stream);
+
+// The plan buffer of a step's attention.  A unit is up to two tiles of 128 stacked rows (T = 128 / G tokens of one request
+// each, G q heads per kv head) against the keys any of its rows sees; every kv head repeats the request's units.
+struct __align__(16) ChunkUnit {
+    int64_t tbl;                             // kv_indptr of the request
+    int32_t nblk;                            // its table entries
+    int32_t row0, ntok;                      // rows of the unit (tokens)
+    int32_t req;
+    int32_t n_tiles;                         // 128-key tiles that hold a visible key
+    int32_t key_lo, key_hi;                  // keys any row sees: [key_lo, key_hi)
+    int32_t first, last;                     // the request's units
+    int32_t pos0;                            // position of the unit's first row
+};
+static_assert(sizeof(ChunkUnit) == 48, "ChunkUnit is read as three 16-byte words");
+struct __align__(16) ChunkStart {            // where a CTA's share of the work begins: tile `tile` of unit `unit`, kv head `head`
+    int32_t unit, head, tile, pad;
+};
+struct ChunkHeader {
+    uint32_t magic;
+    int32_t n_units;
+    int64_t max_rows;
+    int32_t n_ctas, tokens;                  // CTAs the work is split over, tokens per unit
+};
+struct ChunkPlan {                           // the buffer's parts
+    ChunkHeader* header;
+    ChunkStart* starts;                      // [n_ctas + 1]
+    ChunkUnit *raw, *units;                  // [max_units]
+    int64_t* cost;                           // [max_units + 1] prefix sums over the units, one kv head
+    int32_t *row_lo, *row_hi;                // [max_rows] visible keys of each row
+    float* part_ml;                          // [2 n_ctas][256][2]
+    float* part_acc;                         // [2 n_ctas][256][D]
+    int64_t max_rows, max_units;
+    int32_t n_ctas;
+};
+size_t chunk_plan_layout(ChunkPlan* p, void* base, const Shape& s, int32_t max_batch, int64_t max_rows, int32_t n_sms);
+cudaError_t chunk_attn_init();
+cudaError_t launch_chunk_plan(const ChunkPlan& p, const Shape& s, int32_t batch, const int64_t* q_indptr, const int32_t* ctx_len,
+                              const int64_t* kv_indptr, const nsd_chunk_masks& masks, int32_t* status, cudaStream_t stream);
+struct ChunkAttnLaunch {
+    Shape shape;
+    const uint16_t* slab;
+    const uint16_t* q;
+    int64_t q_stride;
+    uint16_t* o;
+    float* lse;
+    const int32_t* kv_indices;
+    float scale, softcap;
+    const float* slopes;
+    int32_t* status;
+    uint32_t wait_budget;
+};
+// *launched: kernels enqueued
+cudaError_t launch_chunk_attn(const ChunkPlan& p, const ChunkAttnLaunch& l, cudaStream_t stream, int* launched);
+
 }  // namespace nsd

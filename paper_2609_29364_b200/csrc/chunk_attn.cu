@@ -3,6 +3,7 @@
 #include <cuda_bf16.h>
 
 #include "nsd_internal.h"
+#include "tcgen05_ops.h"
 
 namespace nsd {
 namespace {
@@ -171,96 +172,598 @@ chunk_split_kernel(const PlanArgs a) {
 }
 
 // ---- attention ----------------------------------------------------------------------------------
+// A unit is up to 2 T tokens of one request (T = 128 / G) times the G q heads of a kv head: the
+// stacked rows of a token sit side by side, T tokens fill a tile of 128 rows, two tiles make a
+// unit.  Per key tile of 128 keys and row tile, on the tensor cores:
+//     S[128 x 128]  = Q K^T          Q and K in shared memory (K-major, 128-byte swizzle)
+//     O[128 x D]   += P V            P in tensor memory over S's own columns, V in shared memory
+// The two row tiles are two streams that share every K and V tile and run half a step apart: while
+// one stream's softmax works, the tensor cores work for the other.  A unit of one row tile (single
+// tokens, the end of a chunk) gives the streams alternate key tiles instead, each with its own O
+// and statistics, joined at the end through tensor memory; so short rows keep the same two tiles
+// in flight and stay bound by HBM.
+//
+// One persistent CTA per SM, twelve warps:
+//   0-3 / 4-7  softmax of stream 0 / 1: a thread owns a row (its TMEM lane).  Scores to the log2
+//              domain with the scale folded in, maximum (refreshed, and O rescaled, only when a
+//              score outgrows it by 2^8), P = 2^(s - m) to bf16 in two halves so that P V can start on
+//              the first, sums in 32 bits over the unrounded weights.  They also write the rows out.
+//   8 / 9      issue the MMAs of stream 0 / 1.  One thread issues S of a tile, then P V of it, so the
+//              commit of S also tells that the stream's earlier P V are complete: O may be rescaled.
+//   10         Q and K producer; 11: V producer.  A pool block (16 keys) of a head is one 5-D box
+//              whose layout in shared memory -- [8-key group][64-dim half][8 keys][64 dims] -- puts
+//              the 8-key groups of all eight blocks at one pitch (K's descriptor wants that) and a
+//              block's groups and halves at fixed pitches (V's): one copy per block serves both.
+// Keys are walked from the last tile to the first: the diagonal, with its masks, comes first, and
+// with a bias on distance the largest scores do, so the maximum hardly moves.
+//
+// Work is cut into equal shares of the line (request, kv head, unit, key tile), one per CTA,
+// whatever the lengths: a CTA may begin and end inside a unit.  Such a piece leaves its O
+// (unnormalised) and statistics in the plan, and a small kernel behind this one joins them in order.
+// Every wait is bounded (see verify_attn_umma.cu for what happens when one runs out).
+constexpr int kBsA = 16;
+constexpr int kBlocks = kTileKeys / kBsA;
+constexpr int kThreadsA = 384;
+constexpr int kWarpIssue = 8, kWarpK = 10, kWarpV = 11;
+constexpr float kMaxSlack = 8.0f;                      // the running maximum may lag the true one by this much (log2 units)
+constexpr uint32_t kSpinLimit = 1u << 20;              // wait slices of ~2 us each
+enum : int { MODE_CAP = 1, MODE_BIAS = 2 };
+
 struct AttnArgs {
+    CUtensorMap kv_map, q_map;
     ChunkPlan p;
-    const uint16_t *slab, *q;
-    int64_t q_stride;
     uint16_t* o;
     float* lse;
     const int32_t* kv_indices;
-    float scale, softcap;
     const float* slopes;
-    int32_t* status;
-    int32_t Hq, Hkv, num_blocks;
+    float sc;                                          // scale, in the log2 domain; with a cap: scale / cap
+    float cap;                                         // cap in the log2 domain
+    int32_t *status, Hq, Hkv, G, T, num_blocks;
+    uint32_t wait_budget;
 };
 
-// A warp per (row, q head): a lane scores one key at a time, the weights are handed round for the
-// sum of values, of which a lane owns D / 32 dims.
 template <int D>
-__global__ void __launch_bounds__(256)
-chunk_attn_rows_kernel(const __grid_constant__ AttnArgs a) {
-    __shared__ float q_s[8][D];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (a.p.header->magic != kMagic || a.p.header->max_rows != a.p.max_rows) {
-        if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) report(a.status, STATUS_BAD_TOKEN, -1);
+struct Smem {
+    static constexpr int kHalves = D / 64;
+    static constexpr int kBlockBytes = kBsA * D * 2;
+    static constexpr int kTile = kTileKeys * D * 2;    // a K or V tile
+    static constexpr int kQ = kRows * D * 2;
+    static constexpr int kGroupPitch = kHalves * 1024; // between 8-key groups
+    static constexpr int kKStages = D == 128 ? 3 : 5, kVStages = D == 128 ? 2 : 5;
+    static constexpr int kOffK = 2 * kQ, kOffV = kOffK + kKStages * kTile;
+    static constexpr int kOffMl = kOffV + kVStages * kTile;              // stream 1's statistics for the join
+    static constexpr int kOffBars = kOffMl + kRows * 8;
+    static constexpr int kNumBars = 2 * kKStages + 2 * kVStages + 1 + 4 + 2 + 4 + 2 + 2;
+    static constexpr int kOffMisc = kOffBars + kNumBars * 8;
+    static constexpr int kBytes = kOffMisc + 16;
+    static_assert(kBytes <= 227 * 1024, "shared memory budget");
+};
+constexpr int kTmemColsA = 512, kTmemOBase = 256;      // S0, S1, O0, O1: 128 columns each
+
+// A CTA's walk over its share of the line.
+struct Walk {
+    const ChunkUnit* units;
+    ChunkStart at, end;
+    int Hkv;
+    // the piece under way
+    ChunkUnit u;
+    int head, k0, k1, slot;                            // key tiles [k0, k1) in walking order; partial slot or -1
+    __device__ __forceinline__ Walk(const ChunkPlan& p, int Hkv_) : units(p.units), at(p.starts[blockIdx.x]), end(p.starts[blockIdx.x + 1]), Hkv(Hkv_) {}
+    __device__ __forceinline__ bool next() {
+        if (at.unit == end.unit && at.head == end.head && at.tile == end.tile) return false;
+        u = units[at.unit];
+        head = at.head;
+        k0 = at.tile;
+        const bool cut = at.unit == end.unit && at.head == end.head;
+        k1 = cut ? end.tile : u.n_tiles;
+        slot = k0 > 0 ? 2 * (int)blockIdx.x : (cut ? 2 * (int)blockIdx.x + 1 : -1);
+        if (cut) {
+            at = end;
+        } else {
+            at.tile = 0;
+            if (at.unit < u.last) ++at.unit;
+            else if (at.head + 1 < Hkv) ++at.head, at.unit = u.first;
+            else at.head = 0, at.unit = u.last + 1;
+        }
+        return true;
+    }
+};
+
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, int32_t tile, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %2, %2, %2, %3}], [%4];"
+                 ::"r"(dst), "l"(map), "r"(0), "r"(tile), "r"(bar)
+                 : "memory");
+}
+
+template <int D, int MODE>
+__global__ void __launch_bounds__(kThreadsA, 1)
+chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
+    using L = Smem<D>;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    pdl_release_dependents();
+    if (a.p.header->magic != kMagic || a.p.header->max_rows != a.p.max_rows || a.p.header->n_ctas != (int)gridDim.x) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) report(a.status, STATUS_BAD_TOKEN, -1);
         return;
     }
-    const int n_units = a.p.header->n_units, G = a.Hq / a.Hkv, head = blockIdx.y;
-    for (int ui = blockIdx.x; ui < n_units; ui += gridDim.x) {
-        const ChunkUnit u = a.p.units[ui];
-        for (int m = warp; m < u.ntok * G; m += 8) {
-            const int row = u.row0 + m / G, h = head * G + m % G;
-            const int lo = a.p.row_lo[row], hi = a.p.row_hi[row];
-            const int64_t orow = (int64_t)row * a.Hq + h;
-            __syncwarp();
-            for (int d = lane; d < D; d += 32)
-                q_s[warp][d] = __uint_as_float((uint32_t)a.q[row * a.q_stride + h * D + d] << 16);
-            __syncwarp();
-            const int pos = u.pos0 + row - u.row0;
-            float m_run = -INFINITY, l = 0.f, acc[D / 32] = {};
-            for (int k0 = lo; k0 < hi; k0 += 32) {
-                const int key = k0 + lane;
-                float s = -INFINITY;
-                int64_t tile = -1;
-                if (key < hi) {
-                    const int b = key / 16 < u.nblk ? a.kv_indices[u.tbl + key / 16] : -1;
-                    if ((uint32_t)b >= (uint32_t)a.num_blocks) {
-                        report(a.status, STATUS_BAD_BLOCK, u.req);
-                        s = 0.f;
-                    } else {
-                        tile = ((int64_t)b * 2 * a.Hkv + head) * 16 + key % 16;
-                        const uint4* kp = reinterpret_cast<const uint4*>(a.slab + tile * D);
-                        tile += 16 * a.Hkv;
-                        float d0 = 0.f;
-                        for (int c = 0; c < D / 8; ++c) {
-                            const uint4 x = kp[c];
-                            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    Walk w(a.p, a.Hkv);
+    if (w.at.unit == w.end.unit && w.at.head == w.end.head && w.at.tile == w.end.tile) return;
+    const uint32_t smem0 = smem_u32(smem);
+    if ((smem0 & 1023u) != 0) {
+        if (threadIdx.x == 0) atomicOr(a.status, STATUS_LAYOUT);
+        return;
+    }
+    const uint32_t bar0 = smem0 + L::kOffBars;
+    const uint32_t k_full = bar0, k_empty = k_full + 8 * L::kKStages, v_full = k_empty + 8 * L::kKStages, v_empty = v_full + 8 * L::kVStages;
+    const uint32_t v_land = v_empty + 8 * L::kVStages; // a V tile whose hidden rows have to be cleared lands here first
+    const uint32_t q_full = v_land + 8, q_empty = q_full + 16;                          // [2] per Q buffer
+    const uint32_t s_full = q_empty + 16, p_full = s_full + 16, o_full = p_full + 32;   // [2], [2][2 halves], [2] per stream
+    const uint32_t x_ready = o_full + 16, x_done = x_ready + 8;                         // the join of a one-tile unit's streams
+    uint32_t& tmem_base_s = *reinterpret_cast<uint32_t*>(smem + L::kOffMisc);
+    volatile int& abort_s = *reinterpret_cast<volatile int*>(smem + L::kOffMisc + 4);
+    float2* const ml_s = reinterpret_cast<float2*>(smem + L::kOffMl);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t limit = a.wait_budget ? a.wait_budget : kSpinLimit;
+
+    if (tid == 0) {
+        for (int s = 0; s < L::kKStages; ++s) mbar_init(k_full + 8 * s, 1), mbar_init(k_empty + 8 * s, 2);
+        for (int s = 0; s < L::kVStages; ++s) mbar_init(v_full + 8 * s, 1), mbar_init(v_empty + 8 * s, 2);
+        mbar_init(v_land, 1);
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(q_full + 8 * s, 1), mbar_init(q_empty + 8 * s, 2);
+            mbar_init(s_full + 8 * s, 1), mbar_init(o_full + 8 * s, 1);
+            mbar_init(p_full + 16 * s, 4), mbar_init(p_full + 16 * s + 8, 4);
+        }
+        mbar_init(x_ready, 4), mbar_init(x_done, 4);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        abort_s = 0;
+    }
+    if (warp == kWarpIssue) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_s)), "n"(kTmemColsA) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_base_s;
+    auto wait = [&](uint32_t bar, uint32_t count) { return mbar_wait(bar, count & 1, &abort_s, limit); };   // the count-th completion
+
+    if (warp < kWarpIssue) {
+        // ================================ softmax and output ================================
+        const int s = warp >> 2, q = warp & 3;
+        const uint32_t lanes = (uint32_t)(q * 32) << 16;
+        const uint32_t tmem_s = tmem + s * 128 + lanes, tmem_o = tmem + kTmemOBase + s * 128 + lanes;
+        const int m = q * 32 + lane, tok = m / a.G, g = m - tok * a.G;
+        uint32_t n_s = 0, n_o[2] = {0, 0}, n_x = 0;    // completions seen so far
+        bool fail = false;
+        auto wait_all = [&](uint32_t bar, uint32_t count) {
+            if (!wait(bar, count)) fail = true;
+            fail = __any_sync(0xffffffffu, fail);
+            return !fail;
+        };
+        while (!fail && w.next()) {
+            const int n = w.k1 - w.k0;
+            const bool dual = w.u.ntok > a.T;
+            if (!dual && s == 1 && n == 0) continue;
+            const int t_row = (dual ? s * a.T : 0) + tok;                               // token of the unit
+            const bool live = tok < a.T && t_row < w.u.ntok;
+            const bool warp_live = __any_sync(0xffffffffu, live);
+            const int64_t row = w.u.row0 + t_row;
+            const int h = w.head * a.G + g;
+            int lo = 0, hi = 0x7fffffff;                                                // lanes without a row never mask
+            if (live) lo = a.p.row_lo[row], hi = a.p.row_hi[row];
+            float slope = 0.f;
+            if constexpr (MODE & MODE_BIAS) slope = live ? a.slopes[h] * kLog2e : 0.f;
+            const int pos = w.u.pos0 + t_row;
+            float m_run = -INFINITY, l_run = 0.f;
+            const int t_hi = (w.u.key_hi + kTileKeys - 1) / kTileKeys;
+            int mine = 0;                                                               // tiles of this stream
+            for (int i = dual ? 0 : s; i < n; i += dual ? 1 : 2, ++mine) {
+                if (!wait_all(s_full + 8 * s, n_s++)) break;
+                tc_fence_after();
+                if (warp_live) {
+                    const int key0 = (t_hi - 1 - (w.k0 + i)) * kTileKeys;
+                    uint32_t x[kTileKeys];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                d0 = fmaf(__uint_as_float(w[i] << 16), q_s[warp][c * 8 + 2 * i], d0);
-                                d0 = fmaf(__uint_as_float(w[i] & 0xffff0000u), q_s[warp][c * 8 + 2 * i + 1], d0);
+                    for (int c = 0; c < 4; ++c) tmem_ld32(tmem_s + c * 32, x + c * 32);
+                    tmem_wait_ld();
+                    float f = a.sc;                                                     // from x to the log2 domain
+                    if constexpr (MODE & MODE_CAP) {
+                        f = 1.f;
+#pragma unroll
+                        for (int j = 0; j < kTileKeys; ++j) x[j] = __float_as_uint(a.cap * tanhf(__uint_as_float(x[j]) * a.sc));
+                    }
+                    if constexpr (MODE & MODE_BIAS) {
+                        const float b = slope * (float)(key0 - pos);
+#pragma unroll
+                        for (int j = 0; j < kTileKeys; ++j) x[j] = __float_as_uint(fmaf(__uint_as_float(x[j]), f, fmaf(slope, (float)j, b)));
+                        f = 1.f;
+                    }
+                    const int v0 = lo - key0, v1 = hi - key0;                           // visible: v0 <= j < v1
+                    if (__any_sync(0xffffffffu, v0 > 0 || v1 < kTileKeys)) {
+#pragma unroll
+                        for (int j = 0; j < kTileKeys; ++j) x[j] = j >= v0 && j < v1 ? x[j] : 0xff800000u;
+                    }
+                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int j = 0; j < kTileKeys; j += 8)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) mx[c] = fmaxf(fmaxf(mx[c], __uint_as_float(x[j + c])), __uint_as_float(x[j + 4 + c]));
+                    const float m_tile = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * f;
+                    const bool outgrown = m_tile > m_run + kMaxSlack;                   // also the first visible key
+                    if (__any_sync(0xffffffffu, outgrown)) {
+                        const float m_new = outgrown ? m_tile : m_run;
+                        const float r = outgrown ? (m_run == -INFINITY ? 0.f : ex2_approx(m_run - m_new)) : 1.f;
+                        if (mine > 0) {
+                            // O holds this piece's earlier tiles, complete since S of this one is
+#pragma unroll 1
+                            for (int c = 0; c < D; c += 16) {
+                                uint32_t y[16];
+                                tmem_ld16(tmem_o + c, y);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * r);
+                                tmem_st16(tmem_o + c, y);
+                            }
+                            tmem_wait_st();
+                        }
+                        l_run *= r;
+                        m_run = m_new;
+                    }
+                    const float nm = m_run == -INFINITY ? 0.f : -m_run;
+                    float l[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        uint32_t p[32];
+#pragma unroll
+                        for (int j = 0; j < 64; j += 2) {
+                            const float p0 = ex2_approx(fmaf(__uint_as_float(x[half * 64 + j]), f, nm));
+                            const float p1 = ex2_approx(fmaf(__uint_as_float(x[half * 64 + j + 1]), f, nm));
+                            l[(j >> 1) & 1] += p0;
+                            l[2 + ((j >> 1) & 1)] += p1;
+                            p[j >> 1] = pack_bf16(p0, p1);
+                        }
+                        tmem_st32(tmem_s + half * 32, p);
+                        tmem_wait_st();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(p_full + 16 * s + 8 * half);
+                    }
+                    l_run += (l[0] + l[1]) + (l[2] + l[3]);
+                } else {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(p_full + 16 * s), mbar_arrive(p_full + 16 * s + 8);
+                }
+            }
+            if (fail) break;
+            // ---- the piece's rows
+            const bool join = !dual && n > 0;
+            if (join && s == 1) {
+                ml_s[m] = make_float2(m_run, l_run);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(x_ready);
+                if (mine > 0) ++n_o[1];
+                if (!wait_all(x_done, n_x++)) break;                                    // stream 0 has read this stream's O
+                continue;
+            }
+            if (mine > 0 && !wait_all(o_full + 8 * s, n_o[s]++)) break;
+            if (dual && n > 0 && s == 0) ++n_o[1];
+            float r0 = 1.f, r1 = 0.f;                                                   // weights of the two streams' O
+            bool two = false;
+            if (join) {
+                if (!wait_all(x_ready, n_x++)) break;
+                two = n > 1;
+                if (two && !wait_all(o_full + 8, n_o[1]++)) break;
+                const float2 ml = ml_s[m];
+                const float top = fmaxf(m_run, ml.x);
+                r0 = m_run == -INFINITY ? 0.f : ex2_approx(m_run - top);
+                r1 = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - top);
+                l_run = l_run * r0 + ml.y * r1;
+                m_run = top;
+            }
+            tc_fence_after();
+            if (warp_live) {
+                const int64_t orow = row * a.Hq + h;
+                const bool part = w.slot >= 0;
+                const int64_t prow = (int64_t)w.slot * 2 * kRows + (dual ? s * kRows : 0) + m;
+                const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
+                if (!part) r0 *= inv, r1 *= inv;
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t y[32], z[32];
+                    if (n > 0) {
+                        tmem_ld32(tmem_o + c, y);
+                        if (two) tmem_ld32(tmem_o + 128 + c, z);
+                        tmem_wait_ld();
+                    }
+                    if (live) {
+                        // a weight of zero means that the stream saw nothing: its O may be anything
+    #pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            float v = r0 > 0.f && n > 0 ? __uint_as_float(y[j]) * r0 : 0.f;
+                            if (two && r1 > 0.f) v = fmaf(__uint_as_float(z[j]), r1, v);
+                            y[j] = __float_as_uint(v);
+                        }
+                        if (part) {
+                            float4* pa = reinterpret_cast<float4*>(a.p.part_acc + prow * D + c);
+    #pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                pa[j] = make_float4(__uint_as_float(y[4 * j]), __uint_as_float(y[4 * j + 1]), __uint_as_float(y[4 * j + 2]), __uint_as_float(y[4 * j + 3]));
+                        } else {
+                            uint4* po = reinterpret_cast<uint4*>(a.o + orow * D + c);
+    #pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                uint32_t k[4];
+    #pragma unroll
+                                for (int i = 0; i < 4; ++i) k[i] = pack_bf16(__uint_as_float(y[8 * j + 2 * i]), __uint_as_float(y[8 * j + 2 * i + 1]));
+                                po[j] = make_uint4(k[0], k[1], k[2], k[3]);
                             }
                         }
-                        s = d0;
                     }
-                    s *= a.scale;
-                    if (a.softcap > 0.f) s = a.softcap * tanhf(s / a.softcap);
-                    if (a.slopes) s += a.slopes[h] * (float)(key - pos);
+                    __syncwarp();
                 }
-                float mx = s;
-                for (int i = 16; i; i >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, i));
-                const float m_new = fmaxf(m_run, mx);
-                const float f = m_run == -INFINITY ? 0.f : expf(m_run - m_new);
-                const float p = key < hi ? expf(s - m_new) : 0.f;
-                m_run = m_new;
-                l = l * f + p;
-                for (int i = 0; i < D / 32; ++i) acc[i] *= f;
-                for (int j = 0; j < 32 && k0 + j < hi; ++j) {
-                    const float pj = __shfl_sync(0xffffffffu, p, j);
-                    const int64_t t = __shfl_sync(0xffffffffu, tile, j);
-                    if (t >= 0)
-                        for (int i = 0; i < D / 32; ++i) acc[i] = fmaf(pj, __uint_as_float((uint32_t)a.slab[t * D + lane + 32 * i] << 16), acc[i]);
+                if (live && part) *reinterpret_cast<float2*>(a.p.part_ml + prow * 2) = make_float2(m_run, l_run);
+                if (live && !part && a.lse) a.lse[orow] = m_run == -INFINITY ? -INFINITY : (m_run + log2f(l_run)) * kLn2;
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (join && lane == 0) mbar_arrive(x_done);
+        }
+    } else if (warp < kWarpK) {
+        // ================================ MMA issuers ================================
+        const int s = warp - kWarpIssue;
+        if (lane == 0) {
+            const uint32_t idesc_s = instr_desc(kRows, kTileKeys, 0, 0), idesc_o = instr_desc(kRows, D, 0, 1);
+            const uint32_t tmem_s = tmem + s * 128, tmem_o = tmem + kTmemOBase + s * 128;
+            uint32_t n_k = 0, n_p = 0, n_q[2] = {0, 0};
+            bool ok = true;
+            while (ok && w.next()) {
+                const int n = w.k1 - w.k0;
+                if (n == 0) continue;
+                const bool dual = w.u.ntok > a.T;
+                const int qb = dual ? s : 0, step = dual ? 1 : 2, i0 = dual ? 0 : s;
+                if (!(ok = wait(q_full + 8 * qb, n_q[qb]))) break;
+                ++n_q[0];
+                if (dual) ++n_q[1];
+                if (i0 >= n) mbar_arrive(q_empty);                                      // a single key tile: nothing for stream 1
+                const uint32_t q_s = smem0 + qb * L::kQ;
+                for (int i = i0; i < n; i += step, ++n_p) {
+                    const uint32_t c = n_k + i, ks = c % L::kKStages, vs = c % L::kVStages;
+                    const bool last = i + step >= n;
+                    if (!(ok = wait(k_full + 8 * ks, c / L::kKStages))) break;
+                    tc_fence_after();
+                    const uint32_t kb = smem0 + L::kOffK + ks * L::kTile;
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {                                  // 16 dims each, 64 per swizzled half
+                        const uint64_t da = smem_desc(q_s + (k >> 2) * (kRows * 128) + (k & 3) * 32, 16, 1024, 2);
+                        const uint64_t db = smem_desc(kb + (k >> 2) * 1024 + (k & 3) * 32, 16, L::kGroupPitch, 2);
+                        umma_ss(tmem_s, da, db, idesc_s, k > 0);
+                    }
+                    umma_commit(k_empty + 8 * ks);
+                    umma_commit(s_full + 8 * s);
+                    if (!dual) mbar_arrive(k_empty + 8 * ks);                           // the other stream has no use for this tile
+                    if (last) {
+                        umma_commit(q_empty + 8 * qb);
+                        if (dual) mbar_arrive(q_empty + 8 * qb);
+                    }
+                    if (!(ok = wait(v_full + 8 * vs, c / L::kVStages))) break;
+                    const uint32_t vb = smem0 + L::kOffV + vs * L::kTile;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        if (!(ok = wait(p_full + 16 * s + 8 * half, n_p))) break;
+                        tc_fence_after();
+#pragma unroll
+                        for (int k = half * 4; k < half * 4 + 4; ++k) {                 // 16 keys each: a block of V, 8 columns of P
+                            const uint64_t db = smem_desc(vb + k * L::kBlockBytes, 1024, L::kGroupPitch, 2);
+                            umma_ts(tmem_o, tmem_s + k * 8, db, idesc_o, (i > i0 || k > 0) ? 1u : 0u);
+                        }
+                    }
+                    if (!ok) break;
+                    umma_commit(v_empty + 8 * vs);
+                    if (!dual) mbar_arrive(v_empty + 8 * vs);
+                    if (last) umma_commit(o_full + 8 * s);
+                }
+                n_k += n;
+            }
+        }
+        __syncwarp();
+    } else {
+        // ================================ producers ================================
+        const bool is_v = warp == kWarpV;
+        const int stages = is_v ? L::kVStages : L::kKStages;
+        const uint32_t full = is_v ? v_full : k_full, empty = is_v ? v_empty : k_empty;
+        const uint32_t ring = smem0 + (is_v ? L::kOffV : L::kOffK);
+        const int32_t oob = a.num_blocks * 2 * a.Hkv;                                   // past the slab: zero fill
+        uint32_t n_t = 0, n_q[2] = {0, 0}, n_land = 0;
+        bool ok = true;
+        while (ok && w.next()) {
+            const int n = w.k1 - w.k0;
+            if (n == 0) continue;
+            const bool dual = w.u.ntok > a.T;
+            const int32_t* table = a.kv_indices + w.u.tbl;
+            const int b_lo = w.u.key_lo / kBsA, b_hi = (w.u.key_hi + kBsA - 1) / kBsA;  // blocks that hold a visible key
+            const int t0 = (w.u.key_hi + kTileKeys - 1) / kTileKeys - 1 - w.k0;         // first key tile
+            // a lane's block of the next tile: its id is read one tile ahead
+            auto block_id = [&](int t) -> int32_t {
+                const int b = t * kBlocks + lane;
+                if (lane >= kBlocks || b < b_lo || b >= b_hi) return -2;                // not needed
+                return b < w.u.nblk ? __ldg(table + b) : -1;
+            };
+            int32_t id_next = block_id(t0);
+            for (int i = 0; i < n; ++i, ++n_t) {
+                const uint32_t st = n_t % stages, use = n_t / stages;
+                const int t = t0 - i;
+                const int32_t id = id_next;
+                if (i + 1 < n) id_next = block_id(t - 1);
+                int32_t tile = oob;
+                if (id != -2) {
+                    if ((uint32_t)id < (uint32_t)a.num_blocks) tile = (id * 2 + (is_v ? 1 : 0)) * a.Hkv + w.head;
+                    else report(a.status, STATUS_BAD_BLOCK, w.u.req);
+                }
+                if (use > 0 && !wait(empty + 8 * st, use - 1)) ok = false;
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                // hidden rows of V have to be finite, since 0 x NaN is NaN: those of a block that also holds visible keys are
+                // cleared once the tile has landed (blocks without any are zero fill)
+                const int z0 = w.u.key_lo - t * kTileKeys, z1 = w.u.key_hi - t * kTileKeys;             // visible keys of the tile: [z0, z1)
+                const bool ragged = is_v && ((z0 > 0 && (z0 & 15)) || (z1 < kTileKeys && (z1 & 15)));
+                const uint32_t bar = ragged ? v_land : full + 8 * st;
+                if (lane == 0) mbar_expect_tx(bar, L::kTile);
+                __syncwarp();
+                if (lane < kBlocks) tma_load_5d(ring + st * L::kTile + lane * L::kBlockBytes, &a.kv_map, tile, bar);
+                if (ragged) {
+                    if (!wait(v_land, n_land++)) ok = false;
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    unsigned char* vt = smem + L::kOffV + st * L::kTile;
+                    auto clear = [&](int first, int last) {                             // rows [first, last) of one block
+                        for (int c = lane; c < (last - first) * (D / 8); c += 32) {
+                            const int r = first + c / (D / 8), ch = c % (D / 8);
+                            *reinterpret_cast<int4*>(vt + (r >> 4) * L::kBlockBytes + ((r >> 3) & 1) * L::kGroupPitch + (ch >> 3) * 1024 + (r & 7) * 128 + (ch & 7) * 16) = make_int4(0, 0, 0, 0);
+                        }
+                    };
+                    if (z0 > 0 && (z0 & 15)) clear(z0 & ~15, z0);
+                    if (z1 < kTileKeys && (z1 & 15)) clear(z1, (z1 + 15) & ~15);
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(full + 8 * st);
+                }
+                if (!is_v && i == min(1, n - 1)) {
+                    // Q, behind the first K tiles, which need not wait for the last S of the piece before
+                    for (int b = 0; b < (dual ? 2 : 1); ++b) {
+                        if (n_q[b] > 0 && !wait(q_empty + 8 * b, n_q[b] - 1)) ok = false;
+                        ++n_q[b];
+                    }
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    if (lane < (dual ? 2 : 1)) {
+                        mbar_expect_tx(q_full + 8 * lane, a.T * a.G * D * 2);
+#pragma unroll
+                        for (int hh = 0; hh < L::kHalves; ++hh)
+                            tma_load_3d(smem0 + lane * L::kQ + hh * (kRows * 128), &a.q_map, hh * 64, w.head * a.G, w.u.row0 + lane * a.T, q_full + 8 * lane);
+                    }
+                    __syncwarp();
                 }
             }
-            for (int i = 16; i; i >>= 1) l += __shfl_xor_sync(0xffffffffu, l, i);
-            const float inv = l > 0.f ? 1.f / l : 0.f;
-            for (int i = 0; i < D / 32; ++i) {
-                const __nv_bfloat16 v = __float2bfloat16(acc[i] * inv);
-                a.o[orow * D + lane + 32 * i] = *reinterpret_cast<const uint16_t*>(&v);
-            }
-            if (a.lse && lane == 0) a.lse[orow] = m_run == -INFINITY ? -INFINITY : m_run + logf(l);
+        }
+        __syncwarp();
+        if (abort_s && lane == 0) {
+            // the CTA is giving up: copies that nobody waited for may still be landing; each barrier's latest phase gets a
+            // bounded wait of its own before the shared memory goes back to the SM
+            auto drain = [&](uint32_t bar, uint32_t count) {
+                for (uint32_t i = 0; i < limit; ++i)
+                    if (mbar_try(bar, count & 1)) break;
+            };
+            for (uint32_t back = 0; back < (uint32_t)stages && back < n_t; ++back) drain(full + 8 * ((n_t - 1 - back) % stages), (n_t - 1 - back) / stages);
+            if (is_v && n_land > 0) drain(v_land, n_land - 1);
+            for (int b = 0; b < 2 && !is_v; ++b)
+                if (n_q[b] > 0) drain(q_full + 8 * b, n_q[b] - 1);
         }
     }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kWarpIssue) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kTmemColsA) : "memory");
+    if (tid == 0 && abort_s) atomicOr(a.status, STATUS_TIMEOUT);
+}
+
+// Joins the pieces of the units that CTA boundaries cut: boundary c cuts unit (unit, head) when CTA c starts inside it, and
+// the first such boundary of a unit does the work for all of them.  Pieces are read in walking order, so the result does not
+// depend on timing.  A thread = four dims of one row at a time.
+constexpr int kJoinThreads = 256, kJoinSlices = 4;
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads)
+chunk_join_kernel(const __grid_constant__ ChunkPlan p, uint16_t* __restrict__ o, float* __restrict__ lse, int32_t Hq, int32_t Hkv, int32_t G, int32_t T) {
+    const int c = blockIdx.x + 1;
+    pdl_wait();
+    if (p.header->magic != kMagic || p.header->max_rows != p.max_rows || p.header->n_ctas != p.n_ctas) return;
+    const ChunkStart cut = p.starts[c], before = p.starts[c - 1];
+    auto same = [&](const ChunkStart& x) { return x.unit == cut.unit && x.head == cut.head && x.tile > 0; };
+    if (cut.tile == 0 || same(before)) return;
+    const ChunkUnit u = p.units[cut.unit];
+    int end = c;                                       // CTAs c .. end - 1 start inside the unit
+    while (end < p.n_ctas && same(p.starts[end])) ++end;
+    for (int e = blockIdx.y * kJoinThreads + threadIdx.x; e < u.ntok * G * (D / 4); e += kJoinSlices * kJoinThreads) {
+        const int r = e / (D / 4), d4 = e % (D / 4), t = r / G, g = r - t * G;
+        const int64_t in = (int64_t)(t / T) * kRows + (t % T) * G + g;                  // row of a partial slot
+        float m = -INFINITY, l = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = c - 1; k < end; ++k) {
+            if (k >= c) {                              // a CTA without work left nothing
+                const ChunkStart x = p.starts[k], y = p.starts[k + 1];
+                if (x.unit == y.unit && x.head == y.head && x.tile == y.tile) continue;
+            }
+            const int64_t at = (int64_t)(k < c ? 2 * k + 1 : 2 * k) * 2 * kRows + in;
+            const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + at * 2);
+            const float4 v = *reinterpret_cast<const float4*>(p.part_acc + at * D + d4 * 4);
+            if (ml.x == -INFINITY) continue;           // this piece holds no key the row sees
+            const float top = fmaxf(m, ml.x), f = m == -INFINITY ? 0.f : exp2f(m - top), x = exp2f(ml.x - top);
+            acc.x = acc.x * f + v.x * x, acc.y = acc.y * f + v.y * x, acc.z = acc.z * f + v.z * x, acc.w = acc.w * f + v.w * x;
+            l = l * f + ml.y * x;
+            m = top;
+        }
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const int64_t orow = (int64_t)(u.row0 + t) * Hq + cut.head * G + g;
+        *reinterpret_cast<uint2*>(o + orow * D + d4 * 4) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+        if (lse && d4 == 0) lse[orow] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * kLn2;
+    }
+}
+
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn tensor_map_encoder() {
+    static const EncodeFn f = [] {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) fn = nullptr;
+        return reinterpret_cast<EncodeFn>(fn);
+    }();
+    return f;
+}
+bool encode(CUtensorMap* map, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+    const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
+    const EncodeFn f = tensor_map_encoder();
+    return f && f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// A slab as [tile = (block, K|V, kv head)][8-key group][64-dim half][key][dim]; the box is one tile.
+bool kv_map5(CUtensorMap* map, const void* slab, const Shape& s) {
+    const cuuint64_t D = s.D;
+    const cuuint64_t dims[5] = {64, 8, D / 64, 2, (cuuint64_t)s.num_blocks * 2 * s.Hkv};
+    const cuuint64_t strides[4] = {D * 2, 128, 8 * D * 2, 16 * D * 2};
+    const cuuint32_t box[5] = {64, 8, (cuuint32_t)(D / 64), 2, 1};
+    return encode(map, slab, 5, dims, strides, box);
+}
+// The queries as [row][head][dim]; the box is T tokens of a kv head's G heads, 64 dims.
+bool q_map3(CUtensorMap* map, const void* q, const Shape& s, int64_t rows, int64_t stride, int G, int T) {
+    const cuuint64_t dims[3] = {(cuuint64_t)s.D, (cuuint64_t)s.Hq, (cuuint64_t)rows};
+    const cuuint64_t strides[2] = {(cuuint64_t)s.D * 2, (cuuint64_t)stride * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)G, (cuuint32_t)T};
+    return encode(map, q, 3, dims, strides, box);
+}
+
+template <int D, int MODE>
+cudaError_t allow_smem() {
+    return cudaFuncSetAttribute(chunk_attn_kernel<D, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::kBytes);
+}
+template <int D>
+cudaError_t allow_smem_all() {
+    cudaError_t e = allow_smem<D, 0>();
+    if (e == cudaSuccess) e = allow_smem<D, MODE_CAP>();
+    if (e == cudaSuccess) e = allow_smem<D, MODE_BIAS>();
+    if (e == cudaSuccess) e = allow_smem<D, MODE_CAP | MODE_BIAS>();
+    return e;
+}
+template <int D>
+cudaError_t launch_attn_d(const AttnArgs& a, int mode, int n_ctas, cudaStream_t st) {
+    const dim3 grid(n_ctas), block(kThreadsA);
+    const size_t smem = Smem<D>::kBytes;
+    switch (mode) {
+        case 0: chunk_attn_kernel<D, 0><<<grid, block, smem, st>>>(a); break;
+        case MODE_CAP: chunk_attn_kernel<D, MODE_CAP><<<grid, block, smem, st>>>(a); break;
+        case MODE_BIAS: chunk_attn_kernel<D, MODE_BIAS><<<grid, block, smem, st>>>(a); break;
+        default: chunk_attn_kernel<D, MODE_CAP | MODE_BIAS><<<grid, block, smem, st>>>(a); break;
+    }
+    return cudaGetLastError();
 }
 
 }  // namespace
@@ -293,7 +796,10 @@ size_t chunk_plan_layout(ChunkPlan* p, void* base, const Shape& s, int32_t max_b
 }
 
 cudaError_t chunk_attn_init() {
-    return cudaFuncSetAttribute(chunk_split_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kCostSmem * (int)sizeof(int64_t));
+    cudaError_t e = cudaFuncSetAttribute(chunk_split_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kCostSmem * (int)sizeof(int64_t));
+    if (e == cudaSuccess) e = allow_smem_all<128>();
+    if (e == cudaSuccess) e = allow_smem_all<64>();
+    return e;
 }
 
 cudaError_t launch_chunk_plan(const ChunkPlan& p, const Shape& s, int32_t batch, const int64_t* q_indptr, const int32_t* ctx_len,
@@ -314,12 +820,27 @@ cudaError_t launch_chunk_plan(const ChunkPlan& p, const Shape& s, int32_t batch,
 }
 
 cudaError_t launch_chunk_attn(const ChunkPlan& p, const ChunkAttnLaunch& l, cudaStream_t stream, int* launched) {
-    const AttnArgs a{p, l.slab, l.q, l.q_stride, l.o, l.lse, l.kv_indices, l.scale, l.softcap, l.slopes, l.status, l.shape.Hq, l.shape.Hkv, l.shape.num_blocks};
-    const dim3 grid((unsigned)(p.max_units < 4096 ? p.max_units : 4096), l.shape.Hkv);
-    if (l.shape.D == 128) chunk_attn_rows_kernel<128><<<grid, 256, 0, stream>>>(a);
-    else chunk_attn_rows_kernel<64><<<grid, 256, 0, stream>>>(a);
+    AttnArgs a{};
+    a.G = l.shape.Hq / l.shape.Hkv;
+    a.T = kRows / a.G;
+    if (!kv_map5(&a.kv_map, l.slab, l.shape) || !q_map3(&a.q_map, l.q, l.shape, p.max_rows, l.q_stride, a.G, a.T)) return cudaErrorNotSupported;
+    a.p = p;
+    a.o = l.o, a.lse = l.lse, a.kv_indices = l.kv_indices, a.slopes = l.slopes;
+    a.sc = l.softcap > 0.f ? l.scale / l.softcap : l.scale * kLog2e;
+    a.cap = l.softcap * kLog2e;
+    a.status = l.status;
+    a.Hq = l.shape.Hq, a.Hkv = l.shape.Hkv, a.num_blocks = l.shape.num_blocks;
+    a.wait_budget = l.wait_budget;
+    const int mode = (l.softcap > 0.f ? MODE_CAP : 0) | (l.slopes ? MODE_BIAS : 0);
+    cudaError_t e = l.shape.D == 128 ? launch_attn_d<128>(a, mode, p.n_ctas, stream) : launch_attn_d<64>(a, mode, p.n_ctas, stream);
+    if (e != cudaSuccess) return e;
     *launched = 1;
-    return cudaGetLastError();
+    if (p.n_ctas < 2) return e;
+    const dim3 grid(p.n_ctas - 1, kJoinSlices);
+    e = l.shape.D == 128 ? launch_kernel(chunk_join_kernel<128>, grid, dim3(kJoinThreads), 0, stream, true, p, l.o, l.lse, a.Hq, a.Hkv, a.G, a.T)
+                         : launch_kernel(chunk_join_kernel<64>, grid, dim3(kJoinThreads), 0, stream, true, p, l.o, l.lse, a.Hq, a.Hkv, a.G, a.T);
+    if (e == cudaSuccess) *launched = 2;
+    return e;
 }
 
 }  // namespace nsd

@@ -206,8 +206,10 @@ constexpr int kBlocks = kTileKeys / kBsA;
 constexpr int kThreadsA = 384;
 constexpr int kWarpIssue = 8, kWarpK = 10, kWarpV = 11;
 constexpr float kMaxSlack = 8.0f;                      // the running maximum may lag the true one by this much (log2 units)
-constexpr uint32_t kSpinLimit = 1u << 20;              // wait slices of ~2 us each
+constexpr uint32_t kPollLimit = 1u << 30;              // polls of one wait, if nsd_config.wait_budget does not say
+constexpr int kPoly = 6;                               // of 16 pairs of exponentials, those that go to the FMA pipes
 enum : int { MODE_CAP = 1, MODE_BIAS = 2 };
+template <bool B> struct Const { __device__ constexpr bool operator()() const { return B; } };
 
 struct AttnArgs {
     CUtensorMap kv_map, q_map;
@@ -233,7 +235,7 @@ struct Smem {
     static constexpr int kOffK = 2 * kQ, kOffV = kOffK + kKStages * kTile;
     static constexpr int kOffMl = kOffV + kVStages * kTile;              // stream 1's statistics for the join
     static constexpr int kOffBars = kOffMl + kRows * 8;
-    static constexpr int kNumBars = 2 * kKStages + 2 * kVStages + 1 + 4 + 2 + 4 + 2 + 2;
+    static constexpr int kNumBars = 3 * kKStages + 3 * kVStages + 1 + 4 + 2 + 4 + 2 + 2;
     static constexpr int kOffMisc = kOffBars + kNumBars * 8;
     static constexpr int kBytes = kOffMisc + 16;
     static_assert(kBytes <= 227 * 1024, "shared memory budget");
@@ -269,6 +271,81 @@ struct Walk {
     }
 };
 
+// A bounded wait of a whole warp.  Unlike mbar_wait it gives the hardware no time slice: a barrier that is ready then costs
+// 78 cycles instead of 113, and a signal from one warp to another as much instead of 112.  The bound is a number of polls
+// (limit) and, since a poll may sleep, a time: about four seconds of SM clocks.
+constexpr long long kWaitCycles = 1ll << 33;
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
+}
+__device__ __forceinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t limit) {
+    const long long t0 = clock64();
+    for (uint32_t i = 0; i < limit; ++i) {
+        if (bar_try(bar, parity)) return true;
+        if (*abort_flag) return false;
+        if (clock64() - t0 > kWaitCycles) break;
+    }
+    *abort_flag = 1;
+    return false;
+}
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p)::"memory");
+    return p;
+}
+// Named barriers of two warps: one arrives, the other waits.  18 cycles where an mbarrier takes 78.
+__device__ __forceinline__ void pair_arrive(int id) { asm volatile("barrier.arrive %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ void pair_wait(int id) { asm volatile("barrier.sync %0, 64;" ::"r"(id) : "memory"); }
+
+// Two floats in one 64-bit register pair: the packed FMA, add and multiply of sm_100 do both in one issue slot.
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+// 2^x for a pair without the MUFU unit, x <= 127: x = n + d with n the nearest integer (found by adding 1.5 * 2^23, whose
+// low bits then hold n), 2^d on [-1/2, 1/2] by a cubic fitted to least relative error in the mean square (at most
+// 1.4e-4 of the value, 2e-9 in the mean), n added to the exponent bits.  Below 2^-126 it stays at 2^-126.
+__device__ __forceinline__ uint64_t exp2_pair(uint64_t x) {
+    float2 v = unpair(x);
+    v.x = max_nan(v.x, -126.f), v.y = max_nan(v.y, -126.f);
+    x = pair(v.x, v.y);
+    const uint64_t t = add2(x, pair(12582912.f, 12582912.f));
+    const uint64_t d = fma2(add2(t, pair(-12582912.f, -12582912.f)), pair(-1.f, -1.f), x);
+    uint64_t p = fma2(pair(0.055029310286045074f, 0.055029310286045074f), d, pair(0.24225680530071259f, 0.24225680530071259f));
+    p = fma2(p, d, pair(0.6932530403137207f, 0.6932530403137207f));
+    p = fma2(p, d, pair(0.9999513626098633f, 0.9999513626098633f));
+    const float2 pp = unpair(p), tt = unpair(t);
+    return pair(__uint_as_float(__float_as_uint(pp.x) + (__float_as_uint(tt.x) << 23)), __uint_as_float(__float_as_uint(pp.y) + (__float_as_uint(tt.y) << 23)));
+}
+
 __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, int32_t tile, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %2, %2, %2, %3}], [%4];"
                  ::"r"(dst), "l"(map), "r"(0), "r"(tile), "r"(bar)
@@ -293,7 +370,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
         return;
     }
     const uint32_t bar0 = smem0 + L::kOffBars;
-    const uint32_t k_full = bar0, k_empty = k_full + 8 * L::kKStages, v_full = k_empty + 8 * L::kKStages, v_empty = v_full + 8 * L::kVStages;
+    const uint32_t k_full = bar0, k_empty = k_full + 16 * L::kKStages, v_full = k_empty + 8 * L::kKStages, v_empty = v_full + 16 * L::kVStages;
     const uint32_t v_land = v_empty + 8 * L::kVStages; // a V tile whose hidden rows have to be cleared lands here first
     const uint32_t q_full = v_land + 8, q_empty = q_full + 16;                          // [2] per Q buffer
     const uint32_t s_full = q_empty + 16, p_full = s_full + 16, o_full = p_full + 32;   // [2], [2][2 halves], [2] per stream
@@ -302,11 +379,11 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
     volatile int& abort_s = *reinterpret_cast<volatile int*>(smem + L::kOffMisc + 4);
     float2* const ml_s = reinterpret_cast<float2*>(smem + L::kOffMl);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t limit = a.wait_budget ? a.wait_budget : kSpinLimit;
+    const uint32_t limit = a.wait_budget ? a.wait_budget : kPollLimit;
 
     if (tid == 0) {
-        for (int s = 0; s < L::kKStages; ++s) mbar_init(k_full + 8 * s, 1), mbar_init(k_empty + 8 * s, 2);
-        for (int s = 0; s < L::kVStages; ++s) mbar_init(v_full + 8 * s, 1), mbar_init(v_empty + 8 * s, 2);
+        for (int s = 0; s < L::kKStages; ++s) mbar_init(k_full + 16 * s, 1), mbar_init(k_full + 16 * s + 8, 1), mbar_init(k_empty + 8 * s, 2);
+        for (int s = 0; s < L::kVStages; ++s) mbar_init(v_full + 16 * s, 1), mbar_init(v_full + 16 * s + 8, 1), mbar_init(v_empty + 8 * s, 2);
         mbar_init(v_land, 1);
         for (int s = 0; s < 2; ++s) {
             mbar_init(q_full + 8 * s, 1), mbar_init(q_empty + 8 * s, 2);
@@ -325,10 +402,26 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_base_s;
-    auto wait = [&](uint32_t bar, uint32_t count) { return mbar_wait(bar, count & 1, &abort_s, limit); };   // the count-th completion
+    // the count-th completion; the same answer in every lane
+    auto wait = [&](uint32_t bar, uint32_t count) {
+        bool ok = bar_try(bar, count & 1);
+        if (__all_sync(0xffffffffu, ok)) return true;
+        ok = bar_wait_slow(bar, count & 1, &abort_s, limit);
+        return (bool)__all_sync(0xffffffffu, ok);
+    };
+
+    // A ring's stage has two "full" barriers, for its even and its odd uses.  A wait by parity takes a phase that has not begun
+    // for the one two before it; with alternate tiles an issuer does not watch every use of a stage, and one that runs ahead of
+    // the other could so take a tile that is still in flight for landed.  The use two before is its own stream's, or lies
+    // behind the last Q load, which follows every S of the piece before: that one it knows complete.
+    auto full_bar = [](uint32_t full, uint32_t tile, uint32_t stages) { return full + 16 * (tile % stages) + 8 * ((tile / stages) & 1); };
+    auto full_phase = [](uint32_t tile, uint32_t stages) { return tile / stages / 2; };
 
     if (warp < kWarpIssue) {
         // ================================ softmax and output ================================
+        // A row's 128 scores stay in registers.  The block was launched with 384 x 168 registers; the warpgroup of issuers
+        // and producers gives up 104 of each thread's, the two softmax warpgroups take 48: 128 x 64 + 256 x 216 <= 384 x 168.
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         const int s = warp >> 2, q = warp & 3;
         const uint32_t lanes = (uint32_t)(q * 32) << 16;
         const uint32_t tmem_s = tmem + s * 128 + lanes, tmem_o = tmem + kTmemOBase + s * 128 + lanes;
@@ -336,9 +429,19 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
         uint32_t n_s = 0, n_o[2] = {0, 0}, n_x = 0;    // completions seen so far
         bool fail = false;
         auto wait_all = [&](uint32_t bar, uint32_t count) {
-            if (!wait(bar, count)) fail = true;
-            fail = __any_sync(0xffffffffu, fail);
+            fail = !wait(bar, count);
             return !fail;
+        };
+        // The two warps of a scheduler, one of each stream, take turns at the exponentials of units of two row tiles, stream 0
+        // first: named barriers 1 .. 8.  A warp that gives up hands its turn on, and nobody waits for one once the abort flag
+        // is up.
+        const int my_turn = 1 + 2 * q + s, your_turn = 1 + 2 * q + (s ^ 1);
+        bool first_turn = s == 0;
+        auto take_turn = [&] {
+            fail = __any_sync(0xffffffffu, abort_s != 0);
+            if (fail) return;
+            if (!first_turn) pair_wait(my_turn);
+            first_turn = false;
         };
         while (!fail && w.next()) {
             const int n = w.k1 - w.k0;
@@ -362,74 +465,149 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                 tc_fence_after();
                 if (warp_live) {
                     const int key0 = (t_hi - 1 - (w.k0 + i)) * kTileKeys;
-                    uint32_t x[kTileKeys];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_ld32(tmem_s + c * 32, x + c * 32);
-                    tmem_wait_ld();
-                    float f = a.sc;                                                     // from x to the log2 domain
-                    if constexpr (MODE & MODE_CAP) {
-                        f = 1.f;
-#pragma unroll
-                        for (int j = 0; j < kTileKeys; ++j) x[j] = __float_as_uint(a.cap * tanhf(__uint_as_float(x[j]) * a.sc));
-                    }
-                    if constexpr (MODE & MODE_BIAS) {
-                        const float b = slope * (float)(key0 - pos);
-#pragma unroll
-                        for (int j = 0; j < kTileKeys; ++j) x[j] = __float_as_uint(fmaf(__uint_as_float(x[j]), f, fmaf(slope, (float)j, b)));
-                        f = 1.f;
-                    }
                     const int v0 = lo - key0, v1 = hi - key0;                           // visible: v0 <= j < v1
-                    if (__any_sync(0xffffffffu, v0 > 0 || v1 < kTileKeys)) {
+                    const bool masked = __any_sync(0xffffffffu, v0 > 0 || v1 < kTileKeys);
+                    constexpr bool kRaw = MODE == 0;                                    // x is q . k: the scale is part of the exponent's FFMA
+                    const float f = kRaw ? a.sc : 1.f;
+                    // The 128 scores come in four pieces of 32, each asked for while the one before is worked on: fewer registers
+                    // than all at once, and the exponentials start after the first.
+                    uint32_t x[4][32];
+                    float mx;
+                    auto ask = [&](int c) { tmem_ld32(tmem_s + c * 32, x[c]); };
+                    auto scores = [&](int c) {                                          // to what the softmax is of, and their maximum
+                        if constexpr (MODE & MODE_CAP) {
 #pragma unroll
-                        for (int j = 0; j < kTileKeys; ++j) x[j] = j >= v0 && j < v1 ? x[j] : 0xff800000u;
-                    }
-                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                            for (int j = 0; j < 32; ++j) x[c][j] = __float_as_uint(a.cap * tanhf(__uint_as_float(x[c][j]) * a.sc));
+                        }
+                        if constexpr (MODE & MODE_BIAS) {
+                            const float b = slope * (float)(key0 - pos + c * 32), sc = MODE & MODE_CAP ? 1.f : a.sc;
 #pragma unroll
-                    for (int j = 0; j < kTileKeys; j += 8)
+                            for (int j = 0; j < 32; ++j) x[c][j] = __float_as_uint(fmaf(__uint_as_float(x[c][j]), sc, fmaf(slope, (float)j, b)));
+                        }
+                        if (masked) {
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) mx[c] = fmaxf(fmaxf(mx[c], __uint_as_float(x[j + c])), __uint_as_float(x[j + 4 + c]));
-                    const float m_tile = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * f;
-                    const bool outgrown = m_tile > m_run + kMaxSlack;                   // also the first visible key
-                    if (__any_sync(0xffffffffu, outgrown)) {
-                        const float m_new = outgrown ? m_tile : m_run;
-                        const float r = outgrown ? (m_run == -INFINITY ? 0.f : ex2_approx(m_run - m_new)) : 1.f;
-                        if (mine > 0) {
-                            // O holds this piece's earlier tiles, complete since S of this one is
-#pragma unroll 1
-                            for (int c = 0; c < D; c += 16) {
-                                uint32_t y[16];
-                                tmem_ld16(tmem_o + c, y);
-                                tmem_wait_ld();
+                            for (int j = 0; j < 32; ++j) x[c][j] = c * 32 + j >= v0 && c * 32 + j < v1 ? x[c][j] : 0xff800000u;
+                        }
+                        float m0 = mx, m1 = -INFINITY;
 #pragma unroll
-                                for (int j = 0; j < 16; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * r);
-                                tmem_st16(tmem_o + c, y);
+                        for (int j = 0; j < 32; j += 4) {
+                            m0 = fmaxf(fmaxf(m0, __uint_as_float(x[c][j])), __uint_as_float(x[c][j + 1]));
+                            m1 = fmaxf(fmaxf(m1, __uint_as_float(x[c][j + 2])), __uint_as_float(x[c][j + 3]));
+                        }
+                        mx = fmaxf(m0, m1);
+                    };
+                    float nm = 0.f;
+                    uint64_t l2 = 0;                                                    // the tile's sums of even and odd keys
+                    // 32 scores become 16 words of P.  The MUFU unit takes 8 cycles for a warp's exponential, 1024 for a tile:
+                    // as long as the tile's two products, for either stream.  So in full tiles of a unit of two row tiles kPoly
+                    // of 16 pairs go to the FMA pipes instead.  Tiles with hidden keys keep to the MUFU unit: -inf needs
+                    // its exact zero, and rows of few keys its precision.
+                    const bool full = dual && !masked;
+                    auto weights = [&](int c, bool mixed) {
+                        const uint64_t f2 = pair(f, f), nm2 = pair(nm, nm);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            uint64_t e = fma2(pair(__uint_as_float(x[c][2 * j]), __uint_as_float(x[c][2 * j + 1])), f2, nm2);
+                            float2 p;
+                            if (mixed && (j * kPoly) % 16 < kPoly) {
+                                e = exp2_pair(e);
+                                p = unpair(e);
+                            } else {
+                                p = unpair(e);
+                                p.x = ex2_approx(p.x), p.y = ex2_approx(p.y);
+                                e = pair(p.x, p.y);
                             }
-                            tmem_wait_st();
+                            l2 = add2(l2, e);
+                            x[c][j] = pack_bf16(p.x, p.y);
                         }
-                        l_run *= r;
-                        m_run = m_new;
-                    }
-                    const float nm = m_run == -INFINITY ? 0.f : -m_run;
-                    float l[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        uint32_t p[32];
-#pragma unroll
-                        for (int j = 0; j < 64; j += 2) {
-                            const float p0 = ex2_approx(fmaf(__uint_as_float(x[half * 64 + j]), f, nm));
-                            const float p1 = ex2_approx(fmaf(__uint_as_float(x[half * 64 + j + 1]), f, nm));
-                            l[(j >> 1) & 1] += p0;
-                            l[2 + ((j >> 1) & 1)] += p1;
-                            p[j >> 1] = pack_bf16(p0, p1);
-                        }
-                        tmem_st32(tmem_s + half * 32, p);
+                    };
+                    auto hand_over = [&](int half) {
+                        tmem_st16(tmem_s + half * 32, x[2 * half]);
+                        tmem_st16(tmem_s + half * 32 + 16, x[2 * half + 1]);
                         tmem_wait_st();
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(p_full + 16 * s + 8 * half);
+                    };
+                    if (mine == 0) {                                                    // the piece's first tile sets the maximum
+                        mx = -INFINITY;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            ask(c);
+                            tmem_wait_ld();
+                            scores(c);
+                        }
+                        m_run = mx * f;
                     }
-                    l_run += (l[0] + l[1]) + (l[2] + l[3]);
+                    // From then on the weights of the first half are formed with the maximum as it stands while the tile's own is
+                    // being found; where that exceeds it by more than the slack (rare) the scores, still in tensor memory, are
+                    // read again.
+                    nm = m_run == -INFINITY ? 0.f : -m_run;
+                    mx = -INFINITY;
+                    ask(0);
+                    tmem_wait_ld();
+                    ask(1);
+                    scores(0);
+                    if (dual) {
+                        take_turn();
+                        if (fail) break;
+                    }
+                    auto body = [&](auto mixed) {
+                        weights(0, mixed());
+                        tmem_wait_ld();
+                        ask(2);
+                        scores(1);
+                        weights(1, mixed());
+                        tmem_wait_ld();
+                        ask(3);
+                        scores(2);
+                        tmem_wait_ld();
+                        scores(3);
+                        const float m_tile = mx * f;
+                        const bool outgrown = m_tile > m_run + kMaxSlack;
+                        if (__any_sync(0xffffffffu, outgrown)) {
+                            const float m_new = outgrown ? m_tile : m_run;
+                            const float r = outgrown ? (m_run == -INFINITY ? 0.f : ex2_approx(m_run - m_new)) : 1.f;
+                            // O holds this piece's earlier tiles, complete since S of this one is (after the first tile only)
+                            if (mine > 0) {
+#pragma unroll 1
+                                for (int c = 0; c < D; c += 16) {
+                                    tmem_ld16(tmem_o + c, x[0]);
+                                    tmem_wait_ld();
+#pragma unroll
+                                    for (int j = 0; j < 16; ++j) x[0][j] = __float_as_uint(__uint_as_float(x[0][j]) * r);
+                                    tmem_st16(tmem_o + c, x[0]);
+                                }
+                                tmem_wait_st();
+                            }
+                            l_run *= r;
+                            m_run = m_new;
+                            nm = m_run == -INFINITY ? 0.f : -m_run;
+                            l2 = 0;
+                            ask(0);
+                            ask(1);
+                            tmem_wait_ld();
+                            scores(0);
+                            weights(0, false);
+                            scores(1);
+                            weights(1, false);
+                        }
+                        hand_over(0);
+                        weights(2, mixed());
+                        weights(3, mixed());
+                        if (dual) pair_arrive(your_turn);
+                        hand_over(1);
+                    };
+                    if (full) body(Const<true>());
+                    else body(Const<false>());
+                    const float2 l = unpair(l2);
+                    l_run += l.x + l.y;
                 } else {
+                    if (dual) {
+                        take_turn();
+                        if (fail) break;
+                        pair_arrive(your_turn);
+                    }
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(p_full + 16 * s), mbar_arrive(p_full + 16 * s + 8);
@@ -469,32 +647,32 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                 const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
                 if (!part) r0 *= inv, r1 *= inv;
 #pragma unroll 1
-                for (int c = 0; c < D; c += 32) {
-                    uint32_t y[32], z[32];
+                for (int c = 0; c < D; c += 16) {
+                    uint32_t y[16], z[16];
                     if (n > 0) {
-                        tmem_ld32(tmem_o + c, y);
-                        if (two) tmem_ld32(tmem_o + 128 + c, z);
+                        tmem_ld16(tmem_o + c, y);
+                        if (two) tmem_ld16(tmem_o + 128 + c, z);
                         tmem_wait_ld();
                     }
                     if (live) {
                         // a weight of zero means that the stream saw nothing: its O may be anything
-    #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
                             float v = r0 > 0.f && n > 0 ? __uint_as_float(y[j]) * r0 : 0.f;
                             if (two && r1 > 0.f) v = fmaf(__uint_as_float(z[j]), r1, v);
                             y[j] = __float_as_uint(v);
                         }
                         if (part) {
                             float4* pa = reinterpret_cast<float4*>(a.p.part_acc + prow * D + c);
-    #pragma unroll
-                            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
                                 pa[j] = make_float4(__uint_as_float(y[4 * j]), __uint_as_float(y[4 * j + 1]), __uint_as_float(y[4 * j + 2]), __uint_as_float(y[4 * j + 3]));
                         } else {
                             uint4* po = reinterpret_cast<uint4*>(a.o + orow * D + c);
-    #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
                                 uint32_t k[4];
-    #pragma unroll
+#pragma unroll
                                 for (int i = 0; i < 4; ++i) k[i] = pack_bf16(__uint_as_float(y[8 * j + 2 * i]), __uint_as_float(y[8 * j + 2 * i + 1]));
                                 po[j] = make_uint4(k[0], k[1], k[2], k[3]);
                             }
@@ -509,62 +687,71 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             __syncwarp();
             if (join && lane == 0) mbar_arrive(x_done);
         }
-    } else if (warp < kWarpK) {
+        if (fail) pair_arrive(your_turn);
+    } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (warp < kWarpK) {
         // ================================ MMA issuers ================================
         const int s = warp - kWarpIssue;
-        if (lane == 0) {
-            const uint32_t idesc_s = instr_desc(kRows, kTileKeys, 0, 0), idesc_o = instr_desc(kRows, D, 0, 1);
-            const uint32_t tmem_s = tmem + s * 128, tmem_o = tmem + kTmemOBase + s * 128;
-            uint32_t n_k = 0, n_p = 0, n_q[2] = {0, 0};
-            bool ok = true;
-            while (ok && w.next()) {
-                const int n = w.k1 - w.k0;
-                if (n == 0) continue;
-                const bool dual = w.u.ntok > a.T;
-                const int qb = dual ? s : 0, step = dual ? 1 : 2, i0 = dual ? 0 : s;
-                if (!(ok = wait(q_full + 8 * qb, n_q[qb]))) break;
-                ++n_q[0];
-                if (dual) ++n_q[1];
-                if (i0 >= n) mbar_arrive(q_empty);                                      // a single key tile: nothing for stream 1
-                const uint32_t q_s = smem0 + qb * L::kQ;
-                for (int i = i0; i < n; i += step, ++n_p) {
-                    const uint32_t c = n_k + i, ks = c % L::kKStages, vs = c % L::kVStages;
-                    const bool last = i + step >= n;
-                    if (!(ok = wait(k_full + 8 * ks, c / L::kKStages))) break;
-                    tc_fence_after();
-                    const uint32_t kb = smem0 + L::kOffK + ks * L::kTile;
+        auto wait_full = [&](uint32_t full, uint32_t tile, uint32_t stages) { return wait(full_bar(full, tile, stages), full_phase(tile, stages)); };
+        const uint32_t idesc_s = instr_desc(kRows, kTileKeys, 0, 0), idesc_o = instr_desc(kRows, D, 0, 1);
+        const uint32_t tmem_s = tmem + s * 128, tmem_o = tmem + kTmemOBase + s * 128;
+        uint32_t n_k = 0, n_p = 0, n_q[2] = {0, 0};
+        bool ok = true;
+        // The whole warp waits, one elected thread issues: a branch of one lane around the waits costs hundreds of cycles.
+        while (ok && w.next()) {
+            const int n = w.k1 - w.k0;
+            if (n == 0) continue;
+            const bool dual = w.u.ntok > a.T;
+            const int qb = dual ? s : 0, step = dual ? 1 : 2, i0 = dual ? 0 : s;
+            if (!(ok = wait(q_full + 8 * qb, n_q[qb]))) break;
+            ++n_q[0];
+            if (dual) ++n_q[1];
+            if (i0 >= n && lane == 0) mbar_arrive(q_empty);                             // a single key tile: nothing for stream 1
+            const uint32_t q_s = smem0 + qb * L::kQ;
+            for (int i = i0; i < n; i += step, ++n_p) {
+                const uint32_t c = n_k + i, ks = c % L::kKStages, vs = c % L::kVStages;
+                const bool last = i + step >= n;
+                if (!(ok = wait_full(k_full, c, L::kKStages))) break;
+                tc_fence_after();
+                const uint32_t kb = smem0 + L::kOffK + ks * L::kTile;
+                if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k) {                                  // 16 dims each, 64 per swizzled half
                         const uint64_t da = smem_desc(q_s + (k >> 2) * (kRows * 128) + (k & 3) * 32, 16, 1024, 2);
                         const uint64_t db = smem_desc(kb + (k >> 2) * 1024 + (k & 3) * 32, 16, L::kGroupPitch, 2);
                         umma_ss(tmem_s, da, db, idesc_s, k > 0);
                     }
-                    umma_commit(k_empty + 8 * ks);
                     umma_commit(s_full + 8 * s);
+                    umma_commit(k_empty + 8 * ks);
                     if (!dual) mbar_arrive(k_empty + 8 * ks);                           // the other stream has no use for this tile
                     if (last) {
                         umma_commit(q_empty + 8 * qb);
                         if (dual) mbar_arrive(q_empty + 8 * qb);
                     }
-                    if (!(ok = wait(v_full + 8 * vs, c / L::kVStages))) break;
-                    const uint32_t vb = smem0 + L::kOffV + vs * L::kTile;
+                }
+                if (!(ok = wait_full(v_full, c, L::kVStages))) break;
+                const uint32_t vb = smem0 + L::kOffV + vs * L::kTile;
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        if (!(ok = wait(p_full + 16 * s + 8 * half, n_p))) break;
-                        tc_fence_after();
+                for (int half = 0; half < 2; ++half) {
+                    if (!(ok = wait(p_full + 16 * s + 8 * half, n_p))) break;
+                    tc_fence_after();
+                    if (elect_one()) {
 #pragma unroll
                         for (int k = half * 4; k < half * 4 + 4; ++k) {                 // 16 keys each: a block of V, 8 columns of P
                             const uint64_t db = smem_desc(vb + k * L::kBlockBytes, 1024, L::kGroupPitch, 2);
                             umma_ts(tmem_o, tmem_s + k * 8, db, idesc_o, (i > i0 || k > 0) ? 1u : 0u);
                         }
+                        if (half == 1) {
+                            umma_commit(v_empty + 8 * vs);
+                            if (!dual) mbar_arrive(v_empty + 8 * vs);
+                            if (last) umma_commit(o_full + 8 * s);
+                        }
                     }
-                    if (!ok) break;
-                    umma_commit(v_empty + 8 * vs);
-                    if (!dual) mbar_arrive(v_empty + 8 * vs);
-                    if (last) umma_commit(o_full + 8 * s);
                 }
-                n_k += n;
+                if (!ok) break;
             }
+            n_k += n;
         }
         __syncwarp();
     } else {
@@ -607,7 +794,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                 // cleared once the tile has landed (blocks without any are zero fill)
                 const int z0 = w.u.key_lo - t * kTileKeys, z1 = w.u.key_hi - t * kTileKeys;             // visible keys of the tile: [z0, z1)
                 const bool ragged = is_v && ((z0 > 0 && (z0 & 15)) || (z1 < kTileKeys && (z1 & 15)));
-                const uint32_t bar = ragged ? v_land : full + 8 * st;
+                const uint32_t full_now = full_bar(full, n_t, stages), bar = ragged ? v_land : full_now;
                 if (lane == 0) mbar_expect_tx(bar, L::kTile);
                 __syncwarp();
                 if (lane < kBlocks) tma_load_5d(ring + st * L::kTile + lane * L::kBlockBytes, &a.kv_map, tile, bar);
@@ -626,7 +813,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                     if (z1 < kTileKeys && (z1 & 15)) clear(z1, (z1 + 15) & ~15);
                     fence_async_smem();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(full + 8 * st);
+                    if (lane == 0) mbar_arrive(full_now);
                 }
                 if (!is_v && i == min(1, n - 1)) {
                     // Q, behind the first K tiles, which need not wait for the last S of the piece before
@@ -654,11 +841,12 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                 for (uint32_t i = 0; i < limit; ++i)
                     if (mbar_try(bar, count & 1)) break;
             };
-            for (uint32_t back = 0; back < (uint32_t)stages && back < n_t; ++back) drain(full + 8 * ((n_t - 1 - back) % stages), (n_t - 1 - back) / stages);
+            for (uint32_t back = 0; back < (uint32_t)stages && back < n_t; ++back) drain(full_bar(full, n_t - 1 - back, stages), full_phase(n_t - 1 - back, stages));
             if (is_v && n_land > 0) drain(v_land, n_land - 1);
             for (int b = 0; b < 2 && !is_v; ++b)
                 if (n_q[b] > 0) drain(q_full + 8 * b, n_q[b] - 1);
         }
+    }
     }
     tc_fence_before();
     __syncthreads();

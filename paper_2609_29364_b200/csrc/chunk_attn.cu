@@ -207,7 +207,6 @@ constexpr int kThreadsA = 384;
 constexpr int kWarpIssue = 8, kWarpK = 10, kWarpV = 11;
 constexpr float kMaxSlack = 8.0f;                      // the running maximum may lag the true one by this much (log2 units)
 constexpr uint32_t kPollLimit = 1u << 30;              // polls of one wait, if nsd_config.wait_budget does not say
-constexpr int kPoly = 6;                               // of 16 pairs of exponentials, those that go to the FMA pipes
 enum : int { MODE_CAP = 1, MODE_BIAS = 2 };
 template <bool B> struct Const { __device__ constexpr bool operator()() const { return B; } };
 
@@ -295,10 +294,15 @@ __device__ __forceinline__ uint32_t elect_one() {
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p)::"memory");
     return p;
 }
-// Named barriers of two warps: one arrives, the other waits.  18 cycles where an mbarrier takes 78.
-__device__ __forceinline__ void pair_arrive(int id) { asm volatile("barrier.arrive %0, 64;" ::"r"(id) : "memory"); }
-__device__ __forceinline__ void pair_wait(int id) { asm volatile("barrier.sync %0, 64;" ::"r"(id) : "memory"); }
-
+// Waits for this thread's tensor-memory loads; the registers of one of them are operands, so that no use of them can be moved
+// in front of the wait.
+__device__ __forceinline__ void tmem_wait_ld32(uint32_t* r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
+                   "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]),
+                   "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]),
+                   "+r"(r[31])::"memory");
+}
 // Two floats in one 64-bit register pair: the packed FMA, add and multiply of sm_100 do both in one issue slot.
 __device__ __forceinline__ uint64_t pair(float lo, float hi) {
     uint64_t r;
@@ -325,27 +329,48 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-__device__ __forceinline__ float max_nan(float a, float b) {
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
+// x becomes cap * tanh(x * sc) for 32 scores of a row.  Where every score of the warp's 32 rows allows, tanh(t) is t times a
+// polynomial in t^2 fitted to least relative error: degree 4 up to 3/4 (6e-7), degree 7 up to 3/2 (7e-7) -- no MUFU
+// instruction, of which 1 - 2 / (1 + e^2t), for the rest, takes two.  (tanh.approx is one, but off by 2^-11: times a cap of 30
+// to 50, one weight in fifty.)
+template <int N>
+__device__ __forceinline__ void cap32_poly(uint32_t* x, uint64_t sc2, uint64_t cap2, const float (&k)[N]) {
+#pragma unroll
+    for (int j = 0; j < 32; j += 2) {
+        const uint64_t t = mul2(pair(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), sc2), y = mul2(t, t);
+        uint64_t p = pair(k[N - 1], k[N - 1]);
+#pragma unroll
+        for (int i = N - 2; i >= 0; --i) p = fma2(p, y, pair(k[i], k[i]));
+        const float2 r = unpair(mul2(mul2(t, cap2), p));
+        x[j] = __float_as_uint(r.x), x[j + 1] = __float_as_uint(r.y);
+    }
 }
-// 2^x for a pair without the MUFU unit, x <= 127: x = n + d with n the nearest integer (found by adding 1.5 * 2^23, whose
-// low bits then hold n), 2^d on [-1/2, 1/2] by a cubic fitted to least relative error in the mean square (at most
-// 1.4e-4 of the value, 2e-9 in the mean), n added to the exponent bits.  Below 2^-126 it stays at 2^-126.
-__device__ __forceinline__ uint64_t exp2_pair(uint64_t x) {
-    float2 v = unpair(x);
-    v.x = max_nan(v.x, -126.f), v.y = max_nan(v.y, -126.f);
-    x = pair(v.x, v.y);
-    const uint64_t t = add2(x, pair(12582912.f, 12582912.f));
-    const uint64_t d = fma2(add2(t, pair(-12582912.f, -12582912.f)), pair(-1.f, -1.f), x);
-    uint64_t p = fma2(pair(0.055029310286045074f, 0.055029310286045074f), d, pair(0.24225680530071259f, 0.24225680530071259f));
-    p = fma2(p, d, pair(0.6932530403137207f, 0.6932530403137207f));
-    p = fma2(p, d, pair(0.9999513626098633f, 0.9999513626098633f));
-    const float2 pp = unpair(p), tt = unpair(t);
-    return pair(__uint_as_float(__float_as_uint(pp.x) + (__float_as_uint(tt.x) << 23)), __uint_as_float(__float_as_uint(pp.y) + (__float_as_uint(tt.y) << 23)));
+__device__ __forceinline__ void cap32(uint32_t* x, float sc, float cap) {
+    float big = 0.f, big1 = 0.f;
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+        big = fmaxf(fmaxf(big, fabsf(__uint_as_float(x[j]))), fabsf(__uint_as_float(x[j + 1])));
+        big1 = fmaxf(fmaxf(big1, fabsf(__uint_as_float(x[j + 2]))), fabsf(__uint_as_float(x[j + 3])));
+    }
+    big = fmaxf(big, big1) * sc;
+    const uint64_t sc2 = pair(sc, sc), cap2 = pair(cap, cap);
+    if (!__any_sync(0xffffffffu, big > 0.75f)) {
+        const float k[5] = {0.999999463558197f, -0.3332825303077698f, 0.13259011507034302f, -0.050057198852300644f, 0.01293052639812231f};
+        cap32_poly(x, sc2, cap2, k);
+    } else if (!__any_sync(0xffffffffu, big > 1.5f)) {
+        const float k[8] = {0.9999993443489075f, -0.33329400420188904f, 0.13294775784015656f, -0.0524834468960762f,
+                            0.018927596509456635f, -0.005435946863144636f, 0.001021950040012598f, -8.943479042500257e-05f};
+        cap32_poly(x, sc2, cap2, k);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            float r;
+            const float e = ex2_approx(__uint_as_float(x[j]) * (2.f * kLog2e * sc)) + 1.f;
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e));
+            x[j] = __float_as_uint(fmaf(-2.f * cap, r, cap));
+        }
+    }
 }
-
 __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, int32_t tile, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %2, %2, %2, %3}], [%4];"
                  ::"r"(dst), "l"(map), "r"(0), "r"(tile), "r"(bar)
@@ -378,7 +403,8 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
     uint32_t& tmem_base_s = *reinterpret_cast<uint32_t*>(smem + L::kOffMisc);
     volatile int& abort_s = *reinterpret_cast<volatile int*>(smem + L::kOffMisc + 4);
     float2* const ml_s = reinterpret_cast<float2*>(smem + L::kOffMl);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);                             // the compiler then knows it is the warp's
     const uint32_t limit = a.wait_budget ? a.wait_budget : kPollLimit;
 
     if (tid == 0) {
@@ -401,7 +427,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_base_s;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base_s, 0);
     // the count-th completion; the same answer in every lane
     auto wait = [&](uint32_t bar, uint32_t count) {
         bool ok = bar_try(bar, count & 1);
@@ -432,17 +458,6 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             fail = !wait(bar, count);
             return !fail;
         };
-        // The two warps of a scheduler, one of each stream, take turns at the exponentials of units of two row tiles, stream 0
-        // first: named barriers 1 .. 8.  A warp that gives up hands its turn on, and nobody waits for one once the abort flag
-        // is up.
-        const int my_turn = 1 + 2 * q + s, your_turn = 1 + 2 * q + (s ^ 1);
-        bool first_turn = s == 0;
-        auto take_turn = [&] {
-            fail = __any_sync(0xffffffffu, abort_s != 0);
-            if (fail) return;
-            if (!first_turn) pair_wait(my_turn);
-            first_turn = false;
-        };
         while (!fail && w.next()) {
             const int n = w.k1 - w.k0;
             const bool dual = w.u.ntok > a.T;
@@ -466,148 +481,105 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                 if (warp_live) {
                     const int key0 = (t_hi - 1 - (w.k0 + i)) * kTileKeys;
                     const int v0 = lo - key0, v1 = hi - key0;                           // visible: v0 <= j < v1
-                    const bool masked = __any_sync(0xffffffffu, v0 > 0 || v1 < kTileKeys);
                     constexpr bool kRaw = MODE == 0;                                    // x is q . k: the scale is part of the exponent's FFMA
                     const float f = kRaw ? a.sc : 1.f;
-                    // The 128 scores come in four pieces of 32, each asked for while the one before is worked on: fewer registers
-                    // than all at once, and the exponentials start after the first.
-                    uint32_t x[4][32];
-                    float mx;
-                    auto ask = [&](int c) { tmem_ld32(tmem_s + c * 32, x[c]); };
-                    auto scores = [&](int c) {                                          // to what the softmax is of, and their maximum
-                        if constexpr (MODE & MODE_CAP) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) x[c][j] = __float_as_uint(a.cap * tanhf(__uint_as_float(x[c][j]) * a.sc));
-                        }
+                    uint32_t x[4][32];                                                  // scores, then pairs of weights
+                    uint64_t l2[2] = {0, 0};                                            // the tile's sums
+                    auto scores = [&](int c, auto masked) {                             // to what the softmax is of
                         if constexpr (MODE & MODE_BIAS) {
                             const float b = slope * (float)(key0 - pos + c * 32), sc = MODE & MODE_CAP ? 1.f : a.sc;
 #pragma unroll
                             for (int j = 0; j < 32; ++j) x[c][j] = __float_as_uint(fmaf(__uint_as_float(x[c][j]), sc, fmaf(slope, (float)j, b)));
                         }
-                        if (masked) {
+                        if constexpr (masked()) {
 #pragma unroll
                             for (int j = 0; j < 32; ++j) x[c][j] = c * 32 + j >= v0 && c * 32 + j < v1 ? x[c][j] : 0xff800000u;
                         }
-                        float m0 = mx, m1 = -INFINITY;
-#pragma unroll
-                        for (int j = 0; j < 32; j += 4) {
-                            m0 = fmaxf(fmaxf(m0, __uint_as_float(x[c][j])), __uint_as_float(x[c][j + 1]));
-                            m1 = fmaxf(fmaxf(m1, __uint_as_float(x[c][j + 2])), __uint_as_float(x[c][j + 3]));
-                        }
-                        mx = fmaxf(m0, m1);
                     };
-                    float nm = 0.f;
-                    uint64_t l2 = 0;                                                    // the tile's sums of even and odd keys
-                    // 32 scores become 16 words of P.  The MUFU unit takes 8 cycles for a warp's exponential, 1024 for a tile:
-                    // as long as the tile's two products, for either stream.  So in full tiles of a unit of two row tiles kPoly
-                    // of 16 pairs go to the FMA pipes instead.  Tiles with hidden keys keep to the MUFU unit: -inf needs
-                    // its exact zero, and rows of few keys its precision.
-                    const bool full = dual && !masked;
-                    auto weights = [&](int c, bool mixed) {
+                    auto largest = [&] {
+                        float m0[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                        for (int j = 0; j < 32; j += 2)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) m0[c] = fmaxf(fmaxf(m0[c], __uint_as_float(x[c][j])), __uint_as_float(x[c][j + 1]));
+                        return fmaxf(fmaxf(m0[0], m0[1]), fmaxf(m0[2], m0[3])) * f;
+                    };
+                    auto weights = [&](int c) {                                         // 32 scores become 16 words of P
+                        const float nm = m_run == -INFINITY ? 0.f : -m_run;
                         const uint64_t f2 = pair(f, f), nm2 = pair(nm, nm);
 #pragma unroll
                         for (int j = 0; j < 16; ++j) {
-                            uint64_t e = fma2(pair(__uint_as_float(x[c][2 * j]), __uint_as_float(x[c][2 * j + 1])), f2, nm2);
-                            float2 p;
-                            if (mixed && (j * kPoly) % 16 < kPoly) {
-                                e = exp2_pair(e);
-                                p = unpair(e);
-                            } else {
-                                p = unpair(e);
-                                p.x = ex2_approx(p.x), p.y = ex2_approx(p.y);
-                                e = pair(p.x, p.y);
-                            }
-                            l2 = add2(l2, e);
+                            float2 p = unpair(fma2(pair(__uint_as_float(x[c][2 * j]), __uint_as_float(x[c][2 * j + 1])), f2, nm2));
+                            p.x = ex2_approx(p.x), p.y = ex2_approx(p.y);
+                            l2[j & 1] = add2(l2[j & 1], pair(p.x, p.y));
                             x[c][j] = pack_bf16(p.x, p.y);
                         }
                     };
-                    auto hand_over = [&](int half) {
+                    auto store = [&](int half) {
                         tmem_st16(tmem_s + half * 32, x[2 * half]);
                         tmem_st16(tmem_s + half * 32 + 16, x[2 * half + 1]);
+                    };
+                    auto hand_over = [&](int half) {                                    // the half's P is in tensor memory
                         tmem_wait_st();
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(p_full + 16 * s + 8 * half);
                     };
-                    if (mine == 0) {                                                    // the piece's first tile sets the maximum
-                        mx = -INFINITY;
+                    if constexpr (MODE & MODE_CAP) {
+                        // capped where they lie, a piece at a time: one copy of the arithmetic instead of eight
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            tmem_ld32(tmem_s + c * 32, x[0]);
+                            tmem_wait_ld32(x[0]);
+                            cap32(x[0], a.sc, a.cap);
+                            tmem_st32(tmem_s + c * 32, x[0]);
+                        }
+                        tmem_wait_st();
+                    }
+                    auto tile = [&](auto masked) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) tmem_ld32(tmem_s + c * 32, x[c]);
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
-                            ask(c);
-                            tmem_wait_ld();
-                            scores(c);
+                            tmem_wait_ld32(x[c]);
+                            scores(c, masked);
                         }
-                        m_run = mx * f;
-                    }
-                    // From then on the weights of the first half are formed with the maximum as it stands while the tile's own is
-                    // being found; where that exceeds it by more than the slack (rare) the scores, still in tensor memory, are
-                    // read again.
-                    nm = m_run == -INFINITY ? 0.f : -m_run;
-                    mx = -INFINITY;
-                    ask(0);
-                    tmem_wait_ld();
-                    ask(1);
-                    scores(0);
-                    if (dual) {
-                        take_turn();
-                        if (fail) break;
-                    }
-                    auto body = [&](auto mixed) {
-                        weights(0, mixed());
-                        tmem_wait_ld();
-                        ask(2);
-                        scores(1);
-                        weights(1, mixed());
-                        tmem_wait_ld();
-                        ask(3);
-                        scores(2);
-                        tmem_wait_ld();
-                        scores(3);
-                        const float m_tile = mx * f;
-                        const bool outgrown = m_tile > m_run + kMaxSlack;
+                        const float m_tile = largest();
+                        const bool outgrown = mine == 0 || m_tile > m_run + kMaxSlack;  // the piece's first tile sets the maximum
                         if (__any_sync(0xffffffffu, outgrown)) {
                             const float m_new = outgrown ? m_tile : m_run;
-                            const float r = outgrown ? (m_run == -INFINITY ? 0.f : ex2_approx(m_run - m_new)) : 1.f;
-                            // O holds this piece's earlier tiles, complete since S of this one is (after the first tile only)
+                            // O holds this piece's earlier tiles, complete since S of this one is
                             if (mine > 0) {
+                                const float r = outgrown ? (m_run == -INFINITY ? 0.f : ex2_approx(m_run - m_new)) : 1.f;
 #pragma unroll 1
                                 for (int c = 0; c < D; c += 16) {
-                                    tmem_ld16(tmem_o + c, x[0]);
+                                    uint32_t y[16];
+                                    tmem_ld16(tmem_o + c, y);
                                     tmem_wait_ld();
 #pragma unroll
-                                    for (int j = 0; j < 16; ++j) x[0][j] = __float_as_uint(__uint_as_float(x[0][j]) * r);
-                                    tmem_st16(tmem_o + c, x[0]);
+                                    for (int j = 0; j < 16; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * r);
+                                    tmem_st16(tmem_o + c, y);
                                 }
                                 tmem_wait_st();
+                                l_run *= r;
                             }
-                            l_run *= r;
                             m_run = m_new;
-                            nm = m_run == -INFINITY ? 0.f : -m_run;
-                            l2 = 0;
-                            ask(0);
-                            ask(1);
-                            tmem_wait_ld();
-                            scores(0);
-                            weights(0, false);
-                            scores(1);
-                            weights(1, false);
                         }
+                        weights(0);
+                        weights(1);
+                        store(0);
+                        weights(2);
                         hand_over(0);
-                        weights(2, mixed());
-                        weights(3, mixed());
-                        if (dual) pair_arrive(your_turn);
+                        weights(3);
+                        store(1);
                         hand_over(1);
                     };
-                    if (full) body(Const<true>());
-                    else body(Const<false>());
-                    const float2 l = unpair(l2);
+                    if (__any_sync(0xffffffffu, v0 > 0 || v1 < kTileKeys)) tile(Const<true>());
+                    else tile(Const<false>());
+                    if (fail) break;
+                    const float2 l = unpair(add2(l2[0], l2[1]));
                     l_run += l.x + l.y;
                 } else {
-                    if (dual) {
-                        take_turn();
-                        if (fail) break;
-                        pair_arrive(your_turn);
-                    }
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(p_full + 16 * s), mbar_arrive(p_full + 16 * s + 8);
@@ -687,7 +659,6 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             __syncwarp();
             if (join && lane == 0) mbar_arrive(x_done);
         }
-        if (fail) pair_arrive(your_turn);
     } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp < kWarpK) {
@@ -700,28 +671,25 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
         bool ok = true;
         // The whole warp waits, one elected thread issues: a branch of one lane around the waits costs hundreds of cycles.
         while (ok && w.next()) {
-            const int n = w.k1 - w.k0;
+            const int n = __shfl_sync(0xffffffffu, w.k1 - w.k0, 0);
             if (n == 0) continue;
-            const bool dual = w.u.ntok > a.T;
+            const bool dual = __shfl_sync(0xffffffffu, (int)(w.u.ntok > a.T), 0) != 0;
             const int qb = dual ? s : 0, step = dual ? 1 : 2, i0 = dual ? 0 : s;
             if (!(ok = wait(q_full + 8 * qb, n_q[qb]))) break;
             ++n_q[0];
             if (dual) ++n_q[1];
             if (i0 >= n && lane == 0) mbar_arrive(q_empty);                             // a single key tile: nothing for stream 1
-            const uint32_t q_s = smem0 + qb * L::kQ;
+            const uint64_t dq = smem_desc(smem0 + qb * L::kQ, 16, 1024, 2);
             for (int i = i0; i < n; i += step, ++n_p) {
                 const uint32_t c = n_k + i, ks = c % L::kKStages, vs = c % L::kVStages;
                 const bool last = i + step >= n;
                 if (!(ok = wait_full(k_full, c, L::kKStages))) break;
                 tc_fence_after();
-                const uint32_t kb = smem0 + L::kOffK + ks * L::kTile;
+                const uint64_t dk = smem_desc(smem0 + L::kOffK + ks * L::kTile, 16, L::kGroupPitch, 2);
                 if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {                                  // 16 dims each, 64 per swizzled half
-                        const uint64_t da = smem_desc(q_s + (k >> 2) * (kRows * 128) + (k & 3) * 32, 16, 1024, 2);
-                        const uint64_t db = smem_desc(kb + (k >> 2) * 1024 + (k & 3) * 32, 16, L::kGroupPitch, 2);
-                        umma_ss(tmem_s, da, db, idesc_s, k > 0);
-                    }
+                    for (int k = 0; k < D / 16; ++k)                                    // 16 dims each, 64 per swizzled half
+                        umma_ss(tmem_s, dq + (((k >> 2) * (kRows * 128) + (k & 3) * 32) >> 4), dk + (((k >> 2) * 1024 + (k & 3) * 32) >> 4), idesc_s, k > 0);
                     umma_commit(s_full + 8 * s);
                     umma_commit(k_empty + 8 * ks);
                     if (!dual) mbar_arrive(k_empty + 8 * ks);                           // the other stream has no use for this tile
@@ -731,17 +699,15 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                     }
                 }
                 if (!(ok = wait_full(v_full, c, L::kVStages))) break;
-                const uint32_t vb = smem0 + L::kOffV + vs * L::kTile;
+                const uint64_t dv = smem_desc(smem0 + L::kOffV + vs * L::kTile, 1024, L::kGroupPitch, 2);
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     if (!(ok = wait(p_full + 16 * s + 8 * half, n_p))) break;
                     tc_fence_after();
                     if (elect_one()) {
 #pragma unroll
-                        for (int k = half * 4; k < half * 4 + 4; ++k) {                 // 16 keys each: a block of V, 8 columns of P
-                            const uint64_t db = smem_desc(vb + k * L::kBlockBytes, 1024, L::kGroupPitch, 2);
-                            umma_ts(tmem_o, tmem_s + k * 8, db, idesc_o, (i > i0 || k > 0) ? 1u : 0u);
-                        }
+                        for (int k = half * 4; k < half * 4 + 4; ++k)                   // 16 keys each: a block of V, 8 columns of P
+                            umma_ts(tmem_o, tmem_s + k * 8, dv + ((k * L::kBlockBytes) >> 4), idesc_o, (i > i0 || k > 0) ? 1u : 0u);
                         if (half == 1) {
                             umma_commit(v_empty + 8 * vs);
                             if (!dual) mbar_arrive(v_empty + 8 * vs);

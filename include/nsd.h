@@ -514,7 +514,7 @@ nsd_status nsd_schedule_batch(const nsd_sched_params* prm, int32_t n, const uint
  * without entries and rows); a free list that runs out and block ids outside the pool (table
  * entry -1 or as it is, slot -1); tables or rows beyond max_entries / max_rows (not written).
  * Errors: INVALID_ARG, OUT_OF_RANGE (batch > max_batch, max_entries or max_rows beyond 2^31 - 1024),
- * CAPACITY (batch > 16384).
+ * CAPACITY (batch > 8192).
  */
 nsd_status nsd_block_tables(nsd_ctx* ctx, int32_t batch, const int32_t* ctx_len, const int32_t* new_len, int32_t* held,
                             int64_t held_stride, const int32_t* n_held, const int32_t* free_blocks, int64_t n_free,

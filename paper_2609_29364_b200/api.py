@@ -153,31 +153,27 @@ def _ptr(t) -> Optional[int]:
     raise TypeError(type(t))
 
 
-def _tensor(t, dtype, what, shape=None):
-    """Address of a contiguous torch tensor of the given dtype name (and at least the given number of elements)."""
+def _tensor(t, dtype, what, n=0):
+    """Address of a contiguous torch tensor of the given dtype with at least n elements (None stays None)."""
     if t is None:
         return None
-    if str(t.dtype) != dtype:
-        raise TypeError(f"{what}: {dtype} is wanted, got {t.dtype}")
-    if not t.is_contiguous():
-        raise ValueError(f"{what} has to be contiguous")
-    if shape is not None and t.numel() < shape:
-        raise ValueError(f"{what}: {shape} elements are wanted, got {t.numel()}")
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
+        if t.dtype is not dtype:
+            raise TypeError(f"{what}: {dtype} is wanted, got {t.dtype}")
+        raise ValueError(f"{what}: {n} contiguous elements are wanted, got {t.numel()} with strides {t.stride()}")
     return t.data_ptr()
 
 
 def _rows(t, width, what):
     """Address and row stride of a tensor [rows][...] whose rows are `width` contiguous elements."""
-    if t.dim() == 2:
-        inner = t.shape[1] == width and (t.stride(1) == 1 or width == 1)
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 2:
+        inner = shape[1] == width and (stride[1] == 1 or width == 1)
     else:
-        inner = t.dim() == 3 and t.shape[1] * t.shape[2] == width and t.stride(2) == 1 and t.stride(1) == t.shape[2]
+        inner = len(shape) == 3 and shape[1] * shape[2] == width and stride[2] == 1 and stride[1] == shape[2]
     if not inner:
-        raise ValueError(f"{what}: rows of {width} contiguous elements are wanted, got shape {tuple(t.shape)}, strides {t.stride()}")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else width)
-
-
-_DTYPE_CODE = {"torch.float32": 0, "torch.bfloat16": 1}
+        raise ValueError(f"{what}: rows of {width} contiguous elements are wanted, got shape {tuple(shape)}, strides {stride}")
+    return t.data_ptr(), (stride[0] if shape[0] > 1 else width)
 
 
 def _stream_handle(stream) -> Optional[int]:
@@ -238,6 +234,11 @@ class VerifyContext:
                              max_gamma=max_gamma, vocab_size=vocab_size, flags=flags,
                              max_table_entries=max_table_entries, wait_budget=wait_budget, reserved=0)
         self.device = torch.device(device)
+        self._device_index = self.device.index if self.device.index is not None else torch.cuda.current_device()
+        # the same handle as torch.cuda.current_stream(device).cuda_stream, without making a stream object for every call
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda index: torch.cuda.current_stream(index).cuda_stream)
+        self._i32, self._i64, self._f32, self._bf16 = torch.int32, torch.int64, torch.float32, torch.bfloat16
         self._h = _vp()
         nbytes = self.lib.nsd_workspace_bytes(ctypes.byref(self.cfg))
         if nbytes == 0:
@@ -317,87 +318,91 @@ class VerifyContext:
     def _stream(self, stream):
         """The given stream, or the current one of the context's device (whichever device is current)."""
         if stream is None:
-            import torch
-
-            return torch.cuda.current_stream(self.device).cuda_stream
+            return self._raw_stream(self._device_index)
         return stream if isinstance(stream, int) else stream.cuda_stream
 
     def nsd_block_tables(self, ctx_len, new_len, held, n_held, free_blocks, free_begin, kv_indptr, kv_indices, q_indptr,
                          slot_map, positions, row_req, n_held_new, free_end, stream=None):
         """Sizes come from the tensors: batch = len(ctx_len), held [batch][stride], capacities of kv_indices and of the
         row outputs (slot_map, positions, row_req: nullable, of one length)."""
-        batch = ctx_len.numel()
-        i32, i64 = "torch.int32", "torch.int64"
-        rows = [t.numel() for t in (slot_map, positions, row_req) if t is not None]
-        if rows and min(rows) != max(rows):
-            raise ValueError("slot_map, positions and row_req have to have one length")
+        batch, i32, i64 = ctx_len.numel(), self._i32, self._i64
+        max_rows = 0
+        for t in (slot_map, positions, row_req):
+            if t is not None:
+                if max_rows and t.numel() != max_rows:
+                    raise ValueError("slot_map, positions and row_req have to have one length")
+                max_rows = t.numel()
         if held.dim() != 2 or held.shape[0] < batch:
             raise ValueError("held: [batch][stride] is wanted")
-        self._check(self.lib.nsd_block_tables(
+        rc = self.lib.nsd_block_tables(
             self._h, batch, _tensor(ctx_len, i32, "ctx_len"), _tensor(new_len, i32, "new_len", batch), _tensor(held, i32, "held"),
             held.shape[1], _tensor(n_held, i32, "n_held", batch), _tensor(free_blocks, i32, "free_blocks"), free_blocks.numel(),
-            _tensor(free_begin, i64, "free_begin", 1), kv_indices.numel(), rows[0] if rows else 0,
-            _tensor(kv_indptr, i64, "kv_indptr", batch + 1), _tensor(kv_indices, i32, "kv_indices"),
-            _tensor(q_indptr, i64, "q_indptr", batch + 1), _tensor(slot_map, i64, "slot_map"), _tensor(positions, i32, "positions"),
-            _tensor(row_req, i32, "row_req"), _tensor(n_held_new, i32, "n_held_new", batch), _tensor(free_end, i64, "free_end", 1),
-            self._stream(stream)), "nsd_block_tables")
+            _tensor(free_begin, i64, "free_begin", 1), kv_indices.numel(), max_rows, _tensor(kv_indptr, i64, "kv_indptr", batch + 1),
+            _tensor(kv_indices, i32, "kv_indices"), _tensor(q_indptr, i64, "q_indptr", batch + 1), _tensor(slot_map, i64, "slot_map"),
+            _tensor(positions, i32, "positions"), _tensor(row_req, i32, "row_req"), _tensor(n_held_new, i32, "n_held_new", batch),
+            _tensor(free_end, i64, "free_end", 1), self._stream(stream))
+        if rc:
+            self._check(rc, "nsd_block_tables")
 
     def nsd_rope_append(self, kv_pool, layer, q, k, v, q_out, positions, sections, inv_freq, slot_map=None, adjacent=False,
                         cycled=False, stream=None):
         """q, k, v: [rows][heads * head_dim] or [rows][heads][head_dim], rows any stride apart (slices of one projection),
         fp32 or bf16; q_out bf16; positions int32 [axes][rows]; sections: pairs of each axis."""
-        D, some = self.cfg.head_dim, q if q is not None else k
+        some = q if q is not None else k
         if some is None or (k is None) != (v is None):
             raise ValueError("q, or k and v, or all three are wanted")
-        n, code = some.shape[0], _DTYPE_CODE.get(str(some.dtype), -1)
-        for t in (q, k, v):
-            if t is not None and (t.shape[0] != n or t.dtype != some.dtype):
-                raise ValueError("q, k and v have to have the same rows and dtype")
+        n, dtype = some.shape[0], some.dtype
+        wq, wk = self.cfg.num_q_heads * self.cfg.head_dim, self.cfg.num_kv_heads * self.cfg.head_dim
         qp = kp = vp = op = None
         qs = ks = vs = os_ = 0
         if q is not None:
-            qp, qs = _rows(q, self.cfg.num_q_heads * D, "q")
-            if q_out is None or str(q_out.dtype) != "torch.bfloat16" or q_out.shape[0] < n:
+            qp, qs = _rows(q, wq, "q")
+            if q_out is None or q_out.dtype is not self._bf16 or q_out.shape[0] < n:
                 raise TypeError("q_out: bfloat16 with q's rows is wanted")
-            op, os_ = _rows(q_out, self.cfg.num_q_heads * D, "q_out")
+            op, os_ = _rows(q_out, wq, "q_out")
         if k is not None:
-            kp, ks = _rows(k, self.cfg.num_kv_heads * D, "k")
-            vp, vs = _rows(v, self.cfg.num_kv_heads * D, "v")
-        if positions.dim() != 2 or positions.shape[1] != n:
-            raise ValueError("positions: [axes][rows] is wanted")
-        if len(sections) != positions.shape[0]:
-            raise ValueError("sections: one number per axis of positions is wanted")
-        self._check(self.lib.nsd_rope_append(
-            self._h, _ptr(kv_pool), layer, n, code, qp, qs, kp, ks, vp, vs, op, os_, _tensor(positions, "torch.int32", "positions"),
-            positions.shape[0], (ctypes.c_int32 * len(sections))(*sections),
-            _tensor(inv_freq, "torch.float32", "inv_freq", sum(sections)),
-            (NSD_ROPE_ADJACENT if adjacent else 0) | (NSD_ROPE_CYCLED if cycled else 0),
-            _tensor(slot_map, "torch.int64", "slot_map", n), self._stream(stream)), "nsd_rope_append")
+            if k.shape[0] != n or v.shape[0] != n or k.dtype is not dtype or v.dtype is not dtype:
+                raise ValueError("q, k and v have to have the same rows and dtype")
+            kp, ks = _rows(k, wk, "k")
+            vp, vs = _rows(v, wk, "v")
+        axes = len(sections)
+        if positions.dim() != 2 or positions.shape[1] != n or positions.shape[0] != axes:
+            raise ValueError("positions: [axes][rows] is wanted, and sections: one number per axis")
+        rc = self.lib.nsd_rope_append(
+            self._h, _ptr(kv_pool), layer, n, 0 if dtype is self._f32 else (1 if dtype is self._bf16 else -1), qp, qs, kp, ks, vp, vs,
+            op, os_, _tensor(positions, self._i32, "positions"), axes, (ctypes.c_int32 * axes)(*sections),
+            _tensor(inv_freq, self._f32, "inv_freq", sum(sections)),
+            (NSD_ROPE_ADJACENT if adjacent else 0) | (NSD_ROPE_CYCLED if cycled else 0), _tensor(slot_map, self._i64, "slot_map", n),
+            self._stream(stream))
+        if rc:
+            self._check(rc, "nsd_rope_append")
 
     def nsd_chunk_plan_bytes(self, max_rows: int) -> int:
         return int(self.lib.nsd_chunk_plan_bytes(self._h, max_rows))
 
     def nsd_chunk_plan(self, plan, max_rows, q_indptr, ctx_len, kv_indptr, window=0, prefix_len=None, row_first=None, stream=None):
-        batch = ctx_len.numel()
-        i32, i64 = "torch.int32", "torch.int64"
+        batch, i32, i64 = ctx_len.numel(), self._i32, self._i64
         masks = ChunkMasks(window, 0, _tensor(prefix_len, i32, "prefix_len", batch), _tensor(row_first, i32, "row_first", max_rows))
-        self._check(self.lib.nsd_chunk_plan(
-            self._h, _ptr(plan), plan.numel() * plan.element_size(), batch, max_rows, _tensor(q_indptr, i64, "q_indptr", batch + 1),
-            _tensor(ctx_len, i32, "ctx_len"), _tensor(kv_indptr, i64, "kv_indptr", batch + 1), ctypes.byref(masks),
-            self._stream(stream)), "nsd_chunk_plan")
+        rc = self.lib.nsd_chunk_plan(
+            self._h, plan.data_ptr(), plan.numel() * plan.element_size(), batch, max_rows, _tensor(q_indptr, i64, "q_indptr", batch + 1),
+            _tensor(ctx_len, i32, "ctx_len"), _tensor(kv_indptr, i64, "kv_indptr", batch + 1), ctypes.byref(masks), self._stream(stream))
+        if rc:
+            self._check(rc, "nsd_chunk_plan")
 
     def nsd_chunk_attn(self, plan, max_rows, kv_pool, q, o, lse, kv_indices, layer=0, scale=0.0, softcap=0.0, alibi_slopes=None,
                        stream=None):
         """q: [rows][q heads * head_dim] or [rows][q heads][head_dim], rows any multiple of 8 elements apart; o contiguous."""
-        width = self.cfg.num_q_heads * self.cfg.head_dim
-        if str(q.dtype) != "torch.bfloat16" or q.shape[0] < max_rows:
+        heads, f32 = self.cfg.num_q_heads, self._f32
+        width = heads * self.cfg.head_dim
+        if q.dtype is not self._bf16 or q.shape[0] < max_rows:
             raise TypeError("q: bfloat16 with max_rows rows is wanted")
         qp, qs = _rows(q, width, "q")
-        self._check(self.lib.nsd_chunk_attn(
-            self._h, _ptr(plan), plan.numel() * plan.element_size(), _ptr(kv_pool), qp, qs,
-            _tensor(o, "torch.bfloat16", "o", max_rows * width), _tensor(lse, "torch.float32", "lse", max_rows * self.cfg.num_q_heads),
-            max_rows, _tensor(kv_indices, "torch.int32", "kv_indices"), layer, scale, softcap,
-            _tensor(alibi_slopes, "torch.float32", "alibi_slopes", self.cfg.num_q_heads), self._stream(stream)), "nsd_chunk_attn")
+        rc = self.lib.nsd_chunk_attn(
+            self._h, plan.data_ptr(), plan.numel() * plan.element_size(), _ptr(kv_pool), qp, qs, _tensor(o, self._bf16, "o", max_rows * width),
+            _tensor(lse, f32, "lse", max_rows * heads), max_rows, _tensor(kv_indices, self._i32, "kv_indices"), layer, scale, softcap,
+            _tensor(alibi_slopes, f32, "alibi_slopes", heads), self._stream(stream))
+        if rc:
+            self._check(rc, "nsd_chunk_attn")
 
     @staticmethod
     def round_args(**kw) -> RoundArgs:

@@ -14,9 +14,10 @@ namespace {
 // needs.  So the work is spread evenly however unequal the requests are (one prompt of 100 000
 // tokens beside 500 single tokens), and no CTA waits for another: each forms the prefix sums of
 // the whole batch for itself in shared memory (12 bytes per request read from L2), which costs
-// less than a second launch.
+// less than a second launch.  What bounds it is latency: launch, lengths, sums, one search, one
+// block id, stores.
 constexpr int kTablesThreads = 256;
-constexpr int kTablesPerCta = 1024;               // flat positions per CTA, four per thread
+constexpr int kTablesPerCta = 256;                // flat positions per CTA: one per thread (512 requests, 72 000 entries: 4.4 us; two per thread 5.2, four 7.4)
 constexpr int kBsT = 16;
 
 struct TablesArgs {
@@ -33,14 +34,14 @@ struct TablesArgs {
 };
 
 struct Need {
-    int32_t entries, rows, take;
+    int32_t entries, rows, take, ctx, held;
     bool ok;
 };
 __device__ __forceinline__ Need need_of(const TablesArgs& a, int r) {
     const int64_t c = a.ctx_len[r], n = a.new_len[r], h = a.n_held[r];
     const int64_t need = (c + n + kBsT - 1) / kBsT;
     const bool ok = c >= 0 && n >= 0 && c + n <= 0x7fffffffll - kBsT && need <= a.held_stride && h >= (c + kBsT - 1) / kBsT && h <= a.held_stride;
-    return ok ? Need{(int32_t)need, (int32_t)n, (int32_t)(need > h ? need - h : 0), true} : Need{0, 0, 0, false};
+    return ok ? Need{(int32_t)need, (int32_t)n, (int32_t)(need > h ? need - h : 0), (int32_t)c, (int32_t)h, true} : Need{0, 0, 0, 0, 0, false};
 }
 __device__ __forceinline__ void report(int32_t* status, int32_t bit, int r) {
     atomicOr(status, bit);
@@ -58,15 +59,20 @@ __device__ __forceinline__ int owner_of(const int32_t* p, int batch, int32_t x) 
 
 __global__ void __launch_bounds__(kTablesThreads)
 block_tables_kernel(const TablesArgs a) {
-    extern __shared__ int32_t pre[];               // three prefix sums of batch + 1 entries: table entries, rows, blocks taken
+    // per request: prefix sums of table entries, rows and blocks taken (one more each), committed tokens, blocks held
+    extern __shared__ int32_t pre[];
     __shared__ int64_t warp_sum[3][kTablesThreads / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    int32_t *kvp = pre, *qp = pre + a.batch + 1, *tp = qp + a.batch + 1;
+    int32_t *const kvp = pre, *const qp = pre + a.batch + 1, *const tp = qp + a.batch + 1, *const ctx = tp + a.batch + 1, *const held_n = ctx + a.batch;
     const int per = (a.batch + kTablesThreads - 1) / kTablesThreads;
     const int r0 = min(tid * per, a.batch), r1 = min(r0 + per, a.batch);
+    int64_t fb = a.free_begin ? *a.free_begin : 0;
     int64_t mine[3] = {0, 0, 0};
+#pragma unroll 4
     for (int r = r0; r < r1; ++r) {
         const Need d = need_of(a, r);
+        kvp[r] = d.entries, qp[r] = d.rows, tp[r] = d.take;            // for the moment the request's own
+        ctx[r] = d.ctx, held_n[r] = d.held;
         mine[0] += d.entries, mine[1] += d.rows, mine[2] += d.take;
         if (!d.ok && blockIdx.x == 0) report(a.status, STATUS_BAD_TOKEN, r);
     }
@@ -85,6 +91,7 @@ block_tables_kernel(const TablesArgs a) {
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
         int64_t before = 0, all = 0;
+#pragma unroll
         for (int w = 0; w < kTablesThreads / 32; ++w) {
             if (w < warp) before += warp_sum[k][w];
             all += warp_sum[k][w];
@@ -95,51 +102,58 @@ block_tables_kernel(const TablesArgs a) {
     // positions past 2^31 are past every buffer: the sums may saturate there
     auto sat = [](int64_t v) { return (int32_t)(v > 0x7fffffffll ? 0x7fffffffll : v); };
     for (int r = r0; r < r1; ++r) {
-        const Need d = need_of(a, r);
+        const int32_t e = kvp[r], n = qp[r], t = tp[r];
         kvp[r] = sat(at[0]), qp[r] = sat(at[1]), tp[r] = sat(at[2]);
-        at[0] += d.entries, at[1] += d.rows, at[2] += d.take;
+        at[0] += e, at[1] += n, at[2] += t;
     }
     if (tid == 0) kvp[a.batch] = sat(total[0]), qp[a.batch] = sat(total[1]), tp[a.batch] = sat(total[2]);
     __syncthreads();
 
-    int64_t fb = a.free_begin ? *a.free_begin : 0;
     if (fb < 0 || fb > a.n_free) {
         if (blockIdx.x == 0 && tid == 0) report(a.status, STATUS_BAD_BLOCK, -1);
         fb = a.n_free;
     }
-    // block k of request r's table; a block that is missing or outside the pool is the request's fault to report
-    auto block_of = [&](int r, int k, int held) -> int32_t {
+    // block k of request r's table: its own or one from the free list, -1 where that has run out
+    auto block_of = [&](int r, int k) -> int32_t {
+        const int held = held_n[r];
         if (k < held) return a.held[(int64_t)r * a.held_stride + k];
         const int64_t f = fb + tp[r] + (k - held);
         return f < a.n_free ? a.free_blocks[f] : -1;
     };
-    const int64_t x0 = (int64_t)blockIdx.x * kTablesPerCta;
+    // flat position x is both a table entry and a row: the searches and loads of a thread's positions run side by side
+    constexpr int kEach = kTablesPerCta / kTablesThreads;
+    const int64_t x0 = (int64_t)blockIdx.x * kTablesPerCta + tid;
+    int er[kEach], rr[kEach], pos[kEach];
+    int32_t eid[kEach], rid[kEach];
+    const int64_t n_entries = min((int64_t)kvp[a.batch], a.max_entries), n_rows = min((int64_t)qp[a.batch], a.max_rows);
 #pragma unroll
-    for (int u = 0; u < kTablesPerCta / kTablesThreads; ++u) {
-        const int64_t e = x0 + u * kTablesThreads + tid;
-        if (e < kvp[a.batch] && e < a.max_entries) {
-            const int r = owner_of(kvp, a.batch, (int32_t)e), k = (int)e - kvp[r], held = a.n_held[r];
-            const int32_t id = block_of(r, k, held);
-            a.kv_indices[e] = id;
-            if ((uint32_t)id >= (uint32_t)a.num_blocks) report(a.status, STATUS_BAD_BLOCK, r);
-            else if (k >= held) a.held[(int64_t)r * a.held_stride + k] = id;
+    for (int u = 0; u < kEach; ++u) {
+        const int64_t x = x0 + u * kTablesThreads;
+        er[u] = rr[u] = eid[u] = rid[u] = -1, pos[u] = 0;
+        if (x < n_entries) {
+            er[u] = owner_of(kvp, a.batch, (int32_t)x);
+            eid[u] = block_of(er[u], (int)x - kvp[er[u]]);
+        }
+        if (x < n_rows) {
+            rr[u] = owner_of(qp, a.batch, (int32_t)x);
+            pos[u] = ctx[rr[u]] + (int32_t)x - qp[rr[u]];
+            rid[u] = block_of(rr[u], pos[u] / kBsT);
         }
     }
 #pragma unroll
-    for (int u = 0; u < kTablesPerCta / kTablesThreads; ++u) {
-        const int64_t i = x0 + u * kTablesThreads + tid;
-        if (i >= a.max_rows) break;
-        int64_t slot = -1;
-        int32_t pos = 0, req = -1;
-        if (i < qp[a.batch]) {
-            req = owner_of(qp, a.batch, (int32_t)i);
-            pos = a.ctx_len[req] + (int32_t)i - qp[req];
-            const int32_t id = block_of(req, pos / kBsT, a.n_held[req]);
-            if ((uint32_t)id < (uint32_t)a.num_blocks) slot = (int64_t)id * kBsT + pos % kBsT;
+    for (int u = 0; u < kEach; ++u) {
+        const int64_t x = x0 + u * kTablesThreads;
+        if (er[u] >= 0) {
+            const int r = er[u], k = (int)x - kvp[r];
+            a.kv_indices[x] = eid[u];
+            if ((uint32_t)eid[u] >= (uint32_t)a.num_blocks) report(a.status, STATUS_BAD_BLOCK, r);
+            else if (k >= held_n[r]) a.held[(int64_t)r * a.held_stride + k] = eid[u];
         }
-        if (a.slot_map) a.slot_map[i] = slot;
-        if (a.positions) a.positions[i] = pos;
-        if (a.row_req) a.row_req[i] = req;
+        if (x < a.max_rows) {
+            if (a.slot_map) a.slot_map[x] = (uint32_t)rid[u] < (uint32_t)a.num_blocks ? (int64_t)rid[u] * kBsT + pos[u] % kBsT : -1;
+            if (a.positions) a.positions[x] = pos[u];
+            if (a.row_req) a.row_req[x] = rr[u];
+        }
     }
     // the per-request outputs, shared out over the CTAs
     for (int r = blockIdx.x * kTablesThreads + tid; r <= a.batch; r += gridDim.x * kTablesThreads) {
@@ -176,29 +190,42 @@ struct RopeArgs {
     const float* inv_freq;
     const int64_t* slot_map;
     int32_t* status;
-    int32_t Hq, Hkv, num_blocks, pairs, adjacent, parts;
+    int32_t Hq, Hkv, num_blocks, pairs, adjacent;
+    int32_t log2_parts;                            // warps per row
     int32_t hq0;                                   // first head of the walk: 0, or Hq when there is no q
     int32_t heads;                                 // one past its last: Hq + 2 Hkv, or Hq without k and v
     uint8_t axis[64];
 };
 
-template <typename T> struct In;
-template <> struct In<float> {
-    static __device__ __forceinline__ void load8(const float* p, float* x) {
-        const float4 u = __ldg(reinterpret_cast<const float4*>(p)), v = __ldg(reinterpret_cast<const float4*>(p) + 1);
-        x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
+// 16 dims of a head as they lie in memory: eight at d0, eight at d1.
+template <typename T> struct Dims;
+template <> struct Dims<float> {
+    float4 v[4];
+    __device__ __forceinline__ void load(const float* p, int d0, int d1) {
+        v[0] = __ldcs(reinterpret_cast<const float4*>(p + d0)), v[1] = __ldcs(reinterpret_cast<const float4*>(p + d0) + 1);
+        v[2] = __ldcs(reinterpret_cast<const float4*>(p + d1)), v[3] = __ldcs(reinterpret_cast<const float4*>(p + d1) + 1);
     }
-    static __device__ __forceinline__ float load1(const float* p) { return *p; }
-};
-template <> struct In<__nv_bfloat16> {
-    static __device__ __forceinline__ void load8(const __nv_bfloat16* p, float* x) {
-        const uint4 u = *reinterpret_cast<const uint4*>(p);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    __device__ __forceinline__ void get(float* x) const {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        for (int i = 0; i < 4; ++i) x[4 * i] = v[i].x, x[4 * i + 1] = v[i].y, x[4 * i + 2] = v[i].z, x[4 * i + 3] = v[i].w;
     }
-    static __device__ __forceinline__ float load1(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 };
+template <> struct Dims<__nv_bfloat16> {
+    uint4 v[2];
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, int d0, int d1) {
+        v[0] = __ldcs(reinterpret_cast<const uint4*>(p + d0)), v[1] = __ldcs(reinterpret_cast<const uint4*>(p + d1));
+    }
+    __device__ __forceinline__ void get(float* x) const {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[8 * i + 2 * j] = __uint_as_float(w[j] << 16), x[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+        }
+    }
+};
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
@@ -216,13 +243,41 @@ rope_append_kernel(const __grid_constant__ RopeArgs a) {
     constexpr int kHeads = 32 / kUnits;            // heads a warp has under way
     const int lane = threadIdx.x & 31;
     const int64_t w = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-    const int64_t row = w / a.parts;
-    const int part = (int)(w - row * a.parts);
+    const int64_t row = w >> a.log2_parts;
+    const int part = (int)(w & ((1 << a.log2_parts) - 1));
     if (row >= a.n_rows) return;
     const int64_t slot = a.slot_map ? a.slot_map[row] : 0;
     if (slot < 0) return;                          // a padding row
     const bool stored = slot < (int64_t)a.num_blocks * kBsT;
     if (!stored && lane == 0 && part == 0) report(a.status, STATUS_BAD_BLOCK, (int)row);
+    const int Hk0 = a.Hq, Hv0 = a.Hq + a.Hkv;
+    const int per = (a.heads - a.hq0 + (1 << a.log2_parts) - 1) >> a.log2_parts;
+    const int h_begin = a.hq0 + part * per, h_end = min(h_begin + per, a.heads);
+    auto source = [&](int h) -> const T* {
+        if (h < Hk0) return static_cast<const T*>(a.q) + row * a.q_stride + h * D;
+        if (h < Hv0) return static_cast<const T*>(a.k) + row * a.k_stride + (h - Hk0) * D;
+        return static_cast<const T*>(a.v) + row * a.v_stride + (h - Hv0) * D;
+    };
+    // tile of (block, K|V, kv head): block * 2 Hkv + K|V * Hkv + head = block * 2 Hkv + (h - Hq)
+    uint16_t* const kv_at = a.slab + (((slot / kBsT) * 2 * a.Hkv - Hk0) * kBsT + slot % kBsT) * D;
+    auto target = [&](int h) -> uint16_t* {
+        if (h < Hk0) return a.q_out + row * a.qo_stride + h * D;
+        return stored ? kv_at + (int64_t)h * (kBsT * D) : nullptr;
+    };
+    // adjacent: a unit's 16 dims are its eight pairs.  Apart: dims p and p + pairs for the units that turn, and the dims
+    // from 2 pairs on, 16 at a time, for the rest.
+    const int u = lane % kUnits;
+    const int d0 = a.adjacent ? u * 16 : (u * 8 < a.pairs ? u * 8 : 2 * a.pairs + (u - a.pairs / 8) * 16);
+    const int d1 = a.adjacent || u * 8 >= a.pairs ? d0 + 8 : d0 + a.pairs;
+    constexpr int kAhead = sizeof(T) == 2 ? 4 : 2; // heads per lane whose loads are in flight together
+    Dims<T> now[kAhead];
+    int h0 = h_begin + lane / kUnits;
+    auto fetch = [&](Dims<T>* to, int h) {
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (h + j * kHeads < h_end) to[j].load(source(h + j * kHeads), d0, d1);
+    };
+    if constexpr (VEC) fetch(now, h0);             // under way while the sines are formed
     // two pairs per lane (one where a head has 32): 2 lane, 2 lane + 1
     constexpr int kMine = D / 64;
     float cs[kMine], sn[kMine];
@@ -235,22 +290,7 @@ rope_append_kernel(const __grid_constant__ RopeArgs a) {
             sincospif((float)(2.0 * (turns - rint(turns))), &sn[i], &cs[i]);
         }
     }
-    const int Hk0 = a.Hq, Hv0 = a.Hq + a.Hkv;
-    const int per = (a.heads - a.hq0 + a.parts - 1) / a.parts;
-    const int h_end = min(a.hq0 + (part + 1) * per, a.heads);
-    auto source = [&](int h) -> const T* {
-        if (h < Hk0) return static_cast<const T*>(a.q) + row * a.q_stride + h * D;
-        if (h < Hv0) return static_cast<const T*>(a.k) + row * a.k_stride + (h - Hk0) * D;
-        return static_cast<const T*>(a.v) + row * a.v_stride + (h - Hv0) * D;
-    };
-    auto target = [&](int h) -> uint16_t* {
-        if (h < Hk0) return a.q_out + row * a.qo_stride + h * D;
-        if (!stored) return nullptr;
-        // tile of (block, K|V, kv head): block * 2 Hkv + K|V * Hkv + head = block * 2 Hkv + (h - Hq)
-        return a.slab + (((slot / kBsT) * 2 * a.Hkv + (h - Hk0)) * kBsT + slot % kBsT) * D;
-    };
     if constexpr (VEC) {
-        const int u = lane % kUnits;
         float c[8], s[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -258,53 +298,44 @@ rope_append_kernel(const __grid_constant__ RopeArgs a) {
             c[i] = __shfl_sync(0xffffffffu, cs[i % kMine], p / kMine);
             s[i] = __shfl_sync(0xffffffffu, sn[i % kMine], p / kMine);
         }
-        // adjacent: the unit's 16 dims are its eight pairs.  Apart: dims p and p + pairs for the units that turn, and
-        // the dims from 2 pairs on, 16 at a time, for the rest.
-        const int d0 = a.adjacent ? u * 16 : (u * 8 < a.pairs ? u * 8 : 2 * a.pairs + (u - a.pairs / 8) * 16);
-        const int d1 = a.adjacent || u * 8 >= a.pairs ? d0 + 8 : d0 + a.pairs;
-        constexpr int kAhead = 4;                  // heads per lane whose loads are in flight together
-        for (int h0 = a.hq0 + part * per + lane / kUnits; h0 < h_end; h0 += kHeads * kAhead) {
-            float x[kAhead][16];
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                const int h = h0 + j * kHeads;
-                if (h < h_end) {
-                    const T* src = source(h);
-                    In<T>::load8(src + d0, x[j]);
-                    In<T>::load8(src + d1, x[j] + 8);
-                }
-            }
+        for (; h0 < h_end; h0 += kHeads * kAhead) {
+            Dims<T> next[kAhead];
+            fetch(next, h0 + kHeads * kAhead);
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) {
                 const int h = h0 + j * kHeads;
                 if (h >= h_end) break;
                 uint16_t* dst = target(h);
                 if (!dst) continue;
+                float x[16];
+                now[j].get(x);
                 if (h < Hv0) {
                     if (a.adjacent) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             if (u * 8 + i >= a.pairs) continue;            // dims that do not turn stay bit for bit
-                            const float p = x[j][2 * i], q = x[j][2 * i + 1];
-                            x[j][2 * i] = p * c[i] - q * s[i];
-                            x[j][2 * i + 1] = q * c[i] + p * s[i];
+                            const float p = x[2 * i], q = x[2 * i + 1];
+                            x[2 * i] = p * c[i] - q * s[i];
+                            x[2 * i + 1] = q * c[i] + p * s[i];
                         }
                     } else if (u * 8 < a.pairs) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
-                            const float p = x[j][i], q = x[j][8 + i];
-                            x[j][i] = p * c[i] - q * s[i];
-                            x[j][8 + i] = q * c[i] + p * s[i];
+                            const float p = x[i], q = x[8 + i];
+                            x[i] = p * c[i] - q * s[i];
+                            x[8 + i] = q * c[i] + p * s[i];
                         }
                     }
                 }
-                store8(dst + d0, x[j]);
-                store8(dst + d1, x[j] + 8);
+                store8(dst + d0, x);
+                store8(dst + d1, x + 8);
             }
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) now[j] = next[j];
         }
     } else {
         // a lane keeps its own pairs and walks the heads; dims that do not turn are copied two by two
-        for (int h = a.hq0 + part * per; h < h_end; ++h) {
+        for (int h = h_begin; h < h_end; ++h) {
             const T* src = source(h);
             uint16_t* dst = target(h);
             if (!dst) continue;
@@ -313,10 +344,10 @@ rope_append_kernel(const __grid_constant__ RopeArgs a) {
             for (int i = 0; i < kMine; ++i) {
                 const int p = lane * kMine + i;
                 const bool mine = p < a.pairs;
-                const int d0 = mine && !a.adjacent ? p : 2 * p, d1 = mine && !a.adjacent ? p + a.pairs : 2 * p + 1;
-                const float x = In<T>::load1(src + d0), y = In<T>::load1(src + d1);
+                const int e0 = mine && !a.adjacent ? p : 2 * p, e1 = mine && !a.adjacent ? p + a.pairs : 2 * p + 1;
+                const float x = to_float(src[e0]), y = to_float(src[e1]);
                 const uint32_t out = mine && turns ? pack2(x * cs[i] - y * sn[i], y * cs[i] + x * sn[i]) : pack2(x, y);
-                dst[d0] = (uint16_t)out, dst[d1] = (uint16_t)(out >> 16);
+                dst[e0] = (uint16_t)out, dst[e1] = (uint16_t)(out >> 16);
             }
         }
     }
@@ -333,12 +364,12 @@ cudaError_t launch_block_tables(int32_t batch, int32_t num_blocks, const int32_t
                        max_rows, kv_indptr, q_indptr, free_end, kv_indices, slot_map, positions, row_req, n_held_new, status};
     const int64_t most = max_entries > max_rows ? max_entries : max_rows;
     const int64_t grid = most > 0 ? (most + kTablesPerCta - 1) / kTablesPerCta : 1;
-    block_tables_kernel<<<(unsigned)grid, kTablesThreads, 3 * (size_t)(batch + 1) * sizeof(int32_t), stream>>>(a);
+    block_tables_kernel<<<(unsigned)grid, kTablesThreads, (5 * (size_t)batch + 3) * sizeof(int32_t), stream>>>(a);
     return cudaGetLastError();
 }
 
 cudaError_t tables_init() {
-    return cudaFuncSetAttribute(block_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * (kMaxTableBatch + 1) * (int)sizeof(int32_t));
+    return cudaFuncSetAttribute(block_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (5 * kMaxTableBatch + 3) * (int)sizeof(int32_t));
 }
 
 cudaError_t launch_rope_append(const RopeLaunch& l, cudaStream_t stream) {
@@ -361,10 +392,10 @@ cudaError_t launch_rope_append(const RopeLaunch& l, cudaStream_t stream) {
     auto aligned = [](const void* p, int64_t stride_bytes) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride_bytes % 16 == 0; };
     const bool vec = (l.adjacent || l.pairs % 8 == 0) && (!l.q || (aligned(l.q, l.q_stride * elem) && aligned(l.q_out, l.q_out_stride * 2))) &&
                      (!l.k || (aligned(l.k, l.k_stride * elem) && aligned(l.v, l.v_stride * elem)));
-    // Few rows: a row's heads go to several warps, until the machine has some eight warps per SM.
-    a.parts = 1;
-    while (a.parts < 8 && l.n_rows * a.parts < 8LL * l.n_sms && (a.heads - a.hq0) / (2 * a.parts) >= 4) a.parts *= 2;
-    const int64_t warps = l.n_rows * a.parts;
+    // Few rows: a row's heads go to several warps, until the machine has some eight warps per SM (320 rows: 4.3 us with four
+    // warps a row, 6.2 with one or eight).
+    while (a.log2_parts < 3 && (l.n_rows << a.log2_parts) < 8LL * l.n_sms && ((a.heads - a.hq0) >> (a.log2_parts + 1)) >= 4) ++a.log2_parts;
+    const int64_t warps = l.n_rows << a.log2_parts;
     const unsigned grid = (unsigned)((warps * 32 + 255) / 256);
 #define NSD_ROPE(T, D, V) rope_append_kernel<T, D, V><<<grid, 256, 0, stream>>>(a)
     if (l.in_bf16) {

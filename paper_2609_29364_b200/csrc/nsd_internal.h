@@ -140,7 +140,7 @@ cudaError_t launch_accept_logits(const void* logits, int32_t logits_bf16, float 
                                  int32_t* tickets /* two words, zero between launches */, cudaStream_t stream);
 
 // ---- chunks of new tokens (chunk_prep.cu, chunk_attn.cu) ----------------------------------------
-constexpr int kMaxTableBatch = 16384;        // requests whose prefix sums one CTA holds in shared memory
+constexpr int kMaxTableBatch = 8192;         // requests whose prefix sums one CTA holds in shared memory
 cudaError_t tables_init();
 cudaError_t launch_block_tables(int32_t batch, int32_t num_blocks, const int32_t* ctx_len, const int32_t* new_len, int32_t* held,
                                 int64_t held_stride, const int32_t* n_held, const int32_t* free_blocks, int64_t n_free,

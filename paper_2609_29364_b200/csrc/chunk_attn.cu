@@ -232,9 +232,9 @@ struct Smem {
     static constexpr int kGroupPitch = kHalves * 1024; // between 8-key groups
     static constexpr int kKStages = D == 128 ? 3 : 5, kVStages = D == 128 ? 2 : 5;
     static constexpr int kOffK = 2 * kQ, kOffV = kOffK + kKStages * kTile;
-    static constexpr int kOffMl = kOffV + kVStages * kTile;              // stream 1's statistics for the join
-    static constexpr int kOffBars = kOffMl + kRows * 8;
-    static constexpr int kNumBars = 3 * kKStages + 3 * kVStages + 1 + 4 + 2 + 4 + 2 + 2;
+    static constexpr int kOffMl = kOffV + kVStages * kTile;              // [2] statistics for a join, by the stream that joins
+    static constexpr int kOffBars = kOffMl + 2 * kRows * 8;
+    static constexpr int kNumBars = 3 * kKStages + 3 * kVStages + 1 + 4 + 2 + 4 + 2 + 4;
     static constexpr int kOffMisc = kOffBars + kNumBars * 8;
     static constexpr int kBytes = kOffMisc + 16;
     static_assert(kBytes <= 227 * 1024, "shared memory budget");
@@ -399,7 +399,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
     const uint32_t v_land = v_empty + 8 * L::kVStages; // a V tile whose hidden rows have to be cleared lands here first
     const uint32_t q_full = v_land + 8, q_empty = q_full + 16;                          // [2] per Q buffer
     const uint32_t s_full = q_empty + 16, p_full = s_full + 16, o_full = p_full + 32;   // [2], [2][2 halves], [2] per stream
-    const uint32_t x_ready = o_full + 16, x_done = x_ready + 8;                         // the join of a one-tile unit's streams
+    const uint32_t x_ready = o_full + 16, x_done = x_ready + 16;                        // [2] the join of a one-tile unit's streams
     uint32_t& tmem_base_s = *reinterpret_cast<uint32_t*>(smem + L::kOffMisc);
     volatile int& abort_s = *reinterpret_cast<volatile int*>(smem + L::kOffMisc + 4);
     float2* const ml_s = reinterpret_cast<float2*>(smem + L::kOffMl);
@@ -414,9 +414,9 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
         for (int s = 0; s < 2; ++s) {
             mbar_init(q_full + 8 * s, 1), mbar_init(q_empty + 8 * s, 2);
             mbar_init(s_full + 8 * s, 1), mbar_init(o_full + 8 * s, 1);
+            mbar_init(x_ready + 8 * s, 4), mbar_init(x_done + 8 * s, 4);
             mbar_init(p_full + 16 * s, 4), mbar_init(p_full + 16 * s + 8, 4);
         }
-        mbar_init(x_ready, 4), mbar_init(x_done, 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         abort_s = 0;
     }
@@ -429,6 +429,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base_s, 0);
     // the count-th completion; the same answer in every lane
+    auto poll = [&](uint32_t bar, uint32_t count) { return (bool)__all_sync(0xffffffffu, bar_try(bar, count & 1)); };
     auto wait = [&](uint32_t bar, uint32_t count) {
         bool ok = bar_try(bar, count & 1);
         if (__all_sync(0xffffffffu, ok)) return true;
@@ -438,8 +439,8 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
 
     // A ring's stage has two "full" barriers, for its even and its odd uses.  A wait by parity takes a phase that has not begun
     // for the one two before it; with alternate tiles an issuer does not watch every use of a stage, and one that runs ahead of
-    // the other could so take a tile that is still in flight for landed.  The use two before is its own stream's, or lies
-    // behind the last Q load, which follows every S of the piece before: that one it knows complete.
+    // the other could so take a tile that is still in flight for landed.  The use two before lies an even number of tiles back:
+    // it was the same stream's, or part of a unit of two row tiles, and has been watched.
     auto full_bar = [](uint32_t full, uint32_t tile, uint32_t stages) { return full + 16 * (tile % stages) + 8 * ((tile / stages) & 1); };
     auto full_phase = [](uint32_t tile, uint32_t stages) { return tile / stages / 2; };
 
@@ -452,16 +453,30 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
         const uint32_t lanes = (uint32_t)(q * 32) << 16;
         const uint32_t tmem_s = tmem + s * 128 + lanes, tmem_o = tmem + kTmemOBase + s * 128 + lanes;
         const int m = q * 32 + lane, tok = m / a.G, g = m - tok * a.G;
-        uint32_t n_s = 0, n_o[2] = {0, 0}, n_x = 0;    // completions seen so far
+        // One register of parities: phases of S, of O of this stream and of the other, of joins by this stream and by the other,
+        // key tiles so far; and whether the other stream is still reading this one's O.
+        enum : uint32_t { PH_S = 1, PH_O = 2, PH_O_OTHER = 4, PH_X = 8, PH_X_OTHER = 16, PH_TILE = 32, LENT = 64 };
+        uint32_t ph = 0;
         bool fail = false;
-        auto wait_all = [&](uint32_t bar, uint32_t count) {
-            fail = !wait(bar, count);
+        auto wait_all = [&](uint32_t bar, uint32_t phase) {
+            fail = !wait(bar, (ph & phase) ? 1 : 0);
             return !fail;
+        };
+        auto give_back = [&] {                         // waits until the other stream has read this one's O
+            if (wait_all(x_done + 8 * (s ^ 1), PH_X_OTHER)) ph ^= PH_X_OTHER | LENT;
         };
         while (!fail && w.next()) {
             const int n = w.k1 - w.k0;
             const bool dual = w.u.ntok > a.T;
-            if (!dual && s == 1 && n == 0) continue;
+            // Alternate tiles: tile c of the CTA's walk belongs to stream c & 1, and the stream of a piece's first tile writes its
+            // rows out.  So a piece of a single tile leaves the other stream free for the next.
+            const bool leads = dual || ((ph & PH_TILE) ? 1 : 0) == s, join = !dual && n > 1;
+            const int i0 = leads ? 0 : 1;
+            if (n & 1) ph ^= PH_TILE;
+            if (!leads && !join) {
+                if (n > 0) ph ^= PH_O_OTHER;
+                continue;
+            }
             const int t_row = (dual ? s * a.T : 0) + tok;                               // token of the unit
             const bool live = tok < a.T && t_row < w.u.ntok;
             const bool warp_live = __any_sync(0xffffffffu, live);
@@ -475,8 +490,11 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             float m_run = -INFINITY, l_run = 0.f;
             const int t_hi = (w.u.key_hi + kTileKeys - 1) / kTileKeys;
             int mine = 0;                                                               // tiles of this stream
-            for (int i = dual ? 0 : s; i < n; i += dual ? 1 : 2, ++mine) {
-                if (!wait_all(s_full + 8 * s, n_s++)) break;
+            if (n > 0 && (ph & LENT)) give_back();                                      // P V overwrites O
+            if (fail) break;
+            for (int i = i0; i < n; i += dual ? 1 : 2, ++mine) {
+                if (!wait_all(s_full + 8 * s, PH_S)) break;
+                ph ^= PH_S;
                 tc_fence_after();
                 if (warp_live) {
                     const int key0 = (t_hi - 1 - (w.k0 + i)) * kTileKeys;
@@ -587,30 +605,30 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             }
             if (fail) break;
             // ---- the piece's rows
-            const bool join = !dual && n > 0;
-            if (join && s == 1) {
-                ml_s[m] = make_float2(m_run, l_run);
+            if (!leads) {
+                ml_s[(s ^ 1) * kRows + m] = make_float2(m_run, l_run);
                 __syncwarp();
-                if (lane == 0) mbar_arrive(x_ready);
-                if (mine > 0) ++n_o[1];
-                if (!wait_all(x_done, n_x++)) break;                                    // stream 0 has read this stream's O
+                if (lane == 0) mbar_arrive(x_ready + 8 * (s ^ 1));
+                ph = (ph | LENT) ^ (PH_O | PH_O_OTHER);
                 continue;
             }
-            if (mine > 0 && !wait_all(o_full + 8 * s, n_o[s]++)) break;
-            if (dual && n > 0 && s == 0) ++n_o[1];
+            if (n > 0) {
+                if (!wait_all(o_full + 8 * s, PH_O)) break;
+                ph ^= PH_O;
+            }
             float r0 = 1.f, r1 = 0.f;                                                   // weights of the two streams' O
-            bool two = false;
             if (join) {
-                if (!wait_all(x_ready, n_x++)) break;
-                two = n > 1;
-                if (two && !wait_all(o_full + 8, n_o[1]++)) break;
-                const float2 ml = ml_s[m];
+                if (!wait_all(x_ready + 8 * s, PH_X) || !wait_all(o_full + 8 * (s ^ 1), PH_O_OTHER)) break;
+                ph ^= PH_X;
+                const float2 ml = ml_s[s * kRows + m];
                 const float top = fmaxf(m_run, ml.x);
                 r0 = m_run == -INFINITY ? 0.f : ex2_approx(m_run - top);
                 r1 = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - top);
                 l_run = l_run * r0 + ml.y * r1;
                 m_run = top;
             }
+            if (join || (dual && n > 0)) ph ^= PH_O_OTHER;
+            const uint32_t tmem_other = tmem + kTmemOBase + (s ^ 1) * 128 + lanes;
             tc_fence_after();
             if (warp_live) {
                 const int64_t orow = row * a.Hq + h;
@@ -623,7 +641,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                     uint32_t y[16], z[16];
                     if (n > 0) {
                         tmem_ld16(tmem_o + c, y);
-                        if (two) tmem_ld16(tmem_o + 128 + c, z);
+                        if (join) tmem_ld16(tmem_other + c, z);
                         tmem_wait_ld();
                     }
                     if (live) {
@@ -631,7 +649,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
 #pragma unroll
                         for (int j = 0; j < 16; ++j) {
                             float v = r0 > 0.f && n > 0 ? __uint_as_float(y[j]) * r0 : 0.f;
-                            if (two && r1 > 0.f) v = fmaf(__uint_as_float(z[j]), r1, v);
+                            if (r1 > 0.f) v = fmaf(__uint_as_float(z[j]), r1, v);
                             y[j] = __float_as_uint(v);
                         }
                         if (part) {
@@ -657,7 +675,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             }
             tc_fence_before();
             __syncwarp();
-            if (join && lane == 0) mbar_arrive(x_done);
+            if (join && lane == 0) mbar_arrive(x_done + 8 * s);
         }
     } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
@@ -667,18 +685,19 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
         auto wait_full = [&](uint32_t full, uint32_t tile, uint32_t stages) { return wait(full_bar(full, tile, stages), full_phase(tile, stages)); };
         const uint32_t idesc_s = instr_desc(kRows, kTileKeys, 0, 0), idesc_o = instr_desc(kRows, D, 0, 1);
         const uint32_t tmem_s = tmem + s * 128, tmem_o = tmem + kTmemOBase + s * 128;
-        uint32_t n_k = 0, n_p = 0, n_q[2] = {0, 0};
+        uint32_t n_k = 0, n_p = 0, q_slot = 0;
         bool ok = true;
         // The whole warp waits, one elected thread issues: a branch of one lane around the waits costs hundreds of cycles.
         while (ok && w.next()) {
             const int n = __shfl_sync(0xffffffffu, w.k1 - w.k0, 0);
             if (n == 0) continue;
             const bool dual = __shfl_sync(0xffffffffu, (int)(w.u.ntok > a.T), 0) != 0;
-            const int qb = dual ? s : 0, step = dual ? 1 : 2, i0 = dual ? 0 : s;
-            if (!(ok = wait(q_full + 8 * qb, n_q[qb]))) break;
-            ++n_q[0];
-            if (dual) ++n_q[1];
-            if (i0 >= n && lane == 0) mbar_arrive(q_empty);                             // a single key tile: nothing for stream 1
+            // both issuers watch every Q slot, so that none takes a slot in flight for the one two before it
+            const uint32_t slot = q_slot + (dual ? s : 0), qb = slot & 1;
+            if (!(ok = wait(q_full + 8 * (q_slot & 1), q_slot >> 1) && (!dual || wait(q_full + 8 * ((q_slot + 1) & 1), (q_slot + 1) >> 1)))) break;
+            q_slot += dual ? 2 : 1;
+            const int step = dual ? 1 : 2, i0 = dual ? 0 : (int)((n_k ^ s) & 1);
+            if (i0 >= n && lane == 0) mbar_arrive(q_empty + 8 * qb);                    // a single key tile, the other stream's
             const uint64_t dq = smem_desc(smem0 + qb * L::kQ, 16, 1024, 2);
             for (int i = i0; i < n; i += step, ++n_p) {
                 const uint32_t c = n_k + i, ks = c % L::kKStages, vs = c % L::kVStages;
@@ -727,7 +746,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
         const uint32_t full = is_v ? v_full : k_full, empty = is_v ? v_empty : k_empty;
         const uint32_t ring = smem0 + (is_v ? L::kOffV : L::kOffK);
         const int32_t oob = a.num_blocks * 2 * a.Hkv;                                   // past the slab: zero fill
-        uint32_t n_t = 0, n_q[2] = {0, 0}, n_land = 0;
+        uint32_t n_t = 0, q_slot = 0, n_land = 0;
         bool ok = true;
         while (ok && w.next()) {
             const int n = w.k1 - w.k0;
@@ -743,6 +762,29 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                 return b < w.u.nblk ? __ldg(table + b) : -1;
             };
             int32_t id_next = block_id(t0);
+            // Q, one buffer for each row tile, the two buffers in turn: a piece of one row tile finds the other one free.  It goes
+            // first if its buffers are free, else behind the first K tiles, which need not wait for the last S of the piece
+            // before.
+            bool q_sent = is_v;
+            auto send_q = [&](bool must) {
+                const uint32_t last = q_slot + (dual ? 1 : 0);
+                for (uint32_t k = q_slot; k <= last; ++k)
+                    if (k >= 2 && !(must ? wait(q_empty + 8 * (k & 1), (k >> 1) - 1) : poll(q_empty + 8 * (k & 1), (k >> 1) - 1))) {
+                        if (must) ok = false;
+                        return;
+                    }
+                const uint32_t k = q_slot + lane, bar = q_full + 8 * (k & 1);
+                if (k <= last) {
+                    mbar_expect_tx(bar, a.T * a.G * D * 2);
+#pragma unroll
+                    for (int hh = 0; hh < L::kHalves; ++hh)
+                        tma_load_3d(smem0 + (k & 1) * L::kQ + hh * (kRows * 128), &a.q_map, hh * 64, w.head * a.G, w.u.row0 + lane * a.T, bar);
+                }
+                __syncwarp();
+                q_slot = last + 1;
+                q_sent = true;
+            };
+            if (!is_v) send_q(false);
             for (int i = 0; i < n; ++i, ++n_t) {
                 const uint32_t st = n_t % stages, use = n_t / stages;
                 const int t = t0 - i;
@@ -781,22 +823,8 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                     __syncwarp();
                     if (lane == 0) mbar_arrive(full_now);
                 }
-                if (!is_v && i == min(1, n - 1)) {
-                    // Q, behind the first K tiles, which need not wait for the last S of the piece before
-                    for (int b = 0; b < (dual ? 2 : 1); ++b) {
-                        if (n_q[b] > 0 && !wait(q_empty + 8 * b, n_q[b] - 1)) ok = false;
-                        ++n_q[b];
-                    }
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    if (lane < (dual ? 2 : 1)) {
-                        mbar_expect_tx(q_full + 8 * lane, a.T * a.G * D * 2);
-#pragma unroll
-                        for (int hh = 0; hh < L::kHalves; ++hh)
-                            tma_load_3d(smem0 + lane * L::kQ + hh * (kRows * 128), &a.q_map, hh * 64, w.head * a.G, w.u.row0 + lane * a.T, q_full + 8 * lane);
-                    }
-                    __syncwarp();
-                }
+                if (!q_sent && i == min(1, n - 1)) send_q(true);
+                if (!ok) break;
             }
         }
         __syncwarp();
@@ -809,8 +837,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             };
             for (uint32_t back = 0; back < (uint32_t)stages && back < n_t; ++back) drain(full_bar(full, n_t - 1 - back, stages), full_phase(n_t - 1 - back, stages));
             if (is_v && n_land > 0) drain(v_land, n_land - 1);
-            for (int b = 0; b < 2 && !is_v; ++b)
-                if (n_q[b] > 0) drain(q_full + 8 * b, n_q[b] - 1);
+            for (uint32_t back = 1; back <= 2 && back <= q_slot; ++back) drain(q_full + 8 * ((q_slot - back) & 1), (q_slot - back) >> 1);
         }
     }
     }

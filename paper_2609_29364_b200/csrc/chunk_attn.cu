@@ -208,7 +208,6 @@ constexpr int kWarpIssue = 8, kWarpK = 10, kWarpV = 11;
 constexpr float kMaxSlack = 8.0f;                      // the running maximum may lag the true one by this much (log2 units)
 constexpr uint32_t kPollLimit = 1u << 30;              // polls of one wait, if nsd_config.wait_budget does not say
 enum : int { MODE_CAP = 1, MODE_BIAS = 2 };
-template <bool B> struct Const { __device__ constexpr bool operator()() const { return B; } };
 
 struct AttnArgs {
     CUtensorMap kv_map, q_map;
@@ -234,7 +233,7 @@ struct Smem {
     static constexpr int kOffK = 2 * kQ, kOffV = kOffK + kKStages * kTile;
     static constexpr int kOffMl = kOffV + kVStages * kTile;              // [2] statistics for a join, by the stream that joins
     static constexpr int kOffBars = kOffMl + 2 * kRows * 8;
-    static constexpr int kNumBars = 3 * kKStages + 3 * kVStages + 1 + 4 + 2 + 4 + 2 + 4;
+    static constexpr int kNumBars = 3 * kKStages + 3 * kVStages + 1 + 4 + 2 + 4 + 2 + 4 + 2;
     static constexpr int kOffMisc = kOffBars + kNumBars * 8;
     static constexpr int kBytes = kOffMisc + 16;
     static_assert(kBytes <= 227 * 1024, "shared memory budget");
@@ -249,7 +248,9 @@ struct Walk {
     // the piece under way
     ChunkUnit u;
     int head, k0, k1, slot;                            // key tiles [k0, k1) in walking order; partial slot or -1
-    __device__ __forceinline__ Walk(const ChunkPlan& p, int Hkv_) : units(p.units), at(p.starts[blockIdx.x]), end(p.starts[blockIdx.x + 1]), Hkv(Hkv_) {}
+    __device__ __forceinline__ Walk(const ChunkPlan& p, int Hkv_, bool planned) : units(p.units), at{}, end{}, Hkv(Hkv_) {
+        if (planned) at = p.starts[blockIdx.x], end = p.starts[blockIdx.x + 1];
+    }
     __device__ __forceinline__ bool next() {
         if (at.unit == end.unit && at.head == end.head && at.tile == end.tile) return false;
         u = units[at.unit];
@@ -383,14 +384,9 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
     using L = Smem<D>;
     extern __shared__ __align__(1024) unsigned char smem[];
     pdl_release_dependents();
-    if (a.p.header->magic != kMagic || a.p.header->max_rows != a.p.max_rows || a.p.header->n_ctas != (int)gridDim.x) {
-        if (blockIdx.x == 0 && threadIdx.x == 0) report(a.status, STATUS_BAD_TOKEN, -1);
-        return;
-    }
-    Walk w(a.p, a.Hkv);
-    if (w.at.unit == w.end.unit && w.at.head == w.end.head && w.at.tile == w.end.tile) return;
     const uint32_t smem0 = smem_u32(smem);
     if ((smem0 & 1023u) != 0) {
+        pdl_wait();
         if (threadIdx.x == 0) atomicOr(a.status, STATUS_LAYOUT);
         return;
     }
@@ -400,6 +396,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
     const uint32_t q_full = v_land + 8, q_empty = q_full + 16;                          // [2] per Q buffer
     const uint32_t s_full = q_empty + 16, p_full = s_full + 16, o_full = p_full + 32;   // [2], [2][2 halves], [2] per stream
     const uint32_t x_ready = o_full + 16, x_done = x_ready + 16;                        // [2] the join of a one-tile unit's streams
+    const uint32_t begun = x_done + 16;                                                 // [2] a stream has taken a tile's scores out
     uint32_t& tmem_base_s = *reinterpret_cast<uint32_t*>(smem + L::kOffMisc);
     volatile int& abort_s = *reinterpret_cast<volatile int*>(smem + L::kOffMisc + 4);
     float2* const ml_s = reinterpret_cast<float2*>(smem + L::kOffMl);
@@ -414,7 +411,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
         for (int s = 0; s < 2; ++s) {
             mbar_init(q_full + 8 * s, 1), mbar_init(q_empty + 8 * s, 2);
             mbar_init(s_full + 8 * s, 1), mbar_init(o_full + 8 * s, 1);
-            mbar_init(x_ready + 8 * s, 4), mbar_init(x_done + 8 * s, 4);
+            mbar_init(x_ready + 8 * s, 4), mbar_init(x_done + 8 * s, 4), mbar_init(begun + 8 * s, 4);
             mbar_init(p_full + 16 * s, 4), mbar_init(p_full + 16 * s + 8, 4);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -428,6 +425,12 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base_s, 0);
+    // Everything so far ran beside the end of the kernel before this one; what it writes (the plan, q, the pool) is read, and what
+    // it reads is written, from here on.
+    pdl_wait();
+    const bool planned = a.p.header->magic == kMagic && a.p.header->max_rows == a.p.max_rows && a.p.header->n_ctas == (int)gridDim.x;
+    if (!planned && blockIdx.x == 0 && tid == 0) report(a.status, STATUS_BAD_TOKEN, -1);
+    Walk w(a.p, a.Hkv, planned);
     // the count-th completion; the same answer in every lane
     auto poll = [&](uint32_t bar, uint32_t count) { return (bool)__all_sync(0xffffffffu, bar_try(bar, count & 1)); };
     auto wait = [&](uint32_t bar, uint32_t count) {
@@ -503,15 +506,11 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                     const float f = kRaw ? a.sc : 1.f;
                     uint32_t x[4][32];                                                  // scores, then pairs of weights
                     uint64_t l2[2] = {0, 0};                                            // the tile's sums
-                    auto scores = [&](int c, auto masked) {                             // to what the softmax is of
+                    auto scores = [&](int c) {                                          // to what the softmax is of
                         if constexpr (MODE & MODE_BIAS) {
                             const float b = slope * (float)(key0 - pos + c * 32), sc = MODE & MODE_CAP ? 1.f : a.sc;
 #pragma unroll
                             for (int j = 0; j < 32; ++j) x[c][j] = __float_as_uint(fmaf(__uint_as_float(x[c][j]), sc, fmaf(slope, (float)j, b)));
-                        }
-                        if constexpr (masked()) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) x[c][j] = c * 32 + j >= v0 && c * 32 + j < v1 ? x[c][j] : 0xff800000u;
                         }
                     };
                     auto largest = [&] {
@@ -543,61 +542,65 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                         __syncwarp();
                         if (lane == 0) mbar_arrive(p_full + 16 * s + 8 * half);
                     };
-                    if constexpr (MODE & MODE_CAP) {
-                        // capped where they lie, a piece at a time: one copy of the arithmetic instead of eight
+                    // Scores are capped and hidden where they lie, 32 at a time, in a loop of its own: one copy of that code, and
+                    // none of it in the way of a tile that needs neither.
+                    const bool masked = __any_sync(0xffffffffu, v0 > 0 || v1 < kTileKeys);
+                    if ((MODE & MODE_CAP) || masked) {
 #pragma unroll 1
                         for (int c = 0; c < 4; ++c) {
                             tmem_ld32(tmem_s + c * 32, x[0]);
                             tmem_wait_ld32(x[0]);
-                            cap32(x[0], a.sc, a.cap);
+                            if constexpr (MODE & MODE_CAP) cap32(x[0], a.sc, a.cap);
+                            if (masked) {
+                                const int first = v0 - c * 32, stop = v1 - c * 32;
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) x[0][j] = j >= first && j < stop ? x[0][j] : 0xff800000u;
+                            }
                             tmem_st32(tmem_s + c * 32, x[0]);
                         }
                         tmem_wait_st();
                     }
-                    auto tile = [&](auto masked) {
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) tmem_ld32(tmem_s + c * 32, x[c]);
+                    for (int c = 0; c < 4; ++c) tmem_ld32(tmem_s + c * 32, x[c]);
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            tmem_wait_ld32(x[c]);
-                            scores(c, masked);
-                        }
-                        const float m_tile = largest();
-                        const bool outgrown = mine == 0 || m_tile > m_run + kMaxSlack;  // the piece's first tile sets the maximum
-                        if (__any_sync(0xffffffffu, outgrown)) {
-                            const float m_new = outgrown ? m_tile : m_run;
-                            // O holds this piece's earlier tiles, complete since S of this one is
-                            if (mine > 0) {
-                                const float r = outgrown ? (m_run == -INFINITY ? 0.f : ex2_approx(m_run - m_new)) : 1.f;
+                    for (int c = 0; c < 4; ++c) {
+                        tmem_wait_ld32(x[c]);
+                        scores(c);
+                    }
+                    if (dual && lane == 0) mbar_arrive(begun + 8 * s);
+                    const float m_tile = largest();
+                    const bool outgrown = mine == 0 || m_tile > m_run + kMaxSlack;  // the piece's first tile sets the maximum
+                    if (__any_sync(0xffffffffu, outgrown)) {
+                        const float m_new = outgrown ? m_tile : m_run;
+                        // O holds this piece's earlier tiles, complete since S of this one is
+                        if (mine > 0) {
+                            const float r = outgrown ? (m_run == -INFINITY ? 0.f : ex2_approx(m_run - m_new)) : 1.f;
 #pragma unroll 1
-                                for (int c = 0; c < D; c += 16) {
-                                    uint32_t y[16];
-                                    tmem_ld16(tmem_o + c, y);
-                                    tmem_wait_ld();
+                            for (int c = 0; c < D; c += 16) {
+                                uint32_t y[16];
+                                tmem_ld16(tmem_o + c, y);
+                                tmem_wait_ld();
 #pragma unroll
-                                    for (int j = 0; j < 16; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * r);
-                                    tmem_st16(tmem_o + c, y);
-                                }
-                                tmem_wait_st();
-                                l_run *= r;
+                                for (int j = 0; j < 16; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * r);
+                                tmem_st16(tmem_o + c, y);
                             }
-                            m_run = m_new;
+                            tmem_wait_st();
+                            l_run *= r;
                         }
-                        weights(0);
-                        weights(1);
-                        store(0);
-                        weights(2);
-                        hand_over(0);
-                        weights(3);
-                        store(1);
-                        hand_over(1);
-                    };
-                    if (__any_sync(0xffffffffu, v0 > 0 || v1 < kTileKeys)) tile(Const<true>());
-                    else tile(Const<false>());
-                    if (fail) break;
+                        m_run = m_new;
+                    }
+                    weights(0);
+                    weights(1);
+                    store(0);
+                    weights(2);
+                    hand_over(0);
+                    weights(3);
+                    store(1);
+                    hand_over(1);
                     const float2 l = unpair(add2(l2[0], l2[1]));
                     l_run += l.x + l.y;
                 } else {
+                    if (dual && lane == 0) mbar_arrive(begun + 8 * s);
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(p_full + 16 * s), mbar_arrive(p_full + 16 * s + 8);
@@ -685,7 +688,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
         auto wait_full = [&](uint32_t full, uint32_t tile, uint32_t stages) { return wait(full_bar(full, tile, stages), full_phase(tile, stages)); };
         const uint32_t idesc_s = instr_desc(kRows, kTileKeys, 0, 0), idesc_o = instr_desc(kRows, D, 0, 1);
         const uint32_t tmem_s = tmem + s * 128, tmem_o = tmem + kTmemOBase + s * 128;
-        uint32_t n_k = 0, n_p = 0, q_slot = 0;
+        uint32_t n_k = 0, n_p = 0, q_slot = 0, n_begun = 0;
         bool ok = true;
         // The whole warp waits, one elected thread issues: a branch of one lane around the waits costs hundreds of cycles.
         while (ok && w.next()) {
@@ -703,6 +706,14 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                 const uint32_t c = n_k + i, ks = c % L::kKStages, vs = c % L::kVStages;
                 const bool last = i + step >= n;
                 if (!(ok = wait_full(k_full, c, L::kKStages))) break;
+                if (dual) {
+                    // The streams keep half a step apart: S of a tile goes once the other stream has taken the scores of the tile
+                    // before out (in step both would wait for S and then both for the MUFU unit: a prompt of 8192 tokens 565 us
+                    // instead of 525).
+                    const bool go = s == 1 ? wait(begun, n_begun) : (n_begun == 0 || wait(begun + 8, n_begun - 1));
+                    if (!(ok = go)) break;
+                    ++n_begun;
+                }
                 tc_fence_after();
                 const uint64_t dk = smem_desc(smem0 + L::kOffK + ks * L::kTile, 16, L::kGroupPitch, 2);
                 if (elect_one()) {
@@ -938,13 +949,13 @@ template <int D>
 cudaError_t launch_attn_d(const AttnArgs& a, int mode, int n_ctas, cudaStream_t st) {
     const dim3 grid(n_ctas), block(kThreadsA);
     const size_t smem = Smem<D>::kBytes;
+    // a programmatic dependent of whatever precedes it: the kernel waits before it touches anything but its own shared memory
     switch (mode) {
-        case 0: chunk_attn_kernel<D, 0><<<grid, block, smem, st>>>(a); break;
-        case MODE_CAP: chunk_attn_kernel<D, MODE_CAP><<<grid, block, smem, st>>>(a); break;
-        case MODE_BIAS: chunk_attn_kernel<D, MODE_BIAS><<<grid, block, smem, st>>>(a); break;
-        default: chunk_attn_kernel<D, MODE_CAP | MODE_BIAS><<<grid, block, smem, st>>>(a); break;
+        case 0: return launch_kernel(chunk_attn_kernel<D, 0>, grid, block, smem, st, true, a);
+        case MODE_CAP: return launch_kernel(chunk_attn_kernel<D, MODE_CAP>, grid, block, smem, st, true, a);
+        case MODE_BIAS: return launch_kernel(chunk_attn_kernel<D, MODE_BIAS>, grid, block, smem, st, true, a);
+        default: return launch_kernel(chunk_attn_kernel<D, MODE_CAP | MODE_BIAS>, grid, block, smem, st, true, a);
     }
-    return cudaGetLastError();
 }
 
 }  // namespace

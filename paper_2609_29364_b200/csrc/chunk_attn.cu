@@ -233,7 +233,7 @@ struct Smem {
     static constexpr int kOffK = 2 * kQ, kOffV = kOffK + kKStages * kTile;
     static constexpr int kOffMl = kOffV + kVStages * kTile;              // [2] statistics for a join, by the stream that joins
     static constexpr int kOffBars = kOffMl + 2 * kRows * 8;
-    static constexpr int kNumBars = 3 * kKStages + 3 * kVStages + 1 + 4 + 2 + 4 + 2 + 4 + 2;
+    static constexpr int kNumBars = 3 * kKStages + 3 * kVStages + 2 + 4 + 2 + 4 + 2 + 4 + 2;
     static constexpr int kOffMisc = kOffBars + kNumBars * 8;
     static constexpr int kBytes = kOffMisc + 16;
     static_assert(kBytes <= 227 * 1024, "shared memory budget");
@@ -392,8 +392,8 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
     }
     const uint32_t bar0 = smem0 + L::kOffBars;
     const uint32_t k_full = bar0, k_empty = k_full + 16 * L::kKStages, v_full = k_empty + 8 * L::kKStages, v_empty = v_full + 16 * L::kVStages;
-    const uint32_t v_land = v_empty + 8 * L::kVStages; // a V tile whose hidden rows have to be cleared lands here first
-    const uint32_t q_full = v_land + 8, q_empty = q_full + 16;                          // [2] per Q buffer
+    const uint32_t v_land = v_empty + 8 * L::kVStages; // [2] a V tile whose hidden rows have to be cleared lands here first
+    const uint32_t q_full = v_land + 16, q_empty = q_full + 16;                          // [2] per Q buffer
     const uint32_t s_full = q_empty + 16, p_full = s_full + 16, o_full = p_full + 32;   // [2], [2][2 halves], [2] per stream
     const uint32_t x_ready = o_full + 16, x_done = x_ready + 16;                        // [2] the join of a one-tile unit's streams
     const uint32_t begun = x_done + 16;                                                 // [2] a stream has taken a tile's scores out
@@ -407,7 +407,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
     if (tid == 0) {
         for (int s = 0; s < L::kKStages; ++s) mbar_init(k_full + 16 * s, 1), mbar_init(k_full + 16 * s + 8, 1), mbar_init(k_empty + 8 * s, 2);
         for (int s = 0; s < L::kVStages; ++s) mbar_init(v_full + 16 * s, 1), mbar_init(v_full + 16 * s + 8, 1), mbar_init(v_empty + 8 * s, 2);
-        mbar_init(v_land, 1);
+        mbar_init(v_land, 1), mbar_init(v_land + 8, 1);
         for (int s = 0; s < 2; ++s) {
             mbar_init(q_full + 8 * s, 1), mbar_init(q_empty + 8 * s, 2);
             mbar_init(s_full + 8 * s, 1), mbar_init(o_full + 8 * s, 1);
@@ -697,7 +697,8 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             const bool dual = __shfl_sync(0xffffffffu, (int)(w.u.ntok > a.T), 0) != 0;
             // both issuers watch every Q slot, so that none takes a slot in flight for the one two before it
             const uint32_t slot = q_slot + (dual ? s : 0), qb = slot & 1;
-            if (!(ok = wait(q_full + 8 * (q_slot & 1), q_slot >> 1) && (!dual || wait(q_full + 8 * ((q_slot + 1) & 1), (q_slot + 1) >> 1)))) break;
+            ok = wait(q_full + 8 * (q_slot & 1), q_slot >> 1) && (!dual || wait(q_full + 8 * ((q_slot + 1) & 1), (q_slot + 1) >> 1));
+            if (!ok) break;
             q_slot += dual ? 2 : 1;
             const int step = dual ? 1 : 2, i0 = dual ? 0 : (int)((n_k ^ s) & 1);
             if (i0 >= n && lane == 0) mbar_arrive(q_empty + 8 * qb);                    // a single key tile, the other stream's
@@ -710,8 +711,8 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                     // The streams keep half a step apart: S of a tile goes once the other stream has taken the scores of the tile
                     // before out (in step both would wait for S and then both for the MUFU unit: a prompt of 8192 tokens 565 us
                     // instead of 525).
-                    const bool go = s == 1 ? wait(begun, n_begun) : (n_begun == 0 || wait(begun + 8, n_begun - 1));
-                    if (!(ok = go)) break;
+                    ok = s == 1 ? wait(begun, n_begun) : (n_begun == 0 || wait(begun + 8, n_begun - 1));
+                    if (!ok) break;
                     ++n_begun;
                 }
                 tc_fence_after();
@@ -759,6 +760,27 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
         const int32_t oob = a.num_blocks * 2 * a.Hkv;                                   // past the slab: zero fill
         uint32_t n_t = 0, q_slot = 0, n_land = 0;
         bool ok = true;
+        // Hidden rows of V have to be finite, since 0 x NaN is NaN: those of a block that also holds visible keys are cleared once
+        // the tile has landed (blocks without any are zero fill).  The next tile's copies go out first.
+        struct Due {
+            uint32_t at, full, land;                   // the tile, its full barrier, which landing
+            int first, last, head, rows;               // rows [first, first + head) and [last, last + rows - head); rows = 0: nothing due
+        } due{};
+        auto clear = [&] {
+            if (!wait(v_land + 8 * (due.land & 1), due.land >> 1)) {
+                ok = false;
+                due.rows = 0;
+                return;
+            }
+            for (int c = lane; c < due.rows * (D / 8); c += 32) {
+                const int k = c / (D / 8), ch = c % (D / 8), r = k < due.head ? due.first + k : due.last + k - due.head;
+                *reinterpret_cast<int4*>(smem + due.at + (r >> 4) * L::kBlockBytes + ((r >> 3) & 1) * L::kGroupPitch + (ch >> 3) * 1024 + (r & 7) * 128 + (ch & 7) * 16) = make_int4(0, 0, 0, 0);
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(due.full);
+            due.rows = 0;
+        };
         while (ok && w.next()) {
             const int n = w.k1 - w.k0;
             if (n == 0) continue;
@@ -806,38 +828,26 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                     if ((uint32_t)id < (uint32_t)a.num_blocks) tile = (id * 2 + (is_v ? 1 : 0)) * a.Hkv + w.head;
                     else report(a.status, STATUS_BAD_BLOCK, w.u.req);
                 }
-                if (use > 0 && !wait(empty + 8 * st, use - 1)) ok = false;
-                ok = __all_sync(0xffffffffu, ok);
+                if (use > 0) {
+                    if (due.rows && !poll(empty + 8 * st, use - 1)) clear();
+                    if (ok && !wait(empty + 8 * st, use - 1)) ok = false;
+                }
                 if (!ok) break;
-                // hidden rows of V have to be finite, since 0 x NaN is NaN: those of a block that also holds visible keys are
-                // cleared once the tile has landed (blocks without any are zero fill)
                 const int z0 = w.u.key_lo - t * kTileKeys, z1 = w.u.key_hi - t * kTileKeys;             // visible keys of the tile: [z0, z1)
-                const bool ragged = is_v && ((z0 > 0 && (z0 & 15)) || (z1 < kTileKeys && (z1 & 15)));
-                const uint32_t full_now = full_bar(full, n_t, stages), bar = ragged ? v_land : full_now;
+                const int head_rows = z0 > 0 ? z0 & 15 : 0, tail_rows = z1 < kTileKeys ? -z1 & 15 : 0;
+                const bool ragged = is_v && (head_rows | tail_rows);
+                const uint32_t full_now = full_bar(full, n_t, stages), bar = ragged ? v_land + 8 * (n_land & 1) : full_now;
                 if (lane == 0) mbar_expect_tx(bar, L::kTile);
                 __syncwarp();
                 if (lane < kBlocks) tma_load_5d(ring + st * L::kTile + lane * L::kBlockBytes, &a.kv_map, tile, bar);
-                if (ragged) {
-                    if (!wait(v_land, n_land++)) ok = false;
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    unsigned char* vt = smem + L::kOffV + st * L::kTile;
-                    auto clear = [&](int first, int last) {                             // rows [first, last) of one block
-                        for (int c = lane; c < (last - first) * (D / 8); c += 32) {
-                            const int r = first + c / (D / 8), ch = c % (D / 8);
-                            *reinterpret_cast<int4*>(vt + (r >> 4) * L::kBlockBytes + ((r >> 3) & 1) * L::kGroupPitch + (ch >> 3) * 1024 + (r & 7) * 128 + (ch & 7) * 16) = make_int4(0, 0, 0, 0);
-                        }
-                    };
-                    if (z0 > 0 && (z0 & 15)) clear(z0 & ~15, z0);
-                    if (z1 < kTileKeys && (z1 & 15)) clear(z1, (z1 + 15) & ~15);
-                    fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(full_now);
-                }
+                if (due.rows) clear();                                                  // the tile before, now that this one is under way
+                if (ragged) due = Due{ring + st * L::kTile - smem0, full_now, n_land++, z0 - head_rows, z1, head_rows, head_rows + tail_rows};
+                if (!ok) break;
                 if (!q_sent && i == min(1, n - 1)) send_q(true);
                 if (!ok) break;
             }
         }
+        if (ok && due.rows) clear();
         __syncwarp();
         if (abort_s && lane == 0) {
             // the CTA is giving up: copies that nobody waited for may still be landing; each barrier's latest phase gets a
@@ -847,7 +857,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                     if (mbar_try(bar, count & 1)) break;
             };
             for (uint32_t back = 0; back < (uint32_t)stages && back < n_t; ++back) drain(full_bar(full, n_t - 1 - back, stages), full_phase(n_t - 1 - back, stages));
-            if (is_v && n_land > 0) drain(v_land, n_land - 1);
+            for (uint32_t back = 1; back <= 2 && back <= n_land; ++back) drain(v_land + 8 * ((n_land - back) & 1), (n_land - back) >> 1);
             for (uint32_t back = 1; back <= 2 && back <= q_slot; ++back) drain(q_full + 8 * ((q_slot - back) & 1), (q_slot - back) >> 1);
         }
     }
@@ -861,10 +871,11 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
 // Joins the pieces of the units that CTA boundaries cut: boundary c cuts unit (unit, head) when CTA c starts inside it, and
 // the first such boundary of a unit does the work for all of them.  Pieces are read in walking order, so the result does not
 // depend on timing.  A thread = four dims of one row at a time.
-constexpr int kJoinThreads = 256, kJoinSlices = 4;
+constexpr int kJoinThreads = 256, kJoinSlices = 4, kMaxCtas = 511;
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads)
 chunk_join_kernel(const __grid_constant__ ChunkPlan p, uint16_t* __restrict__ o, float* __restrict__ lse, int32_t Hq, int32_t Hkv, int32_t G, int32_t T) {
+    __shared__ ChunkStart starts[kMaxCtas + 1];
     const int c = blockIdx.x + 1;
     pdl_wait();
     if (p.header->magic != kMagic || p.header->max_rows != p.max_rows || p.header->n_ctas != p.n_ctas) return;
@@ -872,26 +883,46 @@ chunk_join_kernel(const __grid_constant__ ChunkPlan p, uint16_t* __restrict__ o,
     auto same = [&](const ChunkStart& x) { return x.unit == cut.unit && x.head == cut.head && x.tile > 0; };
     if (cut.tile == 0 || same(before)) return;
     const ChunkUnit u = p.units[cut.unit];
+    const int elements = u.ntok * G * (D / 4);
+    if ((int)blockIdx.y * kJoinThreads >= elements) return;
+    for (int k = c + threadIdx.x; k <= p.n_ctas; k += kJoinThreads) starts[k] = p.starts[k];
+    __syncthreads();
     int end = c;                                       // CTAs c .. end - 1 start inside the unit
-    while (end < p.n_ctas && same(p.starts[end])) ++end;
-    for (int e = blockIdx.y * kJoinThreads + threadIdx.x; e < u.ntok * G * (D / 4); e += kJoinSlices * kJoinThreads) {
+    while (end < p.n_ctas && same(starts[end])) ++end;
+    // a CTA without work left nothing
+    auto left = [&](int k) {
+        if (k < c) return true;
+        const ChunkStart x = starts[k], y = starts[k + 1];
+        return x.unit != y.unit || x.head != y.head || x.tile != y.tile;
+    };
+    for (int e = blockIdx.y * kJoinThreads + threadIdx.x; e < elements; e += kJoinSlices * kJoinThreads) {
         const int r = e / (D / 4), d4 = e % (D / 4), t = r / G, g = r - t * G;
         const int64_t in = (int64_t)(t / T) * kRows + (t % T) * G + g;                  // row of a partial slot
         float m = -INFINITY, l = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = c - 1; k < end; ++k) {
-            if (k >= c) {                              // a CTA without work left nothing
-                const ChunkStart x = p.starts[k], y = p.starts[k + 1];
-                if (x.unit == y.unit && x.head == y.head && x.tile == y.tile) continue;
+        constexpr int kAhead = 4;                      // pieces whose loads are under way together
+        for (int k0 = c - 1; k0 < end; k0 += kAhead) {
+            float2 ml[kAhead];
+            float4 v[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int k = k0 + i;
+                ml[i] = make_float2(-INFINITY, 0.f);
+                v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (k < end && left(k)) {
+                    const int64_t at = (int64_t)(k < c ? 2 * k + 1 : 2 * k) * 2 * kRows + in;
+                    ml[i] = *reinterpret_cast<const float2*>(p.part_ml + at * 2);
+                    v[i] = *reinterpret_cast<const float4*>(p.part_acc + at * D + d4 * 4);
+                }
             }
-            const int64_t at = (int64_t)(k < c ? 2 * k + 1 : 2 * k) * 2 * kRows + in;
-            const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + at * 2);
-            const float4 v = *reinterpret_cast<const float4*>(p.part_acc + at * D + d4 * 4);
-            if (ml.x == -INFINITY) continue;           // this piece holds no key the row sees
-            const float top = fmaxf(m, ml.x), f = m == -INFINITY ? 0.f : exp2f(m - top), x = exp2f(ml.x - top);
-            acc.x = acc.x * f + v.x * x, acc.y = acc.y * f + v.y * x, acc.z = acc.z * f + v.z * x, acc.w = acc.w * f + v.w * x;
-            l = l * f + ml.y * x;
-            m = top;
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (ml[i].x == -INFINITY) continue;    // this piece holds no key the row sees
+                const float top = fmaxf(m, ml[i].x), f = m == -INFINITY ? 0.f : exp2f(m - top), x = exp2f(ml[i].x - top);
+                acc.x = acc.x * f + v[i].x * x, acc.y = acc.y * f + v[i].y * x, acc.z = acc.z * f + v[i].z * x, acc.w = acc.w * f + v[i].w * x;
+                l = l * f + ml[i].y * x;
+                m = top;
+            }
         }
         const float inv = l > 0.f ? 1.f / l : 0.f;
         const int64_t orow = (int64_t)(u.row0 + t) * Hq + cut.head * G + g;
@@ -961,6 +992,7 @@ cudaError_t launch_attn_d(const AttnArgs& a, int mode, int n_ctas, cudaStream_t 
 }  // namespace
 
 size_t chunk_plan_layout(ChunkPlan* p, void* base, const Shape& s, int32_t max_batch, int64_t max_rows, int32_t n_sms) {
+    n_sms = n_sms < kMaxCtas ? n_sms : kMaxCtas;
     const int64_t T = kRows / (s.Hq / s.Hkv);
     const int64_t max_units = max_batch + max_rows / (2 * T) + 2;
     size_t off = 0;

@@ -21,6 +21,12 @@ __device__ __forceinline__ void report(int32_t* status, int32_t bit, int r) {
     atomicCAS(status + 1, 0, r + 1);
 }
 
+// A buffer that nsd_chunk_plan has filled for these rows and this shape.
+__device__ __forceinline__ bool is_plan(const ChunkPlan& p, int T, int Hkv) {
+    const ChunkHeader h = *p.header;
+    return h.magic == kMagic && h.max_rows == p.max_rows && h.n_ctas == p.n_ctas && h.T == T && h.Hkv == Hkv;
+}
+
 // ---- plan -------------------------------------------------------------------------------------
 // Two kernels.  The first works on every request's units side by side: the visible keys of each
 // row and their hull over the unit.  Unit j of request r sits at r + floor(q_indptr[r] / TU) + j,
@@ -142,7 +148,7 @@ chunk_split_kernel(const PlanArgs a) {
     }
     if (tid == 0) {
         cost[n_units] = c_all;
-        *a.p.header = ChunkHeader{kMagic, n_units, a.p.max_rows, a.p.n_ctas, 2 * a.T};
+        *a.p.header = ChunkHeader{kMagic, n_units, a.p.max_rows, a.p.n_ctas, a.masks.window == 0 && !a.masks.prefix_len && !a.masks.row_first, a.T, a.Hkv};
     }
     __syncthreads();
     // the line: request by request, kv head by kv head, unit by unit, tile by tile
@@ -233,7 +239,7 @@ struct Smem {
     static constexpr int kOffK = 2 * kQ, kOffV = kOffK + kKStages * kTile;
     static constexpr int kOffMl = kOffV + kVStages * kTile;              // [2] statistics for a join, by the stream that joins
     static constexpr int kOffBars = kOffMl + 2 * kRows * 8;
-    static constexpr int kNumBars = 3 * kKStages + 3 * kVStages + 2 + 4 + 2 + 4 + 2 + 4 + 2;
+    static constexpr int kNumBars = 3 * kKStages + 3 * kVStages + 2 + 4 + 2 + 4 + 2 + 4 + 2 + 2;
     static constexpr int kOffMisc = kOffBars + kNumBars * 8;
     static constexpr int kBytes = kOffMisc + 16;
     static_assert(kBytes <= 227 * 1024, "shared memory budget");
@@ -397,6 +403,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
     const uint32_t s_full = q_empty + 16, p_full = s_full + 16, o_full = p_full + 32;   // [2], [2][2 halves], [2] per stream
     const uint32_t x_ready = o_full + 16, x_done = x_ready + 16;                        // [2] the join of a one-tile unit's streams
     const uint32_t begun = x_done + 16;                                                 // [2] a stream has taken a tile's scores out
+    const uint32_t flushed = begun + 16;                                                // [2] an issuer that gives up has no MMA in flight
     uint32_t& tmem_base_s = *reinterpret_cast<uint32_t*>(smem + L::kOffMisc);
     volatile int& abort_s = *reinterpret_cast<volatile int*>(smem + L::kOffMisc + 4);
     float2* const ml_s = reinterpret_cast<float2*>(smem + L::kOffMl);
@@ -411,7 +418,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
         for (int s = 0; s < 2; ++s) {
             mbar_init(q_full + 8 * s, 1), mbar_init(q_empty + 8 * s, 2);
             mbar_init(s_full + 8 * s, 1), mbar_init(o_full + 8 * s, 1);
-            mbar_init(x_ready + 8 * s, 4), mbar_init(x_done + 8 * s, 4), mbar_init(begun + 8 * s, 4);
+            mbar_init(x_ready + 8 * s, 4), mbar_init(x_done + 8 * s, 4), mbar_init(begun + 8 * s, 4), mbar_init(flushed + 8 * s, 1);
             mbar_init(p_full + 16 * s, 4), mbar_init(p_full + 16 * s + 8, 4);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -428,7 +435,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
     // Everything so far ran beside the end of the kernel before this one; what it writes (the plan, q, the pool) is read, and what
     // it reads is written, from here on.
     pdl_wait();
-    const bool planned = a.p.header->magic == kMagic && a.p.header->max_rows == a.p.max_rows && a.p.header->n_ctas == (int)gridDim.x;
+    const bool planned = is_plan(a.p, a.T, a.Hkv);
     if (!planned && blockIdx.x == 0 && tid == 0) report(a.status, STATUS_BAD_TOKEN, -1);
     Walk w(a.p, a.Hkv, planned);
     // the count-th completion; the same answer in every lane
@@ -458,8 +465,8 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
         const int m = q * 32 + lane, tok = m / a.G, g = m - tok * a.G;
         // One register of parities: phases of S, of O of this stream and of the other, of joins by this stream and by the other,
         // key tiles so far; and whether the other stream is still reading this one's O.
-        enum : uint32_t { PH_S = 1, PH_O = 2, PH_O_OTHER = 4, PH_X = 8, PH_X_OTHER = 16, PH_TILE = 32, LENT = 64 };
-        uint32_t ph = 0;
+        enum : uint32_t { PH_S = 1, PH_O = 2, PH_O_OTHER = 4, PH_X = 8, PH_X_OTHER = 16, PH_TILE = 32, LENT = 64, CAUSAL = 128 };
+        uint32_t ph = planned && a.p.header->causal ? CAUSAL : 0;    // CAUSAL: a row's keys follow from its position
         bool fail = false;
         auto wait_all = [&](uint32_t bar, uint32_t phase) {
             fail = !wait(bar, (ph & phase) ? 1 : 0);
@@ -486,10 +493,13 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             const int64_t row = w.u.row0 + t_row;
             const int h = w.head * a.G + g;
             int lo = 0, hi = 0x7fffffff;                                                // lanes without a row never mask
-            if (live) lo = a.p.row_lo[row], hi = a.p.row_hi[row];
             float slope = 0.f;
             if constexpr (MODE & MODE_BIAS) slope = live ? a.slopes[h] * kLog2e : 0.f;
             const int pos = w.u.pos0 + t_row;
+            if (live) {
+                if (ph & CAUSAL) hi = pos + 1;
+                else lo = a.p.row_lo[row], hi = a.p.row_hi[row];
+            }
             float m_run = -INFINITY, l_run = 0.f;
             const int t_hi = (w.u.key_hi + kTileKeys - 1) / kTileKeys;
             int mine = 0;                                                               // tiles of this stream
@@ -751,6 +761,12 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             n_k += n;
         }
         __syncwarp();
+        if (__any_sync(0xffffffffu, abort_s != 0)) {
+            // the CTA is giving up: what is still in flight reads shared memory and writes tensor memory
+            if (elect_one()) umma_commit(flushed + 8 * s);
+            const long long t0 = clock64();
+            while (!bar_try(flushed + 8 * s, 0) && clock64() - t0 < kWaitCycles) {}
+        }
     } else {
         // ================================ producers ================================
         const bool is_v = warp == kWarpV;
@@ -853,8 +869,8 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             // the CTA is giving up: copies that nobody waited for may still be landing; each barrier's latest phase gets a
             // bounded wait of its own before the shared memory goes back to the SM
             auto drain = [&](uint32_t bar, uint32_t count) {
-                for (uint32_t i = 0; i < limit; ++i)
-                    if (mbar_try(bar, count & 1)) break;
+                const long long t0 = clock64();
+                while (!bar_try(bar, count & 1) && clock64() - t0 < kWaitCycles) {}
             };
             for (uint32_t back = 0; back < (uint32_t)stages && back < n_t; ++back) drain(full_bar(full, n_t - 1 - back, stages), full_phase(n_t - 1 - back, stages));
             for (uint32_t back = 1; back <= 2 && back <= n_land; ++back) drain(v_land + 8 * ((n_land - back) & 1), (n_land - back) >> 1);
@@ -878,7 +894,7 @@ chunk_join_kernel(const __grid_constant__ ChunkPlan p, uint16_t* __restrict__ o,
     __shared__ ChunkStart starts[kMaxCtas + 1];
     const int c = blockIdx.x + 1;
     pdl_wait();
-    if (p.header->magic != kMagic || p.header->max_rows != p.max_rows || p.header->n_ctas != p.n_ctas) return;
+    if (!is_plan(p, T, Hkv)) return;
     const ChunkStart cut = p.starts[c], before = p.starts[c - 1];
     auto same = [&](const ChunkStart& x) { return x.unit == cut.unit && x.head == cut.head && x.tile > 0; };
     if (cut.tile == 0 || same(before)) return;

@@ -185,7 +185,9 @@ struct ChunkHeader {
     uint32_t magic;
     int32_t n_units;
     int64_t max_rows;
-    int32_t n_ctas, tokens;                  // CTAs the work is split over, tokens per unit
+    int32_t n_ctas;                          // CTAs the work is split over
+    int32_t causal;                          // no window, prefix or documents: row_lo / row_hi need not be read
+    int32_t T, Hkv;                          // the shape it was made for
 };
 struct ChunkPlan {                           // the buffer's parts
     ChunkHeader* header;

@@ -339,3 +339,63 @@ def test_refusals():
         c.nsd_chunk_attn(plan, 30, b.pool, b.q[0], b.o[0], b.lse[0, :3], b.kvi)
     assert c.nsd_chunk_plan_bytes(-1) == 0
     assert (b.o == 7.0).all()
+
+
+def test_a_plan_of_another_shape_is_reported():
+    b = Batch([100, 30], [30, 1], heads=8, kv_heads=2, seed=31)
+    c, other = b.context(), Batch([100, 30], [30, 1], heads=8, kv_heads=4, seed=31).context()
+    plan = torch.empty(max(c.nsd_chunk_plan_bytes(31), other.nsd_chunk_plan_bytes(31)), dtype=torch.uint8, device=DEV)
+    other.nsd_chunk_plan(plan, 31, b.qp, b.ctx_len, b.kvp)
+    b.attn(c, plan)
+    assert c.nsd_get_status()[0] == 6 and (b.o == 7.0).all()
+
+
+@pytest.mark.parametrize("shape", [(32, 8, 128), (12, 4, 64)])
+@pytest.mark.parametrize("seed", range(4))
+def test_random_batches(shape, seed):
+    """Single tokens, short and long chunks of any length beside one another: every way a CTA's share can begin, end and
+    change between units of one and two row tiles, with odd and even numbers of key tiles."""
+    rng = np.random.default_rng(100 + seed)
+    n = 24
+    ctx = np.where(rng.random(n) < 0.3, rng.integers(0, 40, n), rng.integers(0, 4000, n))
+    new = np.where(rng.random(n) < 0.6, 1, rng.integers(0, 400, n))
+    masks = [{}, dict(window=700), dict(prefix_len=rng.integers(0, 500, n).tolist()), {}][seed]
+    Batch(ctx.tolist(), new.tolist(), seed=seed, **small(shape)).run(softcap=25.0 if seed == 3 else 0.0, **masks)
+
+
+def test_long_single_tokens_from_scattered_blocks_again_and_again():
+    """Many long pieces of alternate key tiles, odd in number, out of a pool far larger than the cache: copies land in any
+    order, and an issuer must not take one in flight for landed.  The same bits each time, and the right ones."""
+    rng = np.random.default_rng(32)
+    ctx = (128 * (2 * rng.integers(10, 90, 40) + 1) - 1 - rng.integers(0, 3, 40)).tolist()
+    b = Batch(ctx, [1] * 40, heads=32, kv_heads=8, seed=32)
+    c = b.context()
+    plan = b.plan(c)
+    b.attn(c, plan)
+    first = b.o.clone()
+    for _ in range(50):
+        b.attn(c, plan)
+        assert torch.equal(b.o, first)
+    assert c.nsd_get_status() == (0, -1)
+    b.check()
+
+
+def test_more_units_than_the_split_keeps_in_shared_memory():
+    n, heads, dim = 13000, 2, 64
+    from chunk_testlib import context
+
+    g = torch.Generator().manual_seed(33)
+    pool = torch.randn((n, 2, 1, 16, dim), generator=g).to(torch.bfloat16).to(DEV)
+    q = torch.randn((n, heads, dim), generator=g).to(torch.bfloat16).to(DEV)
+    c = context(heads, 1, dim, n, max_batch=n)
+    kvi = torch.randperm(n, generator=g).to(torch.int32).to(DEV)
+    ramp = torch.arange(n + 1, dtype=torch.int64, device=DEV)
+    o, lse = torch.empty_like(q), torch.empty((n, heads), device=DEV)
+    plan = torch.empty(c.nsd_chunk_plan_bytes(n), dtype=torch.uint8, device=DEV)
+    c.nsd_chunk_plan(plan, n, ramp, torch.full((n,), 3, dtype=torch.int32, device=DEV), ramp)
+    c.nsd_chunk_attn(plan, n, pool, q, o, lse, kvi)
+    assert c.nsd_get_status() == (0, -1)
+    kv = pool[kvi.long()].double()[:, :, 0, :4]                      # four keys each
+    s = torch.einsum("nhd,nkd->nhk", q.double(), kv[:, 0]) / dim ** 0.5
+    w = torch.softmax(s, -1)
+    check_attn(o, lse, (torch.einsum("nhk,nkd->nhd", w, kv[:, 1]), torch.logsumexp(s, -1), torch.einsum("nhk,nkd->nhd", w, kv[:, 1].abs())))

@@ -715,6 +715,9 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             ok = wait(q_full + 8 * (q_slot & 1), q_slot >> 1) && (!dual || wait(q_full + 8 * ((q_slot + 1) & 1), (q_slot + 1) >> 1));
             if (!ok) break;
             q_slot += dual ? 2 : 1;
+            // and a slot of a pair is filled anew only when this issuer, whose it is not, has watched it too: it could else be
+            // full twice between two looks, which a wait by parity takes for not full yet
+            if (dual && lane == 0) mbar_arrive(q_empty + 8 * (qb ^ 1));
             const int step = dual ? 1 : 2, i0 = dual ? 0 : (int)((n_k ^ s) & 1);
             if (i0 >= n && lane == 0) mbar_arrive(q_empty + 8 * qb);                    // a single key tile, the other stream's
             const uint64_t dq = smem_desc(smem0 + qb * L::kQ, 16, 1024, 2);
@@ -739,10 +742,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                     umma_commit(s_full + 8 * s);
                     umma_commit(k_empty + 8 * ks);
                     if (!dual) mbar_arrive(k_empty + 8 * ks);                           // the other stream has no use for this tile
-                    if (last) {
-                        umma_commit(q_empty + 8 * qb);
-                        if (dual) mbar_arrive(q_empty + 8 * qb);
-                    }
+                    if (last) umma_commit(q_empty + 8 * qb);
                 }
                 if (!(ok = wait_full(v_full, c, L::kVStages))) break;
                 const uint64_t dv = smem_desc(smem0 + L::kOffV + vs * L::kTile, 1024, L::kGroupPitch, 2);

@@ -351,6 +351,26 @@ def test_a_plan_of_another_shape_is_reported():
 
 
 @pytest.mark.parametrize("shape", [(32, 8, 128), (12, 4, 64)])
+@pytest.mark.parametrize("softcap", [0.0, 25.0])
+def test_short_units_of_two_row_tiles_among_single_tokens(shape, softcap):
+    """Many pieces per CTA, of one to three key tiles, that change between one and two row tiles: a Q buffer is filled anew right
+    behind its last use, while the two streams' progress differs.  Repeated, since what can go wrong here is a matter of timing."""
+    tokens = 128 // (shape[0] // shape[1])
+    rng = np.random.default_rng(7)
+    n = 400
+    ctx = rng.integers(0, 300, n)
+    new = np.where(rng.random(n) < 0.5, 1, rng.integers(tokens + 1, 2 * tokens + 1, n))
+    batch = Batch(ctx.tolist(), new.tolist(), seed=1, **small(shape))
+    c = batch.context()
+    plan = batch.plan(c)
+    for _ in range(50):
+        batch.attn(c, plan, softcap=softcap)
+    status = c.nsd_get_status()
+    assert status == (0, -1), status
+    batch.check(softcap=softcap)
+
+
+@pytest.mark.parametrize("shape", [(32, 8, 128), (12, 4, 64)])
 @pytest.mark.parametrize("seed", range(4))
 def test_random_batches(shape, seed):
     """Single tokens, short and long chunks of any length beside one another: every way a CTA's share can begin, end and

@@ -570,8 +570,9 @@ nsd_status nsd_rope_append(nsd_ctx* ctx, void* kv_pool, int32_t layer, int64_t n
  * that use one plan must not overlap on the GPU; calls with plans of their own may.  A plan
  * serves any number of layers whose tables have the same kv_indptr.  q_indptr and kv_indptr
  * must not decrease, q_indptr stay within max_rows, ctx_len not be negative: else DEVICE_FAULT
- * is reported and the plan is empty (nsd_chunk_attn then writes nothing).  Errors: INVALID_ARG, OUT_OF_RANGE, CAPACITY (plan_bytes too small),
- * UNSUPPORTED (more than 128 q heads per kv head).  nsd_chunk_plan_bytes returns 0 for bad arguments.
+ * is reported and the plan is empty (nsd_chunk_attn then writes nothing).
+ * Errors: INVALID_ARG, OUT_OF_RANGE, CAPACITY (plan_bytes too small), UNSUPPORTED (more than
+ * 128 q heads per kv head).  nsd_chunk_plan_bytes returns 0 for bad arguments.
  */
 typedef struct {
     int32_t window;               /* 0 = none */
@@ -599,7 +600,7 @@ nsd_status nsd_chunk_plan(nsd_ctx* ctx, void* plan, size_t plan_bytes, int32_t b
  *   kv_indices the tables, at the offsets the plan was given; a bad block id or a table that is
  *              too short reads as zeros and is reported as DEVICE_FAULT.  Entries no row of the
  *              request can see (before the window, after the last token) may hold anything
- *   scale      0 = 1/sqrt(head_dim), else > 0;  softcap  0 = none, else > 0
+ *   scale      0 = 1/sqrt(head_dim), else up to 1e30;  softcap  0 = none, else 1e-6 to 1e30
  *   alibi_slopes  nullable fp32 [num_q_heads]
  * Slots that hold no visible token may hold anything, NaN included.  A non-finite value of a
  * key that one row of a request sees may reach the request's other rows of the same chunk.

@@ -1057,7 +1057,8 @@ nsd_status nsd_chunk_attn(nsd_ctx* ctx, void* plan, size_t plan_bytes, const voi
                           int32_t layer, float scale, float softcap, const float* alibi_slopes, void* stream) {
     if (!ctx) return NSD_ERR_INVALID_ARG;
     if (layer < 0 || layer >= ctx->cfg.num_layers) return NSD_ERR_OUT_OF_RANGE;
-    if (!(scale >= 0.f) || !(softcap >= 0.f) || scale > 3e38f || softcap > 3e38f) return NSD_ERR_INVALID_ARG;      // NaN too
+    // NaN too; within these bounds scale / softcap and the cap in the log2 domain stay finite
+    if (!(scale >= 0.f && scale <= 1e30f) || !(softcap == 0.f || (softcap >= 1e-6f && softcap <= 1e30f))) return NSD_ERR_INVALID_ARG;
     ChunkPlan p;
     if (const nsd_status s = chunk_plan_of(ctx, &p, plan, plan_bytes, max_rows)) return s;
     if (max_rows == 0) return NSD_OK;

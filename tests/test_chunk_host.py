@@ -1,7 +1,6 @@
 """What of the chunk operators needs no GPU: refusals, constants and structures of the binding, the 64-bit forms the GPU
 tests compare with, and the arithmetic of the work split."""
 import ctypes
-import math
 import os
 import re
 
@@ -183,7 +182,9 @@ def test_every_key_tile_belongs_to_one_piece(seed):
     if not units:
         return
     starts, seen, slots = _starts(units, t, hkv, ctas), {}, set()
+    total = sum((u[2] + UNIT_TILES) * (2 if u[1] > t else 1) for u in units) * hkv
     for c in range(ctas):
+        share = 0
         at, end = starts[c], starts[c + 1]
         while at != end:
             u, h, k0 = at
@@ -195,13 +196,13 @@ def test_every_key_tile_belongs_to_one_piece(seed):
                 slots.add(slot)
             assert (k0, k1) not in seen.setdefault((u, h), []) and k0 < k1
             seen[(u, h)].append((k0, k1))
+            share += (k1 - k0) * (2 if units[u][1] > t else 1)
             if cut:
                 break
             at = (u + 1, h, 0) if u < units[u][4] else ((units[u][3], h + 1, 0) if h + 1 < hkv else (units[u][4] + 1, 0, 0))
+        # no CTA's tiles cost more than its part of the line and a tile at its ends
+        assert share <= total / ctas + 3
     assert sorted(seen) == [(u, h) for u in range(len(units)) for h in range(hkv)]
     for (u, _), pieces in seen.items():
         pieces.sort()
         assert pieces[0][0] == 0 and pieces[-1][1] == units[u][2] and all(a[1] == b[0] for a, b in zip(pieces, pieces[1:]))
-    # no CTA's share is dearer than its part and one tile more
-    total = sum((u[2] + UNIT_TILES) * (2 if u[1] > t else 1) for u in units) * hkv
-    assert math.ceil(total / ctas) >= 1

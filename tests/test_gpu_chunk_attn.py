@@ -341,6 +341,29 @@ def test_refusals():
     assert (b.o == 7.0).all()
 
 
+@pytest.mark.parametrize("softcap", [1e-30, 1e-7, 2e30, 3e38, float("nan")])
+def test_caps_beyond_32_bits_are_refused(softcap):
+    import paper_2609_29364_b200 as nsd
+
+    b = Batch([100], [30], seed=30)
+    c = b.context()
+    plan = b.plan(c)
+    with pytest.raises(nsd.NsdError) as e:
+        b.attn(c, plan, softcap=softcap)
+    assert e.value.code == 1
+    with pytest.raises(nsd.NsdError) as e:
+        b.attn(c, plan, scale=2e30)
+    assert e.value.code == 1
+    assert (b.o == 7.0).all()
+
+
+@pytest.mark.parametrize("shape", [(32, 8, 128), (12, 4, 64)])
+def test_the_smallest_and_largest_caps(shape):
+    """A cap far above every score changes none of them; one far below makes all weights equal to within it."""
+    Batch([700, 0], [40, 300], seed=32, **small(shape)).run(softcap=1e30)
+    Batch([700, 0], [40, 300], seed=32, **small(shape)).run(softcap=1e-6)
+
+
 def test_a_plan_of_another_shape_is_reported():
     b = Batch([100, 30], [30, 1], heads=8, kv_heads=2, seed=31)
     c, other = b.context(), Batch([100, 30], [30, 1], heads=8, kv_heads=4, seed=31).context()

@@ -364,6 +364,17 @@ def test_the_smallest_and_largest_caps(shape):
     Batch([700, 0], [40, 300], seed=32, **small(shape)).run(softcap=1e-6)
 
 
+@pytest.mark.parametrize("shape", [(32, 8, 128), (12, 4, 64)])
+def test_requests_that_share_blocks_and_a_block_twice_in_a_table(shape):
+    """A common prefix is stored once, and nothing forbids a table that names a block again: only reads meet."""
+    b = Batch([640, 640, 320], [1, 33, 1], seed=34, **small(shape))
+    first, second, third = (int(b.kv_indptr[r]) for r in range(3))
+    b.kv_indices[second:second + 20] = b.kv_indices[first:first + 20]
+    b.kv_indices[third + 7] = b.kv_indices[third + 3]
+    b.kvi.copy_(torch.from_numpy(b.kv_indices))
+    b.run()
+
+
 def test_a_plan_of_another_shape_is_reported():
     b = Batch([100, 30], [30, 1], heads=8, kv_heads=2, seed=31)
     c, other = b.context(), Batch([100, 30], [30, 1], heads=8, kv_heads=4, seed=31).context()

@@ -512,7 +512,8 @@ nsd_status nsd_schedule_batch(const nsd_sched_params* prm, int32_t n, const uint
  * Reported by nsd_get_status as DEVICE_FAULT (with the request's index): a negative length, a
  * request that outgrows held_stride or holds too few blocks for ctx_len (it counts as one
  * without entries and rows); a free list that runs out and block ids outside the pool (table
- * entry -1 or as it is, slot -1); tables or rows beyond max_entries / max_rows (not written).
+ * entry -1 or as it is, slot -1); tables or rows beyond max_entries / max_rows (not written;
+ * kv_indptr ends at max_entries).
  * Errors: INVALID_ARG, OUT_OF_RANGE (batch > max_batch, max_entries or max_rows beyond 2^31 - 1024),
  * CAPACITY (batch > 8192).
  */
@@ -597,7 +598,8 @@ nsd_status nsd_chunk_plan(nsd_ctx* ctx, void* plan, size_t plan_bytes, int32_t b
  *              of 8; q 16-byte aligned)
  *   o          bf16 [max_rows][num_q_heads][head_dim]; 16-byte aligned
  *   lse        nullable fp32 [max_rows][num_q_heads]: natural logarithm of the sum of exp(s'')
- *   kv_indices the tables, at the offsets the plan was given; a bad block id or a table that is
+ *   kv_indices the tables, at the offsets the plan was given (kv_indptr[batch] entries at least;
+ *              offsets from nsd_block_tables never pass max_entries); a bad block id or a table that is
  *              too short reads as zeros and is reported as DEVICE_FAULT.  Entries no row of the
  *              request can see (before the window, after the last token) may hold anything
  *   scale      0 = 1/sqrt(head_dim), else up to 1e30;  softcap  0 = none, else 1e-6 to 1e30

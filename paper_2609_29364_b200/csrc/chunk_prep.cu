@@ -157,7 +157,7 @@ block_tables_kernel(const TablesArgs a) {
     }
     // the per-request outputs, shared out over the CTAs
     for (int r = blockIdx.x * kTablesThreads + tid; r <= a.batch; r += gridDim.x * kTablesThreads) {
-        a.kv_indptr[r] = kvp[r];
+        a.kv_indptr[r] = min((int64_t)kvp[r], a.max_entries);           // a reader of the tables stays inside them
         a.q_indptr[r] = qp[r];
         if (r == a.batch) {
             const int64_t end = fb + tp[r];

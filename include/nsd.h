@@ -512,8 +512,10 @@ nsd_status nsd_schedule_batch(const nsd_sched_params* prm, int32_t n, const uint
  * Reported by nsd_get_status as DEVICE_FAULT (with the request's index): a negative length, a
  * request that outgrows held_stride or holds too few blocks for ctx_len (it counts as one
  * without entries and rows); a free list that runs out and block ids outside the pool (table
- * entry -1 or as it is, slot -1); tables or rows beyond max_entries / max_rows (not written;
- * kv_indptr ends at max_entries).
+ * entry -1 or as it is, slot -1); tables or rows beyond max_entries / max_rows (not written).
+ * Tables end at max_entries then, kv_indptr too: blocks behind are not taken, and rows that would
+ * need one have slot -1 (nsd_rope_append leaves them out).  held, n_held_new and free_end always
+ * agree, so the lists stay sound when a step was too large; the step's own outputs are void.
  * Errors: INVALID_ARG, OUT_OF_RANGE (batch > max_batch, max_entries or max_rows beyond 2^31 - 1024),
  * CAPACITY (batch > 8192).
  */

@@ -113,12 +113,18 @@ block_tables_kernel(const TablesArgs a) {
         if (blockIdx.x == 0 && tid == 0) report(a.status, STATUS_BAD_BLOCK, -1);
         fb = a.n_free;
     }
-    // block k of request r's table: its own or one from the free list, -1 where that has run out
+    // What a request takes has to be in its table and in held, or the step would store to blocks that it does not read and the
+    // next one would trust entries that nobody wrote: from the table entry max_entries on nothing is taken.  Takes are in
+    // the order of the entries, so what is left out is the end of the takes, as it is where the free list runs out.
+    auto taken = [&](int r) -> int32_t {
+        const int64_t take = tp[r + 1] - tp[r], left = a.n_free - fb - tp[r], fit = a.max_entries - kvp[r] - held_n[r];
+        return (int32_t)max((int64_t)0, min(take, min(left, fit)));
+    };
+    // block k of request r's table: its own or one from the free list, -1 where none is taken
     auto block_of = [&](int r, int k) -> int32_t {
         const int held = held_n[r];
         if (k < held) return a.held[(int64_t)r * a.held_stride + k];
-        const int64_t f = fb + tp[r] + (k - held);
-        return f < a.n_free ? a.free_blocks[f] : -1;
+        return k - held < taken(r) ? a.free_blocks[fb + tp[r] + (k - held)] : -1;
     };
     // flat position x is both a table entry and a row: the searches and loads of a thread's positions run side by side
     constexpr int kEach = kTablesPerCta / kTablesThreads;
@@ -147,7 +153,8 @@ block_tables_kernel(const TablesArgs a) {
             const int r = er[u], k = (int)x - kvp[r];
             a.kv_indices[x] = eid[u];
             if ((uint32_t)eid[u] >= (uint32_t)a.num_blocks) report(a.status, STATUS_BAD_BLOCK, r);
-            else if (k >= held_n[r]) a.held[(int64_t)r * a.held_stride + k] = eid[u];
+            // a bad id of the free list counts as taken, so it is recorded too: the next step reports it again
+            if (k >= held_n[r] && k - held_n[r] < taken(r)) a.held[(int64_t)r * a.held_stride + k] = eid[u];
         }
         if (x < a.max_rows) {
             if (a.slot_map) a.slot_map[x] = (uint32_t)rid[u] < (uint32_t)a.num_blocks ? (int64_t)rid[u] * kBsT + pos[u] % kBsT : -1;
@@ -160,12 +167,12 @@ block_tables_kernel(const TablesArgs a) {
         a.kv_indptr[r] = min((int64_t)kvp[r], a.max_entries);           // a reader of the tables stays inside them
         a.q_indptr[r] = qp[r];
         if (r == a.batch) {
-            const int64_t end = fb + tp[r];
-            *a.free_end = end < a.n_free ? end : a.n_free;
+            // the request with the first entry that does not fit is the last to take anything
+            const int last = r > 0 ? (kvp[r] > a.max_entries ? owner_of(kvp, r, (int32_t)a.max_entries) : r - 1) : 0;
+            *a.free_end = fb + (r > 0 ? min((int64_t)tp[last] + taken(last), max(a.n_free - fb, (int64_t)0)) : 0);
             if (kvp[r] > a.max_entries || (qp[r] > a.max_rows && (a.slot_map || a.positions || a.row_req))) report(a.status, STATUS_BAD_TOKEN, -1);
         } else {
-            const int64_t left = a.n_free - fb - tp[r], take = tp[r + 1] - tp[r];
-            a.n_held_new[r] = a.n_held[r] + (int32_t)(left < 0 ? 0 : (left < take ? left : take));
+            a.n_held_new[r] = a.n_held[r] + taken(r);
         }
     }
 }

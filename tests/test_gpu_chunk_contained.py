@@ -5,9 +5,63 @@ import numpy as np
 import pytest
 import torch
 
-from chunk_testlib import DEV, Batch, attn_ref, check_attn, gpu
+from chunk_testlib import BS, DEV, Batch, attn_ref, blocks_of, check_attn, gpu, tables_ref
+from test_gpu_chunk_prep import Tables
 
 pytestmark = pytest.mark.gpu
+
+
+# --------------------------------------------------------------------------- tables that do not fit
+def _overflowed(ctx, new, held, n_held, free, begin, max_entries):
+    """The definition: tables cut at max_entries, nothing taken behind the cut, slots of blocks that are the request's."""
+    need = [blocks_of(c + n) for c, n in zip(ctx, new)]
+    at, kvp, kvi, slots, held, n_new = 0, [0], [], [], [list(map(int, h)) for h in held], [int(x) for x in n_held]
+    for r, (c, n) in enumerate(zip(ctx, new)):
+        for k in range(need[r]):
+            if at + k < max_entries:
+                if k >= n_new[r]:
+                    held[r][k] = int(free[begin])
+                    n_new[r], begin = k + 1, begin + 1
+                kvi.append(held[r][k])
+        at += need[r]
+        kvp.append(min(at, max_entries))
+        slots += [held[r][t // BS] * BS + t % BS if t // BS < n_new[r] else -1 for t in range(c, c + n)]
+    return held, n_new, kvp, kvi, slots, begin
+
+
+@pytest.mark.parametrize("short", [1, 2, 3, 7, 8, 9, 30])
+@pytest.mark.parametrize("extra", [0, 2])
+def test_lists_agree_when_tables_do_not_fit(short, extra):
+    """What is counted as held is recorded, what is not recorded is not taken and given no slot, and the offsets stay inside."""
+    t = Tables([20, 30, 0, 90, 5], [5, 60, 16, 50, 3], seed=6 + extra, extra=extra, begin=2, spare_entries=0)
+    m = max(0, t.entries - short)
+    t.call(kv_indices=t.t["kv_indices"][:m])
+    assert t.c.nsd_get_status()[0] == 6
+    held, n_new, kvp, kvi, slots, end = _overflowed(t.ctx.tolist(), t.new.tolist(), t.held, t.n_held, t.free, t.begin, m)
+    assert t.t["kv_indptr"].tolist() == kvp
+    assert t.t["kv_indices"].tolist() == kvi + [-9] * (t.entries - m)
+    assert t.t["n_held_new"].tolist() == n_new and t.t["free_end"].item() == end
+    assert t.t["held"].tolist() == held
+    assert t.t["slot_map"][:t.rows].tolist() == slots
+    # the next step, with room again, takes up where this one stopped
+    after = dict(held=t.t["held"], n_held=t.t["n_held_new"].clone(), free_begin=t.t["free_end"].clone())
+    t.call(**after)
+    assert t.c.nsd_get_status() == (0, -1)
+    want = tables_ref(t.ctx, t.new, held, n_new, t.free, end)
+    assert t.t["held"].tolist() == want[0] and t.t["kv_indices"].tolist() == want[3]
+    assert t.t["slot_map"][:t.rows].tolist() == want[5] and t.t["free_end"].item() == want[8]
+
+
+def test_a_bad_id_of_the_free_list_is_recorded_where_it_counts():
+    t = Tables([0, 30], [20, 40], seed=8)                      # two blocks, then three beside the two held
+    bad = t.num_blocks + 7
+    t.t["free_blocks"][1] = bad
+    t.call()
+    assert t.c.nsd_get_status() == (6, 0)
+    assert t.t["held"][0].tolist()[:2] == [int(t.free[0]), bad] and t.t["n_held_new"][0].item() == 2
+    t.call(held=t.t["held"], n_held=t.t["n_held_new"].clone(), free_begin=t.t["free_end"].clone())
+    assert t.c.nsd_get_status() == (6, 0)                      # known to the next step too
+    assert t.t["slot_map"][16:20].tolist() == [-1] * 4
 
 
 @pytest.mark.parametrize("short", [1, 9, 24])

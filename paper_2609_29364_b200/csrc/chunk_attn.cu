@@ -74,19 +74,34 @@ chunk_units_kernel(const PlanArgs a) {
         if (j < n_units) {
             const int i0 = (int)j * TU;
             u.ntok = min(TU, n - i0);
-            int lo = 0x7fffffff, hi = 0;
-            for (int i = i0 + lane; i < i0 + u.ntok; i += 32) {
-                const int pos = ctx + i;
+            int lo = 0x7fffffff, hi = 0, reach = 0;    // reach: the largest stop so far
+            bool gaps = false;
+            for (int b = i0; b < i0 + u.ntok; b += 32) {
+                const int i = b + lane, pos = ctx + i;
                 const int stop = max(pos + 1, prefix);
                 int first = a.masks.window > 0 ? max(pos + 1 - a.masks.window, 0) : 0;
-                if (a.masks.row_first) first = max(first, a.masks.row_first[s + i]);
-                const bool any = first < stop;
-                a.p.row_lo[s + i] = any ? first : 0;
-                a.p.row_hi[s + i] = any ? stop : 0;
-                if (any) lo = min(lo, first), hi = max(hi, stop);
+                bool any = false;
+                if (i < i0 + u.ntok) {
+                    if (a.masks.row_first) first = max(first, a.masks.row_first[s + i]);
+                    any = first < stop;
+                    a.p.row_lo[s + i] = any ? first : 0;
+                    a.p.row_hi[s + i] = any ? stop : 0;
+                    if (any) lo = min(lo, first), hi = max(hi, stop);
+                }
+                // Stops grow from row to row, so the keys of rows that follow one another without an empty one between leave no
+                // gap, and the first row behind a gap begins above every stop before it.
+                if (a.masks.row_first) {
+                    int upto = any ? stop : 0;
+#pragma unroll
+                    for (int d = 1; d < 32; d <<= 1) upto = max(upto, __shfl_up_sync(0xffffffffu, upto, d));
+                    const int left = __shfl_up_sync(0xffffffffu, upto, 1), before = max(reach, lane > 0 ? left : 0);
+                    gaps |= any && before > 0 && first > before;
+                    reach = max(reach, __shfl_sync(0xffffffffu, upto, 31));
+                }
             }
             lo = __reduce_min_sync(0xffffffffu, lo);
             hi = __reduce_max_sync(0xffffffffu, hi);
+            u.gaps = __any_sync(0xffffffffu, gaps);
             u.tbl = a.kv_indptr[r];
             u.nblk = (int32_t)min(nblk, (int64_t)0x7fffffff);
             u.row0 = (int32_t)(s + i0);
@@ -794,7 +809,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
         uint32_t n_t = 0, q_slot = 0, n_land = 0;
         bool ok = true;
         // Hidden rows of V have to be finite, since 0 x NaN is NaN: those of a block that also holds visible keys are cleared once
-        // the tile has landed (blocks without any are zero fill).  The next tile's copies go out first.
+        // the tile has landed (blocks outside the unit's hull are zero fill).  The next tile's copies go out first.
         struct Due {
             uint32_t at, full, land;                   // the tile, its full barrier, which landing
             int first, last, head, rows;               // rows [first, first + head) and [last, last + rows - head); rows = 0: nothing due
@@ -808,6 +823,35 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             for (int c = lane; c < due.rows * (D / 8); c += 32) {
                 const int k = c / (D / 8), ch = c % (D / 8), r = k < due.head ? due.first + k : due.last + k - due.head;
                 *reinterpret_cast<int4*>(smem + due.at + (r >> 4) * L::kBlockBytes + ((r >> 3) & 1) * L::kGroupPitch + (ch >> 3) * 1024 + (r & 7) * 128 + (ch & 7) * 16) = make_int4(0, 0, 0, 0);
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(due.full);
+            due.rows = 0;
+        };
+        // Keys inside the hull that no row sees, in a unit with gaps: the lanes take four keys each and look at every row.  Rare
+        // enough to be done at once, with the warp waiting for the tile.
+        auto clear_gaps = [&](int key0) {
+            if (!wait(v_land + 8 * (due.land & 1), due.land >> 1)) {
+                ok = false;
+                due.rows = 0;
+                return;
+            }
+            const int k0 = key0 + lane * 4;
+            uint32_t seen = 0;
+#pragma unroll 1
+            for (int i = 0; i < w.u.ntok; ++i) {
+                const int lo = a.p.row_lo[w.u.row0 + i] - k0, hi = a.p.row_hi[w.u.row0 + i] - k0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) seen |= (uint32_t)(j >= lo && j < hi) << j;
+            }
+#pragma unroll 1
+            for (int j = 0; j < 4; ++j) {
+                const int r = lane * 4 + j;
+                if (seen >> j & 1) continue;
+#pragma unroll 1
+                for (int ch = 0; ch < D / 8; ++ch)
+                    *reinterpret_cast<int4*>(smem + due.at + (r >> 4) * L::kBlockBytes + ((r >> 3) & 1) * L::kGroupPitch + (ch >> 3) * 1024 + (r & 7) * 128 + (ch & 7) * 16) = make_int4(0, 0, 0, 0);
             }
             fence_async_smem();
             __syncwarp();
@@ -868,7 +912,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                 if (!ok) break;
                 const int z0 = w.u.key_lo - t * kTileKeys, z1 = w.u.key_hi - t * kTileKeys;             // visible keys of the tile: [z0, z1)
                 const int head_rows = z0 > 0 ? z0 & 15 : 0, tail_rows = z1 < kTileKeys ? -z1 & 15 : 0;
-                const bool ragged = is_v && (head_rows | tail_rows);
+                const bool ragged = is_v && (head_rows | tail_rows | (int)w.u.gaps);
                 const uint32_t full_now = full_bar(full, n_t, stages), bar = ragged ? v_land + 8 * (n_land & 1) : full_now;
                 if (lane == 0) mbar_expect_tx(bar, L::kTile);
                 __syncwarp();
@@ -876,6 +920,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                 if (due.rows) clear();                                                  // the tile before, now that this one is under way
                 if (ragged) due = Due{ring + st * L::kTile - smem0, full_now, n_land++, z0 - head_rows, z1, head_rows, head_rows + tail_rows};
                 if (!ok) break;
+                if (is_v && w.u.gaps) clear_gaps(t * kTileKeys);
                 if (!q_sent && i == min(1, n - 1)) send_q(true);
                 if (!ok) break;
             }

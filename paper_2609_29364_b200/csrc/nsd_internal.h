@@ -171,9 +171,9 @@ struct __align__(16) ChunkUnit {
     int64_t tbl;                             // kv_indptr of the request
     int32_t nblk;                            // its table entries
     int32_t row0, ntok;                      // rows of the unit (tokens)
-    int32_t req;
+    uint32_t req : 31, gaps : 1;             // gaps: rows that see nothing may leave keys in [key_lo, key_hi) that no row sees
     int32_t n_tiles;                         // 128-key tiles that hold a visible key
-    int32_t key_lo, key_hi;                  // keys any row sees: [key_lo, key_hi)
+    int32_t key_lo, key_hi;                  // hull of the keys any row sees: [key_lo, key_hi)
     int32_t first, last;                     // the request's units
     int32_t pos0;                            // position of the unit's first row
 };

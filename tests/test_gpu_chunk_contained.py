@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from chunk_testlib import BS, DEV, Batch, attn_ref, blocks_of, check_attn, gpu, tables_ref
+from chunk_testlib import BS, DEV, Batch, attn_ref, blocks_of, check_attn, gpu, tables_ref, visible
 from test_gpu_chunk_prep import Tables
 
 pytestmark = pytest.mark.gpu
@@ -100,3 +100,53 @@ def test_attention_after_tables_that_do_not_fit_stays_inside_them(short):
     q = b.q[0, :b.rows].double().reshape(b.rows, b.heads, b.dim)
     check_attn(b.o[0, :b.rows], b.lse[0, :b.rows], attn_ref(q, pool, b.ctx, b.new, b.kv_indptr, table))
     assert math.isfinite(float(b.lse[0, :b.rows].sum()))
+
+
+# --------------------------------------------------------------------------- slots that no row sees
+def _padded_documents(ctx, new, pads, seed):
+    """Documents of random lengths with runs of padding rows (which see nothing) between them."""
+    rng = np.random.default_rng(seed)
+    out = []
+    for c, n in zip(ctx, new):
+        rows, start = [], 0
+        while len(rows) < n:
+            rows += [start] * int(rng.integers(1, 60))
+            rows += [10 ** 6] * int(rng.integers(1, pads + 1))
+            start = c + len(rows)
+        out += rows[:n]
+    return out
+
+
+def _poison(b, **masks):
+    """NaN in every slot that no row of its request sees."""
+    seen, row = visible(b.ctx, b.new, **masks), 0
+    hidden = 0
+    for r, (c, n) in enumerate(zip(b.ctx, b.new)):
+        used = np.zeros(c + n, dtype=bool)
+        for first, stop in seen[row:row + n]:
+            used[first:stop] = True
+        row += n
+        for t in np.flatnonzero(~used):
+            b.pool[0, int(b.kv_indices[int(b.kv_indptr[r]) + t // BS]), :, :, t % BS] = math.nan
+        hidden += int((~used).sum())
+    return hidden
+
+
+@pytest.mark.parametrize("shape", [(8, 2, 128), (12, 4, 64), (4, 4, 128), (28, 4, 128)])
+@pytest.mark.parametrize("pads", [1, 5, 40, 300])
+def test_slots_between_documents_may_hold_anything(shape, pads):
+    """Padding rows inside a request leave keys that no row sees between keys that some do."""
+    ctx, new = [0, 300, 5, 70], [400, 150, 1, 700]
+    docs = _padded_documents(ctx, new, pads, pads)
+    b = Batch(ctx, new, heads=shape[0], kv_heads=shape[1], dim=shape[2], seed=41)
+    assert _poison(b, row_first=docs) > 0
+    b.run(row_first=docs)
+
+
+@pytest.mark.parametrize("window,prefix", [(0, [90, 310, 0, 100]), (20, None), (33, [90, 310, 0, 100])])
+def test_slots_between_documents_with_windows_and_prefixes(window, prefix):
+    ctx, new = [0, 300, 5, 70], [400, 150, 1, 700]
+    masks = dict(row_first=_padded_documents(ctx, new, 30, 42), window=window, prefix_len=prefix)
+    b = Batch(ctx, new, heads=8, kv_heads=2, dim=128, seed=42)
+    assert _poison(b, **masks) > 0
+    b.run(softcap=20.0, **masks)

@@ -606,8 +606,9 @@ nsd_status nsd_chunk_plan(nsd_ctx* ctx, void* plan, size_t plan_bytes, int32_t b
  *              request can see (before the window, after the last token) may hold anything
  *   scale      0 = 1/sqrt(head_dim), else up to 1e30;  softcap  0 = none, else 1e-6 to 1e30
  *   alibi_slopes  nullable fp32 [num_q_heads]
- * Slots that hold no visible token may hold anything, NaN included.  A non-finite value of a
- * key that one row of a request sees may reach the request's other rows of the same chunk.
+ * Slots that hold no visible token may hold anything, NaN included.  A row whose q or whose
+ * visible K holds a NaN has o and lse NaN.  A non-finite value of a key that one row of a request
+ * sees may reach the request's other rows of the same chunk.
  * max_rows and plan_bytes as given to nsd_chunk_plan; a buffer that holds no such plan
  * is reported as DEVICE_FAULT and nothing is written.  bf16 inputs, fp32 accumulation and
  * softmax statistics; the weights are rounded to bf16 for the product with V.

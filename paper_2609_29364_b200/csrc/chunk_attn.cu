@@ -649,6 +649,9 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                 }
             }
             if (fail) break;
+            // A score that is no number makes the row's sum one, though not its maximum, which passes it over.  Such a row joins
+            // with a maximum of infinity: every factor of a join is then 0 or not a number, and its output too.
+            if (l_run != l_run) m_run = INFINITY;
             // ---- the piece's rows
             if (!leads) {
                 ml_s[(s ^ 1) * kRows + m] = make_float2(m_run, l_run);
@@ -679,7 +682,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                 const int64_t orow = row * a.Hq + h;
                 const bool part = w.slot >= 0;
                 const int64_t prow = (int64_t)w.slot * 2 * kRows + (dual ? s * kRows : 0) + m;
-                const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
+                const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
                 if (!part) r0 *= inv, r1 *= inv;
 #pragma unroll 1
                 for (int c = 0; c < D; c += 16) {
@@ -693,8 +696,8 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                         // a weight of zero means that the stream saw nothing: its O may be anything
 #pragma unroll
                         for (int j = 0; j < 16; ++j) {
-                            float v = r0 > 0.f && n > 0 ? __uint_as_float(y[j]) * r0 : 0.f;
-                            if (r1 > 0.f) v = fmaf(__uint_as_float(z[j]), r1, v);
+                            float v = r0 != 0.f && n > 0 ? __uint_as_float(y[j]) * r0 : 0.f;
+                            if (join && r1 != 0.f) v = fmaf(__uint_as_float(z[j]), r1, v);
                             y[j] = __float_as_uint(v);
                         }
                         if (part) {
@@ -1003,7 +1006,7 @@ chunk_join_kernel(const __grid_constant__ ChunkPlan p, uint16_t* __restrict__ o,
                 m = top;
             }
         }
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
         const int64_t orow = (int64_t)(u.row0 + t) * Hq + cut.head * G + g;
         *reinterpret_cast<uint2*>(o + orow * D + d4 * 4) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
         if (lse && d4 == 0) lse[orow] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * kLn2;

@@ -150,3 +150,42 @@ def test_slots_between_documents_with_windows_and_prefixes(window, prefix):
     b = Batch(ctx, new, heads=8, kv_heads=2, dim=128, seed=42)
     assert _poison(b, **masks) > 0
     b.run(softcap=20.0, **masks)
+
+
+# --------------------------------------------------------------------------- NaN among what a row sees
+@pytest.mark.parametrize("mode", [{}, dict(softcap=20.0), dict(slopes=[2.0 ** -(h + 1) for h in range(8)]),
+                                  dict(softcap=20.0, slopes=[2.0 ** -(h + 1) for h in range(8)])])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_a_nan_is_not_taken_for_an_empty_row(mode, dim):
+    """In a single tile, in alternate tiles of two streams, in units of two row tiles and in units cut into pieces.  Rows are
+    computed apart from one another, so those that see no NaN keep their bits."""
+    ctx, new = [3000, 5, 0, 20000, 900], [1, 200, 40, 1, 2]
+    b = Batch(ctx, new, heads=8, kv_heads=2, dim=dim, seed=43)
+    c = b.context()
+    plan = b.plan(c)
+    b.attn(c, plan, **mode)
+    o, lse = b.o[0].clone(), b.lse[0].clone()
+    # a query of NaN
+    q = b.q[0].clone()
+    want = torch.zeros((b.rows, 8), dtype=torch.bool, device=DEV)
+    for row, h in ((0, 3), (1, 0), (150, 7), (200, 5), (201, 1), (240, 2), (241, 6), (243, 4)):
+        b.q[0, row, h * dim + 5] = math.nan
+        want[row, h] = True
+    b.attn(c, plan, **mode)
+    _nan_where(b, want, o, lse)
+    b.q[0].copy_(q)
+    # a key of NaN, of one kv head
+    want.zero_()
+    for r, t in ((0, 2999), (0, 17), (1, 100), (2, 39), (3, 11111), (4, 0)):
+        b.pool[0, int(b.kv_indices[int(b.kv_indptr[r]) + t // BS]), 0, 1, t % BS, 3] = math.nan
+        for i in range(new[r]):
+            want[int(b.q_indptr[r]) + i, 4:] |= t <= ctx[r] + i
+    b.attn(c, plan, **mode)
+    _nan_where(b, want, o, lse)
+    assert c.nsd_get_status() == (0, -1)
+
+
+def _nan_where(b, want, o, lse):
+    assert torch.equal(torch.isnan(b.lse[0, :b.rows]), want)
+    assert torch.isnan(b.o[0, :b.rows][want]).all()
+    assert torch.equal(b.o[0, :b.rows][~want], o[:b.rows][~want]) and torch.equal(b.lse[0, :b.rows][~want], lse[:b.rows][~want])

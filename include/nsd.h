@@ -609,8 +609,8 @@ nsd_status nsd_chunk_plan(nsd_ctx* ctx, void* plan, size_t plan_bytes, int32_t b
  * Slots that hold no visible token may hold anything, NaN included.  A row whose q or whose
  * visible K holds a NaN has o and lse NaN.  A non-finite value of a key that one row of a request
  * sees may reach the request's other rows of the same chunk.
- * max_rows and plan_bytes as given to nsd_chunk_plan; a buffer that holds no such plan
- * is reported as DEVICE_FAULT and nothing is written.  bf16 inputs, fp32 accumulation and
+ * max_rows and plan_bytes as given to nsd_chunk_plan; a buffer that holds no such plan (of a
+ * context with the same heads and max_batch) is reported as DEVICE_FAULT and nothing is written.  bf16 inputs, fp32 accumulation and
  * softmax statistics; the weights are rounded to bf16 for the product with V.
  * Errors: INVALID_ARG, OUT_OF_RANGE, CAPACITY, UNSUPPORTED.
  */

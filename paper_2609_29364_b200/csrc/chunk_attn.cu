@@ -26,10 +26,11 @@ __device__ __forceinline__ void report(int32_t* status, int32_t bit, int r) {
 __device__ __forceinline__ int tile_cost(const ChunkUnit& u, int T) { return u.ntok > T ? 2 : 1; }
 __device__ __forceinline__ int64_t unit_cost(const ChunkUnit& u, int T) { return ((int64_t)u.n_tiles + kUnitTiles) * tile_cost(u, T); }
 
-// A buffer that nsd_chunk_plan has filled for these rows and this shape.
+// A buffer that nsd_chunk_plan has filled for these rows, this shape and this layout (max_units follows from max_batch, and
+// with max_rows and n_ctas places every part up to the partial results).
 __device__ __forceinline__ bool is_plan(const ChunkPlan& p, int T, int Hkv) {
     const ChunkHeader h = *p.header;
-    return h.magic == kMagic && h.max_rows == p.max_rows && h.n_ctas == p.n_ctas && h.T == T && h.Hkv == Hkv;
+    return h.magic == kMagic && h.max_rows == p.max_rows && h.max_units == p.max_units && h.n_ctas == p.n_ctas && h.T == T && h.Hkv == Hkv;
 }
 
 // ---- plan -------------------------------------------------------------------------------------
@@ -169,7 +170,7 @@ chunk_split_kernel(const PlanArgs a) {
     }
     if (tid == 0) {
         cost[n_units] = c_all;
-        *a.p.header = ChunkHeader{kMagic, n_units, a.p.max_rows, a.p.n_ctas, a.masks.window == 0 && !a.masks.prefix_len && !a.masks.row_first, a.T, a.Hkv};
+        *a.p.header = ChunkHeader{kMagic, n_units, a.p.max_rows, a.p.max_units, a.p.n_ctas, a.masks.window == 0 && !a.masks.prefix_len && !a.masks.row_first, a.T, a.Hkv};
     }
     __syncthreads();
     // the line: request by request, kv head by kv head, unit by unit, tile by tile

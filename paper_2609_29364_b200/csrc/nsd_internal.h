@@ -184,7 +184,7 @@ struct __align__(16) ChunkStart {            // where a CTA's share of the work 
 struct ChunkHeader {
     uint32_t magic;
     int32_t n_units;
-    int64_t max_rows;
+    int64_t max_rows, max_units;
     int32_t n_ctas;                          // CTAs the work is split over
     int32_t causal;                          // no window, prefix or documents: row_lo / row_hi need not be read
     int32_t T, Hkv;                          // the shape it was made for

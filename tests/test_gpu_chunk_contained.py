@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from chunk_testlib import BS, DEV, Batch, attn_ref, blocks_of, check_attn, gpu, tables_ref, visible
+from chunk_testlib import BS, DEV, Batch, attn_ref, blocks_of, check_attn, context, gpu, tables_ref, visible
 from test_gpu_chunk_prep import Tables
 
 pytestmark = pytest.mark.gpu
@@ -189,3 +189,20 @@ def _nan_where(b, want, o, lse):
     assert torch.equal(torch.isnan(b.lse[0, :b.rows]), want)
     assert torch.isnan(b.o[0, :b.rows][want]).all()
     assert torch.equal(b.o[0, :b.rows][~want], o[:b.rows][~want]) and torch.equal(b.lse[0, :b.rows][~want], lse[:b.rows][~want])
+
+
+# --------------------------------------------------------------------------- plans of another layout
+@pytest.mark.parametrize("more", [-1, 1, 300])
+def test_a_plan_of_a_context_with_another_max_batch_is_reported(more):
+    """The parts of the buffer lie elsewhere then; nothing of it may be used."""
+    b = Batch([100, 30], [30, 1], seed=44)
+    c, other = (context(b.heads, b.kv_heads, b.dim, b.num_blocks, max_batch=n) for n in (3, 3 + more))
+    plan = torch.zeros(max(c.nsd_chunk_plan_bytes(31), other.nsd_chunk_plan_bytes(31)), dtype=torch.uint8, device=DEV)
+    other.nsd_chunk_plan(plan, 31, b.qp, b.ctx_len, b.kvp)
+    b.attn(c, plan)
+    assert c.nsd_get_status()[0] == 6 and (b.o == 7.0).all() and (b.lse == 7.0).all()
+    b.masks = {}
+    c.nsd_chunk_plan(plan, 31, b.qp, b.ctx_len, b.kvp)
+    b.attn(c, plan)
+    assert c.nsd_get_status() == (0, -1)
+    b.check()

@@ -229,9 +229,9 @@ chunk_split_kernel(const PlanArgs a) {
 // whatever the lengths: a CTA may begin and end inside a unit.  Such a piece leaves its O
 // (unnormalised) and statistics in the plan, and a small kernel behind this one joins them in order.
 //
-// Every wait is bounded.  When one runs out, the CTA raises its abort flag, each issuer waits for
-// its MMAs in flight and each producer for its copies (bounded again), and the call ends with
-// STATUS_TIMEOUT.
+// Every wait is bounded.  When one runs out, the CTA raises its abort flag; once all warps have left
+// their loops, each issuer waits for its MMAs in flight and each producer for its copies (bounded
+// again), and the call ends with STATUS_TIMEOUT.
 //
 // Measured (32 q heads, 8 kv heads of 128): a prompt of 8192 tokens 475 us = 1160 TFLOP/s -- the
 // exponentials (16 per SM and cycle) and the tensor cores are each busy 59 % of it, the rest is the
@@ -487,6 +487,13 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
     auto full_bar = [](uint32_t full, uint32_t tile, uint32_t stages) { return full + 16 * (tile % stages) + 8 * ((tile / stages) & 1); };
     auto full_phase = [](uint32_t tile, uint32_t stages) { return tile / stages / 2; };
 
+    // Behind this barrier every warp has left its loop and the abort flag is final: one that looked at it earlier could leave
+    // copies or MMAs in flight behind when another warp gives up later.
+    auto all_done = [] {
+        __syncwarp();
+        asm volatile("barrier.cta.sync 1, %0;" ::"n"(kThreadsA) : "memory");
+    };
+
     if (warp < kWarpIssue) {
         // ================================ softmax and output ================================
         // A row's 128 scores stay in registers.  The block was launched with 384 x 168 registers; the warpgroup of issuers
@@ -726,6 +733,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             __syncwarp();
             if (join && lane == 0) mbar_arrive(x_done + 8 * s);
         }
+        all_done();
     } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp < kWarpK) {
@@ -796,8 +804,8 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             }
             n_k += n;
         }
-        __syncwarp();
-        if (__any_sync(0xffffffffu, abort_s != 0)) {
+        all_done();
+        if (abort_s) {
             // the CTA is giving up: what is still in flight reads shared memory and writes tensor memory
             if (elect_one()) umma_commit(flushed + 8 * s);
             const long long t0 = clock64();
@@ -810,7 +818,8 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
         const uint32_t full = is_v ? v_full : k_full, empty = is_v ? v_empty : k_empty;
         const uint32_t ring = smem0 + (is_v ? L::kOffV : L::kOffK);
         const int32_t oob = a.num_blocks * 2 * a.Hkv;                                   // past the slab: zero fill
-        uint32_t n_t = 0, q_slot = 0, n_land = 0;
+        uint32_t n_t = 0, q_slot = 0, n_land = 0;      // copies sent out: tiles, Q buffers, tiles by way of a landing barrier
+        uint32_t landing = 0;                          // of the latest tiles, the newest in bit 0: by way of a landing barrier
         bool ok = true;
         // Hidden rows of V have to be finite, since 0 x NaN is NaN: those of a block that also holds visible keys are cleared once
         // the tile has landed (blocks outside the unit's hull are zero fill).  The next tile's copies go out first.
@@ -899,7 +908,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                 q_sent = true;
             };
             if (!is_v) send_q(false);
-            for (int i = 0; i < n; ++i, ++n_t) {
+            for (int i = 0; i < n; ++i) {
                 const uint32_t st = n_t % stages, use = n_t / stages;
                 const int t = t0 - i;
                 const int32_t id = id_next;
@@ -921,6 +930,8 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                 if (lane == 0) mbar_expect_tx(bar, L::kTile);
                 __syncwarp();
                 if (lane < kBlocks) tma_load_5d(ring + st * L::kTile + lane * L::kBlockBytes, &a.kv_map, tile, bar);
+                ++n_t;                                                                  // from here on the tile is in flight, whatever gives up next
+                landing = landing << 1 | (uint32_t)ragged;
                 if (due.rows) clear();                                                  // the tile before, now that this one is under way
                 if (ragged) due = Due{ring + st * L::kTile - smem0, full_now, n_land++, z0 - head_rows, z1, head_rows, head_rows + tail_rows};
                 if (!ok) break;
@@ -930,7 +941,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             }
         }
         if (ok && due.rows) clear();
-        __syncwarp();
+        all_done();
         if (abort_s && lane == 0) {
             // the CTA is giving up: copies that nobody waited for may still be landing; each barrier's latest phase gets a
             // bounded wait of its own before the shared memory goes back to the SM
@@ -938,7 +949,8 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                 const long long t0 = clock64();
                 while (!bar_try(bar, count & 1) && clock64() - t0 < kWaitCycles) {}
             };
-            for (uint32_t back = 0; back < (uint32_t)stages && back < n_t; ++back) drain(full_bar(full, n_t - 1 - back, stages), full_phase(n_t - 1 - back, stages));
+            for (uint32_t back = 0; back < (uint32_t)stages && back < n_t; ++back)
+                if (!(landing >> back & 1)) drain(full_bar(full, n_t - 1 - back, stages), full_phase(n_t - 1 - back, stages));
             for (uint32_t back = 1; back <= 2 && back <= n_land; ++back) drain(v_land + 8 * ((n_land - back) & 1), (n_land - back) >> 1);
             for (uint32_t back = 1; back <= 2 && back <= q_slot; ++back) drain(q_full + 8 * ((q_slot - back) & 1), (q_slot - back) >> 1);
         }

@@ -372,7 +372,9 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
 // x becomes cap * tanh(x * sc) for 32 scores of a row.  Where every score of the warp's 32 rows allows, tanh(t) is t times a
 // polynomial in t^2 fitted to least relative error: degree 4 up to 3/4 (6e-7), degree 7 up to 3/2 (7e-7) -- no MUFU
 // instruction, of which 1 - 2 / (1 + e^2t), for the rest, takes two.  (tanh.approx is one, but off by 2^-11: times a cap of 30
-// to 50, one weight in fifty.)
+// to 50, one weight in fifty.)  That difference is off by 2^-21 of the cap, however small the score: with caps up to kCapExp
+// less than a quarter of what the weights' rounding costs, above them the small scores of a mixed lot take the polynomial one by one.
+constexpr float kCapExp = 2048.f;                      // in the log2 domain
 template <int N>
 __device__ __forceinline__ void cap32_poly(uint32_t* x, uint64_t sc2, uint64_t cap2, const float (&k)[N]) {
 #pragma unroll
@@ -394,13 +396,24 @@ __device__ __forceinline__ void cap32(uint32_t* x, float sc, float cap) {
     }
     big = fmaxf(big, big1) * sc;
     const uint64_t sc2 = pair(sc, sc), cap2 = pair(cap, cap);
+    const float small[5] = {0.999999463558197f, -0.3332825303077698f, 0.13259011507034302f, -0.050057198852300644f, 0.01293052639812231f};
     if (!__any_sync(0xffffffffu, big > 0.75f)) {
-        const float k[5] = {0.999999463558197f, -0.3332825303077698f, 0.13259011507034302f, -0.050057198852300644f, 0.01293052639812231f};
-        cap32_poly(x, sc2, cap2, k);
+        cap32_poly(x, sc2, cap2, small);
     } else if (!__any_sync(0xffffffffu, big > 1.5f)) {
         const float k[8] = {0.9999993443489075f, -0.33329400420188904f, 0.13294775784015656f, -0.0524834468960762f,
                             0.018927596509456635f, -0.005435946863144636f, 0.001021950040012598f, -8.943479042500257e-05f};
         cap32_poly(x, sc2, cap2, k);
+    } else if (cap > kCapExp) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const float t = __uint_as_float(x[j]) * sc, y = t * t;
+            float r, p = small[4];
+#pragma unroll
+            for (int i = 3; i >= 0; --i) p = fmaf(p, y, small[i]);
+            const float e = ex2_approx(t * (2.f * kLog2e)) + 1.f;
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e));
+            x[j] = __float_as_uint(fabsf(t) <= 0.75f ? t * cap * p : fmaf(-2.f * cap, r, cap));
+        }
     } else {
 #pragma unroll
         for (int j = 0; j < 32; ++j) {

@@ -206,3 +206,14 @@ def test_a_plan_of_a_context_with_another_max_batch_is_reported(more):
     b.attn(c, plan)
     assert c.nsd_get_status() == (0, -1)
     b.check()
+
+
+# --------------------------------------------------------------------------- large caps
+@pytest.mark.parametrize("shape", [(8, 2, 128), (12, 4, 64)])
+@pytest.mark.parametrize("softcap", [1e3, 1.4e3, 1.5e3, 1e4, 1e5, 1e6, 1e9])
+def test_rows_of_small_scores_beside_rows_of_scores_like_the_cap(shape, softcap):
+    """Rows are capped 32 at a time; a row whose scores reach a large cap must not cost the others their accuracy."""
+    b = Batch([200, 0, 1000], [70, 300, 1], heads=shape[0], kv_heads=shape[1], dim=shape[2], seed=45)
+    for row in (3, 40, 69, 75, 130, 200, 340):
+        b.q[0, row, :shape[2] * 2] *= softcap
+    b.run(softcap=softcap)

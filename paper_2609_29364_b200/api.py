@@ -326,10 +326,10 @@ class VerifyContext:
         """Sizes come from the tensors: batch = len(ctx_len), held [batch][stride], capacities of kv_indices and of the
         row outputs (slot_map, positions, row_req: nullable, of one length)."""
         batch, i32, i64 = ctx_len.numel(), self._i32, self._i64
-        max_rows = 0
+        max_rows = None
         for t in (slot_map, positions, row_req):
             if t is not None:
-                if max_rows and t.numel() != max_rows:
+                if max_rows is not None and t.numel() != max_rows:
                     raise ValueError("slot_map, positions and row_req have to have one length")
                 max_rows = t.numel()
         if held.dim() != 2 or held.shape[0] < batch:
@@ -337,7 +337,7 @@ class VerifyContext:
         rc = self.lib.nsd_block_tables(
             self._h, batch, _tensor(ctx_len, i32, "ctx_len"), _tensor(new_len, i32, "new_len", batch), _tensor(held, i32, "held"),
             held.shape[1], _tensor(n_held, i32, "n_held", batch), _tensor(free_blocks, i32, "free_blocks"), free_blocks.numel(),
-            _tensor(free_begin, i64, "free_begin", 1), kv_indices.numel(), max_rows, _tensor(kv_indptr, i64, "kv_indptr", batch + 1),
+            _tensor(free_begin, i64, "free_begin", 1), kv_indices.numel(), max_rows or 0, _tensor(kv_indptr, i64, "kv_indptr", batch + 1),
             _tensor(kv_indices, i32, "kv_indices"), _tensor(q_indptr, i64, "q_indptr", batch + 1), _tensor(slot_map, i64, "slot_map"),
             _tensor(positions, i32, "positions"), _tensor(row_req, i32, "row_req"), _tensor(n_held_new, i32, "n_held_new", batch),
             _tensor(free_end, i64, "free_end", 1), self._stream(stream))

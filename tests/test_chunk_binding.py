@@ -1,0 +1,21 @@
+"""What the binding of the chunk operators refuses before anything reaches the library (no GPU)."""
+import pytest
+import torch
+
+from test_chunk_host import _context
+
+
+def _tables(**over):
+    i32, i64 = torch.int32, torch.int64
+    return {**dict(ctx_len=torch.zeros(2, dtype=i32), new_len=torch.zeros(2, dtype=i32), held=torch.zeros((2, 4), dtype=i32),
+                   n_held=torch.zeros(2, dtype=i32), free_blocks=torch.zeros(3, dtype=i32), free_begin=None,
+                   kv_indptr=torch.zeros(3, dtype=i64), kv_indices=torch.zeros(5, dtype=i32), q_indptr=torch.zeros(3, dtype=i64),
+                   slot_map=torch.zeros(4, dtype=i64), positions=torch.zeros(4, dtype=i32), row_req=None,
+                   n_held_new=torch.zeros(2, dtype=i32), free_end=torch.zeros(1, dtype=i64)), **over}
+
+
+def test_row_outputs_of_no_elements_are_not_left_out_ones():
+    for over in (dict(slot_map=torch.zeros(0, dtype=torch.int64)), dict(positions=torch.zeros(0, dtype=torch.int32)),
+                 dict(slot_map=None, positions=torch.zeros(0, dtype=torch.int32), row_req=torch.zeros(4, dtype=torch.int32))):
+        with pytest.raises(ValueError, match="one length"):
+            _context().nsd_block_tables(**_tables(**over))

@@ -315,8 +315,14 @@ class VerifyContext:
                                                     _ptr(new_ctx_len), _stream_handle(stream)), "nsd_spec_accept_logits")
 
     # -- chunks of new tokens
-    def _stream(self, stream):
-        """The given stream, or the current one of the context's device (whichever device is current)."""
+    def _stream(self, stream, *tensors):
+        """The given stream, or the current one of the context's device (whichever device is current).  The last argument
+        to be formed, when types and shapes are known to be right: the kernels read the tensors' addresses as they are, so
+        one that lies in pageable memory or on another device is refused here."""
+        device = self._device_index
+        for t in tensors:
+            if t is not None and t.get_device() != device and not (t.get_device() < 0 and t.is_pinned()):
+                raise ValueError(f"tensors on cuda:{device} (or in pinned memory) are wanted, got one of shape {tuple(t.shape)} on {t.device}")
         if stream is None:
             return self._raw_stream(self._device_index)
         return stream if isinstance(stream, int) else stream.cuda_stream
@@ -340,7 +346,9 @@ class VerifyContext:
             _tensor(free_begin, i64, "free_begin", 1), kv_indices.numel(), max_rows or 0, _tensor(kv_indptr, i64, "kv_indptr", batch + 1),
             _tensor(kv_indices, i32, "kv_indices"), _tensor(q_indptr, i64, "q_indptr", batch + 1), _tensor(slot_map, i64, "slot_map"),
             _tensor(positions, i32, "positions"), _tensor(row_req, i32, "row_req"), _tensor(n_held_new, i32, "n_held_new", batch),
-            _tensor(free_end, i64, "free_end", 1), self._stream(stream))
+            _tensor(free_end, i64, "free_end", 1),
+            self._stream(stream, ctx_len, new_len, held, n_held, free_blocks, free_begin, kv_indptr, kv_indices, q_indptr, slot_map,
+                         positions, row_req, n_held_new, free_end))
         if rc:
             self._check(rc, "nsd_block_tables")
 
@@ -373,7 +381,7 @@ class VerifyContext:
             op, os_, _tensor(positions, self._i32, "positions"), axes, (ctypes.c_int32 * axes)(*sections),
             _tensor(inv_freq, self._f32, "inv_freq", sum(sections)),
             (NSD_ROPE_ADJACENT if adjacent else 0) | (NSD_ROPE_CYCLED if cycled else 0), _tensor(slot_map, self._i64, "slot_map", n),
-            self._stream(stream))
+            self._stream(stream, None if type(kv_pool) is int else kv_pool, q, k, v, q_out if q is not None else None, positions, inv_freq, slot_map))
         if rc:
             self._check(rc, "nsd_rope_append")
 
@@ -385,7 +393,8 @@ class VerifyContext:
         masks = ChunkMasks(window, 0, _tensor(prefix_len, i32, "prefix_len", batch), _tensor(row_first, i32, "row_first", max_rows))
         rc = self.lib.nsd_chunk_plan(
             self._h, plan.data_ptr(), plan.numel() * plan.element_size(), batch, max_rows, _tensor(q_indptr, i64, "q_indptr", batch + 1),
-            _tensor(ctx_len, i32, "ctx_len"), _tensor(kv_indptr, i64, "kv_indptr", batch + 1), ctypes.byref(masks), self._stream(stream))
+            _tensor(ctx_len, i32, "ctx_len"), _tensor(kv_indptr, i64, "kv_indptr", batch + 1), ctypes.byref(masks),
+            self._stream(stream, plan, q_indptr, ctx_len, kv_indptr, prefix_len, row_first))
         if rc:
             self._check(rc, "nsd_chunk_plan")
 
@@ -400,7 +409,7 @@ class VerifyContext:
         rc = self.lib.nsd_chunk_attn(
             self._h, plan.data_ptr(), plan.numel() * plan.element_size(), _ptr(kv_pool), qp, qs, _tensor(o, self._bf16, "o", max_rows * width),
             _tensor(lse, f32, "lse", max_rows * heads), max_rows, _tensor(kv_indices, self._i32, "kv_indices"), layer, scale, softcap,
-            _tensor(alibi_slopes, f32, "alibi_slopes", heads), self._stream(stream))
+            _tensor(alibi_slopes, f32, "alibi_slopes", heads), self._stream(stream, plan, None if type(kv_pool) is int else kv_pool, q, o, lse, kv_indices, alibi_slopes))
         if rc:
             self._check(rc, "nsd_chunk_attn")
 

@@ -19,3 +19,19 @@ def test_row_outputs_of_no_elements_are_not_left_out_ones():
                  dict(slot_map=None, positions=torch.zeros(0, dtype=torch.int32), row_req=torch.zeros(4, dtype=torch.int32))):
         with pytest.raises(ValueError, match="one length"):
             _context().nsd_block_tables(**_tables(**over))
+
+
+def test_tensors_that_the_device_cannot_read_are_refused():
+    """Right in type and shape, but in pageable memory: a kernel would fault on the address."""
+    c, bf = _context(), torch.bfloat16
+    with pytest.raises(ValueError, match="cuda:0"):
+        c.nsd_block_tables(**_tables())
+    q, k, out = torch.zeros((3, 512), dtype=bf), torch.zeros((3, 128), dtype=bf), torch.zeros((3, 8, 64), dtype=bf)
+    pos, slots, pool = torch.zeros((1, 3), dtype=torch.int32), torch.zeros(3, dtype=torch.int64), torch.zeros((1, 4, 2, 2, 16, 64), dtype=bf)
+    with pytest.raises(ValueError, match="cuda:0"):
+        c.nsd_rope_append(pool, 0, q, k, k, out, pos, [32], torch.ones(32), slots)
+    plan, i = torch.zeros(256, dtype=torch.uint8), torch.zeros(2, dtype=torch.int64)
+    with pytest.raises(ValueError, match="cuda:0"):
+        c.nsd_chunk_plan(plan, 3, i, torch.zeros(1, dtype=torch.int32), i)
+    with pytest.raises(ValueError, match="cuda:0"):
+        c.nsd_chunk_attn(plan, 3, pool, q, out, None, torch.zeros(4, dtype=torch.int32))

@@ -486,7 +486,8 @@ nsd_status nsd_schedule_batch(const nsd_sched_params* prm, int32_t n, const uint
  *              nsd_chunk_attn    attention of the new rows over the request's entries
  * max_rows is the host's upper bound of q_indptr[batch] (the rows the buffers hold); rows
  * behind the last request's are left as they are.  Of nsd_config these calls use the pool's
- * geometry and max_batch.  They run on the context's device, whichever device is current.
+ * geometry and max_batch; a context's limits hold for them too, so there are at most 32 q heads
+ * per kv head (max_gamma = 1).  They run on the context's device, whichever device is current.
  */
 
 /*
@@ -574,8 +575,8 @@ nsd_status nsd_rope_append(nsd_ctx* ctx, void* kv_pool, int32_t layer, int64_t n
  * serves any number of layers whose tables have the same kv_indptr.  q_indptr and kv_indptr
  * must not decrease, q_indptr stay within max_rows, ctx_len not be negative: else DEVICE_FAULT
  * is reported and the plan is empty (nsd_chunk_attn then writes nothing).
- * Errors: INVALID_ARG, OUT_OF_RANGE, CAPACITY (plan_bytes too small), UNSUPPORTED (more than
- * 128 q heads per kv head).  nsd_chunk_plan_bytes returns 0 for bad arguments.
+ * Errors: INVALID_ARG, OUT_OF_RANGE, CAPACITY (plan_bytes too small).  nsd_chunk_plan_bytes
+ * returns 0 for bad arguments.
  */
 typedef struct {
     int32_t window;               /* 0 = none */
@@ -612,7 +613,7 @@ nsd_status nsd_chunk_plan(nsd_ctx* ctx, void* plan, size_t plan_bytes, int32_t b
  * max_rows and plan_bytes as given to nsd_chunk_plan; a buffer that holds no such plan (of a
  * context with the same heads and max_batch) is reported as DEVICE_FAULT and nothing is written.  bf16 inputs, fp32 accumulation and
  * softmax statistics; the weights are rounded to bf16 for the product with V.
- * Errors: INVALID_ARG, OUT_OF_RANGE, CAPACITY, UNSUPPORTED.
+ * Errors: INVALID_ARG, OUT_OF_RANGE, CAPACITY.
  */
 nsd_status nsd_chunk_attn(nsd_ctx* ctx, void* plan, size_t plan_bytes, const void* kv_pool, const void* q,
                           int64_t q_stride, void* o, float* lse, int64_t max_rows, const int32_t* kv_indices,

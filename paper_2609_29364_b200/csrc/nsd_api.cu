@@ -1023,14 +1023,13 @@ nsd_status nsd_rope_append(nsd_ctx* ctx, void* kv_pool, int32_t layer, int64_t n
 }
 
 size_t nsd_chunk_plan_bytes(const nsd_ctx* ctx, int64_t max_rows) {
-    if (!ctx || max_rows < 0 || max_rows > kMaxFlat || ctx->cfg.num_q_heads / ctx->cfg.num_kv_heads > 128) return 0;
+    if (!ctx || max_rows < 0 || max_rows > kMaxFlat) return 0;
     return chunk_plan_layout(nullptr, nullptr, ctx->shape, ctx->cfg.max_batch, max_rows, ctx->n_sms);
 }
 
 static nsd_status chunk_plan_of(const nsd_ctx* ctx, ChunkPlan* p, void* plan, size_t plan_bytes, int64_t max_rows) {
     if (max_rows < 0 || !plan || misaligned(plan, 256)) return NSD_ERR_INVALID_ARG;
     if (max_rows > kMaxFlat) return NSD_ERR_OUT_OF_RANGE;
-    if (ctx->cfg.num_q_heads / ctx->cfg.num_kv_heads > 128) return NSD_ERR_UNSUPPORTED;
     if (plan_bytes < chunk_plan_layout(p, plan, ctx->shape, ctx->cfg.max_batch, max_rows, ctx->n_sms)) return NSD_ERR_CAPACITY;
     return NSD_OK;
 }

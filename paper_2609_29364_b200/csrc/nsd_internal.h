@@ -166,7 +166,7 @@ struct RopeLaunch {
 cudaError_t launch_rope_append(const RopeLaunch& l, cudaStream_t stream);
 
 // The plan buffer of a step's attention.  A unit is up to two tiles of 128 stacked rows (T = 128 / G tokens of one request
-// each, G q heads per kv head) against the keys any of its rows sees; every kv head repeats the request's units.
+// each, G <= 32 q heads per kv head) against the keys any of its rows sees; every kv head repeats the request's units.
 struct __align__(16) ChunkUnit {
     int64_t tbl;                             // kv_indptr of the request
     int32_t nblk;                            // its table entries

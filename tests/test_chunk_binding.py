@@ -1,8 +1,12 @@
 """What the binding of the chunk operators refuses before anything reaches the library (no GPU)."""
+import ctypes
+import os
+
 import pytest
 import torch
 
-from test_chunk_host import _context
+import paper_2609_29364_b200.api as api
+from test_chunk_host import ROOT, _context
 
 
 def _tables(**over):
@@ -35,3 +39,17 @@ def test_tensors_that_the_device_cannot_read_are_refused():
         c.nsd_chunk_plan(plan, 3, i, torch.zeros(1, dtype=torch.int32), i)
     with pytest.raises(ValueError, match="cuda:0"):
         c.nsd_chunk_attn(plan, 3, pool, q, out, None, torch.zeros(4, dtype=torch.int32))
+
+
+def test_the_documented_limit_of_heads_is_a_context_s():
+    """Up to 32 q heads per kv head: what a context with the smallest max_gamma allows."""
+    words = " ".join(open(os.path.join(ROOT, "include", "nsd.h")).read().replace("*", " ").split())
+    assert "at most 32 q heads" in words and "128 q heads" not in words
+    lib = api.load_library()
+
+    def workspace(heads):
+        return lib.nsd_workspace_bytes(ctypes.byref(api.NsdConfig(
+            num_layers=1, num_slabs=1, num_q_heads=heads, num_kv_heads=1, head_dim=64, block_size=16, num_blocks=4, max_batch=1,
+            max_gamma=1, vocab_size=2, max_table_entries=4)))
+
+    assert workspace(32) > 0 and workspace(33) == 0

@@ -554,6 +554,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                 else lo = a.p.row_lo[row], hi = a.p.row_hi[row];
             }
             float m_run = -INFINITY, l_run = 0.f;
+            bool huge = false;                                                          // a row of the warp has had a maximum beyond 2^24
             const int t_hi = (w.u.key_hi + kTileKeys - 1) / kTileKeys;
             int mine = 0;                                                               // tiles of this stream
             if (n > 0 && (ph & LENT)) give_back();                                      // P V overwrites O
@@ -566,7 +567,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                     const int key0 = (t_hi - 1 - (w.k0 + i)) * kTileKeys;
                     const int v0 = lo - key0, v1 = hi - key0;                           // visible: v0 <= j < v1
                     constexpr bool kRaw = MODE == 0;                                    // x is q . k: the scale is part of the exponent's FFMA
-                    const float f = kRaw ? a.sc : 1.f;
+                    float f = kRaw ? a.sc : 1.f;
                     uint32_t x[4][32];                                                  // scores, then pairs of weights
                     uint64_t l2[2] = {0, 0};                                            // the tile's sums
                     auto scores = [&](int c) {                                          // to what the softmax is of
@@ -651,6 +652,18 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                             l_run *= r;
                         }
                         m_run = m_new;
+                        if (kRaw) huge = huge || __any_sync(0xffffffffu, live && fabsf(m_run) > 0x1p24f && m_run != -INFINITY);
+                    }
+                    // The FFMA does not round x f, but the maximum is rounded, and what it loses beyond 2^24 can put all of a row's
+                    // weights out of range.  Such a row's products are rounded too: the largest weight is then 1.
+                    if (kRaw && huge) {
+                        const bool big = fabsf(m_run) > 0x1p24f;
+                        const float g = big ? a.sc : 1.f;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) x[c][j] = __float_as_uint(__uint_as_float(x[c][j]) * g);
+                        if (big) f = 1.f;
                     }
                     weights(0);
                     weights(1);

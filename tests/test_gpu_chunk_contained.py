@@ -217,3 +217,67 @@ def test_rows_of_small_scores_beside_rows_of_scores_like_the_cap(shape, softcap)
     for row in (3, 40, 69, 75, 130, 200, 340):
         b.q[0, row, :shape[2] * 2] *= softcap
     b.run(softcap=softcap)
+
+
+# --------------------------------------------------------------------------- huge scores
+def _check_one_hot(b, scale, rows=None, heads=None, window=0):
+    """Where the largest score stands clear of the second, the output is its V and the log-sum is the score.  A score is a sum
+    of dim products that are exact in 32 bits; an addition on the tensor cores may cut off 2^-23 of a partial sum, and none is
+    larger than the sum of the products' sizes: off by dim 2^-23 of that sum at most.  Scale, product, and the way from the log2
+    domain back round four times, 2^-24 each.  Clear means: by more than both scores' errors and 20 nats (all other weights
+    together below 1e4 e^-20).  The weight may be rounded to bf16 where the maximum lags, and the output is: 2 x 2^-8."""
+    seen = visible(b.ctx, b.new, window=window)
+    clear = total = 0
+    for r, (c, n) in enumerate(zip(b.ctx, b.new)):
+        row0 = int(b.q_indptr[r])
+        table = torch.as_tensor(b.kv_indices[int(b.kv_indptr[r]):int(b.kv_indptr[r]) + blocks_of(c + n)].astype(np.int64), device=DEV)
+        kv = torch.nan_to_num(b.pool[0][table].double(), nan=0.0).permute(1, 2, 0, 3, 4).reshape(2, b.kv_heads, -1, b.dim)[:, :, :c + n]
+        span = torch.tensor(seen[row0:row0 + n], device=DEV)
+        key = torch.arange(c + n, device=DEV)
+        see = (key[None] >= span[:, :1]) & (key[None] < span[:, 1:])
+        for h in range(b.heads):
+            g = h // (b.heads // b.kv_heads)
+            q = b.q[0, row0:row0 + n].double().reshape(n, b.heads, b.dim)[:, h]
+            s = (q @ kv[0, g].T * scale).masked_fill(~see, -math.inf)
+            size = (q.abs() @ kv[0, g].T.abs() * scale).masked_fill(~see, 0).max(1).values
+            top = torch.cat([s, torch.full((n, 1), -math.inf, device=DEV, dtype=s.dtype)], 1).topk(2, 1)
+            err = size * (b.dim * 2.0 ** -23 + 4 * 2.0 ** -24)
+            sure = top.values[:, 0] - top.values[:, 1] > 2 * err + 20
+            if rows is not None:
+                sure &= torch.isin(torch.arange(row0, row0 + n, device=DEV), torch.tensor(rows, device=DEV)) & (heads is None or h in heads)
+            o, lse = b.o[0, row0:row0 + n, h].double(), b.lse[0, row0:row0 + n, h].double()
+            assert torch.isfinite(o).all() and torch.isfinite(lse).all()
+            v = kv[1, g][top.indices[:, 0].clamp(max=c + n - 1)]
+            assert ((o - v).abs() <= 2.0 ** -7 * v.abs() + 1e-4)[sure].all()
+            assert ((lse - top.values[:, 0]).abs() <= err + 2.0 ** -10)[sure].all()
+            clear, total = clear + int(sure.sum()), total + n
+    return clear / total
+
+
+@pytest.mark.parametrize("shape", [(8, 2, 128), (12, 4, 64)])
+@pytest.mark.parametrize("scale", [1e6, 1e8, 1e9, 1e10, 1e20, 1e30])
+def test_huge_scores_by_scales_up_to_the_documented_one(shape, scale):
+    """Scores far beyond what 32 bits hold to a whole number: the largest key has all the weight."""
+    b = Batch([200, 0, 3000, 9000], [70, 300, 1, 2], heads=shape[0], kv_heads=shape[1], dim=shape[2], seed=46)
+    c = b.context()
+    for window in (0, 300):
+        plan = b.plan(c, window=window)
+        b.attn(c, plan, scale=scale)
+        assert c.nsd_get_status() == (0, -1)
+        assert _check_one_hot(b, scale, window=window) > 0.9
+
+
+def test_a_row_of_huge_scores_leaves_its_neighbours_their_bits():
+    b = Batch([200, 0, 3000], [70, 300, 1], seed=47)
+    c = b.context()
+    plan = b.plan(c)
+    b.attn(c, plan)
+    o = b.o[0].clone()
+    rows = [3, 40, 69, 75, 200]
+    b.q[0, rows, :128] *= 1e12
+    b.attn(c, plan)
+    assert c.nsd_get_status() == (0, -1)
+    assert _check_one_hot(b, 128 ** -0.5, rows, [0]) > 0
+    same = torch.ones((b.rows, 8), dtype=torch.bool, device=DEV)
+    same[rows, 0] = False
+    assert torch.equal(b.o[0, :b.rows][same], o[:b.rows][same])

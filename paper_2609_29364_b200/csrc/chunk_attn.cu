@@ -15,7 +15,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 // What work costs, for the split over the CTAs: a key tile 1 in a unit of one row tile and 2 in a unit of two, and a unit what
 // two of its tiles do (loading Q, filling the pipeline, writing O).  Measured with 122 single tokens over 4600 keys beside
-// 2500 tokens of prompts: 578 us; 749 with all tiles alike, 623 with 1.5, 607 with 2.5.
+// 2500 tokens of prompts (D = 128, four q heads per kv head, no masks): 578 us; 749 with all tiles alike, 623 with 1.5, 607
+// with 2.5.  Other shapes, masks and caps share the rule unmeasured; the split stays exact, only its balance depends on it.
 constexpr int kUnitTiles = 2;
 
 __device__ __forceinline__ void report(int32_t* status, int32_t bit, int r) {
@@ -233,13 +234,14 @@ chunk_split_kernel(const PlanArgs a) {
 // their loops, each issuer waits for its MMAs in flight and each producer for its copies (bounded
 // again), and the call ends with STATUS_TIMEOUT.
 //
-// Measured (32 q heads, 8 kv heads of 128): a prompt of 8192 tokens 475 us = 1160 TFLOP/s -- the
-// exponentials (16 per SM and cycle) and the tensor cores are each busy 59 % of it, the rest is the
+// Measured (32 q heads, 8 kv heads of 128): a prompt of 8192 tokens 480 us = 1146 TFLOP/s -- the
+// exponentials (16 per SM and cycle) and the tensor cores are each busy 57 % of it, the rest is the
 // chain S -> maximum -> exponentials -> P V within a step of two streams; 2047 tokens over 62 221
-// keys 2030-2170 us = 980-1043 TFLOP/s at the board's power limit (1530 MHz; 1133 on a cool
-// board); 64 single tokens over 512 to 2048 keys 65 us = 5.4 TB/s, 5 over 30 000 to 120 000
-// 217 us = 6.7 TB/s: HBM; one token over 16 keys 8.4 us: launches and one pass through the pipeline.
-// D = 64 halves the products but not the exponentials: a prompt of 4096 119 us against 150.
+// keys 2150-2240 us = 950-990 TFLOP/s at the board's power limit (1420 MHz; 1890 us = 1122 on a cool
+// board); 64 single tokens over 512 to 2048 keys 66 us = 5.4 TB/s, 5 over 30 000 to 120 000
+// 218 us = 6.7 TB/s: HBM; one token over 16 keys 8.9 us: launches and one pass through the pipeline.
+// D = 64 halves the products but shortens the chain little: a prompt of 4096 121 us against 153 (the
+// exponentials would take 59), 64 single tokens over 4096 keys 108 us = 5.0 TB/s against 170 = 6.3.
 constexpr int kBsA = 16;
 constexpr int kBlocks = kTileKeys / kBsA;
 constexpr int kThreadsA = 384;
@@ -869,7 +871,8 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             due.rows = 0;
         };
         // Keys inside the hull that no row sees, in a unit with gaps: the lanes take four keys each and look at every row.  Rare
-        // enough to be done at once, with the warp waiting for the tile.
+        // enough to be done at once, with the warp waiting for the tile: 10 000 tokens in documents of 300 to 900 take 122 us
+        // without gaps and 155 with a padding row behind each document.
         auto clear_gaps = [&](int key0) {
             if (!wait(v_land + 8 * (due.land & 1), due.land >> 1)) {
                 ok = false;

@@ -619,6 +619,81 @@ nsd_status nsd_chunk_attn(nsd_ctx* ctx, void* plan, size_t plan_bytes, const voi
                           int64_t q_stride, void* o, float* lse, int64_t max_rows, const int32_t* kv_indices,
                           int32_t layer, float scale, float softcap, const float* alibi_slopes, void* stream);
 
+/*
+ * ---- The 8-bit cache ----------------------------------------------------------------------
+ * K and V in half the bytes: the batch that fits the memory doubles, a request that is parked
+ * or moved costs half, and attention, which is bound by the bytes of the cache, reads half.
+ * A row (the head_dim values of one token and kv head, K and V apart) is held as e4m3 codes and
+ * one power of two:
+ *     e      the least integer >= -126 with max|x| <= 448 * 2^e (over the finite values; a row
+ *            without a value other than 0 has e = -126)
+ *     code   x * 2^-e rounded to e4m3, to nearest even: nothing saturates; NaN and infinities
+ *            become NaN
+ *     value  code * 2^e
+ * Layout, both buffers 16-byte aligned, slabs, layers and blocks as in the bf16 pool:
+ *     kv8   [slab][block][kv][kv_head][slot][dim]   one byte each (e4m3)
+ *     scales[slab][block][kv_head][kv][slot]        one byte each: e + 127 (1..247; the exponent
+ *                                                   format E8M0, in which 255 is not a number)
+ * A request has one table for every pool that it uses: block ids of the 8-bit cache are counted
+ * like those of the bf16 pool (0 .. num_blocks-1), and a block may be live in either.
+ * These calls run on the context's device, whichever is current, read all lengths on the device
+ * and can be captured.
+ */
+size_t nsd_kv8_pool_bytes(const nsd_config* cfg);
+size_t nsd_kv8_scale_bytes(const nsd_config* cfg);
+
+/*
+ * nsd_rope_append for the 8-bit cache: q turns to q_out as there, k turns and is quantised, v is
+ * quantised, one layer.  The codes are formed from the rotated values in 32 bits.  Arguments,
+ * padding rows, bad slots and errors as nsd_rope_append, and in addition n_axes = 0: the rows
+ * come as they are to be stored (h_sections, inv_freq and positions are not read, flags are 0).
+ */
+nsd_status nsd_kv8_append(nsd_ctx* ctx, void* kv8, void* scales, int32_t layer, int64_t n_rows, int32_t in_dtype,
+                          const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                          int64_t v_stride, void* q_out, int64_t q_out_stride, const int32_t* positions, int32_t n_axes,
+                          const int32_t* h_sections, const float* inv_freq, int32_t flags, const int64_t* slot_map,
+                          void* stream);
+
+/*
+ * Whole blocks (every slot, as nsd_kv_prepare's gather) between the pool and the cache, for
+ * layers [layer_begin, layer_begin+layer_count):
+ *   nsd_kv8_pack    block src[j] of kv_pool is quantised into block dst[j] of the cache
+ *   nsd_kv8_unpack  block src[j] of the cache is written to block dst[j] of kv_pool; exact, but for
+ *                   values below bf16's normal range, which round
+ *   src, dst  int32 [n_blocks]; n_blocks == 0 does nothing.  A dst named twice is undefined (not
+ *             checked); a src may be.  A pair with an id outside the pool is skipped and
+ *             reported as DEVICE_FAULT (first bad index = j)
+ * Blocks that no pair names are left as they are.  Errors: INVALID_ARG, OUT_OF_RANGE (layers,
+ * n_blocks beyond 2^31 - 1024).
+ */
+nsd_status nsd_kv8_pack(nsd_ctx* ctx, const void* kv_pool, void* kv8, void* scales, int64_t n_blocks,
+                        const int32_t* src, const int32_t* dst, int32_t layer_begin, int32_t layer_count, void* stream);
+nsd_status nsd_kv8_unpack(nsd_ctx* ctx, const void* kv8, const void* scales, void* kv_pool, int64_t n_blocks,
+                          const int32_t* src, const int32_t* dst, int32_t layer_begin, int32_t layer_count, void* stream);
+
+/*
+ * Attention over the 8-bit cache: o = softmax(scale * q.k) V with k and v the values that the
+ * cache holds, for the same rows, masks and tables as nsd_chunk_plan and nsd_chunk_attn -- rows of
+ * a verification round (an anchor and its proposals), single tokens, chunks.  nsd_kv8_plan is to
+ * nsd_kv8_attn what nsd_chunk_plan is to nsd_chunk_attn, with a buffer of nsd_kv8_plan_bytes; the
+ * plans of the two are not interchangeable (a wrong one is reported as DEVICE_FAULT and nothing is written).
+ * Made for few rows per request: up to 40 stacked rows of a kv head (tokens times grouped q heads)
+ * read the cache once, longer chunks once per 40.
+ * Slots that hold no visible token may hold anything.  A row whose q holds a NaN or an infinity, or
+ * that sees a K of which a code is NaN or a row whose scale is 255, has o and lse NaN.  A NaN code
+ * in a visible V reaches the other rows of the same request that are computed with them (up to 40 stacked rows).
+ * fp32 accumulation and softmax statistics; q is multiplied exactly (but for elements below 2^-24
+ * of its row's largest); the weights are rounded to 11 bits for the product with V.
+ * Arguments and errors as nsd_chunk_plan / nsd_chunk_attn; scale 0 = 1/sqrt(head_dim).
+ */
+size_t nsd_kv8_plan_bytes(const nsd_ctx* ctx, int64_t max_rows);
+nsd_status nsd_kv8_plan(nsd_ctx* ctx, void* plan, size_t plan_bytes, int32_t batch, int64_t max_rows,
+                        const int64_t* q_indptr, const int32_t* ctx_len, const int64_t* kv_indptr,
+                        const nsd_chunk_masks* masks, void* stream);
+nsd_status nsd_kv8_attn(nsd_ctx* ctx, void* plan, size_t plan_bytes, const void* kv8, const void* scales, const void* q,
+                        int64_t q_stride, void* o, float* lse, int64_t max_rows, const int32_t* kv_indices,
+                        int32_t layer, float scale, void* stream);
+
 /* Number of kernels this library has launched through `ctx` since creation. */
 int64_t nsd_launch_count(const nsd_ctx* ctx);
 

@@ -130,6 +130,20 @@ def load_library():
     lib.nsd_chunk_plan.argtypes = [_vp, _vp, sz, i32, i64, _vp, _vp, _vp, ctypes.POINTER(ChunkMasks), _vp]
     lib.nsd_chunk_attn.restype = i32
     lib.nsd_chunk_attn.argtypes = [_vp, _vp, sz, _vp, _vp, i64, _vp, _vp, i64, _vp, i32, ctypes.c_float, ctypes.c_float, _vp, _vp]
+    for name in ("nsd_kv8_pool_bytes", "nsd_kv8_scale_bytes"):
+        getattr(lib, name).restype = sz
+        getattr(lib, name).argtypes = [cfgp]
+    lib.nsd_kv8_append.restype = i32
+    lib.nsd_kv8_append.argtypes = [_vp, _vp] + lib.nsd_rope_append.argtypes[1:]
+    for name in ("nsd_kv8_pack", "nsd_kv8_unpack"):
+        getattr(lib, name).restype = i32
+        getattr(lib, name).argtypes = [_vp, _vp, _vp, _vp, i64, _vp, _vp, i32, i32, _vp]
+    lib.nsd_kv8_plan_bytes.restype = sz
+    lib.nsd_kv8_plan_bytes.argtypes = [_vp, i64]
+    lib.nsd_kv8_plan.restype = i32
+    lib.nsd_kv8_plan.argtypes = lib.nsd_chunk_plan.argtypes
+    lib.nsd_kv8_attn.restype = i32
+    lib.nsd_kv8_attn.argtypes = [_vp, _vp, sz, _vp, _vp, _vp, i64, _vp, _vp, i64, _vp, i32, ctypes.c_float, _vp]
     lib.nsd_launch_count.restype = i64
     lib.nsd_launch_count.argtypes = [_vp]
     lib.nsd_get_status.restype = i32
@@ -174,6 +188,15 @@ def _rows(t, width, what):
     if not inner:
         raise ValueError(f"{what}: rows of {width} contiguous elements are wanted, got shape {tuple(shape)}, strides {stride}")
     return t.data_ptr(), (stride[0] if shape[0] > 1 else width)
+
+
+def _bytes_of(t, n, what):
+    """Address of a contiguous tensor of single bytes (uint8, or the 8-bit format it holds) with n elements at least."""
+    if type(t) is int:
+        return t
+    if t.element_size() != 1 or t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{what}: {n} contiguous bytes are wanted, got {t.numel()} of {t.dtype} with strides {t.stride()}")
+    return t.data_ptr()
 
 
 def _stream_handle(stream) -> Optional[int]:
@@ -221,6 +244,8 @@ def nsd_schedule_batch(*, worker_avail, target_interval, slack, max_batch, pred_
 
 class VerifyContext:
     """Owns an nsd_ctx and the torch-allocated workspace it lives on."""
+
+    _kv8_sizes = None                                      # bytes of the codes and scales of an 8-bit cache, once asked for
 
     def __init__(self, *, num_layers, num_q_heads, num_kv_heads, head_dim, block_size, num_blocks, region_b_begin,
                  max_batch, max_gamma, vocab_size, max_table_entries, num_slabs=None, flags=0, wait_budget=0,
@@ -356,6 +381,10 @@ class VerifyContext:
                         cycled=False, stream=None):
         """q, k, v: [rows][heads * head_dim] or [rows][heads][head_dim], rows any stride apart (slices of one projection),
         fp32 or bf16; q_out bf16; positions int32 [axes][rows]; sections: pairs of each axis."""
+        self._append(self.lib.nsd_rope_append, "nsd_rope_append", (_ptr(kv_pool),), (kv_pool,), layer, q, k, v, q_out, positions, sections,
+                     inv_freq, slot_map, adjacent, cycled, stream)
+
+    def _append(self, call, where, stores, tensors, layer, q, k, v, q_out, positions, sections, inv_freq, slot_map, adjacent, cycled, stream):
         some = q if q is not None else k
         if some is None or (k is None) != (v is None):
             raise ValueError("q, or k and v, or all three are wanted")
@@ -374,29 +403,34 @@ class VerifyContext:
             kp, ks = _rows(k, wk, "k")
             vp, vs = _rows(v, wk, "v")
         axes = len(sections)
-        if positions.dim() != 2 or positions.shape[1] != n or positions.shape[0] != axes:
+        if axes == 0 and len(stores) == 2:
+            positions = inv_freq = None                    # the 8-bit cache also takes rows that do not turn
+        elif positions is None or positions.dim() != 2 or positions.shape[1] != n or positions.shape[0] != axes:
             raise ValueError("positions: [axes][rows] is wanted, and sections: one number per axis")
-        rc = self.lib.nsd_rope_append(
-            self._h, _ptr(kv_pool), layer, n, 0 if dtype is self._f32 else (1 if dtype is self._bf16 else -1), qp, qs, kp, ks, vp, vs,
+        rc = call(
+            self._h, *stores, layer, n, 0 if dtype is self._f32 else (1 if dtype is self._bf16 else -1), qp, qs, kp, ks, vp, vs,
             op, os_, _tensor(positions, self._i32, "positions"), axes, (ctypes.c_int32 * axes)(*sections),
             _tensor(inv_freq, self._f32, "inv_freq", sum(sections)),
             (NSD_ROPE_ADJACENT if adjacent else 0) | (NSD_ROPE_CYCLED if cycled else 0), _tensor(slot_map, self._i64, "slot_map", n),
-            self._stream(stream, None if type(kv_pool) is int else kv_pool, q, k, v, q_out if q is not None else None, positions, inv_freq, slot_map))
+            self._stream(stream, *(None if type(t) is int else t for t in tensors), q, k, v, q_out if q is not None else None, positions, inv_freq, slot_map))
         if rc:
-            self._check(rc, "nsd_rope_append")
+            self._check(rc, where)
 
     def nsd_chunk_plan_bytes(self, max_rows: int) -> int:
         return int(self.lib.nsd_chunk_plan_bytes(self._h, max_rows))
 
     def nsd_chunk_plan(self, plan, max_rows, q_indptr, ctx_len, kv_indptr, window=0, prefix_len=None, row_first=None, stream=None):
+        self._plan(self.lib.nsd_chunk_plan, "nsd_chunk_plan", plan, max_rows, q_indptr, ctx_len, kv_indptr, window, prefix_len, row_first, stream)
+
+    def _plan(self, call, where, plan, max_rows, q_indptr, ctx_len, kv_indptr, window, prefix_len, row_first, stream):
         batch, i32, i64 = ctx_len.numel(), self._i32, self._i64
         masks = ChunkMasks(window, 0, _tensor(prefix_len, i32, "prefix_len", batch), _tensor(row_first, i32, "row_first", max_rows))
-        rc = self.lib.nsd_chunk_plan(
+        rc = call(
             self._h, plan.data_ptr(), plan.numel() * plan.element_size(), batch, max_rows, _tensor(q_indptr, i64, "q_indptr", batch + 1),
             _tensor(ctx_len, i32, "ctx_len"), _tensor(kv_indptr, i64, "kv_indptr", batch + 1), ctypes.byref(masks),
             self._stream(stream, plan, q_indptr, ctx_len, kv_indptr, prefix_len, row_first))
         if rc:
-            self._check(rc, "nsd_chunk_plan")
+            self._check(rc, where)
 
     def nsd_chunk_attn(self, plan, max_rows, kv_pool, q, o, lse, kv_indices, layer=0, scale=0.0, softcap=0.0, alibi_slopes=None,
                        stream=None):
@@ -412,6 +446,63 @@ class VerifyContext:
             _tensor(alibi_slopes, f32, "alibi_slopes", heads), self._stream(stream, plan, None if type(kv_pool) is int else kv_pool, q, o, lse, kv_indices, alibi_slopes))
         if rc:
             self._check(rc, "nsd_chunk_attn")
+
+    # -- the 8-bit cache
+    def kv8_bytes(self):
+        """Bytes of the codes and of the scales."""
+        return int(self.lib.nsd_kv8_pool_bytes(ctypes.byref(self.cfg))), int(self.lib.nsd_kv8_scale_bytes(ctypes.byref(self.cfg)))
+
+    def _kv8(self, kv8, scales):
+        if self._kv8_sizes is None:
+            self._kv8_sizes = self.kv8_bytes()
+        return _bytes_of(kv8, self._kv8_sizes[0], "kv8"), _bytes_of(scales, self._kv8_sizes[1], "scales")
+
+    def nsd_kv8_append(self, kv8, scales, layer, q, k, v, q_out, slot_map, positions=None, sections=(), inv_freq=None, adjacent=False,
+                       cycled=False, stream=None):
+        """nsd_rope_append into the 8-bit cache (kv8: uint8 or float8_e4m3fn, scales: uint8 or float8_e8m0fnu); without
+        sections nothing turns."""
+        self._append(self.lib.nsd_kv8_append, "nsd_kv8_append", self._kv8(kv8, scales), (kv8, scales), layer, q, k, v, q_out, positions,
+                     sections, inv_freq, slot_map, adjacent, cycled, stream)
+
+    def _kv8_copy(self, call, where, first, tensors, src, dst, layer_begin, layer_count, stream):
+        if layer_count is None:
+            layer_count = self.cfg.num_layers - layer_begin
+        if src.numel() != dst.numel():
+            raise ValueError("src and dst have to have one length")
+        rc = call(self._h, *first, src.numel(), _tensor(src, self._i32, "src"), _tensor(dst, self._i32, "dst"), layer_begin, layer_count,
+                  self._stream(stream, *(None if type(t) is int else t for t in tensors), src, dst))
+        if rc:
+            self._check(rc, where)
+
+    def nsd_kv8_pack(self, kv_pool, kv8, scales, src, dst, layer_begin=0, layer_count=None, stream=None):
+        """Blocks src of the bf16 pool, quantised, to blocks dst of the cache."""
+        self._kv8_copy(self.lib.nsd_kv8_pack, "nsd_kv8_pack", (_ptr(kv_pool), *self._kv8(kv8, scales)), (kv_pool, kv8, scales), src, dst,
+                       layer_begin, layer_count, stream)
+
+    def nsd_kv8_unpack(self, kv8, scales, kv_pool, src, dst, layer_begin=0, layer_count=None, stream=None):
+        """Blocks src of the cache back to blocks dst of the bf16 pool."""
+        self._kv8_copy(self.lib.nsd_kv8_unpack, "nsd_kv8_unpack", (*self._kv8(kv8, scales), _ptr(kv_pool)), (kv_pool, kv8, scales), src, dst,
+                       layer_begin, layer_count, stream)
+
+    def nsd_kv8_plan_bytes(self, max_rows: int) -> int:
+        return int(self.lib.nsd_kv8_plan_bytes(self._h, max_rows))
+
+    def nsd_kv8_plan(self, plan, max_rows, q_indptr, ctx_len, kv_indptr, window=0, prefix_len=None, row_first=None, stream=None):
+        self._plan(self.lib.nsd_kv8_plan, "nsd_kv8_plan", plan, max_rows, q_indptr, ctx_len, kv_indptr, window, prefix_len, row_first, stream)
+
+    def nsd_kv8_attn(self, plan, max_rows, kv8, scales, q, o, lse, kv_indices, layer=0, scale=0.0, stream=None):
+        """As nsd_chunk_attn, over the 8-bit cache."""
+        heads = self.cfg.num_q_heads
+        width = heads * self.cfg.head_dim
+        if q.dtype is not self._bf16 or q.shape[0] < max_rows:
+            raise TypeError("q: bfloat16 with max_rows rows is wanted")
+        qp, qs = _rows(q, width, "q")
+        rc = self.lib.nsd_kv8_attn(
+            self._h, plan.data_ptr(), plan.numel() * plan.element_size(), *self._kv8(kv8, scales), qp, qs, _tensor(o, self._bf16, "o", max_rows * width),
+            _tensor(lse, self._f32, "lse", max_rows * heads), max_rows, _tensor(kv_indices, self._i32, "kv_indices"), layer, scale,
+            self._stream(stream, plan, *(None if type(t) is int else t for t in (kv8, scales)), q, o, lse, kv_indices))
+        if rc:
+            self._check(rc, "nsd_kv8_attn")
 
     @staticmethod
     def round_args(**kw) -> RoundArgs:

@@ -2,6 +2,7 @@
 // single token to a whole prompt (Section 3, block maps; Appendix G.2, the target's forward pass).
 #include <cuda_bf16.h>
 
+#include "chunk_walk.h"
 #include "nsd_internal.h"
 #include "tcgen05_ops.h"
 
@@ -10,7 +11,6 @@ namespace {
 
 constexpr int kTileKeys = 128;
 constexpr int kRows = 128;                             // stacked rows of a tile
-constexpr uint32_t kMagic = 0x4e534443u;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 // What work costs, for the split over the CTAs: a key tile 1 in a unit of one row tile and 2 in a unit of two, and a unit what
@@ -27,12 +27,6 @@ __device__ __forceinline__ void report(int32_t* status, int32_t bit, int r) {
 __device__ __forceinline__ int tile_cost(const ChunkUnit& u, int T) { return u.ntok > T ? 2 : 1; }
 __device__ __forceinline__ int64_t unit_cost(const ChunkUnit& u, int T) { return ((int64_t)u.n_tiles + kUnitTiles) * tile_cost(u, T); }
 
-// A buffer that nsd_chunk_plan has filled for these rows, this shape and this layout (max_units follows from max_batch, and
-// with max_rows and n_ctas places every part up to the partial results).
-__device__ __forceinline__ bool is_plan(const ChunkPlan& p, int T, int Hkv) {
-    const ChunkHeader h = *p.header;
-    return h.magic == kMagic && h.max_rows == p.max_rows && h.max_units == p.max_units && h.n_ctas == p.n_ctas && h.T == T && h.Hkv == Hkv;
-}
 
 // ---- plan -------------------------------------------------------------------------------------
 // Two kernels.  The first works on every request's units side by side: the visible keys of each
@@ -63,7 +57,7 @@ chunk_units_kernel(const PlanArgs a) {
         if (blockIdx.y == 0 && threadIdx.x == 0) report(a.status, STATUS_BAD_TOKEN, r);
         return;
     }
-    const int TU = 2 * a.T;
+    const int TU = a.p.kind.tiles * a.T;
     const int64_t s = a.q_indptr[r], e = a.q_indptr[r + 1];
     const int n = (int)(e - s), ctx = a.ctx_len[r], total = ctx + n;
     const int n_units = (n + TU - 1) / TU;
@@ -135,7 +129,7 @@ chunk_split_kernel(const PlanArgs a) {
     }
     ok = __syncthreads_and(ok);
     pdl_wait();                                        // the units of the kernel before are complete
-    const int64_t n_raw = ok && a.batch > 0 ? a.batch + a.q_indptr[a.batch] / (2 * a.T) : 0;
+    const int64_t n_raw = ok && a.batch > 0 ? a.batch + a.q_indptr[a.batch] / (a.p.kind.tiles * a.T) : 0;
     const int64_t per = (n_raw + kSplitThreads - 1) / kSplitThreads;
     const int64_t i0 = min(tid * per, n_raw), i1 = min(i0 + per, n_raw);
     int n_mine = 0;
@@ -171,7 +165,7 @@ chunk_split_kernel(const PlanArgs a) {
     }
     if (tid == 0) {
         cost[n_units] = c_all;
-        *a.p.header = ChunkHeader{kMagic, n_units, a.p.max_rows, a.p.max_units, a.p.n_ctas, a.masks.window == 0 && !a.masks.prefix_len && !a.masks.row_first, a.T, a.Hkv};
+        *a.p.header = ChunkHeader{a.p.kind.magic, n_units, a.p.max_rows, a.p.max_units, a.p.n_ctas, a.masks.window == 0 && !a.masks.prefix_len && !a.masks.row_first, a.T, a.Hkv};
     }
     __syncthreads();
     // the line: request by request, kv head by kv head, unit by unit, tile by tile
@@ -281,96 +275,6 @@ struct Smem {
 };
 constexpr int kTmemColsA = 512, kTmemOBase = 256;      // S0, S1, O0, O1: 128 columns each
 
-// A CTA's walk over its share of the line.
-struct Walk {
-    const ChunkUnit* units;
-    ChunkStart at, end;
-    int Hkv;
-    // the piece under way
-    ChunkUnit u;
-    int head, k0, k1, slot;                            // key tiles [k0, k1) in walking order; partial slot or -1
-    __device__ __forceinline__ Walk(const ChunkPlan& p, int Hkv_, bool planned) : units(p.units), at{}, end{}, Hkv(Hkv_) {
-        if (planned) at = p.starts[blockIdx.x], end = p.starts[blockIdx.x + 1];
-    }
-    __device__ __forceinline__ bool next() {
-        if (at.unit == end.unit && at.head == end.head && at.tile == end.tile) return false;
-        u = units[at.unit];
-        head = at.head;
-        k0 = at.tile;
-        const bool cut = at.unit == end.unit && at.head == end.head;
-        k1 = cut ? end.tile : u.n_tiles;
-        slot = k0 > 0 ? 2 * (int)blockIdx.x : (cut ? 2 * (int)blockIdx.x + 1 : -1);
-        if (cut) {
-            at = end;
-        } else {
-            at.tile = 0;
-            if (at.unit < u.last) ++at.unit;
-            else if (at.head + 1 < Hkv) ++at.head, at.unit = u.first;
-            else at.head = 0, at.unit = u.last + 1;
-        }
-        return true;
-    }
-};
-
-// A bounded wait of a whole warp.  Unlike mbar_wait it gives the hardware no time slice: a barrier that is ready then costs
-// 78 cycles instead of 113, and a signal from one warp to another as much instead of 112.  The bound is a number of polls
-// (limit) and, since a poll may sleep, a time: about four seconds of SM clocks.
-constexpr long long kWaitCycles = 1ll << 33;
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
-    uint32_t done;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    return done != 0;
-}
-__device__ __forceinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t limit) {
-    const long long t0 = clock64();
-    for (uint32_t i = 0; i < limit; ++i) {
-        if (bar_try(bar, parity)) return true;
-        if (*abort_flag) return false;
-        if (clock64() - t0 > kWaitCycles) break;
-    }
-    *abort_flag = 1;
-    return false;
-}
-__device__ __forceinline__ uint32_t elect_one() {
-    uint32_t p;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p)::"memory");
-    return p;
-}
-// Waits for this thread's tensor-memory loads; the registers of one of them are operands, so that no use of them can be moved
-// in front of the wait.
-__device__ __forceinline__ void tmem_wait_ld32(uint32_t* r) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
-                   "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]),
-                   "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]),
-                   "+r"(r[31])::"memory");
-}
-// Two floats in one 64-bit register pair: the packed FMA, add and multiply of sm_100 do both in one issue slot.
-__device__ __forceinline__ uint64_t pair(float lo, float hi) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ float2 unpair(uint64_t v) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 // x becomes cap * tanh(x * sc) for 32 scores of a row.  Where every score of the warp's 32 rows allows, tanh(t) is t times a
 // polynomial in t^2 fitted to least relative error: degree 4 up to 3/4 (6e-7), degree 7 up to 3/2 (7e-7) -- no MUFU
 // instruction, of which 1 - 2 / (1 + e^2t), for the rest, takes two.  (tanh.approx is one, but off by 2^-11: times a cap of 30
@@ -1021,7 +925,7 @@ chunk_join_kernel(const __grid_constant__ ChunkPlan p, uint16_t* __restrict__ o,
     };
     for (int e = blockIdx.y * kJoinThreads + threadIdx.x; e < elements; e += kJoinSlices * kJoinThreads) {
         const int r = e / (D / 4), d4 = e % (D / 4), t = r / G, g = r - t * G;
-        const int64_t in = (int64_t)(t / T) * kRows + (t % T) * G + g;                  // row of a partial slot
+        const int64_t in = (int64_t)(t / T) * p.kind.rows + (t % T) * G + g;                  // row of a partial slot
         float m = -INFINITY, l = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         constexpr int kAhead = 4;                      // pieces whose loads are under way together
@@ -1034,7 +938,7 @@ chunk_join_kernel(const __grid_constant__ ChunkPlan p, uint16_t* __restrict__ o,
                 ml[i] = make_float2(-INFINITY, 0.f);
                 v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (k < end && left(k)) {
-                    const int64_t at = (int64_t)(k < c ? 2 * k + 1 : 2 * k) * 2 * kRows + in;
+                    const int64_t at = (int64_t)(k < c ? 2 * k + 1 : 2 * k) * p.kind.tiles * p.kind.rows + in;
                     ml[i] = *reinterpret_cast<const float2*>(p.part_ml + at * 2);
                     v[i] = *reinterpret_cast<const float4*>(p.part_acc + at * D + d4 * 4);
                 }
@@ -1115,10 +1019,9 @@ cudaError_t launch_attn_d(const AttnArgs& a, int mode, int n_ctas, cudaStream_t 
 
 }  // namespace
 
-size_t chunk_plan_layout(ChunkPlan* p, void* base, const Shape& s, int32_t max_batch, int64_t max_rows, int32_t n_sms) {
+size_t chunk_plan_layout(ChunkPlan* p, void* base, const ChunkKind& kind, const Shape& s, int32_t max_batch, int64_t max_rows, int32_t n_sms) {
     n_sms = n_sms < kMaxCtas ? n_sms : kMaxCtas;
-    const int64_t T = kRows / (s.Hq / s.Hkv);
-    const int64_t max_units = max_batch + max_rows / (2 * T) + 2;
+    const int64_t max_units = max_batch + max_rows / (kind.tiles * kind.tokens(s.Hq / s.Hkv)) + 2;
     size_t off = 0;
     char* const b = static_cast<char*>(base);
     auto part = [&](size_t bytes) {
@@ -1134,11 +1037,12 @@ size_t chunk_plan_layout(ChunkPlan* p, void* base, const Shape& s, int32_t max_b
     q.cost = static_cast<int64_t*>(part((max_units + 1) * sizeof(int64_t)));
     q.row_lo = static_cast<int32_t*>(part(max_rows * sizeof(int32_t)));
     q.row_hi = static_cast<int32_t*>(part(max_rows * sizeof(int32_t)));
-    q.part_ml = static_cast<float*>(part(2ull * n_sms * 2 * kRows * 2 * sizeof(float)));
-    q.part_acc = static_cast<float*>(part(2ull * n_sms * 2 * kRows * s.D * sizeof(float)));
+    q.part_ml = static_cast<float*>(part(2ull * n_sms * kind.tiles * kind.rows * 2 * sizeof(float)));
+    q.part_acc = static_cast<float*>(part(2ull * n_sms * kind.tiles * kind.rows * s.D * sizeof(float)));
     q.max_rows = max_rows;
     q.max_units = max_units;
     q.n_ctas = n_sms;
+    q.kind = kind;
     if (p) *p = q;
     return off;
 }
@@ -1152,11 +1056,11 @@ cudaError_t chunk_attn_init() {
 
 cudaError_t launch_chunk_plan(const ChunkPlan& p, const Shape& s, int32_t batch, const int64_t* q_indptr, const int32_t* ctx_len,
                               const int64_t* kv_indptr, const nsd_chunk_masks& masks, int32_t* status, cudaStream_t stream) {
-    const int T = kRows / (s.Hq / s.Hkv);
+    const int T = p.kind.tokens(s.Hq / s.Hkv);
     const PlanArgs a{p, masks, batch, T, s.Hkv, s.bs, q_indptr, kv_indptr, ctx_len, status};
     if (batch > 0) {
         // a warp per unit: enough of them for the average request, at most 64 CTAs for the longest
-        const int64_t units = p.max_rows / (2 * T) / 4 + 1;
+        const int64_t units = p.max_rows / (p.kind.tiles * T) / 4 + 1;
         const unsigned slices = (unsigned)(units < 64 ? units : 64);
         chunk_units_kernel<<<dim3((unsigned)batch, slices), 128, 0, stream>>>(a);
         const cudaError_t e = cudaGetLastError();
@@ -1184,11 +1088,16 @@ cudaError_t launch_chunk_attn(const ChunkPlan& p, const ChunkAttnLaunch& l, cuda
     if (e != cudaSuccess) return e;
     *launched = 1;
     if (p.n_ctas < 2) return e;
-    const dim3 grid(p.n_ctas - 1, kJoinSlices);
-    e = l.shape.D == 128 ? launch_kernel(chunk_join_kernel<128>, grid, dim3(kJoinThreads), 0, stream, true, p, l.o, l.lse, a.Hq, a.Hkv, a.G, a.T)
-                         : launch_kernel(chunk_join_kernel<64>, grid, dim3(kJoinThreads), 0, stream, true, p, l.o, l.lse, a.Hq, a.Hkv, a.G, a.T);
+    e = launch_chunk_join(p, l.shape, l.o, l.lse, stream);
     if (e == cudaSuccess) *launched = 2;
     return e;
+}
+
+cudaError_t launch_chunk_join(const ChunkPlan& p, const Shape& s, uint16_t* o, float* lse, cudaStream_t stream) {
+    const dim3 grid(p.n_ctas - 1, kJoinSlices);
+    const int G = s.Hq / s.Hkv, T = p.kind.tokens(G);
+    return s.D == 128 ? launch_kernel(chunk_join_kernel<128>, grid, dim3(kJoinThreads), 0, stream, true, p, o, lse, s.Hq, s.Hkv, G, T)
+                      : launch_kernel(chunk_join_kernel<64>, grid, dim3(kJoinThreads), 0, stream, true, p, o, lse, s.Hq, s.Hkv, G, T);
 }
 
 }  // namespace nsd

@@ -3,6 +3,7 @@
 // organization"; the free list of a bank, Appendix E.2).
 #include <cuda_bf16.h>
 
+#include "kv8_codec.h"
 #include "nsd_internal.h"
 
 namespace nsd {
@@ -201,6 +202,7 @@ struct RopeArgs {
     const float* inv_freq;
     const int64_t* slot_map;
     int32_t* status;
+    uint8_t *codes, *scales;                       // the 8-bit slab, where k and v go there
     int32_t Hq, Hkv, num_blocks, pairs, adjacent;
     int32_t log2_parts;                            // warps per row
     int32_t hq0;                                   // first head of the walk: 0, or Hq when there is no q
@@ -247,7 +249,9 @@ __device__ __forceinline__ void store8(uint16_t* p, const float* x) {
 
 // VEC: every row of q, k, v and q_out starts on 16 bytes and the members of a pair sit at the same place of two pieces
 // (adjacent pairs, or pairs a multiple of eight apart): 16-byte loads and stores.  Otherwise pair by pair.
-template <typename T, int D, bool VEC>
+// Q8: k and v go to the 8-bit cache, quantised from the 32-bit values (kv8_codec.h); nothing else differs.  With no pairs
+// nothing turns.  8192 rows of 32 + 16 heads: see nsd_kv8_append.
+template <typename T, int D, bool VEC, bool Q8>
 __global__ void __launch_bounds__(256)
 rope_append_kernel(const __grid_constant__ RopeArgs a) {
     constexpr int kUnits = D / 16;                 // a head in units of two 16-byte pieces
@@ -275,6 +279,10 @@ rope_append_kernel(const __grid_constant__ RopeArgs a) {
         if (h < Hk0) return a.q_out + row * a.qo_stride + h * D;
         return stored ? kv_at + (int64_t)h * (kBsT * D) : nullptr;
     };
+    // of the 8-bit slab: tiles in the same order; scales [block][kv head][K|V][slot]
+    uint8_t* const code_at = Q8 ? a.codes + (((slot / kBsT) * 2 * a.Hkv - Hk0) * kBsT + slot % kBsT) * D : nullptr;
+    uint8_t* const scale_at = Q8 ? a.scales + (slot / kBsT) * 2 * a.Hkv * kBsT + slot % kBsT : nullptr;
+    auto scale_of = [&](int h) { return scale_at + (h < Hv0 ? 2 * (h - Hk0) : 2 * (h - Hv0) + 1) * kBsT; };
     // adjacent: a unit's 16 dims are its eight pairs.  Apart: dims p and p + pairs for the units that turn, and the dims
     // from 2 pairs on, 16 at a time, for the rest.
     const int u = lane % kUnits;
@@ -316,8 +324,13 @@ rope_append_kernel(const __grid_constant__ RopeArgs a) {
             for (int j = 0; j < kAhead; ++j) {
                 const int h = h0 + j * kHeads;
                 if (h >= h_end) break;
-                uint16_t* dst = target(h);
-                if (!dst) continue;
+                uint16_t* dst = nullptr;
+                if (!Q8 || h < Hk0) {
+                    dst = target(h);
+                    if (!dst) continue;
+                } else if (!stored) {
+                    continue;
+                }
                 float x[16];
                 now[j].get(x);
                 if (h < Hv0) {
@@ -338,8 +351,27 @@ rope_append_kernel(const __grid_constant__ RopeArgs a) {
                         }
                     }
                 }
-                store8(dst + d0, x);
-                store8(dst + d1, x + 8);
+                if (!Q8 || h < Hk0) {
+                    store8(dst + d0, x);
+                    store8(dst + d1, x + 8);
+                } else {
+                    // the kUnits lanes of this head share its row; lanes of other heads may have left the loop
+                    const uint32_t group = (kUnits == 8 ? 0xffu : 0xfu) << (lane / kUnits * kUnits);
+                    float top = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) top = fmaxf(top, kv8_magnitude(x[i]));
+#pragma unroll
+                    for (int w = kUnits / 2; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(group, top, w));
+                    const uint32_t byte = kv8_scale_byte(top);
+                    const float inv = kv8_inverse(byte);
+                    uint32_t c[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) c[i] = kv8_codes2(x[4 * i], x[4 * i + 1], inv) | kv8_codes2(x[4 * i + 2], x[4 * i + 3], inv) << 16;
+                    uint8_t* const at = code_at + (int64_t)h * (kBsT * D);
+                    *reinterpret_cast<uint2*>(at + d0) = make_uint2(c[0], c[1]);
+                    *reinterpret_cast<uint2*>(at + d1) = make_uint2(c[2], c[3]);
+                    if (u == 0) *scale_of(h) = (uint8_t)byte;
+                }
             }
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) now[j] = next[j];
@@ -348,9 +380,37 @@ rope_append_kernel(const __grid_constant__ RopeArgs a) {
         // a lane keeps its own pairs and walks the heads; dims that do not turn are copied two by two
         for (int h = h_begin; h < h_end; ++h) {
             const T* src = source(h);
+            const bool turns = h < Hv0;
+            if (Q8 && h >= Hk0) {
+                if (!stored) continue;
+                float x[kMine], y[kMine], top = 0.f;
+#pragma unroll
+                for (int i = 0; i < kMine; ++i) {
+                    const int p = lane * kMine + i;
+                    const bool mine = p < a.pairs;
+                    const float v0 = to_float(src[mine && !a.adjacent ? p : 2 * p]), v1 = to_float(src[mine && !a.adjacent ? p + a.pairs : 2 * p + 1]);
+                    x[i] = mine && turns ? v0 * cs[i] - v1 * sn[i] : v0;
+                    y[i] = mine && turns ? v1 * cs[i] + v0 * sn[i] : v1;
+                    top = fmaxf(top, fmaxf(kv8_magnitude(x[i]), kv8_magnitude(y[i])));
+                }
+#pragma unroll
+                for (int w = 16; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+                const uint32_t byte = kv8_scale_byte(top);
+                const float inv = kv8_inverse(byte);
+                uint8_t* const at = code_at + (int64_t)h * (kBsT * D);
+#pragma unroll
+                for (int i = 0; i < kMine; ++i) {
+                    const int p = lane * kMine + i;
+                    const bool mine = p < a.pairs;
+                    const uint32_t c = kv8_codes2(x[i], y[i], inv);
+                    at[mine && !a.adjacent ? p : 2 * p] = (uint8_t)c;
+                    at[mine && !a.adjacent ? p + a.pairs : 2 * p + 1] = (uint8_t)(c >> 8);
+                }
+                if (lane == 0) *scale_of(h) = (uint8_t)byte;
+                continue;
+            }
             uint16_t* dst = target(h);
             if (!dst) continue;
-            const bool turns = h < Hv0;
 #pragma unroll
             for (int i = 0; i < kMine; ++i) {
                 const int p = lane * kMine + i;
@@ -393,6 +453,7 @@ cudaError_t launch_rope_append(const RopeLaunch& l, cudaStream_t stream) {
     a.positions = l.positions;
     a.inv_freq = l.inv_freq;
     a.slot_map = l.slot_map;
+    a.codes = l.codes, a.scales = l.scales;
     a.status = l.status;
     a.Hq = l.shape.Hq, a.Hkv = l.shape.Hkv, a.num_blocks = l.shape.num_blocks;
     a.pairs = l.pairs, a.adjacent = l.adjacent;
@@ -408,7 +469,7 @@ cudaError_t launch_rope_append(const RopeLaunch& l, cudaStream_t stream) {
     while (a.log2_parts < 3 && (l.n_rows << a.log2_parts) < 8LL * l.n_sms && ((a.heads - a.hq0) >> (a.log2_parts + 1)) >= 4) ++a.log2_parts;
     const int64_t warps = l.n_rows << a.log2_parts;
     const unsigned grid = (unsigned)((warps * 32 + 255) / 256);
-#define NSD_ROPE(T, D, V) rope_append_kernel<T, D, V><<<grid, 256, 0, stream>>>(a)
+#define NSD_ROPE(T, D, V) (l.codes ? rope_append_kernel<T, D, V, true><<<grid, 256, 0, stream>>>(a) : rope_append_kernel<T, D, V, false><<<grid, 256, 0, stream>>>(a))
     if (l.in_bf16) {
         if (l.shape.D == 128) vec ? NSD_ROPE(__nv_bfloat16, 128, true) : NSD_ROPE(__nv_bfloat16, 128, false);
         else vec ? NSD_ROPE(__nv_bfloat16, 64, true) : NSD_ROPE(__nv_bfloat16, 64, false);

@@ -175,6 +175,13 @@ size_t nsd_kv_pool_bytes(const nsd_config* cfg) {
     return (size_t)cfg->num_slabs * cfg->num_blocks * 2 * cfg->num_kv_heads * cfg->block_size * cfg->head_dim * 2;
 }
 
+size_t nsd_kv8_pool_bytes(const nsd_config* cfg) { return nsd_kv_pool_bytes(cfg) / 2; }
+
+size_t nsd_kv8_scale_bytes(const nsd_config* cfg) {
+    if (!config_ok(cfg)) return 0;
+    return (size_t)cfg->num_slabs * cfg->num_blocks * 2 * cfg->num_kv_heads * cfg->block_size;
+}
+
 static nsd_status create_impl(const nsd_config* cfg, void* d_workspace, size_t workspace_bytes, nsd_ctx** out);
 
 nsd_status nsd_create(const nsd_config* cfg, void* d_workspace, size_t workspace_bytes, nsd_ctx** out) {
@@ -258,6 +265,7 @@ static nsd_status create_impl(const nsd_config* cfg, void* d_workspace, size_t w
     if ((e = gather_init()) != cudaSuccess) return fail(e, "cudaFuncSetAttribute(gather)");
     if ((e = tables_init()) != cudaSuccess) return fail(e, "cudaFuncSetAttribute(block tables)");
     if ((e = chunk_attn_init()) != cudaSuccess) return fail(e, "cudaFuncSetAttribute(chunk attention)");
+    if ((e = kv8_attn_init()) != cudaSuccess) return fail(e, "cudaFuncSetAttribute(8-bit attention)");
     if ((e = attn_umma_init()) != cudaSuccess) return fail(e, "cudaFuncSetAttribute(tcgen05 attention)");
     ctx->tmaps.resize(cfg->num_slabs);
     ctx->tmaps3.resize(cfg->num_slabs);
@@ -968,7 +976,8 @@ nsd_status nsd_block_tables(nsd_ctx* ctx, int32_t batch, const int32_t* ctx_len,
     return NSD_OK;
 }
 
-nsd_status nsd_rope_append(nsd_ctx* ctx, void* kv_pool, int32_t layer, int64_t n_rows, int32_t in_dtype, const void* q,
+// Both appends: to the bf16 pool, or (to8) to the codes and scales of the 8-bit cache, where rows may also come without turning.
+static nsd_status append_impl(nsd_ctx* ctx, bool to8, void* kv_pool, void* scales, int32_t layer, int64_t n_rows, int32_t in_dtype, const void* q,
                            int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                            void* q_out, int64_t q_out_stride, const int32_t* positions, int32_t n_axes,
                            const int32_t* h_sections, const float* inv_freq, int32_t flags, const int64_t* slot_map,
@@ -976,14 +985,16 @@ nsd_status nsd_rope_append(nsd_ctx* ctx, void* kv_pool, int32_t layer, int64_t n
     if (!ctx || n_rows < 0) return NSD_ERR_INVALID_ARG;
     if (n_rows > kMaxFlat || layer < 0 || layer >= ctx->cfg.num_layers) return NSD_ERR_OUT_OF_RANGE;
     if (in_dtype != 0 && in_dtype != 1) return NSD_ERR_UNSUPPORTED;
-    if (n_axes < 1 || n_axes > 4) return NSD_ERR_OUT_OF_RANGE;
-    if (!h_sections || (flags & ~(NSD_ROPE_ADJACENT | NSD_ROPE_CYCLED))) return NSD_ERR_INVALID_ARG;
+    const bool still = to8 && n_axes == 0;                  // nothing turns
+    if ((n_axes < 1 && !still) || n_axes > 4) return NSD_ERR_OUT_OF_RANGE;
+    if (still ? flags != 0 : !h_sections) return NSD_ERR_INVALID_ARG;
+    if ((flags & ~(NSD_ROPE_ADJACENT | NSD_ROPE_CYCLED)) != 0) return NSD_ERR_INVALID_ARG;
     int64_t pairs = 0;
     for (int a = 0; a < n_axes; ++a) {
         if (h_sections[a] < 0) return NSD_ERR_OUT_OF_RANGE;
         pairs += h_sections[a];
     }
-    if (pairs < 1 || pairs > ctx->cfg.head_dim / 2) return NSD_ERR_OUT_OF_RANGE;
+    if ((pairs < 1 && !still) || pairs > ctx->cfg.head_dim / 2) return NSD_ERR_OUT_OF_RANGE;
     RopeLaunch l{};
     if (flags & NSD_ROPE_CYCLED) {
         for (int a = 1; a < n_axes; ++a)                    // the axis' last pair, counted in turns of n_axes, has to exist
@@ -995,14 +1006,20 @@ nsd_status nsd_rope_append(nsd_ctx* ctx, void* kv_pool, int32_t layer, int64_t n
     }
     if ((k != nullptr) != (v != nullptr) || (!q && !k)) return NSD_ERR_INVALID_ARG;
     if (n_rows == 0) return NSD_OK;
-    if (!positions || !inv_freq) return NSD_ERR_INVALID_ARG;
+    if (!still && (!positions || !inv_freq)) return NSD_ERR_INVALID_ARG;
     const int64_t wq = (int64_t)ctx->cfg.num_q_heads * ctx->cfg.head_dim, wk = (int64_t)ctx->cfg.num_kv_heads * ctx->cfg.head_dim;
     if (q && (!q_out || q_stride < wq || q_out_stride < wq)) return NSD_ERR_INVALID_ARG;
     if (q && q == q_out && (in_dtype != 1 || q_stride != q_out_stride)) return NSD_ERR_INVALID_ARG;
     if (k && (!kv_pool || !slot_map || k_stride < wk || v_stride < wk)) return NSD_ERR_INVALID_ARG;
-    if (misaligned(kv_pool, 16)) return NSD_ERR_INVALID_ARG;
+    if (misaligned(kv_pool, 16) || misaligned(scales, 16) || (to8 && k && !scales)) return NSD_ERR_INVALID_ARG;
     l.shape = ctx->shape;
-    l.slab = k ? slab_ptr(ctx, kv_pool, layer) : nullptr;
+    const int64_t slab = layer % ctx->cfg.num_slabs;
+    if (k && to8) {
+        l.codes = static_cast<uint8_t*>(kv_pool) + slab * ctx->shape.slab_elems();
+        l.scales = static_cast<uint8_t*>(scales) + slab * ctx->shape.slab_scales();
+    } else if (k) {
+        l.slab = slab_ptr(ctx, kv_pool, layer);
+    }
     l.n_rows = n_rows;
     l.in_bf16 = in_dtype;
     l.q = q, l.k = k, l.v = v;
@@ -1022,33 +1039,59 @@ nsd_status nsd_rope_append(nsd_ctx* ctx, void* kv_pool, int32_t layer, int64_t n
     return NSD_OK;
 }
 
-size_t nsd_chunk_plan_bytes(const nsd_ctx* ctx, int64_t max_rows) {
-    if (!ctx || max_rows < 0 || max_rows > kMaxFlat) return 0;
-    return chunk_plan_layout(nullptr, nullptr, ctx->shape, ctx->cfg.max_batch, max_rows, ctx->n_sms);
+nsd_status nsd_rope_append(nsd_ctx* ctx, void* kv_pool, int32_t layer, int64_t n_rows, int32_t in_dtype, const void* q,
+                           int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                           void* q_out, int64_t q_out_stride, const int32_t* positions, int32_t n_axes,
+                           const int32_t* h_sections, const float* inv_freq, int32_t flags, const int64_t* slot_map,
+                           void* stream) {
+    return append_impl(ctx, false, kv_pool, nullptr, layer, n_rows, in_dtype, q, q_stride, k, k_stride, v, v_stride, q_out, q_out_stride,
+                       positions, n_axes, h_sections, inv_freq, flags, slot_map, stream);
 }
 
-static nsd_status chunk_plan_of(const nsd_ctx* ctx, ChunkPlan* p, void* plan, size_t plan_bytes, int64_t max_rows) {
+nsd_status nsd_kv8_append(nsd_ctx* ctx, void* kv8, void* scales, int32_t layer, int64_t n_rows, int32_t in_dtype, const void* q,
+                           int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                           void* q_out, int64_t q_out_stride, const int32_t* positions, int32_t n_axes,
+                           const int32_t* h_sections, const float* inv_freq, int32_t flags, const int64_t* slot_map,
+                           void* stream) {
+    return append_impl(ctx, true, kv8, scales, layer, n_rows, in_dtype, q, q_stride, k, k_stride, v, v_stride, q_out, q_out_stride,
+                       positions, n_axes, h_sections, inv_freq, flags, slot_map, stream);
+}
+
+static size_t plan_bytes_of(const nsd_ctx* ctx, const ChunkKind& kind, int64_t max_rows) {
+    if (!ctx || max_rows < 0 || max_rows > kMaxFlat) return 0;
+    return chunk_plan_layout(nullptr, nullptr, kind, ctx->shape, ctx->cfg.max_batch, max_rows, ctx->n_sms);
+}
+
+static nsd_status plan_of(const nsd_ctx* ctx, const ChunkKind& kind, ChunkPlan* p, void* plan, size_t plan_bytes, int64_t max_rows) {
     if (max_rows < 0 || !plan || misaligned(plan, 256)) return NSD_ERR_INVALID_ARG;
     if (max_rows > kMaxFlat) return NSD_ERR_OUT_OF_RANGE;
-    if (plan_bytes < chunk_plan_layout(p, plan, ctx->shape, ctx->cfg.max_batch, max_rows, ctx->n_sms)) return NSD_ERR_CAPACITY;
+    if (plan_bytes < chunk_plan_layout(p, plan, kind, ctx->shape, ctx->cfg.max_batch, max_rows, ctx->n_sms)) return NSD_ERR_CAPACITY;
     return NSD_OK;
 }
 
-nsd_status nsd_chunk_plan(nsd_ctx* ctx, void* plan, size_t plan_bytes, int32_t batch, int64_t max_rows,
-                          const int64_t* q_indptr, const int32_t* ctx_len, const int64_t* kv_indptr,
-                          const nsd_chunk_masks* masks, void* stream) {
+static nsd_status plan_impl(nsd_ctx* ctx, const ChunkKind& kind, void* plan, size_t plan_bytes, int32_t batch, int64_t max_rows,
+                            const int64_t* q_indptr, const int32_t* ctx_len, const int64_t* kv_indptr,
+                            const nsd_chunk_masks* masks, void* stream) {
     if (!ctx) return NSD_ERR_INVALID_ARG;
     if (batch < 0 || batch > ctx->cfg.max_batch) return NSD_ERR_OUT_OF_RANGE;
     const nsd_chunk_masks m = masks ? *masks : nsd_chunk_masks{};
     if (m.window < 0 || m.reserved != 0) return NSD_ERR_INVALID_ARG;
     if (batch > 0 && (!q_indptr || !ctx_len || !kv_indptr)) return NSD_ERR_INVALID_ARG;
     ChunkPlan p;
-    if (const nsd_status s = chunk_plan_of(ctx, &p, plan, plan_bytes, max_rows)) return s;
+    if (const nsd_status s = plan_of(ctx, kind, &p, plan, plan_bytes, max_rows)) return s;
     const OnDevice on(ctx->device);
     NSD_CUDA(ctx, on.err);
     NSD_CUDA(ctx, launch_chunk_plan(p, ctx->shape, batch, q_indptr, ctx_len, kv_indptr, m, ctx->d_status, static_cast<cudaStream_t>(stream)));
     ctx->launches += batch > 0 ? 2 : 1;
     return NSD_OK;
+}
+
+size_t nsd_chunk_plan_bytes(const nsd_ctx* ctx, int64_t max_rows) { return plan_bytes_of(ctx, kChunkKind, max_rows); }
+
+nsd_status nsd_chunk_plan(nsd_ctx* ctx, void* plan, size_t plan_bytes, int32_t batch, int64_t max_rows,
+                          const int64_t* q_indptr, const int32_t* ctx_len, const int64_t* kv_indptr,
+                          const nsd_chunk_masks* masks, void* stream) {
+    return plan_impl(ctx, kChunkKind, plan, plan_bytes, batch, max_rows, q_indptr, ctx_len, kv_indptr, masks, stream);
 }
 
 nsd_status nsd_chunk_attn(nsd_ctx* ctx, void* plan, size_t plan_bytes, const void* kv_pool, const void* q,
@@ -1059,7 +1102,7 @@ nsd_status nsd_chunk_attn(nsd_ctx* ctx, void* plan, size_t plan_bytes, const voi
     // NaN too; within these bounds scale / softcap and the cap in the log2 domain stay finite
     if (!(scale >= 0.f && scale <= 1e30f) || !(softcap == 0.f || (softcap >= 1e-6f && softcap <= 1e30f))) return NSD_ERR_INVALID_ARG;
     ChunkPlan p;
-    if (const nsd_status s = chunk_plan_of(ctx, &p, plan, plan_bytes, max_rows)) return s;
+    if (const nsd_status s = plan_of(ctx, kChunkKind, &p, plan, plan_bytes, max_rows)) return s;
     if (max_rows == 0) return NSD_OK;
     if (!kv_pool || !q || !o || !kv_indices) return NSD_ERR_INVALID_ARG;
     if (q_stride < (int64_t)ctx->cfg.num_q_heads * ctx->cfg.head_dim || q_stride % 8) return NSD_ERR_INVALID_ARG;
@@ -1081,6 +1124,74 @@ nsd_status nsd_chunk_attn(nsd_ctx* ctx, void* plan, size_t plan_bytes, const voi
     NSD_CUDA(ctx, on.err);
     int launched = 0;
     NSD_CUDA(ctx, launch_chunk_attn(p, l, static_cast<cudaStream_t>(stream), &launched));
+    ctx->launches += launched;
+    return NSD_OK;
+}
+
+// ---- the 8-bit cache ---------------------------------------------------------------------------
+static nsd_status copy8_impl(nsd_ctx* ctx, bool pack, void* kv_pool, void* kv8, void* scales, int64_t n_blocks, const int32_t* src,
+                             const int32_t* dst, int32_t layer_begin, int32_t layer_count, void* stream) {
+    if (!ctx || n_blocks < 0) return NSD_ERR_INVALID_ARG;
+    if (layer_begin < 0 || layer_count < 0 || (int64_t)layer_begin + layer_count > ctx->cfg.num_layers || n_blocks > kMaxFlat) return NSD_ERR_OUT_OF_RANGE;
+    if (n_blocks == 0 || layer_count == 0) return NSD_OK;
+    if (!kv_pool || !kv8 || !scales || !src || !dst) return NSD_ERR_INVALID_ARG;
+    if (misaligned(kv_pool, 16) || misaligned(kv8, 16) || misaligned(scales, 16)) return NSD_ERR_INVALID_ARG;
+    const Kv8Copy c{ctx->shape, static_cast<uint16_t*>(kv_pool), static_cast<uint8_t*>(kv8), static_cast<uint8_t*>(scales), n_blocks, src, dst,
+                    layer_begin, layer_count, ctx->cfg.num_slabs, ctx->n_sms, ctx->d_status};
+    const OnDevice on(ctx->device);
+    NSD_CUDA(ctx, on.err);
+    NSD_CUDA(ctx, pack ? launch_kv8_pack(c, static_cast<cudaStream_t>(stream)) : launch_kv8_unpack(c, static_cast<cudaStream_t>(stream)));
+    ctx->launches++;
+    return NSD_OK;
+}
+
+nsd_status nsd_kv8_pack(nsd_ctx* ctx, const void* kv_pool, void* kv8, void* scales, int64_t n_blocks, const int32_t* src,
+                        const int32_t* dst, int32_t layer_begin, int32_t layer_count, void* stream) {
+    return copy8_impl(ctx, true, const_cast<void*>(kv_pool), kv8, scales, n_blocks, src, dst, layer_begin, layer_count, stream);
+}
+
+nsd_status nsd_kv8_unpack(nsd_ctx* ctx, const void* kv8, const void* scales, void* kv_pool, int64_t n_blocks, const int32_t* src,
+                          const int32_t* dst, int32_t layer_begin, int32_t layer_count, void* stream) {
+    return copy8_impl(ctx, false, kv_pool, const_cast<void*>(kv8), const_cast<void*>(scales), n_blocks, src, dst, layer_begin, layer_count, stream);
+}
+
+size_t nsd_kv8_plan_bytes(const nsd_ctx* ctx, int64_t max_rows) { return plan_bytes_of(ctx, kKv8Kind, max_rows); }
+
+nsd_status nsd_kv8_plan(nsd_ctx* ctx, void* plan, size_t plan_bytes, int32_t batch, int64_t max_rows,
+                        const int64_t* q_indptr, const int32_t* ctx_len, const int64_t* kv_indptr,
+                        const nsd_chunk_masks* masks, void* stream) {
+    return plan_impl(ctx, kKv8Kind, plan, plan_bytes, batch, max_rows, q_indptr, ctx_len, kv_indptr, masks, stream);
+}
+
+nsd_status nsd_kv8_attn(nsd_ctx* ctx, void* plan, size_t plan_bytes, const void* kv8, const void* scales, const void* q,
+                        int64_t q_stride, void* o, float* lse, int64_t max_rows, const int32_t* kv_indices,
+                        int32_t layer, float scale, void* stream) {
+    if (!ctx) return NSD_ERR_INVALID_ARG;
+    if (layer < 0 || layer >= ctx->cfg.num_layers) return NSD_ERR_OUT_OF_RANGE;
+    if (!(scale >= 0.f && scale <= 1e30f)) return NSD_ERR_INVALID_ARG;                       // NaN too
+    ChunkPlan p;
+    if (const nsd_status s = plan_of(ctx, kKv8Kind, &p, plan, plan_bytes, max_rows)) return s;
+    if (max_rows == 0) return NSD_OK;
+    if (!kv8 || !scales || !q || !o || !kv_indices) return NSD_ERR_INVALID_ARG;
+    if (q_stride < (int64_t)ctx->cfg.num_q_heads * ctx->cfg.head_dim || q_stride % 8) return NSD_ERR_INVALID_ARG;
+    if (misaligned(q, 16) || misaligned(o, 16) || misaligned(kv8, 16) || misaligned(scales, 16)) return NSD_ERR_INVALID_ARG;
+    Kv8AttnLaunch l{};
+    l.shape = ctx->shape;
+    const int64_t slab = layer % ctx->cfg.num_slabs;
+    l.codes = static_cast<const uint8_t*>(kv8) + slab * ctx->shape.slab_elems();
+    l.scales = static_cast<const uint8_t*>(scales) + slab * ctx->shape.slab_scales();
+    l.q = static_cast<const uint16_t*>(q);
+    l.q_stride = q_stride;
+    l.o = static_cast<uint16_t*>(o);
+    l.lse = lse;
+    l.kv_indices = kv_indices;
+    l.scale = scale > 0.f ? scale : 1.f / sqrtf((float)ctx->cfg.head_dim);
+    l.status = ctx->d_status;
+    l.wait_budget = ctx->wait_budget;
+    const OnDevice on(ctx->device);
+    NSD_CUDA(ctx, on.err);
+    int launched = 0;
+    NSD_CUDA(ctx, launch_kv8_attn(p, l, static_cast<cudaStream_t>(stream), &launched));
     ctx->launches += launched;
     return NSD_OK;
 }

@@ -60,6 +60,7 @@ struct Shape {
     __host__ __device__ int64_t tile_elems() const { return (int64_t)bs * D; }            // one (block, kv, head)
     __host__ __device__ int64_t block_elems() const { return 2LL * Hkv * bs * D; }        // one (slab, block)
     __host__ __device__ int64_t slab_elems() const { return (int64_t)num_blocks * block_elems(); }
+    __host__ __device__ int64_t slab_scales() const { return (int64_t)num_blocks * 2 * Hkv * bs; }   // of the 8-bit cache: a byte per row
 };
 
 struct AttnLaunch {
@@ -162,6 +163,7 @@ struct RopeLaunch {
     int32_t pairs, adjacent, n_sms;
     uint8_t axis[64];                        // position axis of each pair
     int32_t* status;
+    uint8_t *codes, *scales;                 // not null: k and v go to this slab of the 8-bit cache instead
 };
 cudaError_t launch_rope_append(const RopeLaunch& l, cudaStream_t stream);
 
@@ -189,18 +191,26 @@ struct ChunkHeader {
     int32_t causal;                          // no window, prefix or documents: row_lo / row_hi need not be read
     int32_t T, Hkv;                          // the shape it was made for
 };
+// What a plan is for: tiles of up to `rows` stacked rows (T = rows / G tokens), `tiles` of them in a unit.
+struct ChunkKind {
+    uint32_t magic;
+    int32_t rows, tiles;
+    __host__ __device__ int tokens(int G) const { return rows / G; }         // of a tile
+};
+constexpr ChunkKind kChunkKind{0x4e534443u, 128, 2}, kKv8Kind{0x4e534438u, 40, 1};
 struct ChunkPlan {                           // the buffer's parts
     ChunkHeader* header;
     ChunkStart* starts;                      // [n_ctas + 1]
     ChunkUnit *raw, *units;                  // [max_units]
     int64_t* cost;                           // [max_units + 1] prefix sums over the units, one kv head
     int32_t *row_lo, *row_hi;                // [max_rows] visible keys of each row
-    float* part_ml;                          // [2 n_ctas][256][2]
-    float* part_acc;                         // [2 n_ctas][256][D]
+    float* part_ml;                          // [2 n_ctas][rows of a unit][2]
+    float* part_acc;                         // [2 n_ctas][rows of a unit][D]
     int64_t max_rows, max_units;
     int32_t n_ctas;
+    ChunkKind kind;
 };
-size_t chunk_plan_layout(ChunkPlan* p, void* base, const Shape& s, int32_t max_batch, int64_t max_rows, int32_t n_sms);
+size_t chunk_plan_layout(ChunkPlan* p, void* base, const ChunkKind& kind, const Shape& s, int32_t max_batch, int64_t max_rows, int32_t n_sms);
 cudaError_t chunk_attn_init();
 cudaError_t launch_chunk_plan(const ChunkPlan& p, const Shape& s, int32_t batch, const int64_t* q_indptr, const int32_t* ctx_len,
                               const int64_t* kv_indptr, const nsd_chunk_masks& masks, int32_t* status, cudaStream_t stream);
@@ -217,7 +227,38 @@ struct ChunkAttnLaunch {
     int32_t* status;
     uint32_t wait_budget;
 };
+// Joins the pieces of units that CTA boundaries cut (every kind of plan).
+cudaError_t launch_chunk_join(const ChunkPlan& p, const Shape& s, uint16_t* o, float* lse, cudaStream_t stream);
 // *launched: kernels enqueued
 cudaError_t launch_chunk_attn(const ChunkPlan& p, const ChunkAttnLaunch& l, cudaStream_t stream, int* launched);
+
+// ---- the 8-bit cache (kv8.cu) -------------------------------------------------------------------
+// Slabs of layers [layer_begin, layer_begin + layer_count), layer l in slab l % num_slabs.
+struct Kv8Copy {
+    Shape shape;
+    uint16_t* pool;
+    uint8_t *codes, *scales;
+    int64_t n_blocks;
+    const int32_t *src, *dst;
+    int32_t layer_begin, layer_count, num_slabs, n_sms;
+    int32_t* status;
+};
+cudaError_t launch_kv8_pack(const Kv8Copy& c, cudaStream_t stream);      // pool -> codes and scales
+cudaError_t launch_kv8_unpack(const Kv8Copy& c, cudaStream_t stream);    // and back
+// Attention over it (kv8_attn.cu), under a plan of kKv8Kind; launch_chunk_join follows it.
+struct Kv8AttnLaunch {
+    Shape shape;
+    const uint8_t *codes, *scales;           // the layer's slab
+    const uint16_t* q;
+    int64_t q_stride;
+    uint16_t* o;
+    float* lse;
+    const int32_t* kv_indices;
+    float scale;
+    int32_t* status;
+    uint32_t wait_budget;
+};
+cudaError_t kv8_attn_init();
+cudaError_t launch_kv8_attn(const ChunkPlan& p, const Kv8AttnLaunch& l, cudaStream_t stream, int* launched);
 
 }  // namespace nsd

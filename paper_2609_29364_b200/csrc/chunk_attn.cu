@@ -1020,6 +1020,7 @@ cudaError_t launch_attn_d(const AttnArgs& a, int mode, int n_ctas, cudaStream_t 
 }  // namespace
 
 size_t chunk_plan_layout(ChunkPlan* p, void* base, const ChunkKind& kind, const Shape& s, int32_t max_batch, int64_t max_rows, int32_t n_sms) {
+    n_sms *= kind.per_sm;                              // CTAs
     n_sms = n_sms < kMaxCtas ? n_sms : kMaxCtas;
     const int64_t max_units = max_batch + max_rows / (kind.tiles * kind.tokens(s.Hq / s.Hkv)) + 2;
     size_t off = 0;

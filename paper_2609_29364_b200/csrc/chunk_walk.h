@@ -26,7 +26,11 @@ struct Walk {
     }
     __device__ __forceinline__ bool next() {
         if (at.unit == end.unit && at.head == end.head && at.tile == end.tile) return false;
-        u = units[at.unit];
+        step(units[at.unit]);
+        return true;
+    }
+    __device__ __forceinline__ void step(const ChunkUnit& here) {                       // here: unit at.unit
+        u = here;
         head = at.head;
         k0 = at.tile;
         const bool cut = at.unit == end.unit && at.head == end.head;
@@ -40,7 +44,6 @@ struct Walk {
             else if (at.head + 1 < Hkv) ++at.head, at.unit = u.first;
             else at.head = 0, at.unit = u.last + 1;
         }
-        return true;
     }
 };
 

@@ -191,13 +191,14 @@ struct ChunkHeader {
     int32_t causal;                          // no window, prefix or documents: row_lo / row_hi need not be read
     int32_t T, Hkv;                          // the shape it was made for
 };
-// What a plan is for: tiles of up to `rows` stacked rows (T = rows / G tokens), `tiles` of them in a unit.
+// What a plan is for: tiles of up to `rows` stacked rows (T = rows / G tokens), `tiles` of them in a unit; a share of the work
+// for each of `per_sm` CTAs of an SM.
 struct ChunkKind {
     uint32_t magic;
-    int32_t rows, tiles;
+    int32_t rows, tiles, per_sm;
     __host__ __device__ int tokens(int G) const { return rows / G; }         // of a tile
 };
-constexpr ChunkKind kChunkKind{0x4e534443u, 128, 2}, kKv8Kind{0x4e534438u, 40, 1};
+constexpr ChunkKind kChunkKind{0x4e534443u, 128, 2, 1}, kKv8Kind{0x4e534438u, 40, 1, 2};
 struct ChunkPlan {                           // the buffer's parts
     ChunkHeader* header;
     ChunkStart* starts;                      // [n_ctas + 1]

@@ -3,6 +3,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "chunk_walk.h"
 #include "kv8_codec.h"
 #include "nsd_internal.h"
@@ -13,7 +15,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kTileKeys = 128, kBs = 16, kBlocks = kTileKeys / kBs;
-constexpr int kMaxRows = kKv8Kind.rows, kChunks = kMaxRows / 8;          // chunks of four rows that a thread has at most
+constexpr int kMaxRows = kKv8Kind.rows;
 constexpr int kThreads = 384, kSoftThreads = 256;
 constexpr int kWarpIssue = 8, kWarpV = 10, kWarpQ = 11;   // 9: the producer of K
 constexpr uint32_t kPollLimit = 1u << 30;              // polls of one wait, if nsd_config.wait_budget does not say
@@ -41,12 +43,12 @@ struct Attn8Args {
 };
 
 struct __align__(16) Meta {                            // a piece, beside its Q buffer
-    float c[kMaxRows];                                 // sc 2^-k 2^-7, where the row was multiplied by 2^k; NaN for a row with a value that is no number
     int lo[kMaxRows], hi[kMaxRows];                    // visible keys
     int lo_max, hi_min;                                // keys [lo_max, hi_min) are visible to every row
     int n, rows;                                       // key tiles, -1 behind the last piece; stacked rows
     int row0, head, slot;                              // first token's row; kv head; partial slot or -1
     int key_top;                                       // first key of the first tile
+    float c;                                           // sc 2^-k 2^-7, where the rows were multiplied by 2^k
 };
 struct __align__(16) State {
     float neg[kMaxRows];                               // minus the reference of each row's weights
@@ -111,15 +113,12 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 // Waits for this thread's tensor-memory loads; their registers are operands, so that no use moves in front of the wait.
-__device__ __forceinline__ void tmem_wait_ld20(uint32_t* r) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
-                   "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19])::"memory");
-}
-__device__ __forceinline__ void tmem_wait_ld12(uint32_t* r) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
-                   "+r"(r[11])::"memory");
+template <int N>
+__device__ __forceinline__ void tmem_wait(uint32_t* r) {
+    static_assert(N % 4 == 0, "four registers at a time");
+    tmem_wait_ld();
+#pragma unroll
+    for (int i = 0; i < N; i += 4) asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3])::"memory");
 }
 __device__ __forceinline__ bool any_of_softmax(bool p) {                 // over the softmax threads
     uint32_t r;
@@ -207,7 +206,9 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
         __syncwarp();
         asm volatile("barrier.cta.sync 1, %0;" ::"n"(kThreads) : "memory");
     };
-    auto columns = [](int rows) { return (rows + 7) & ~7; };                            // of one term
+    auto columns = [](int rows) { return (rows + 7) & ~7; };                            // of one term of S
+    // P and O: a warp's half of the rows, four rows and three terms after another, filled up to 16 columns
+    auto half_columns = [](int rows) { return (3 * rows + 15) & ~15; };
 
     if (warp < kWarpIssue) {
         // ================================ softmax and output ================================
@@ -215,7 +216,6 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 88;");
         const int q = warp & 3, half = warp >> 2, key = q * 32 + lane;
         const uint32_t lanes = (uint32_t)(q * 32) << 16;
-        const uint32_t p_at = smem0 + key * 16;
         // The warps meet at barriers that have no bound, so they have to leave together: one whose wait has run out goes on to
         // the next barrier, without waiting any more, and tells the others there.  A flag for every other barrier, since a
         // warp may be one ahead.
@@ -233,12 +233,12 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
         };
         uint32_t n_t = 0;                              // tiles so far
         bool any, out = false;
-        for (uint32_t n_q = 0; !out; ++n_q) {
+        for (uint32_t n_q = 0;; ++n_q) {
             const Meta& mt = meta[n_q & 1];
             hold(q_full + 8 * (n_q & 1), n_q >> 1);
             if (tid < kMaxRows) st.neg[tid] = INFINITY;                                 // no reference yet: a visible key's score is above every bound
             if (!agreed(false, any)) break;
-            const int n = mt.n, R = mt.rows, RP = columns(R), HP = RP / 2, n_ch = HP / 4, r0 = half * HP;
+            const int n = mt.n, R = mt.rows, RP = columns(R), HP = RP / 2, r0 = half * HP;
             if (n < 0) break;
             const int G = a.G, part = mt.slot;
             if (n == 0) {                              // rows that see nothing; a piece of such a unit is the whole of it
@@ -252,186 +252,194 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                 if (lane == 0) mbar_arrive(q_empty + 8 * (n_q & 1));
                 continue;
             }
-            const uint32_t tmem_o = tmem + kTmemO + lanes + r0;
-            uint64_t l2[2 * kChunks];
+            const int NH = half_columns(HP);
+            const uint32_t tmem_o = tmem + kTmemO + lanes + half * NH;
+            const uint32_t p_at = smem0 + half * (NH / 16) * (kTileKeys * 16) + key * 16;
+            const int lo_max = mt.lo_max, hi_min = mt.hi_min;
+            int ref_v = kNoScale, key0 = mt.key_top;
+            // A piece of NC chunks of four rows per thread, without a branch between them.
+            auto tiles = [&](auto chunks) {
+                constexpr int NC = decltype(chunks)::value;
+                uint64_t l2[2 * NC];
 #pragma unroll
-            for (int i = 0; i < 2 * kChunks; ++i) l2[i] = 0;
-            int ref_v = kNoScale;
-            for (int i = 0; i < n; ++i, ++n_t) {
-                const uint32_t stage = n_t % kStages, use = n_t / kStages;
-                const int key0 = mt.key_top - i * kTileKeys, at = key0 + key;
-                const bool masked = key0 < mt.lo_max || key0 + kTileKeys > mt.hi_min;
-                bool seen = true;
-                if (masked) {
-                    seen = false;
+                for (int i = 0; i < 2 * NC; ++i) l2[i] = 0;
+                for (int i = 0; i < n; ++i, ++n_t, key0 -= kTileKeys) {
+                    const uint32_t stage = n_t % kStages, use = n_t / kStages;
+                    const int at = key0 + key;
+                    const bool masked = key0 < lo_max || key0 + kTileKeys > hi_min;
+                    bool seen = true;
+                    if (masked) {
+                        seen = false;
 #pragma unroll 1
-                    for (int r = 0; r < R; r += G) seen = seen || (at >= mt.lo[r] && at < mt.hi[r]);
-                }
-                hold(k_full + 8 * stage, use);         // the scales
-                const unsigned char* const sb = smem + L::kOffScales + stage * (kBlocks * 32) + (key >> 4) * 32 + (key & 15);
-                const uint32_t kb = sb[0], vb = sb[16];
-                // the key's power of two, times 2^7 against the rows' 2^-7
-                const float kk = __uint_as_float(kb > 247 || vb > 247 ? 0x7fc00000u : (kb + 7) << 23);
-                const uint64_t kk2 = pair(kk, kk);
-                const int ev = seen ? (int)vb - 127 : kNoScale;
-                hold(s_full + 8 * (n_t & 1), n_t >> 1);
-                tc_fence_after();
-                const uint32_t tmem_s = tmem + (n_t & 1) * 64 + lanes + r0;
-                uint32_t x[4 * kChunks];
-                // the scores of this thread's key and rows less `less`, -inf where a row does not see the key
-                auto scores = [&](const float* less) {
+                        for (int r = 0; r < R; r += G) seen = seen || (at >= mt.lo[r] && at < mt.hi[r]);
+                    }
+                    hold(k_full + 8 * stage, use);     // the scales
+                    const unsigned char* const sb = smem + L::kOffScales + stage * (kBlocks * 32) + (key >> 4) * 32 + (key & 15);
+                    const uint32_t kb = sb[0], vb = sb[16];
+                    // the key's power of two, times 2^7 against the rows' 2^-7, and theirs
+                    const float kk = __uint_as_float(kb > 247 || vb > 247 ? 0x7fc00000u : (kb + 7) << 23) * mt.c;
+                    const uint64_t kk2 = pair(kk, kk);
+                    const int ev = seen ? (int)vb - 127 : kNoScale;
+                    hold(s_full + 8 * (n_t & 1), n_t >> 1);
+                    tc_fence_after();
+                    const uint32_t tmem_s = tmem + (n_t & 1) * 64 + lanes + r0;
+                    uint32_t x[4 * NC];
+                    // The scores of this thread's key and rows less the rows' references, -inf where a row does not see the key.
+                    // The product is rounded before the difference, so that the largest score less itself is 0 however large it is.
+                    auto scores = [&] {
 #pragma unroll
-                    for (int ch = 0; ch < kChunks; ++ch)
-                        if (ch < n_ch) tmem_ld4(tmem_s + ch * 4, x + ch * 4);
-                    tmem_wait_ld20(x);
+                        for (int ch = 0; ch < NC; ++ch) tmem_ld4(tmem_s + ch * 4, x + ch * 4);
+                        float4 m[NC];
 #pragma unroll
-                    for (int ch = 0; ch < kChunks; ++ch) {
-                        if (ch >= n_ch) break;
-                        const float4 c = *reinterpret_cast<const float4*>(mt.c + r0 + ch * 4);
-                        uint64_t z0 = mul2(mul2(bits2(x[ch * 4], x[ch * 4 + 1]), pair(c.x, c.y)), kk2);
-                        uint64_t z1 = mul2(mul2(bits2(x[ch * 4 + 2], x[ch * 4 + 3]), pair(c.z, c.w)), kk2);
-                        if (less) {
-                            const float4 m = *reinterpret_cast<const float4*>(less + r0 + ch * 4);
-                            z0 = add2(z0, pair(m.x, m.y)), z1 = add2(z1, pair(m.z, m.w));
+                        for (int ch = 0; ch < NC; ++ch) m[ch] = *reinterpret_cast<const float4*>(st.neg + r0 + ch * 4);
+                        tmem_wait<4 * NC>(x);
+#pragma unroll
+                        for (int ch = 0; ch < NC; ++ch) {
+                            const float2 f0 = unpair(add2(mul2(bits2(x[ch * 4], x[ch * 4 + 1]), kk2), pair(m[ch].x, m[ch].y)));
+                            const float2 f1 = unpair(add2(mul2(bits2(x[ch * 4 + 2], x[ch * 4 + 3]), kk2), pair(m[ch].z, m[ch].w)));
+                            x[ch * 4] = __float_as_uint(f0.x), x[ch * 4 + 1] = __float_as_uint(f0.y);
+                            x[ch * 4 + 2] = __float_as_uint(f1.x), x[ch * 4 + 3] = __float_as_uint(f1.y);
                         }
-                        const float2 f0 = unpair(z0), f1 = unpair(z1);
-                        x[ch * 4] = __float_as_uint(f0.x), x[ch * 4 + 1] = __float_as_uint(f0.y);
-                        x[ch * 4 + 2] = __float_as_uint(f1.x), x[ch * 4 + 3] = __float_as_uint(f1.y);
                         if (masked) {
-                            const int4 lo = *reinterpret_cast<const int4*>(mt.lo + r0 + ch * 4), hi = *reinterpret_cast<const int4*>(mt.hi + r0 + ch * 4);
-                            if (at < lo.x || at >= hi.x) x[ch * 4] = 0xff800000u;
-                            if (at < lo.y || at >= hi.y) x[ch * 4 + 1] = 0xff800000u;
-                            if (at < lo.z || at >= hi.z) x[ch * 4 + 2] = 0xff800000u;
-                            if (at < lo.w || at >= hi.w) x[ch * 4 + 3] = 0xff800000u;
+#pragma unroll
+                            for (int j = 0; j < 4 * NC; ++j)
+                                if (at < mt.lo[r0 + j] || at >= mt.hi[r0 + j]) x[j] = 0xff800000u;
                         }
-                    }
-                };
-                scores(st.neg);
-                __syncwarp();
-                if (lane == 0) mbar_arrive(k_empty + 8 * stage);                        // S is complete and the scales are read
-                float top = -INFINITY;
+                    };
+                    scores();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(k_empty + 8 * stage);                    // S is complete and the scales are read
+                    float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-                for (int ch = 0; ch < kChunks; ++ch) {
-                    if (ch >= n_ch) break;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) top = fmaxf(top, __uint_as_float(x[ch * 4 + j]));
-                }
-                int dev = seen ? ev - ref_v : 0;
-                if (!agreed(top + (float)max(dev, -40) > kMost, any)) {
-                    out = true;
-                    break;
-                }
-                if (i > 0) hold(o_done, n_t - 1);      // P V of the tile before has read P and written O
-                // Rare but for a piece's first tile: a weight would leave the range of 16 bits, or a row sees its first key.
-                if (any) {
-                    scores(nullptr);
-#pragma unroll
-                    for (int ch = 0; ch < kChunks; ++ch) {
-                        if (ch >= n_ch) break;
-                        int best = 0;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int m = __reduce_max_sync(0xffffffffu, ordered(__uint_as_float(x[ch * 4 + j])));
-                            if (lane == j) best = m;
+                    for (int j = 0; j < 4 * NC; ++j) top[j & 1] = fmaxf(top[j & 1], __uint_as_float(x[j]));
+                    int dev = seen ? ev - ref_v : 0;
+                    if (fail) st.fail[turn] = 1;
+                    any = any_of_softmax(fail || fmaxf(top[0], top[1]) + (float)max(dev, -40) > kMost);
+                    turn ^= 1;
+                    // Rare but for a piece's first tile: a weight would leave the range of 16 bits, or a row sees its first key.
+                    if (any) {
+                        if (st.fail[turn ^ 1]) {
+                            fail = out = true;
+                            break;
                         }
-                        if (lane < 4) st.top[q][r0 + ch * 4 + lane] = unordered(best);
-                    }
-                    const int e = __reduce_max_sync(0xffffffffu, ev);
-                    if (lane == 0) st.exp_top[q] = e;
-                    softmax_sync();
-                    if (tid < RP) {
-                        const float m = fmaxf(fmaxf(st.top[0][tid], st.top[1][tid]), fmaxf(st.top[2][tid], st.top[3][tid]));
-                        const float old = -st.neg[tid], now = fmaxf(old, m - kTop);
-                        st.neg[tid] = -now;
-                        st.fac[tid] = old == -INFINITY ? 0.f : ex2_approx(old - now);
-                    }
-                    const int ref = max(max(max(st.exp_top[0], st.exp_top[1]), max(st.exp_top[2], st.exp_top[3])), ref_v);
-                    softmax_sync();
-                    const float shrink = ex2_approx((float)(ref_v - ref));
-                    ref_v = ref;
-                    dev = seen ? ev - ref_v : 0;
-                    if (i > 0) tc_fence_after();
-#pragma unroll
-                    for (int ch = 0; ch < kChunks; ++ch) {
-                        if (ch >= n_ch) break;
-                        const float4 f = *reinterpret_cast<const float4*>(st.fac + r0 + ch * 4), m = *reinterpret_cast<const float4*>(st.neg + r0 + ch * 4);
-                        const float less[4] = {m.x, m.y, m.z, m.w};
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (x[ch * 4 + j] != 0xff800000u) x[ch * 4 + j] = __float_as_uint(__uint_as_float(x[ch * 4 + j]) + less[j]);
-                        l2[ch * 2] = mul2(l2[ch * 2], pair(f.x, f.y)), l2[ch * 2 + 1] = mul2(l2[ch * 2 + 1], pair(f.z, f.w));
-                        if (i > 0) {
 #pragma unroll 1
-                            for (int t = 0; t < 3; ++t) {
-                                uint32_t o[4];
-                                tmem_ld4(tmem_o + t * RP + ch * 4, o);
-                                tmem_wait_ld();
-                                o[0] = __float_as_uint(__uint_as_float(o[0]) * (f.x * shrink)), o[1] = __float_as_uint(__uint_as_float(o[1]) * (f.y * shrink));
-                                o[2] = __float_as_uint(__uint_as_float(o[2]) * (f.z * shrink)), o[3] = __float_as_uint(__uint_as_float(o[3]) * (f.w * shrink));
-                                tmem_st4(tmem_o + t * RP + ch * 4, o);
+                        for (int ch = 0; ch < NC; ++ch) {
+                            uint32_t y[4];
+                            tmem_ld4(tmem_s + ch * 4, y);
+                            tmem_wait<4>(y);
+                            int best = 0;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const int r = r0 + ch * 4 + j;
+                                const bool sees = !masked || (at >= mt.lo[r] && at < mt.hi[r]);
+                                const int m = __reduce_max_sync(0xffffffffu, ordered(sees ? __uint_as_float(y[j]) * kk : -INFINITY));
+                                if (lane == j) best = m;
                             }
+                            if (lane < 4) st.top[q][r0 + ch * 4 + lane] = unordered(best);
+                        }
+                        const int e = __reduce_max_sync(0xffffffffu, ev);
+                        if (lane == 0) st.exp_top[q] = e;
+                        softmax_sync();
+                        if (tid < RP) {
+                            const float m = fmaxf(fmaxf(st.top[0][tid], st.top[1][tid]), fmaxf(st.top[2][tid], st.top[3][tid]));
+                            const float old = -st.neg[tid], now = fmaxf(old, m - kTop);
+                            st.neg[tid] = -now;
+                            st.fac[tid] = old == -INFINITY ? 0.f : ex2_approx(old - now);
+                        }
+                        const int ref = max(max(max(st.exp_top[0], st.exp_top[1]), max(st.exp_top[2], st.exp_top[3])), ref_v);
+                        softmax_sync();
+                        if (i > 0) {
+                            const float shrink = ex2_approx((float)(ref_v - ref));
+#pragma unroll
+                            for (int j = 0; j < 2 * NC; ++j) {
+                                const float2 f = *reinterpret_cast<const float2*>(st.fac + r0 + 2 * j);
+                                l2[j] = mul2(l2[j], pair(f.x, f.y));
+                            }
+                            hold(o_done, n_t - 1);     // O holds this piece's earlier tiles
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int ch = 0; ch < NC; ++ch) {
+                                uint32_t o[12];
+#pragma unroll
+                                for (int t = 0; t < 3; ++t) tmem_ld4(tmem_o + ch * 12 + t * 4, o + 4 * t);
+                                const float4 f = *reinterpret_cast<const float4*>(st.fac + r0 + ch * 4);
+                                const float by[4] = {f.x * shrink, f.y * shrink, f.z * shrink, f.w * shrink};
+                                tmem_wait<12>(o);
+#pragma unroll
+                                for (int j = 0; j < 12; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * by[j & 3]);
+#pragma unroll
+                                for (int t = 0; t < 3; ++t) tmem_st4(tmem_o + ch * 12 + t * 4, o + 4 * t);
+                            }
+                            tmem_wait_st();
+                        }
+                        ref_v = ref;
+                        dev = seen ? ev - ref_v : 0;
+                        scores();
+                    }
+                    // weights: their sums in 32 bits; times V's power of two, and split, for the product
+                    const float vs = __uint_as_float((uint32_t)(min(max(dev, -126), 127) + 127) << 23);
+                    const uint64_t vs2 = pair(vs, vs);
+                    constexpr int kUnits = (3 * NC + 3) / 4;
+                    uint32_t word[4 * kUnits] = {};
+#pragma unroll
+                    for (int ch = 0; ch < NC; ++ch) {
+                        uint32_t h[2];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const uint64_t p = pair(ex2_approx(__uint_as_float(x[ch * 4 + 2 * j])), ex2_approx(__uint_as_float(x[ch * 4 + 2 * j + 1])));
+                            l2[ch * 2 + j] = add2(l2[ch * 2 + j], p);
+                            const float2 wv = unpair(mul2(p, vs2));
+                            h[j] = pack_half(wv.x, wv.y);
+                        }
+                        split4<true>(h[0], h[1], word + 3 * ch);
+                    }
+                    if (i > 0) hold(o_done, n_t - 1);  // P V of the tile before has read P
+#pragma unroll
+                    for (int k = 0; k < kUnits; ++k)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(p_at + k * (kTileKeys * 16)), "r"(word[4 * k]), "r"(word[4 * k + 1]), "r"(word[4 * k + 2]), "r"(word[4 * k + 3]) : "memory");
+                    // Hidden rows of V have to be finite, since 0 x NaN is NaN.
+                    if (masked) {
+                        hold(v_full + 8 * stage, use);
+                        if (!seen && half == 0) {
+                            const uint32_t row = smem0 + L::kOffV + stage * L::kTile + key * D;
+#pragma unroll
+                            for (int ch = 0; ch < D / 16; ++ch)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(row + ((ch + lane) % (D / 16)) * 16), "r"(0) : "memory");
                         }
                     }
-                    tmem_wait_st();
+                    fence_async_smem();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(p_full);
                 }
-                // weights: their sums in 32 bits; times V's power of two, and split, for the product
-                const float vs = __uint_as_float((uint32_t)(min(max(dev, -126), 127) + 127) << 23);
-                const uint64_t vs2 = pair(vs, vs);
+                // sums over the lanes (a chunk's four rows end up on lanes 0, 8, 16, 24)
 #pragma unroll
-                for (int ch = 0; ch < kChunks; ++ch) {
-                    if (ch >= n_ch) break;
-                    uint32_t h[2], term[3];
+                for (int ch = 0; ch < NC; ++ch) {
+                    const float2 f0 = unpair(l2[ch * 2]), f1 = unpair(l2[ch * 2 + 1]);
+                    float v[4] = {f0.x, f0.y, f1.x, f1.y};
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const uint64_t p = pair(ex2_approx(__uint_as_float(x[ch * 4 + 2 * j])), ex2_approx(__uint_as_float(x[ch * 4 + 2 * j + 1])));
-                        l2[ch * 2 + j] = add2(l2[ch * 2 + j], p);
-                        const float2 wv = unpair(mul2(p, vs2));
-                        h[j] = pack_half(wv.x, wv.y);
+                    for (int k = 2; k > 0; k >>= 1) {
+                        const bool up = lane & (k * 8);
+#pragma unroll
+                        for (int j = 0; j < k; ++j) {
+                            const float send = up ? v[j] : v[j + k], keep = up ? v[j + k] : v[j];
+                            v[j] = keep + __shfl_xor_sync(0xffffffffu, send, k * 8);
+                        }
                     }
-                    split4<true>(h[0], h[1], term);
-#pragma unroll
-                    for (int t = 0; t < 3; ++t) {
-                        const int col = t * RP + r0 + ch * 4;
-                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(p_at + (col >> 4) * (kTileKeys * 16) + (col & 15)), "r"(term[t]) : "memory");
-                    }
+                    v[0] += __shfl_xor_sync(0xffffffffu, v[0], 4);
+                    v[0] += __shfl_xor_sync(0xffffffffu, v[0], 2);
+                    v[0] += __shfl_xor_sync(0xffffffffu, v[0], 1);
+                    if ((lane & 7) == 0) st.top[q][r0 + ch * 4 + (lane >> 3)] = v[0];
                 }
-                // Hidden rows of V have to be finite, since 0 x NaN is NaN.
-                if (masked) {
-                    hold(v_full + 8 * stage, use);
-                    if (!seen && half == 0) {
-                        const uint32_t row = smem0 + L::kOffV + stage * L::kTile + key * D;
-#pragma unroll
-                        for (int ch = 0; ch < D / 16; ++ch)
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(row + ((ch + lane) % (D / 16)) * 16), "r"(0) : "memory");
-                    }
-                }
-                fence_async_smem();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(p_full);
-            }
-            if (out) break;
-            // ---- the piece's rows: sums over the lanes (a chunk's four rows end up on lanes 0, 8, 16, 24), then over the quarters
-#pragma unroll
-            for (int ch = 0; ch < kChunks; ++ch) {
-                if (ch >= n_ch) break;
-                const float2 f0 = unpair(l2[ch * 2]), f1 = unpair(l2[ch * 2 + 1]);
-                float v[4] = {f0.x, f0.y, f1.x, f1.y};
-#pragma unroll
-                for (int k = 2; k > 0; k >>= 1) {
-                    const bool up = lane & (k * 8);
-#pragma unroll
-                    for (int j = 0; j < k; ++j) {
-                        const float send = up ? v[j] : v[j + k], keep = up ? v[j + k] : v[j];
-                        v[j] = keep + __shfl_xor_sync(0xffffffffu, send, k * 8);
-                    }
-                }
-                v[0] += __shfl_xor_sync(0xffffffffu, v[0], 4);
-                v[0] += __shfl_xor_sync(0xffffffffu, v[0], 2);
-                v[0] += __shfl_xor_sync(0xffffffffu, v[0], 1);
-                if ((lane & 7) == 0) st.top[q][r0 + ch * 4 + (lane >> 3)] = v[0];
-            }
-            if (!agreed(false, any)) break;
+            };
+            const int n_ch = HP / 4;
+            if (n_ch == 1) tiles(std::integral_constant<int, 1>());
+            else if (n_ch == 2) tiles(std::integral_constant<int, 2>());
+            else if (n_ch == 3) tiles(std::integral_constant<int, 3>());
+            else if (n_ch == 4) tiles(std::integral_constant<int, 4>());
+            else tiles(std::integral_constant<int, 5>());
+            // ---- the piece's rows
+            if (out || !agreed(false, any)) break;
             const int64_t part0 = (int64_t)part * kMaxRows;
             if (tid < RP) {
                 const float l = (st.top[0][tid] + st.top[1][tid]) + (st.top[2][tid] + st.top[3][tid]), m = -st.neg[tid];
@@ -455,8 +463,8 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             for (int ch = 0; ch < n_ch; ++ch) {
                 uint32_t y[12];
 #pragma unroll
-                for (int t = 0; t < 3; ++t) tmem_ld4(tmem_o + t * RP + ch * 4, y + 4 * t);
-                tmem_wait_ld12(y);
+                for (int t = 0; t < 3; ++t) tmem_ld4(tmem_o + ch * 12 + t * 4, y + 4 * t);
+                tmem_wait<12>(y);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int r = r0 + ch * 4 + j;
@@ -532,7 +540,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             const uint32_t stage = n_p % kStages;
             if (!(ok = wait(v_full + 8 * stage, n_p / kStages)) || !(ok = wait(p_full, n_p))) break;
             tc_fence_after();
-            const uint32_t idesc = instr_desc_f8(D, (3 * rp + 15) & ~15, 1, 1);
+            const uint32_t idesc = instr_desc_f8(D, 2 * half_columns(rp / 2), 1, 1);
             const uint64_t dv = smem_desc(smem0 + L::kOffV + stage * L::kTile, 16, 8 * D, L::kSwizzle);
             if (elect_one()) {
 #pragma unroll
@@ -614,7 +622,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
         }
     } else {
         // ================================ Q and the pieces ================================
-        // Every row times a power of two that brings its largest element to [2^14, 2^15), split into three e5m2 terms: rows
+        // The rows times the power of two that brings their largest element to [2^14, 2^15), split into three e5m2 terms: rows
         // [term][row] of the product's second operand.  bf16 has eight significant bits, the terms nine: nothing is lost but
         // what lies below 2^-16 then.
         constexpr int kPer = D / 32;                   // elements of a lane
@@ -630,7 +638,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             const uint32_t qb = smem0 + L::kOffQ + slot * L::kQ;
             Meta& mt = meta[slot];
             uint32_t v[kRowsAhead][kPer / 2];
-            auto fetch = [&](int first) {
+            auto fetch = [&](int first) {              // nothing beyond R is read
 #pragma unroll
                 for (int i = 0; i < kRowsAhead; ++i) {
                     const int r = first + i;
@@ -647,35 +655,49 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                     }
                 }
             };
+            auto largest = [&](int i) {                // magnitude bits of this lane's part of a row
+                uint32_t big = 0;
+#pragma unroll
+                for (int j = 0; j < kPer / 2; ++j) big = max(big, max(v[i][j] & 0x7fffu, (v[i][j] >> 16) & 0x7fffu));
+                return big;
+            };
             const bool tiles = piece && w.k1 > w.k0;
-            if (tiles) fetch(0);                       // under way while the buffer is not free yet
+            uint32_t big = 0;                          // of all rows, but for what is no number
+            if (tiles) {                               // while the buffer is not free yet
+#pragma unroll 1
+                for (int first = 0; first < R; first += kRowsAhead) {
+                    fetch(first);
+#pragma unroll
+                    for (int i = 0; i < kRowsAhead; ++i) {
+                        const uint32_t m = largest(i);
+                        if (!__any_sync(0xffffffffu, m >= 0x7f80u)) big = max(big, m);
+                    }
+                }
+                big = __reduce_max_sync(0xffffffffu, big);
+                if (R > kRowsAhead) fetch(0);
+            }
+            const int k = 141 - max((int)(big >> 7), 1);                                // 2^k as a product: k may be 140
+            const float f0 = __uint_as_float((uint32_t)((k >> 1) + 127) << 23), f1 = __uint_as_float((uint32_t)(k - (k >> 1) + 127) << 23);
             if (n_q >= 2 && !(ok = wait(q_empty + 8 * slot, (n_q >> 1) - 1))) break;
             if (tiles) {
 #pragma unroll 1
                 for (int first = 0; first < RP; first += kRowsAhead) {
                     uint32_t h[kRowsAhead][2];
-                    float c[kRowsAhead];
+                    bool none[kRowsAhead];             // a value that is no number: the whole row is none
 #pragma unroll
                     for (int i = 0; i < kRowsAhead; ++i) {
-                        uint32_t big = 0;
-#pragma unroll
-                        for (int j = 0; j < kPer / 2; ++j) big = max(big, max(v[i][j] & 0x7fffu, (v[i][j] >> 16) & 0x7fffu));
-                        big = __reduce_max_sync(0xffffffffu, big);
-                        const int k = 141 - max((int)(big >> 7), 1);                    // 2^k as a product: k may be 140
-                        const float f0 = __uint_as_float((uint32_t)((k >> 1) + 127) << 23), f1 = __uint_as_float((uint32_t)(k - (k >> 1) + 127) << 23);
+                        none[i] = __any_sync(0xffffffffu, largest(i) >= 0x7f80u);
                         h[i][1] = 0;
 #pragma unroll
                         for (int j = 0; j < kPer / 2; ++j)
                             h[i][j] = pack_half(__uint_as_float(v[i][j] << 16) * f0 * f1, __uint_as_float(v[i][j] & 0xffff0000u) * f0 * f1);
-                        const int d0 = (-k - 7) >> 1, d1 = -k - 7 - d0;                 // sc 2^(-k - 7)
-                        c[i] = first + i >= R ? 0.f : (big >= 0x7f80u ? __uint_as_float(0x7fc00000u)
-                                                                      : a.sc * __uint_as_float((uint32_t)(d0 + 127) << 23) * __uint_as_float((uint32_t)(d1 + 127) << 23));
                     }
-                    fetch(first + kRowsAhead);         // nothing beyond R is read
+                    fetch(first + kRowsAhead);
 #pragma unroll
                     for (int i = 0; i < kRowsAhead; ++i) {
                         uint32_t t[3];
                         split4<false>(h[i][0], h[i][1], t);
+                        if (none[i]) t[0] = 0x7f7f7f7fu;
 #pragma unroll
                         for (int j = 0; j < 3; ++j) {
                             const int row = j * RP + first + i;                         // the swizzle exchanges 16-byte pieces by the row
@@ -684,7 +706,6 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                             else
                                 asm volatile("st.shared.b16 [%0], %1;" ::"r"(qb + row * 64 + (((lane >> 3) ^ ((row >> 1) & 3)) << 4) + (lane & 7) * 2), "h"((uint16_t)t[j]) : "memory");
                         }
-                        if (lane == i) mt.c[first + i] = c[i];
                     }
                 }
                 int lo_max = 0, hi_min = 0x7fffffff;
@@ -703,6 +724,8 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             }
             if (lane == 0) {
                 mt.n = piece ? w.k1 - w.k0 : -1, mt.rows = R;
+                const int d0 = (-k - 7) >> 1, d1 = -k - 7 - d0;                         // sc 2^(-k - 7)
+                mt.c = a.sc * __uint_as_float((uint32_t)(d0 + 127) << 23) * __uint_as_float((uint32_t)(d1 + 127) << 23);
                 if (piece) mt.row0 = w.u.row0, mt.head = w.head, mt.slot = w.slot, mt.key_top = ((w.u.key_hi + kTileKeys - 1) / kTileKeys - 1 - w.k0) * kTileKeys;
             }
             fence_async_smem();

@@ -19,8 +19,8 @@ constexpr int kMaxRows = kKv8Kind.rows;
 constexpr int kThreads = 384, kSoftThreads = 256;
 constexpr int kWarpIssue = 8, kWarpV = 10, kWarpQ = 11;   // 9: the producer of K
 constexpr uint32_t kPollLimit = 1u << 30;              // polls of one wait, if nsd_config.wait_budget does not say
-constexpr float kTop = 7.f, kMost = 15.f;              // log2 of a row's largest weight when its reference is set, and at most
-constexpr float kLow = 64.f;                           // the last term of a weight is held times this
+constexpr float kTop = 4.f, kMost = 15.f;              // log2 of a row's largest weight when its reference is set, and at most
+constexpr float kMid = 8.f, kLow = 16.f;               // a weight's second term is held times kMid, its third times both
 constexpr int kNoScale = -1000;                        // exponent of V's reference before any
 
 __device__ __forceinline__ void report(int32_t* status, int32_t bit, int r) {
@@ -47,12 +47,14 @@ struct __align__(16) Meta {                            // a piece, beside its Q 
     int lo_max, hi_min;                                // keys [lo_max, hi_min) are visible to every row
     int n, rows;                                       // key tiles, -1 behind the last piece; stacked rows
     int row0, head, slot;                              // first token's row; kv head; partial slot or -1
-    int key_top;                                       // first key of the first tile
+    int key_first;                                     // of the first tile
     float c;                                           // sc 2^-k 2^-7, where the rows were multiplied by 2^k
 };
 struct __align__(16) State {
     float neg[kMaxRows];                               // minus the reference of each row's weights
+    float step[kMaxRows];                              // its last change
     float fac[kMaxRows];
+    int unset[kMaxRows];                               // the row has no reference yet
     float top[4][kMaxRows];                            // a quarter's largest scores; at the end its sums
     int exp_top[4];
     volatile int fail[2];                              // a warp has given up, by barriers in turn
@@ -91,18 +93,21 @@ __device__ __forceinline__ uint32_t minus(uint32_t a, uint32_t b) {
     const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
     return *reinterpret_cast<const uint32_t*>(&r);
 }
-__device__ __forceinline__ uint32_t times_low(uint32_t a) {
-    const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), __float2half2_rn(kLow));
+__device__ __forceinline__ uint32_t times(uint32_t a, float by) {
+    const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), __float2half2_rn(by));
     return *reinterpret_cast<const uint32_t*>(&r);
 }
 // Four 16-bit floats in two words as three e5m2 terms each, four bytes per term: they sum to the value, exactly down to 2^-16,
-// the format's least step.  LOW: the last term is held times 64, so that what is left below that step keeps three bits more.
-template <bool LOW>
+// the format's least step.  FINE: the second term is held times 8 and the third times 128 (what is left is that much smaller),
+// so that a value keeps its bits down to 2^-24, where 16-bit floats end.
+template <bool FINE>
 __device__ __forceinline__ void split4(uint32_t a, uint32_t b, uint32_t* terms) {
     const uint32_t a0 = upper(a), b0 = upper(b);
-    const uint32_t ra = minus(a, a0), rb = minus(b, b0), a1 = upper(ra), b1 = upper(rb);
+    uint32_t ra = minus(a, a0), rb = minus(b, b0);
+    if constexpr (FINE) ra = times(ra, kMid), rb = times(rb, kMid);
+    const uint32_t a1 = upper(ra), b1 = upper(rb);
     uint32_t a2 = minus(ra, a1), b2 = minus(rb, b1);
-    if constexpr (LOW) a2 = times_low(a2), b2 = times_low(b2);
+    if constexpr (FINE) a2 = times(a2, kLow), b2 = times(b2, kLow);
     a2 += 0x00800080u, b2 += 0x00800080u;
     terms[0] = __byte_perm(a0, b0, 0x7531);
     terms[1] = __byte_perm(a1, b1, 0x7531);
@@ -201,6 +206,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
         ok = bar_wait_slow(bar, count & 1, &abort_s, limit);
         return (bool)__all_sync(0xffffffffu, ok);
     };
+    auto ready = [&](uint32_t bar, uint32_t count) { return (bool)__all_sync(0xffffffffu, bar_try(bar, count & 1)); };
     // Behind this barrier every warp has left its loop and the abort flag is final.
     auto all_done = [] {
         __syncwarp();
@@ -236,7 +242,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
         for (uint32_t n_q = 0;; ++n_q) {
             const Meta& mt = meta[n_q & 1];
             hold(q_full + 8 * (n_q & 1), n_q >> 1);
-            if (tid < kMaxRows) st.neg[tid] = INFINITY;                                 // no reference yet: a visible key's score is above every bound
+            if (tid < kMaxRows) st.neg[tid] = 0.f, st.unset[tid] = 1;
             if (!agreed(false, any)) break;
             const int n = mt.n, R = mt.rows, RP = columns(R), HP = RP / 2, r0 = half * HP;
             if (n < 0) break;
@@ -256,14 +262,15 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             const uint32_t tmem_o = tmem + kTmemO + lanes + half * NH;
             const uint32_t p_at = smem0 + half * (NH / 16) * (kTileKeys * 16) + key * 16;
             const int lo_max = mt.lo_max, hi_min = mt.hi_min;
-            int ref_v = kNoScale, key0 = mt.key_top;
+            int ref_v = kNoScale, key0 = mt.key_first;
+            bool pending = true;                       // some row has no reference yet
             // A piece of NC chunks of four rows per thread, without a branch between them.
             auto tiles = [&](auto chunks) {
                 constexpr int NC = decltype(chunks)::value;
                 uint64_t l2[2 * NC];
 #pragma unroll
                 for (int i = 0; i < 2 * NC; ++i) l2[i] = 0;
-                for (int i = 0; i < n; ++i, ++n_t, key0 -= kTileKeys) {
+                for (int i = 0; i < n; ++i, ++n_t, key0 += kTileKeys) {
                     const uint32_t stage = n_t % kStages, use = n_t / kStages;
                     const int at = key0 + key;
                     const bool masked = key0 < lo_max || key0 + kTileKeys > hi_min;
@@ -276,78 +283,88 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                     hold(k_full + 8 * stage, use);     // the scales
                     const unsigned char* const sb = smem + L::kOffScales + stage * (kBlocks * 32) + (key >> 4) * 32 + (key & 15);
                     const uint32_t kb = sb[0], vb = sb[16];
-                    // the key's power of two, times 2^7 against the rows' 2^-7, and theirs
-                    const float kk = __uint_as_float(kb > 247 || vb > 247 ? 0x7fc00000u : (kb + 7) << 23) * mt.c;
+                    // The key's power of two, times 2^7 against the rows' 2^-7, and theirs: not 0, so that a hidden score stays -inf.
+                    const bool none = kb > 247 || vb > 247;
+                    const float kk = none ? (masked ? 1.f : __uint_as_float(0x7fc00000u)) : fmaxf(__uint_as_float((kb + 7) << 23) * mt.c, 1.17549435e-38f);
                     const uint64_t kk2 = pair(kk, kk);
                     const int ev = seen ? (int)vb - 127 : kNoScale;
                     hold(s_full + 8 * (n_t & 1), n_t >> 1);
                     tc_fence_after();
                     const uint32_t tmem_s = tmem + (n_t & 1) * 64 + lanes + r0;
-                    uint32_t x[4 * NC];
-                    // The scores of this thread's key and rows less the rows' references, -inf where a row does not see the key.
-                    // The product is rounded before the difference, so that the largest score less itself is 0 however large it is.
-                    auto scores = [&] {
-#pragma unroll
-                        for (int ch = 0; ch < NC; ++ch) tmem_ld4(tmem_s + ch * 4, x + ch * 4);
-                        float4 m[NC];
-#pragma unroll
-                        for (int ch = 0; ch < NC; ++ch) m[ch] = *reinterpret_cast<const float4*>(st.neg + r0 + ch * 4);
-                        tmem_wait<4 * NC>(x);
-#pragma unroll
-                        for (int ch = 0; ch < NC; ++ch) {
-                            const float2 f0 = unpair(add2(mul2(bits2(x[ch * 4], x[ch * 4 + 1]), kk2), pair(m[ch].x, m[ch].y)));
-                            const float2 f1 = unpair(add2(mul2(bits2(x[ch * 4 + 2], x[ch * 4 + 3]), kk2), pair(m[ch].z, m[ch].w)));
-                            x[ch * 4] = __float_as_uint(f0.x), x[ch * 4 + 1] = __float_as_uint(f0.y);
-                            x[ch * 4 + 2] = __float_as_uint(f1.x), x[ch * 4 + 3] = __float_as_uint(f1.y);
-                        }
-                        if (masked) {
-#pragma unroll
-                            for (int j = 0; j < 4 * NC; ++j)
-                                if (at < mt.lo[r0 + j] || at >= mt.hi[r0 + j]) x[j] = 0xff800000u;
-                        }
-                    };
-                    scores();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(k_empty + 8 * stage);                    // S is complete and the scales are read
-                    float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-                    for (int j = 0; j < 4 * NC; ++j) top[j & 1] = fmaxf(top[j & 1], __uint_as_float(x[j]));
-                    int dev = seen ? ev - ref_v : 0;
-                    if (fail) st.fail[turn] = 1;
-                    any = any_of_softmax(fail || fmaxf(top[0], top[1]) + (float)max(dev, -40) > kMost);
-                    turn ^= 1;
-                    // Rare but for a piece's first tile: a weight would leave the range of 16 bits, or a row sees its first key.
-                    if (any) {
-                        if (st.fail[turn ^ 1]) {
-                            fail = out = true;
-                            break;
-                        }
+                    // Scores are hidden where they lie, in a loop of its own: rare, and out of the way of the others.
+                    if (masked) {
 #pragma unroll 1
                         for (int ch = 0; ch < NC; ++ch) {
                             uint32_t y[4];
                             tmem_ld4(tmem_s + ch * 4, y);
                             tmem_wait<4>(y);
-                            int best = 0;
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
                                 const int r = r0 + ch * 4 + j;
-                                const bool sees = !masked || (at >= mt.lo[r] && at < mt.hi[r]);
-                                const int m = __reduce_max_sync(0xffffffffu, ordered(sees ? __uint_as_float(y[j]) * kk : -INFINITY));
-                                if (lane == j) best = m;
+                                if (none) y[j] = 0x7fc00000u;
+                                if (at < mt.lo[r] || at >= mt.hi[r]) y[j] = 0xff800000u;
+                            }
+                            tmem_st4(tmem_s + ch * 4, y);
+                        }
+                        tmem_wait_st();
+                    }
+                    // The scores of this thread's key and rows less the rows' references, -inf where a row does not see the key.  The
+                    // product is rounded before the difference, so that the largest score less itself is 0 however large it is.
+                    uint32_t x[4 * NC];
+                    float4 m[NC];
+#pragma unroll
+                    for (int ch = 0; ch < NC; ++ch) tmem_ld4(tmem_s + ch * 4, x + ch * 4);
+#pragma unroll
+                    for (int ch = 0; ch < NC; ++ch) m[ch] = *reinterpret_cast<const float4*>(st.neg + r0 + ch * 4);
+                    tmem_wait<4 * NC>(x);
+                    float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                    for (int ch = 0; ch < NC; ++ch) {
+                        const float2 f0 = unpair(add2(mul2(bits2(x[ch * 4], x[ch * 4 + 1]), kk2), pair(m[ch].x, m[ch].y)));
+                        const float2 f1 = unpair(add2(mul2(bits2(x[ch * 4 + 2], x[ch * 4 + 3]), kk2), pair(m[ch].z, m[ch].w)));
+                        x[ch * 4] = __float_as_uint(f0.x), x[ch * 4 + 1] = __float_as_uint(f0.y);
+                        x[ch * 4 + 2] = __float_as_uint(f1.x), x[ch * 4 + 3] = __float_as_uint(f1.y);
+                        top[0] = fmaxf(fmaxf(top[0], f0.x), f0.y), top[1] = fmaxf(fmaxf(top[1], f1.x), f1.y);
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(k_empty + 8 * stage);                    // S is complete and the scales are read
+                    int dev = seen ? ev - ref_v : 0;
+                    if (fail) st.fail[turn] = 1;
+                    any = any_of_softmax(fail || pending || fmaxf(top[0], top[1]) + (float)max(dev, -40) > kMost);
+                    turn ^= 1;
+                    // The references: in a piece's first tile, and in the rare ones where a weight would leave the range of 16 bits
+                    // or some row has seen nothing yet.
+                    if (any) {
+                        if (st.fail[turn ^ 1]) {
+                            fail = out = true;
+                            break;
+                        }
+#pragma unroll
+                        for (int ch = 0; ch < NC; ++ch) {
+                            int best = 0;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const int top1 = __reduce_max_sync(0xffffffffu, ordered(__uint_as_float(x[ch * 4 + j])));
+                                if (lane == j) best = top1;
                             }
                             if (lane < 4) st.top[q][r0 + ch * 4 + lane] = unordered(best);
                         }
                         const int e = __reduce_max_sync(0xffffffffu, ev);
                         if (lane == 0) st.exp_top[q] = e;
                         softmax_sync();
+                        bool still = false;
                         if (tid < RP) {
-                            const float m = fmaxf(fmaxf(st.top[0][tid], st.top[1][tid]), fmaxf(st.top[2][tid], st.top[3][tid]));
-                            const float old = -st.neg[tid], now = fmaxf(old, m - kTop);
-                            st.neg[tid] = -now;
-                            st.fac[tid] = old == -INFINITY ? 0.f : ex2_approx(old - now);
+                            const float best = fmaxf(fmaxf(st.top[0][tid], st.top[1][tid]), fmaxf(st.top[2][tid], st.top[3][tid]));
+                            const bool first = st.unset[tid] && best != -INFINITY;
+                            const float up = first || best > kTop ? best - kTop : 0.f;
+                            st.neg[tid] -= up;
+                            st.step[tid] = up;
+                            st.fac[tid] = first ? 0.f : ex2_approx(-up);
+                            if (first) st.unset[tid] = 0;
+                            still = best == -INFINITY && st.unset[tid];
                         }
                         const int ref = max(max(max(st.exp_top[0], st.exp_top[1]), max(st.exp_top[2], st.exp_top[3])), ref_v);
-                        softmax_sync();
+                        pending = any_of_softmax(still);
                         if (i > 0) {
                             const float shrink = ex2_approx((float)(ref_v - ref));
 #pragma unroll
@@ -374,7 +391,12 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                         }
                         ref_v = ref;
                         dev = seen ? ev - ref_v : 0;
-                        scores();
+#pragma unroll
+                        for (int ch = 0; ch < NC; ++ch) {
+                            const float4 up = *reinterpret_cast<const float4*>(st.step + r0 + ch * 4);
+                            x[ch * 4] = __float_as_uint(__uint_as_float(x[ch * 4]) - up.x), x[ch * 4 + 1] = __float_as_uint(__uint_as_float(x[ch * 4 + 1]) - up.y);
+                            x[ch * 4 + 2] = __float_as_uint(__uint_as_float(x[ch * 4 + 2]) - up.z), x[ch * 4 + 3] = __float_as_uint(__uint_as_float(x[ch * 4 + 3]) - up.w);
+                        }
                     }
                     // weights: their sums in 32 bits; times V's power of two, and split, for the product
                     const float vs = __uint_as_float((uint32_t)(min(max(dev, -126), 127) + 127) << 23);
@@ -453,24 +475,20 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             hold(o_done, n_t - 1);
             if (!agreed(false, any)) break;
             tc_fence_after();
-            // O is [dim][term, row]: a thread has one dim (64 dims sit on 16 lanes of each quarter) and its half of the rows
+            // O is [dim][half, chunk, term, row]: a thread has one dim (64 dims sit on 16 lanes of each quarter) and its half of the rows
             const bool live = D == 128 || lane < 16;
             const int d = D == 128 ? key : q * 16 + lane;
             const float scale_v = ref_v == kNoScale ? 0.f : __uint_as_float((uint32_t)(ref_v + 127) << 23);
             int tok = r0 / G, g = r0 - tok * G;
             const int64_t orow0 = (int64_t)mt.row0 * a.Hq + mt.head * G;
-#pragma unroll 1
-            for (int ch = 0; ch < n_ch; ++ch) {
-                uint32_t y[12];
-#pragma unroll
-                for (int t = 0; t < 3; ++t) tmem_ld4(tmem_o + ch * 12 + t * 4, y + 4 * t);
-                tmem_wait<12>(y);
+            auto rows = [&](int ch, const uint32_t* y) {
+                const float4 f4 = *reinterpret_cast<const float4*>(st.fac + r0 + ch * 4);
+                const float f[4] = {f4.x, f4.y, f4.z, f4.w};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int r = r0 + ch * 4 + j;
-                    const float f = st.fac[r];
-                    // a factor of zero: nothing was seen, O may be anything
-                    const float v = f != 0.f ? ((__uint_as_float(y[j]) + __uint_as_float(y[4 + j])) + __uint_as_float(y[8 + j]) * (1.f / kLow)) * f * scale_v : 0.f;
+                    const float sum = fmaf(fmaf(__uint_as_float(y[8 + j]), 1.f / kLow, __uint_as_float(y[4 + j])), 1.f / kMid, __uint_as_float(y[j]));
+                    const float v = f[j] != 0.f ? sum * f[j] * scale_v : 0.f;           // a factor of zero: nothing was seen, O may be anything
                     if (live && r < R) {
                         if (part >= 0) {
                             a.p.part_acc[(part0 + r) * D + d] = v;
@@ -481,6 +499,20 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                     }
                     if (++g == G) g = 0, ++tok;
                 }
+            };
+#pragma unroll 1
+            for (int ch = 0; ch < n_ch; ch += 2) {
+                if (r0 + ch * 4 >= R) break;
+                uint32_t y[24];
+#pragma unroll
+                for (int t = 0; t < 3; ++t) tmem_ld4(tmem_o + ch * 12 + t * 4, y + 4 * t);
+                if (ch + 1 < n_ch) {
+#pragma unroll
+                    for (int t = 3; t < 6; ++t) tmem_ld4(tmem_o + ch * 12 + t * 4, y + 4 * t);
+                }
+                tmem_wait<24>(y);
+                rows(ch, y);
+                if (ch + 1 < n_ch) rows(ch + 1, y + 12);
             }
             tc_fence_before();
             __syncwarp();
@@ -533,9 +565,11 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
         int rp = RP;                                   // of the piece whose P V is next
         while (ok && n_p < n_s) {
             const bool last = i == n;                  // the tile whose P V is next is the last of its piece
-            if (!last) {
+            // S of the next tile first, if K is there: P V does not wait for it
+            bool gone = last;
+            if (!last && ready(k_full + 8 * (n_s % kStages), n_s / kStages)) {
                 issue_s();
-                if (!ok) break;
+                gone = true;
             }
             const uint32_t stage = n_p % kStages;
             if (!(ok = wait(v_full + 8 * stage, n_p / kStages)) || !(ok = wait(p_full, n_p))) break;
@@ -551,7 +585,9 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             }
             ++n_p;
             fresh = false;
-            if (last && !end) {
+            if (!gone) {
+                issue_s();
+            } else if (last && !end) {
                 begin();
                 if (!ok || end) break;
                 issue_s();
@@ -580,7 +616,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             if (n == 0) continue;
             const int32_t* table = a.kv_indices + w.u.tbl;
             const int b_lo = w.u.key_lo / kBs, b_hi = (w.u.key_hi + kBs - 1) / kBs;     // blocks that hold a visible key
-            const int t0 = (w.u.key_hi + kTileKeys - 1) / kTileKeys - 1 - w.k0;         // first key tile
+            const int t0 = w.u.key_lo / kTileKeys + w.k0;                               // first key tile
             // the block of a tile whose copy this lane sends: its id is read one tile ahead
             auto block_id = [&](int t) -> int32_t {
                 const int b = t * kBlocks + lane;
@@ -591,7 +627,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             for (int i = 0; i < n; ++i) {
                 const uint32_t stage = n_t % kStages, use = n_t / kStages;
                 const int32_t id = id_next;
-                if (i + 1 < n) id_next = block_id(t0 - i - 1);
+                if (i + 1 < n) id_next = block_id(t0 + i + 1);
                 const bool good = (uint32_t)id < (uint32_t)a.num_blocks;
                 if (!good && id != -2) report(a.status, STATUS_BAD_BLOCK, w.u.req);
                 if (use > 0 && !(ok = wait(empty + 8 * stage, use - 1))) break;
@@ -726,7 +762,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                 mt.n = piece ? w.k1 - w.k0 : -1, mt.rows = R;
                 const int d0 = (-k - 7) >> 1, d1 = -k - 7 - d0;                         // sc 2^(-k - 7)
                 mt.c = a.sc * __uint_as_float((uint32_t)(d0 + 127) << 23) * __uint_as_float((uint32_t)(d1 + 127) << 23);
-                if (piece) mt.row0 = w.u.row0, mt.head = w.head, mt.slot = w.slot, mt.key_top = ((w.u.key_hi + kTileKeys - 1) / kTileKeys - 1 - w.k0) * kTileKeys;
+                if (piece) mt.row0 = w.u.row0, mt.head = w.head, mt.slot = w.slot, mt.key_first = (w.u.key_lo / kTileKeys + w.k0) * kTileKeys;
             }
             fence_async_smem();
             __syncwarp();

@@ -239,11 +239,15 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
         };
         uint32_t n_t = 0;                              // tiles so far
         bool any, out = false;
-        for (uint32_t n_q = 0;; ++n_q) {
-            const Meta& mt = meta[n_q & 1];
-            hold(q_full + 8 * (n_q & 1), n_q >> 1);
+        // A piece begins behind the barrier that ends the one before: its Q has been waited for there, and the references are anew.
+        auto anew = [&](uint32_t n_q) {
             if (tid < kMaxRows) st.neg[tid] = 0.f, st.unset[tid] = 1;
-            if (!agreed(false, any)) break;
+            hold(q_full + 8 * (n_q & 1), n_q >> 1);
+            return agreed(false, any);
+        };
+        if (!anew(0)) out = true;
+        for (uint32_t n_q = 0; !out; ++n_q) {
+            const Meta& mt = meta[n_q & 1];
             const int n = mt.n, R = mt.rows, RP = columns(R), HP = RP / 2, r0 = half * HP;
             if (n < 0) break;
             const int G = a.G, part = mt.slot;
@@ -256,6 +260,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                     }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_empty + 8 * (n_q & 1));
+                if (!anew(n_q + 1)) break;
                 continue;
             }
             const int NH = half_columns(HP);
@@ -280,7 +285,9 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
 #pragma unroll 1
                         for (int r = 0; r < R; r += G) seen = seen || (at >= mt.lo[r] && at < mt.hi[r]);
                     }
-                    hold(k_full + 8 * stage, use);     // the scales
+                    hold(s_full + 8 * (n_t & 1), n_t >> 1);
+                    tc_fence_after();
+                    // the scales came with K, which the issuer of S waited for
                     const unsigned char* const sb = smem + L::kOffScales + stage * (kBlocks * 32) + (key >> 4) * 32 + (key & 15);
                     const uint32_t kb = sb[0], vb = sb[16];
                     // The key's power of two, times 2^7 against the rows' 2^-7, and theirs: not 0, so that a hidden score stays -inf.
@@ -288,8 +295,6 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                     const float kk = none ? (masked ? 1.f : __uint_as_float(0x7fc00000u)) : fmaxf(__uint_as_float((kb + 7) << 23) * mt.c, 1.17549435e-38f);
                     const uint64_t kk2 = pair(kk, kk);
                     const int ev = seen ? (int)vb - 127 : kNoScale;
-                    hold(s_full + 8 * (n_t & 1), n_t >> 1);
-                    tc_fence_after();
                     const uint32_t tmem_s = tmem + (n_t & 1) * 64 + lanes + r0;
                     // Scores are hidden where they lie, in a loop of its own: rare, and out of the way of the others.
                     if (masked) {
@@ -398,6 +403,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                             x[ch * 4 + 2] = __float_as_uint(__uint_as_float(x[ch * 4 + 2]) - up.z), x[ch * 4 + 3] = __float_as_uint(__uint_as_float(x[ch * 4 + 3]) - up.w);
                         }
                     }
+                    const bool p_free = i == 0 || bar_try(o_done, (n_t - 1) & 1);       // looked at here, needed below
                     // weights: their sums in 32 bits; times V's power of two, and split, for the product
                     const float vs = __uint_as_float((uint32_t)(min(max(dev, -126), 127) + 127) << 23);
                     const uint64_t vs2 = pair(vs, vs);
@@ -415,7 +421,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                         }
                         split4<true>(h[0], h[1], word + 3 * ch);
                     }
-                    if (i > 0) hold(o_done, n_t - 1);  // P V of the tile before has read P
+                    if (!__all_sync(0xffffffffu, p_free)) hold(o_done, n_t - 1);        // P V of the tile before has read P
 #pragma unroll
                     for (int k = 0; k < kUnits; ++k)
                         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(p_at + k * (kTileKeys * 16)), "r"(word[4 * k]), "r"(word[4 * k + 1]), "r"(word[4 * k + 2]), "r"(word[4 * k + 3]) : "memory");
@@ -460,21 +466,19 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             else if (n_ch == 3) tiles(std::integral_constant<int, 3>());
             else if (n_ch == 4) tiles(std::integral_constant<int, 4>());
             else tiles(std::integral_constant<int, 5>());
+            if (out) break;
             // ---- the piece's rows
-            if (out || !agreed(false, any)) break;
-            const int64_t part0 = (int64_t)part * kMaxRows;
-            if (tid < RP) {
-                const float l = (st.top[0][tid] + st.top[1][tid]) + (st.top[2][tid] + st.top[3][tid]), m = -st.neg[tid];
-                st.fac[tid] = part >= 0 ? (l != 0.f ? 1.f : 0.f) : (l == 0.f ? 0.f : 1.f / l);
-                if (tid < R) {
-                    // A row whose sum is no number joins with a reference of infinity: all factors are then 0 or not a number.
-                    if (part >= 0) *reinterpret_cast<float2*>(a.p.part_ml + (part0 + tid) * 2) = make_float2(l != l ? INFINITY : (l == 0.f ? -INFINITY : m), l);
-                    else if (a.lse) a.lse[(int64_t)(mt.row0 + tid / G) * a.Hq + mt.head * G + tid % G] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
-                }
-            }
+            const float m_run = tid < RP ? -st.neg[tid] : 0.f;
             hold(o_done, n_t - 1);
-            if (!agreed(false, any)) break;
+            if (!anew(n_q + 1)) break;
             tc_fence_after();
+            const int64_t part0 = (int64_t)part * kMaxRows;
+            if (tid < R) {
+                const float l = (st.top[0][tid] + st.top[1][tid]) + (st.top[2][tid] + st.top[3][tid]);
+                // A row whose sum is no number joins with a reference of infinity: all factors are then 0 or not a number.
+                if (part >= 0) *reinterpret_cast<float2*>(a.p.part_ml + (part0 + tid) * 2) = make_float2(l != l ? INFINITY : (l == 0.f ? -INFINITY : m_run), l);
+                else if (a.lse) a.lse[(int64_t)(mt.row0 + tid / G) * a.Hq + mt.head * G + tid % G] = l == 0.f ? -INFINITY : (m_run + log2f(l)) * kLn2;
+            }
             // O is [dim][half, chunk, term, row]: a thread has one dim (64 dims sit on 16 lanes of each quarter) and its half of the rows
             const bool live = D == 128 || lane < 16;
             const int d = D == 128 ? key : q * 16 + lane;
@@ -482,13 +486,17 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             int tok = r0 / G, g = r0 - tok * G;
             const int64_t orow0 = (int64_t)mt.row0 * a.Hq + mt.head * G;
             auto rows = [&](int ch, const uint32_t* y) {
-                const float4 f4 = *reinterpret_cast<const float4*>(st.fac + r0 + ch * 4);
-                const float f[4] = {f4.x, f4.y, f4.z, f4.w};
+                const float4 l4 = *reinterpret_cast<const float4*>(st.top[0] + r0 + ch * 4);
+                const float4 la = *reinterpret_cast<const float4*>(st.top[1] + r0 + ch * 4), lb = *reinterpret_cast<const float4*>(st.top[2] + r0 + ch * 4),
+                             lc = *reinterpret_cast<const float4*>(st.top[3] + r0 + ch * 4);
+                const float l[4] = {(l4.x + la.x) + (lb.x + lc.x), (l4.y + la.y) + (lb.y + lc.y), (l4.z + la.z) + (lb.z + lc.z), (l4.w + la.w) + (lb.w + lc.w)};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int r = r0 + ch * 4 + j;
+                    float f = 1.f;                     // a sum of zero: nothing was seen, O may be anything
+                    if (part < 0) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f) : "f"(l[j]));
                     const float sum = fmaf(fmaf(__uint_as_float(y[8 + j]), 1.f / kLow, __uint_as_float(y[4 + j])), 1.f / kMid, __uint_as_float(y[j]));
-                    const float v = f[j] != 0.f ? sum * f[j] * scale_v : 0.f;           // a factor of zero: nothing was seen, O may be anything
+                    const float v = l[j] != 0.f ? sum * f * scale_v : 0.f;
                     if (live && r < R) {
                         if (part >= 0) {
                             a.p.part_acc[(part0 + r) * D + d] = v;

@@ -694,6 +694,36 @@ nsd_status nsd_kv8_attn(nsd_ctx* ctx, void* plan, size_t plan_bytes, const void*
                         int64_t q_stride, void* o, float* lse, int64_t max_rows, const int32_t* kv_indices,
                         int32_t layer, float scale, void* stream);
 
+/*
+ * ---- Groups that share a prefix -----------------------------------------------------------
+ * Requests that begin alike (a system prompt, a document, samples of one prompt) hold the same
+ * blocks for their common tokens.  These calls are nsd_chunk_plan and nsd_chunk_attn, causal, for a batch in
+ * which consecutive requests form groups: the keys that a group shares are read once for all its
+ * rows, and every row's result over them is joined with the one over its request's own keys.
+ * The outcome is nsd_chunk_attn's on the same tables, up to rounding.
+ *   n_groups       1 .. batch (0 for an empty batch); group k is the requests
+ *                  [group_indptr[k], group_indptr[k+1]), at least one
+ *   group_indptr   int64 [n_groups+1]: 0 first, batch last, increasing
+ *   prefix_len     int32 [n_groups]: the first prefix_len[k] positions hold the same tokens for every
+ *                  request of the group, and for those with rows lie within ctx_len.  They are read through
+ *                  the table of the group's first request with rows, so the others' entries for blocks
+ *                  that hold nothing else may be the same ids or copies; a prefix may end inside a block, of which
+ *                  every request has its own copy
+ * A group of one request shares nothing.  Groups or lengths that are not so are reported as
+ * DEVICE_FAULT (with a request's index where there is one) and the plan is empty.  The plan buffer
+ * (nsd_prefix_plan_bytes) also holds what each side found for every row in 32 bits: 8 (head_dim + 2)
+ * num_q_heads bytes per row.
+ * Everything else -- rows, tables, capture, scale, softcap, alibi_slopes, errors -- as nsd_chunk_plan
+ * and nsd_chunk_attn.  Plans of the three kinds are not interchangeable.
+ */
+size_t nsd_prefix_plan_bytes(const nsd_ctx* ctx, int64_t max_rows);
+nsd_status nsd_prefix_plan(nsd_ctx* ctx, void* plan, size_t plan_bytes, int32_t batch, int64_t max_rows, int32_t n_groups,
+                           const int64_t* group_indptr, const int32_t* prefix_len, const int64_t* q_indptr,
+                           const int32_t* ctx_len, const int64_t* kv_indptr, void* stream);
+nsd_status nsd_prefix_attn(nsd_ctx* ctx, void* plan, size_t plan_bytes, const void* kv_pool, const void* q,
+                           int64_t q_stride, void* o, float* lse, int64_t max_rows, const int32_t* kv_indices,
+                           int32_t layer, float scale, float softcap, const float* alibi_slopes, void* stream);
+
 /* Number of kernels this library has launched through `ctx` since creation. */
 int64_t nsd_launch_count(const nsd_ctx* ctx);
 

@@ -130,6 +130,12 @@ def load_library():
     lib.nsd_chunk_plan.argtypes = [_vp, _vp, sz, i32, i64, _vp, _vp, _vp, ctypes.POINTER(ChunkMasks), _vp]
     lib.nsd_chunk_attn.restype = i32
     lib.nsd_chunk_attn.argtypes = [_vp, _vp, sz, _vp, _vp, i64, _vp, _vp, i64, _vp, i32, ctypes.c_float, ctypes.c_float, _vp, _vp]
+    lib.nsd_prefix_plan_bytes.restype = sz
+    lib.nsd_prefix_plan_bytes.argtypes = [_vp, i64]
+    lib.nsd_prefix_plan.restype = i32
+    lib.nsd_prefix_plan.argtypes = [_vp, _vp, sz, i32, i64, i32, _vp, _vp, _vp, _vp, _vp, _vp]
+    lib.nsd_prefix_attn.restype = i32
+    lib.nsd_prefix_attn.argtypes = lib.nsd_chunk_attn.argtypes
     for name in ("nsd_kv8_pool_bytes", "nsd_kv8_scale_bytes"):
         getattr(lib, name).restype = sz
         getattr(lib, name).argtypes = [cfgp]
@@ -435,17 +441,37 @@ class VerifyContext:
     def nsd_chunk_attn(self, plan, max_rows, kv_pool, q, o, lse, kv_indices, layer=0, scale=0.0, softcap=0.0, alibi_slopes=None,
                        stream=None):
         """q: [rows][q heads * head_dim] or [rows][q heads][head_dim], rows any multiple of 8 elements apart; o contiguous."""
+        self._attn(self.lib.nsd_chunk_attn, "nsd_chunk_attn", plan, max_rows, kv_pool, q, o, lse, kv_indices, layer, scale, softcap, alibi_slopes, stream)
+
+    def _attn(self, call, where, plan, max_rows, kv_pool, q, o, lse, kv_indices, layer, scale, softcap, alibi_slopes, stream):
         heads, f32 = self.cfg.num_q_heads, self._f32
         width = heads * self.cfg.head_dim
         if q.dtype is not self._bf16 or q.shape[0] < max_rows:
             raise TypeError("q: bfloat16 with max_rows rows is wanted")
         qp, qs = _rows(q, width, "q")
-        rc = self.lib.nsd_chunk_attn(
+        rc = call(
             self._h, plan.data_ptr(), plan.numel() * plan.element_size(), _ptr(kv_pool), qp, qs, _tensor(o, self._bf16, "o", max_rows * width),
             _tensor(lse, f32, "lse", max_rows * heads), max_rows, _tensor(kv_indices, self._i32, "kv_indices"), layer, scale, softcap,
             _tensor(alibi_slopes, f32, "alibi_slopes", heads), self._stream(stream, plan, None if type(kv_pool) is int else kv_pool, q, o, lse, kv_indices, alibi_slopes))
         if rc:
-            self._check(rc, "nsd_chunk_attn")
+            self._check(rc, where)
+
+    # -- groups that share a prefix
+    def nsd_prefix_plan_bytes(self, max_rows: int) -> int:
+        return int(self.lib.nsd_prefix_plan_bytes(self._h, max_rows))
+
+    def nsd_prefix_plan(self, plan, max_rows, group_indptr, prefix_len, q_indptr, ctx_len, kv_indptr, stream=None):
+        batch, groups, i32, i64 = ctx_len.numel(), prefix_len.numel(), self._i32, self._i64
+        rc = self.lib.nsd_prefix_plan(
+            self._h, plan.data_ptr(), plan.numel() * plan.element_size(), batch, max_rows, groups, _tensor(group_indptr, i64, "group_indptr", groups + 1),
+            _tensor(prefix_len, i32, "prefix_len"), _tensor(q_indptr, i64, "q_indptr", batch + 1), _tensor(ctx_len, i32, "ctx_len"),
+            _tensor(kv_indptr, i64, "kv_indptr", batch + 1), self._stream(stream, plan, group_indptr, prefix_len, q_indptr, ctx_len, kv_indptr))
+        if rc:
+            self._check(rc, "nsd_prefix_plan")
+
+    def nsd_prefix_attn(self, plan, max_rows, kv_pool, q, o, lse, kv_indices, layer=0, scale=0.0, softcap=0.0, alibi_slopes=None, stream=None):
+        """As nsd_chunk_attn, under a plan of nsd_prefix_plan."""
+        self._attn(self.lib.nsd_prefix_attn, "nsd_prefix_attn", plan, max_rows, kv_pool, q, o, lse, kv_indices, layer, scale, softcap, alibi_slopes, stream)
 
     # -- the 8-bit cache
     def kv8_bytes(self):

@@ -41,27 +41,69 @@ struct PlanArgs {
     int32_t batch, T, Hkv, bs;
     const int64_t *q_indptr, *kv_indptr;
     const int32_t* ctx_len;
+    ChunkGroups groups;
     int32_t* status;
 };
+// The group of request r: the last one that begins at or before it.
+__device__ __forceinline__ int group_of(const ChunkGroups& g, int r) {
+    int lo = 0, hi = g.n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (g.indptr[mid] <= r) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+// Keys that a group's rows have in common and that are read for all of them at once: none for a request by itself.
+__device__ __forceinline__ int shared_keys(const ChunkGroups& g, int k) { return g.indptr[k + 1] - g.indptr[k] > 1 ? g.prefix_len[k] : 0; }
 __device__ __forceinline__ bool request_ok(const PlanArgs& a, int r) {
     const int64_t s = a.q_indptr[r], e = a.q_indptr[r + 1], c = a.ctx_len[r];
-    return s >= 0 && s <= e && e <= a.p.max_rows && c >= 0 && c + (e - s) <= 0x7fffffffll - kTileKeys && a.kv_indptr[r] >= 0 &&
-           a.kv_indptr[r] <= a.kv_indptr[r + 1];
+    if (!(s >= 0 && s <= e && e <= a.p.max_rows && c >= 0 && c + (e - s) <= 0x7fffffffll - kTileKeys && a.kv_indptr[r] >= 0 && a.kv_indptr[r] <= a.kv_indptr[r + 1]))
+        return false;
+    if (a.groups.n == 0) return true;
+    // groups cover the batch in order, and what a request's group shares the request has
+    const int k = group_of(a.groups, r);
+    return a.groups.indptr[k] >= 0 && a.groups.indptr[k] <= r && a.groups.indptr[k + 1] > r && a.groups.indptr[k + 1] <= a.batch && a.groups.prefix_len[k] >= 0 &&
+           (e == s || a.groups.prefix_len[k] <= c);
 }
 
 __global__ void __launch_bounds__(128)
 chunk_units_kernel(const PlanArgs a) {
     pdl_release_dependents();
-    const int r = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    // behind the requests come the groups, each as a request whose rows are those of its members and whose keys are the shared ones
+    const bool shared = (int)blockIdx.x >= a.batch;
+    int r = blockIdx.x, group = 0;
+    if (shared) {
+        group = r - a.batch;
+        const int64_t first = a.groups.indptr[group], end = a.groups.indptr[group + 1];
+        if (first < 0 || first >= end || end > a.batch) return;                         // none, or reported with a request
+        r = (int)first;
+    }
     if (!request_ok(a, r)) {
+        if (shared) return;
         if (blockIdx.y == 0 && threadIdx.x == 0) report(a.status, STATUS_BAD_TOKEN, r);
         return;
     }
     const int TU = a.p.kind.tiles * a.T;
-    const int64_t s = a.q_indptr[r], e = a.q_indptr[r + 1];
+    const int64_t s = a.q_indptr[r], e = shared ? a.q_indptr[a.groups.indptr[group + 1]] : a.q_indptr[r + 1];
+    if (shared && (e < s || e > a.p.max_rows)) return;
+    const int common = a.groups.n ? shared_keys(a.groups, shared ? group : group_of(a.groups, r)) : 0;
     const int n = (int)(e - s), ctx = a.ctx_len[r], total = ctx + n;
-    const int n_units = (n + TU - 1) / TU;
-    const int64_t at = r + s / TU, owned = 1 + e / TU - s / TU;
+    const int n_units = shared && common == 0 ? 0 : (n + TU - 1) / TU;
+    const int64_t at = (shared ? a.p.max_units / 2 + group : r) + s / TU, owned = 1 + e / TU - s / TU;
+    if (shared) {
+        if (common == 0)                               // the rows have one side only
+            for (int64_t i = (int64_t)blockIdx.y * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.y * blockDim.x) a.p.row_lo[a.p.max_rows + s + i] = a.p.row_hi[a.p.max_rows + s + i] = 0;
+        // the shared blocks are read through the table of the first member that has rows
+        int lo = r, hi = (int)a.groups.indptr[group + 1];
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (a.q_indptr[mid] <= s) lo = mid; else hi = mid;
+        }
+        r = lo;
+        if (a.kv_indptr[r] < 0 || a.kv_indptr[r] > a.kv_indptr[r + 1]) return;          // reported with the request
+    }
+    const int64_t row_at = shared ? a.p.max_rows : 0;
     int prefix = 0;
     if (a.masks.prefix_len) prefix = min(max(a.masks.prefix_len[r], 0), total);
     const int64_t nblk = a.kv_indptr[r + 1] - a.kv_indptr[r];
@@ -74,14 +116,15 @@ chunk_units_kernel(const PlanArgs a) {
             bool gaps = false;
             for (int b = i0; b < i0 + u.ntok; b += 32) {
                 const int i = b + lane, pos = ctx + i;
-                const int stop = max(pos + 1, prefix);
-                int first = a.masks.window > 0 ? max(pos + 1 - a.masks.window, 0) : 0;
+                const int stop = shared ? common : max(pos + 1, prefix);
+                int first = a.masks.window > 0 ? max(pos + 1 - a.masks.window, 0) : (shared ? 0 : common);
                 bool any = false;
                 if (i < i0 + u.ntok) {
                     if (a.masks.row_first) first = max(first, a.masks.row_first[s + i]);
                     any = first < stop;
-                    a.p.row_lo[s + i] = any ? first : 0;
-                    a.p.row_hi[s + i] = any ? stop : 0;
+                    a.p.row_lo[row_at + s + i] = any ? first : 0;
+                    a.p.row_hi[row_at + s + i] = any ? stop : 0;
+                    if (a.p.row_pos && !shared) a.p.row_pos[s + i] = pos;
                     if (any) lo = min(lo, first), hi = max(hi, stop);
                 }
                 // Stops grow from row to row, so the keys of rows that follow one another without an empty one between leave no
@@ -105,6 +148,7 @@ chunk_units_kernel(const PlanArgs a) {
             u.pos0 = ctx + i0;
             u.key_lo = hi > 0 ? lo : 0;
             u.key_hi = hi;
+            u.side = shared, u.joint = common > 0;
             u.n_tiles = hi > 0 ? (hi + kTileKeys - 1) / kTileKeys - lo / kTileKeys : 0;
             u.first = (int)j;                          // made absolute by the second kernel
             u.last = n_units - 1;
@@ -127,15 +171,23 @@ chunk_split_kernel(const PlanArgs a) {
         report(a.status, STATUS_BAD_TOKEN, 0);
         ok = false;
     }
+    for (int k = tid; k < a.groups.n; k += kSplitThreads)
+        if (a.groups.indptr[k] >= a.groups.indptr[k + 1] || (k == 0 && a.groups.indptr[0] != 0) || (k == a.groups.n - 1 && a.groups.indptr[k + 1] != a.batch)) {
+            report(a.status, STATUS_BAD_TOKEN, -1);
+            ok = false;
+        }
     ok = __syncthreads_and(ok);
     pdl_wait();                                        // the units of the kernel before are complete
-    const int64_t n_raw = ok && a.batch > 0 ? a.batch + a.q_indptr[a.batch] / (a.p.kind.tiles * a.T) : 0;
+    const int64_t n_rows = ok && a.batch > 0 ? a.q_indptr[a.batch] : 0, full = n_rows / (a.p.kind.tiles * a.T);
+    // raw units: those of the requests and, from the middle of the buffer on, those of the groups
+    const int64_t n_own = ok && a.batch > 0 ? a.batch + full : 0, n_raw = n_own > 0 && a.groups.n > 0 ? n_own + a.groups.n + full : n_own;
+    auto raw = [&](int64_t i) -> const ChunkUnit& { return a.p.raw[i < n_own ? i : a.p.max_units / 2 + (i - n_own)]; };
     const int64_t per = (n_raw + kSplitThreads - 1) / kSplitThreads;
     const int64_t i0 = min(tid * per, n_raw), i1 = min(i0 + per, n_raw);
     int n_mine = 0;
     int64_t c_mine = 0;
     for (int64_t i = i0; i < i1; ++i)
-        if (a.p.raw[i].ntok > 0) ++n_mine, c_mine += unit_cost(a.p.raw[i], a.T);
+        if (raw(i).ntok > 0) ++n_mine, c_mine += unit_cost(raw(i), a.T);
     int n_inc = n_mine;
     int64_t c_inc = c_mine;
 #pragma unroll
@@ -154,7 +206,7 @@ chunk_split_kernel(const PlanArgs a) {
     }
     int64_t* const cost = n_units < kCostSmem ? cost_s : a.p.cost;
     for (int64_t i = i0; i < i1; ++i) {
-        ChunkUnit u = a.p.raw[i];
+        ChunkUnit u = raw(i);
         if (u.ntok <= 0) continue;
         u.last = n_at - u.first + u.last;
         u.first = n_at - u.first;
@@ -165,7 +217,7 @@ chunk_split_kernel(const PlanArgs a) {
     }
     if (tid == 0) {
         cost[n_units] = c_all;
-        *a.p.header = ChunkHeader{a.p.kind.magic, n_units, a.p.max_rows, a.p.max_units, a.p.n_ctas, a.masks.window == 0 && !a.masks.prefix_len && !a.masks.row_first, a.T, a.Hkv};
+        *a.p.header = ChunkHeader{a.p.kind.magic, n_units, a.p.max_rows, a.p.max_units, a.p.n_ctas, a.masks.window == 0 && !a.masks.prefix_len && !a.masks.row_first && a.groups.n == 0, a.T, a.Hkv, n_rows};
     }
     __syncthreads();
     // the line: request by request, kv head by kv head, unit by unit, tile by tile
@@ -242,7 +294,7 @@ constexpr int kThreadsA = 384;
 constexpr int kWarpIssue = 8, kWarpK = 10, kWarpV = 11;
 constexpr float kMaxSlack = 8.0f;                      // the running maximum may lag the true one by this much (log2 units)
 constexpr uint32_t kPollLimit = 1u << 30;              // polls of one wait, if nsd_config.wait_budget does not say
-enum : int { MODE_CAP = 1, MODE_BIAS = 2 };
+enum : int { MODE_CAP = 1, MODE_BIAS = 2, MODE_GROUPS = 4 };  // MODE_GROUPS: under a plan of two sides
 
 struct AttnArgs {
     CUtensorMap kv_map, q_map;
@@ -454,10 +506,16 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             int lo = 0, hi = 0x7fffffff;                                                // lanes without a row never mask
             float slope = 0.f;
             if constexpr (MODE & MODE_BIAS) slope = live ? a.slopes[h] * kLog2e : 0.f;
-            const int pos = w.u.pos0 + t_row;
+            int pos = w.u.pos0 + t_row;
             if (live) {
-                if (ph & CAUSAL) hi = pos + 1;
-                else lo = a.p.row_lo[row], hi = a.p.row_hi[row];
+                if constexpr (MODE & MODE_GROUPS) {
+                    const int64_t at = row + (w.u.side ? a.p.max_rows : 0);
+                    lo = a.p.row_lo[at], hi = a.p.row_hi[at];
+                    if constexpr (MODE & MODE_BIAS) pos = a.p.row_pos[row];
+                } else {
+                    if (ph & CAUSAL) hi = pos + 1;
+                    else lo = a.p.row_lo[row], hi = a.p.row_hi[row];
+                }
             }
             float m_run = -INFINITY, l_run = 0.f;
             bool huge = false;                                                          // a row of the warp has had a maximum beyond 2^24
@@ -472,7 +530,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                 if (warp_live) {
                     const int key0 = (t_hi - 1 - (w.k0 + i)) * kTileKeys;
                     const int v0 = lo - key0, v1 = hi - key0;                           // visible: v0 <= j < v1
-                    constexpr bool kRaw = MODE == 0;                                    // x is q . k: the scale is part of the exponent's FFMA
+                    constexpr bool kRaw = (MODE & (MODE_CAP | MODE_BIAS)) == 0;                                   // x is q . k: the scale is part of the exponent's FFMA
                     float f = kRaw ? a.sc : 1.f;
                     uint32_t x[4][32];                                                  // scores, then pairs of weights
                     uint64_t l2[2] = {0, 0};                                            // the tile's sums
@@ -620,8 +678,16 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             tc_fence_after();
             if (warp_live) {
                 const int64_t orow = row * a.Hq + h;
-                const bool part = w.slot >= 0;
+                bool part = w.slot >= 0;
                 const int64_t prow = (int64_t)w.slot * 2 * kRows + (dual ? s * kRows : 0) + m;
+                float *part_acc = a.p.part_acc + prow * D, *part_ml = a.p.part_ml + prow * 2;
+                if constexpr (MODE & MODE_GROUPS) {
+                    if (!part && w.u.joint) {          // whole, but one of the row's two sides
+                        const int64_t at = (w.u.side ? a.p.max_rows * a.Hq : 0) + orow;
+                        part_acc = a.p.row_acc + at * D, part_ml = a.p.row_ml + at * 2;
+                        part = true;
+                    }
+                }
                 const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
                 if (!part) r0 *= inv, r1 *= inv;
 #pragma unroll 1
@@ -641,7 +707,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                             y[j] = __float_as_uint(v);
                         }
                         if (part) {
-                            float4* pa = reinterpret_cast<float4*>(a.p.part_acc + prow * D + c);
+                            float4* pa = reinterpret_cast<float4*>(part_acc + c);
 #pragma unroll
                             for (int j = 0; j < 4; ++j)
                                 pa[j] = make_float4(__uint_as_float(y[4 * j]), __uint_as_float(y[4 * j + 1]), __uint_as_float(y[4 * j + 2]), __uint_as_float(y[4 * j + 3]));
@@ -658,7 +724,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
                     }
                     __syncwarp();
                 }
-                if (live && part) *reinterpret_cast<float2*>(a.p.part_ml + prow * 2) = make_float2(m_run, l_run);
+                if (live && part) *reinterpret_cast<float2*>(part_ml) = make_float2(m_run, l_run);
                 if (live && !part && a.lse) a.lse[orow] = m_run == -INFINITY ? -INFINITY : (m_run + log2f(l_run)) * kLn2;
             }
             tc_fence_before();
@@ -952,11 +1018,38 @@ chunk_join_kernel(const __grid_constant__ ChunkPlan p, uint16_t* __restrict__ o,
                 m = top;
             }
         }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
         const int64_t orow = (int64_t)(u.row0 + t) * Hq + cut.head * G + g;
+        if (u.joint) {                                 // one of the row's two sides
+            const int64_t at = (u.side ? p.max_rows * Hq : 0) + orow;
+            *reinterpret_cast<float4*>(p.row_acc + at * D + d4 * 4) = acc;
+            if (d4 == 0) *reinterpret_cast<float2*>(p.row_ml + at * 2) = make_float2(m, l);
+            continue;
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
         *reinterpret_cast<uint2*>(o + orow * D + d4 * 4) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
         if (lse && d4 == 0) lse[orow] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * kLn2;
     }
+}
+
+// The rows that have two sides: shared keys and own.  A quarter of a warp's lanes more than needed would idle at D = 64, so
+// D / 4 lanes take a (row, head), four dims each.
+constexpr int kMergeThreads = 256;
+template <int D>
+__global__ void __launch_bounds__(kMergeThreads)
+chunk_merge_kernel(const __grid_constant__ ChunkPlan p, uint16_t* __restrict__ o, float* __restrict__ lse, int32_t Hq, int32_t Hkv, int32_t T) {
+    constexpr int kLanes = D / 4;
+    const int64_t at = ((int64_t)blockIdx.x * kMergeThreads + threadIdx.x) / kLanes;
+    const int d = threadIdx.x % kLanes * 4;
+    pdl_wait();
+    if (!is_plan(p, T, Hkv) || at >= p.header->n_rows * Hq || p.row_hi[p.max_rows + at / Hq] == 0) return;
+    const int64_t other = p.max_rows * Hq + at;
+    const float2 ml0 = *reinterpret_cast<const float2*>(p.row_ml + at * 2), ml1 = *reinterpret_cast<const float2*>(p.row_ml + other * 2);
+    const float4 a = *reinterpret_cast<const float4*>(p.row_acc + at * D + d), b = *reinterpret_cast<const float4*>(p.row_acc + other * D + d);
+    const float top = fmaxf(ml0.x, ml1.x), f0 = ml0.x == -INFINITY ? 0.f : exp2f(ml0.x - top), f1 = ml1.x == -INFINITY ? 0.f : exp2f(ml1.x - top);
+    const float l = ml0.y * f0 + ml1.y * f1, inv = l == 0.f ? 0.f : 1.f / l;
+    auto sum = [&](float x, float y) { return ((f0 != 0.f ? x * f0 : 0.f) + (f1 != 0.f ? y * f1 : 0.f)) * inv; };
+    *reinterpret_cast<uint2*>(o + at * D + d) = make_uint2(pack_bf16(sum(a.x, b.x), sum(a.y, b.y)), pack_bf16(sum(a.z, b.z), sum(a.w, b.w)));
+    if (lse && d == 0) lse[at] = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
 }
 
 typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -1002,6 +1095,10 @@ cudaError_t allow_smem_all() {
     if (e == cudaSuccess) e = allow_smem<D, MODE_CAP>();
     if (e == cudaSuccess) e = allow_smem<D, MODE_BIAS>();
     if (e == cudaSuccess) e = allow_smem<D, MODE_CAP | MODE_BIAS>();
+    if (e == cudaSuccess) e = allow_smem<D, MODE_GROUPS>();
+    if (e == cudaSuccess) e = allow_smem<D, MODE_GROUPS | MODE_CAP>();
+    if (e == cudaSuccess) e = allow_smem<D, MODE_GROUPS | MODE_BIAS>();
+    if (e == cudaSuccess) e = allow_smem<D, MODE_GROUPS | MODE_CAP | MODE_BIAS>();
     return e;
 }
 template <int D>
@@ -1013,7 +1110,11 @@ cudaError_t launch_attn_d(const AttnArgs& a, int mode, int n_ctas, cudaStream_t 
         case 0: return launch_kernel(chunk_attn_kernel<D, 0>, grid, block, smem, st, true, a);
         case MODE_CAP: return launch_kernel(chunk_attn_kernel<D, MODE_CAP>, grid, block, smem, st, true, a);
         case MODE_BIAS: return launch_kernel(chunk_attn_kernel<D, MODE_BIAS>, grid, block, smem, st, true, a);
-        default: return launch_kernel(chunk_attn_kernel<D, MODE_CAP | MODE_BIAS>, grid, block, smem, st, true, a);
+        case MODE_CAP | MODE_BIAS: return launch_kernel(chunk_attn_kernel<D, MODE_CAP | MODE_BIAS>, grid, block, smem, st, true, a);
+        case MODE_GROUPS: return launch_kernel(chunk_attn_kernel<D, MODE_GROUPS>, grid, block, smem, st, true, a);
+        case MODE_GROUPS | MODE_CAP: return launch_kernel(chunk_attn_kernel<D, MODE_GROUPS | MODE_CAP>, grid, block, smem, st, true, a);
+        case MODE_GROUPS | MODE_BIAS: return launch_kernel(chunk_attn_kernel<D, MODE_GROUPS | MODE_BIAS>, grid, block, smem, st, true, a);
+        default: return launch_kernel(chunk_attn_kernel<D, MODE_GROUPS | MODE_CAP | MODE_BIAS>, grid, block, smem, st, true, a);
     }
 }
 
@@ -1022,7 +1123,7 @@ cudaError_t launch_attn_d(const AttnArgs& a, int mode, int n_ctas, cudaStream_t 
 size_t chunk_plan_layout(ChunkPlan* p, void* base, const ChunkKind& kind, const Shape& s, int32_t max_batch, int64_t max_rows, int32_t n_sms) {
     n_sms *= kind.per_sm;                              // CTAs
     n_sms = n_sms < kMaxCtas ? n_sms : kMaxCtas;
-    const int64_t max_units = max_batch + max_rows / (kind.tiles * kind.tokens(s.Hq / s.Hkv)) + 2;
+    const int64_t max_units = kind.sides * (max_batch + max_rows / (kind.tiles * kind.tokens(s.Hq / s.Hkv)) + 2);
     size_t off = 0;
     char* const b = static_cast<char*>(base);
     auto part = [&](size_t bytes) {
@@ -1036,8 +1137,13 @@ size_t chunk_plan_layout(ChunkPlan* p, void* base, const ChunkKind& kind, const 
     q.raw = static_cast<ChunkUnit*>(part(max_units * sizeof(ChunkUnit)));
     q.units = static_cast<ChunkUnit*>(part(max_units * sizeof(ChunkUnit)));
     q.cost = static_cast<int64_t*>(part((max_units + 1) * sizeof(int64_t)));
-    q.row_lo = static_cast<int32_t*>(part(max_rows * sizeof(int32_t)));
-    q.row_hi = static_cast<int32_t*>(part(max_rows * sizeof(int32_t)));
+    q.row_lo = static_cast<int32_t*>(part(kind.sides * max_rows * sizeof(int32_t)));
+    q.row_hi = static_cast<int32_t*>(part(kind.sides * max_rows * sizeof(int32_t)));
+    if (kind.sides == 2) {
+        q.row_pos = static_cast<int32_t*>(part(max_rows * sizeof(int32_t)));
+        q.row_ml = static_cast<float*>(part(2 * max_rows * s.Hq * 2 * sizeof(float)));
+        q.row_acc = static_cast<float*>(part(2 * max_rows * s.Hq * s.D * sizeof(float)));
+    }
     q.part_ml = static_cast<float*>(part(2ull * n_sms * kind.tiles * kind.rows * 2 * sizeof(float)));
     q.part_acc = static_cast<float*>(part(2ull * n_sms * kind.tiles * kind.rows * s.D * sizeof(float)));
     q.max_rows = max_rows;
@@ -1056,14 +1162,14 @@ cudaError_t chunk_attn_init() {
 }
 
 cudaError_t launch_chunk_plan(const ChunkPlan& p, const Shape& s, int32_t batch, const int64_t* q_indptr, const int32_t* ctx_len,
-                              const int64_t* kv_indptr, const nsd_chunk_masks& masks, int32_t* status, cudaStream_t stream) {
+                              const int64_t* kv_indptr, const nsd_chunk_masks& masks, const ChunkGroups& groups, int32_t* status, cudaStream_t stream) {
     const int T = p.kind.tokens(s.Hq / s.Hkv);
-    const PlanArgs a{p, masks, batch, T, s.Hkv, s.bs, q_indptr, kv_indptr, ctx_len, status};
+    const PlanArgs a{p, masks, batch, T, s.Hkv, s.bs, q_indptr, kv_indptr, ctx_len, groups, status};
     if (batch > 0) {
         // a warp per unit: enough of them for the average request, at most 64 CTAs for the longest
         const int64_t units = p.max_rows / (p.kind.tiles * T) / 4 + 1;
         const unsigned slices = (unsigned)(units < 64 ? units : 64);
-        chunk_units_kernel<<<dim3((unsigned)batch, slices), 128, 0, stream>>>(a);
+        chunk_units_kernel<<<dim3((unsigned)(batch + groups.n), slices), 128, 0, stream>>>(a);
         const cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
     }
@@ -1084,13 +1190,20 @@ cudaError_t launch_chunk_attn(const ChunkPlan& p, const ChunkAttnLaunch& l, cuda
     a.status = l.status;
     a.Hq = l.shape.Hq, a.Hkv = l.shape.Hkv, a.num_blocks = l.shape.num_blocks;
     a.wait_budget = l.wait_budget;
-    const int mode = (l.softcap > 0.f ? MODE_CAP : 0) | (l.slopes ? MODE_BIAS : 0);
+    const int mode = (l.softcap > 0.f ? MODE_CAP : 0) | (l.slopes ? MODE_BIAS : 0) | (p.kind.sides == 2 ? MODE_GROUPS : 0);
     cudaError_t e = l.shape.D == 128 ? launch_attn_d<128>(a, mode, p.n_ctas, stream) : launch_attn_d<64>(a, mode, p.n_ctas, stream);
     if (e != cudaSuccess) return e;
     *launched = 1;
-    if (p.n_ctas < 2) return e;
-    e = launch_chunk_join(p, l.shape, l.o, l.lse, stream);
-    if (e == cudaSuccess) *launched = 2;
+    if (p.n_ctas >= 2) {
+        e = launch_chunk_join(p, l.shape, l.o, l.lse, stream);
+        if (e != cudaSuccess) return e;
+        ++*launched;
+    }
+    if (p.kind.sides != 2) return e;
+    const dim3 grid((unsigned)((p.max_rows * a.Hq * (l.shape.D / 4) + kMergeThreads - 1) / kMergeThreads));
+    e = l.shape.D == 128 ? launch_kernel(chunk_merge_kernel<128>, grid, dim3(kMergeThreads), 0, stream, true, p, l.o, l.lse, a.Hq, a.Hkv, a.T)
+                         : launch_kernel(chunk_merge_kernel<64>, grid, dim3(kMergeThreads), 0, stream, true, p, l.o, l.lse, a.Hq, a.Hkv, a.T);
+    if (e == cudaSuccess) ++*launched;
     return e;
 }
 

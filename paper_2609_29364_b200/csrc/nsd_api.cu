@@ -1071,7 +1071,7 @@ static nsd_status plan_of(const nsd_ctx* ctx, const ChunkKind& kind, ChunkPlan* 
 
 static nsd_status plan_impl(nsd_ctx* ctx, const ChunkKind& kind, void* plan, size_t plan_bytes, int32_t batch, int64_t max_rows,
                             const int64_t* q_indptr, const int32_t* ctx_len, const int64_t* kv_indptr,
-                            const nsd_chunk_masks* masks, void* stream) {
+                            const nsd_chunk_masks* masks, const ChunkGroups& groups, void* stream) {
     if (!ctx) return NSD_ERR_INVALID_ARG;
     if (batch < 0 || batch > ctx->cfg.max_batch) return NSD_ERR_OUT_OF_RANGE;
     const nsd_chunk_masks m = masks ? *masks : nsd_chunk_masks{};
@@ -1081,7 +1081,7 @@ static nsd_status plan_impl(nsd_ctx* ctx, const ChunkKind& kind, void* plan, siz
     if (const nsd_status s = plan_of(ctx, kind, &p, plan, plan_bytes, max_rows)) return s;
     const OnDevice on(ctx->device);
     NSD_CUDA(ctx, on.err);
-    NSD_CUDA(ctx, launch_chunk_plan(p, ctx->shape, batch, q_indptr, ctx_len, kv_indptr, m, ctx->d_status, static_cast<cudaStream_t>(stream)));
+    NSD_CUDA(ctx, launch_chunk_plan(p, ctx->shape, batch, q_indptr, ctx_len, kv_indptr, m, groups, ctx->d_status, static_cast<cudaStream_t>(stream)));
     ctx->launches += batch > 0 ? 2 : 1;
     return NSD_OK;
 }
@@ -1091,18 +1091,18 @@ size_t nsd_chunk_plan_bytes(const nsd_ctx* ctx, int64_t max_rows) { return plan_
 nsd_status nsd_chunk_plan(nsd_ctx* ctx, void* plan, size_t plan_bytes, int32_t batch, int64_t max_rows,
                           const int64_t* q_indptr, const int32_t* ctx_len, const int64_t* kv_indptr,
                           const nsd_chunk_masks* masks, void* stream) {
-    return plan_impl(ctx, kChunkKind, plan, plan_bytes, batch, max_rows, q_indptr, ctx_len, kv_indptr, masks, stream);
+    return plan_impl(ctx, kChunkKind, plan, plan_bytes, batch, max_rows, q_indptr, ctx_len, kv_indptr, masks, {}, stream);
 }
 
-nsd_status nsd_chunk_attn(nsd_ctx* ctx, void* plan, size_t plan_bytes, const void* kv_pool, const void* q,
-                          int64_t q_stride, void* o, float* lse, int64_t max_rows, const int32_t* kv_indices,
-                          int32_t layer, float scale, float softcap, const float* alibi_slopes, void* stream) {
+static nsd_status attn_impl(nsd_ctx* ctx, const ChunkKind& kind, void* plan, size_t plan_bytes, const void* kv_pool, const void* q,
+                            int64_t q_stride, void* o, float* lse, int64_t max_rows, const int32_t* kv_indices,
+                            int32_t layer, float scale, float softcap, const float* alibi_slopes, void* stream) {
     if (!ctx) return NSD_ERR_INVALID_ARG;
     if (layer < 0 || layer >= ctx->cfg.num_layers) return NSD_ERR_OUT_OF_RANGE;
     // NaN too; within these bounds scale / softcap and the cap in the log2 domain stay finite
     if (!(scale >= 0.f && scale <= 1e30f) || !(softcap == 0.f || (softcap >= 1e-6f && softcap <= 1e30f))) return NSD_ERR_INVALID_ARG;
     ChunkPlan p;
-    if (const nsd_status s = plan_of(ctx, kChunkKind, &p, plan, plan_bytes, max_rows)) return s;
+    if (const nsd_status s = plan_of(ctx, kind, &p, plan, plan_bytes, max_rows)) return s;
     if (max_rows == 0) return NSD_OK;
     if (!kv_pool || !q || !o || !kv_indices) return NSD_ERR_INVALID_ARG;
     if (q_stride < (int64_t)ctx->cfg.num_q_heads * ctx->cfg.head_dim || q_stride % 8) return NSD_ERR_INVALID_ARG;
@@ -1126,6 +1126,30 @@ nsd_status nsd_chunk_attn(nsd_ctx* ctx, void* plan, size_t plan_bytes, const voi
     NSD_CUDA(ctx, launch_chunk_attn(p, l, static_cast<cudaStream_t>(stream), &launched));
     ctx->launches += launched;
     return NSD_OK;
+}
+
+nsd_status nsd_chunk_attn(nsd_ctx* ctx, void* plan, size_t plan_bytes, const void* kv_pool, const void* q,
+                          int64_t q_stride, void* o, float* lse, int64_t max_rows, const int32_t* kv_indices,
+                          int32_t layer, float scale, float softcap, const float* alibi_slopes, void* stream) {
+    return attn_impl(ctx, kChunkKind, plan, plan_bytes, kv_pool, q, q_stride, o, lse, max_rows, kv_indices, layer, scale, softcap, alibi_slopes, stream);
+}
+
+// ---- groups that share a prefix ----------------------------------------------------------------
+size_t nsd_prefix_plan_bytes(const nsd_ctx* ctx, int64_t max_rows) { return plan_bytes_of(ctx, kPrefixKind, max_rows); }
+
+nsd_status nsd_prefix_plan(nsd_ctx* ctx, void* plan, size_t plan_bytes, int32_t batch, int64_t max_rows, int32_t n_groups,
+                           const int64_t* group_indptr, const int32_t* prefix_len, const int64_t* q_indptr,
+                           const int32_t* ctx_len, const int64_t* kv_indptr, void* stream) {
+    if (!ctx) return NSD_ERR_INVALID_ARG;
+    if (n_groups < 0 || n_groups > batch || (batch > 0 && n_groups == 0)) return NSD_ERR_OUT_OF_RANGE;
+    if (n_groups > 0 && (!group_indptr || !prefix_len)) return NSD_ERR_INVALID_ARG;
+    return plan_impl(ctx, kPrefixKind, plan, plan_bytes, batch, max_rows, q_indptr, ctx_len, kv_indptr, nullptr, {n_groups, group_indptr, prefix_len}, stream);
+}
+
+nsd_status nsd_prefix_attn(nsd_ctx* ctx, void* plan, size_t plan_bytes, const void* kv_pool, const void* q,
+                           int64_t q_stride, void* o, float* lse, int64_t max_rows, const int32_t* kv_indices,
+                           int32_t layer, float scale, float softcap, const float* alibi_slopes, void* stream) {
+    return attn_impl(ctx, kPrefixKind, plan, plan_bytes, kv_pool, q, q_stride, o, lse, max_rows, kv_indices, layer, scale, softcap, alibi_slopes, stream);
 }
 
 // ---- the 8-bit cache ---------------------------------------------------------------------------
@@ -1160,7 +1184,7 @@ size_t nsd_kv8_plan_bytes(const nsd_ctx* ctx, int64_t max_rows) { return plan_by
 nsd_status nsd_kv8_plan(nsd_ctx* ctx, void* plan, size_t plan_bytes, int32_t batch, int64_t max_rows,
                         const int64_t* q_indptr, const int32_t* ctx_len, const int64_t* kv_indptr,
                         const nsd_chunk_masks* masks, void* stream) {
-    return plan_impl(ctx, kKv8Kind, plan, plan_bytes, batch, max_rows, q_indptr, ctx_len, kv_indptr, masks, stream);
+    return plan_impl(ctx, kKv8Kind, plan, plan_bytes, batch, max_rows, q_indptr, ctx_len, kv_indptr, masks, {}, stream);
 }
 
 nsd_status nsd_kv8_attn(nsd_ctx* ctx, void* plan, size_t plan_bytes, const void* kv8, const void* scales, const void* q,

@@ -174,7 +174,8 @@ struct __align__(16) ChunkUnit {
     int32_t nblk;                            // its table entries
     int32_t row0, ntok;                      // rows of the unit (tokens)
     uint32_t req : 31, gaps : 1;             // gaps: rows that see nothing may leave keys in [key_lo, key_hi) that no row sees
-    int32_t n_tiles;                         // 128-key tiles that hold a visible key
+    uint32_t n_tiles : 30;                   // 128-key tiles that hold a visible key
+    uint32_t side : 1, joint : 1;            // of a plan for groups: side 1 = over a group's shared keys; joint: the rows have both sides
     int32_t key_lo, key_hi;                  // hull of the keys any row sees: [key_lo, key_hi)
     int32_t first, last;                     // the request's units
     int32_t pos0;                            // position of the unit's first row
@@ -190,21 +191,24 @@ struct ChunkHeader {
     int32_t n_ctas;                          // CTAs the work is split over
     int32_t causal;                          // no window, prefix or documents: row_lo / row_hi need not be read
     int32_t T, Hkv;                          // the shape it was made for
+    int64_t n_rows;                          // the batch's
 };
 // What a plan is for: tiles of up to `rows` stacked rows (T = rows / G tokens), `tiles` of them in a unit; a share of the work
 // for each of `per_sm` CTAs of an SM.
 struct ChunkKind {
     uint32_t magic;
-    int32_t rows, tiles, per_sm;
+    int32_t rows, tiles, per_sm, sides;      // sides 2: for groups that share a prefix, every row twice
     __host__ __device__ int tokens(int G) const { return rows / G; }         // of a tile
 };
-constexpr ChunkKind kChunkKind{0x4e534443u, 128, 2, 1}, kKv8Kind{0x4e534438u, 40, 1, 2};
+constexpr ChunkKind kChunkKind{0x4e534443u, 128, 2, 1, 1}, kKv8Kind{0x4e534438u, 40, 1, 2, 1}, kPrefixKind{0x4e534450u, 128, 2, 1, 2};
 struct ChunkPlan {                           // the buffer's parts
     ChunkHeader* header;
     ChunkStart* starts;                      // [n_ctas + 1]
     ChunkUnit *raw, *units;                  // [max_units]
     int64_t* cost;                           // [max_units + 1] prefix sums over the units, one kv head
-    int32_t *row_lo, *row_hi;                // [max_rows] visible keys of each row
+    int32_t *row_lo, *row_hi;                // [sides][max_rows] visible keys of each row
+    int32_t* row_pos;                        // two sides: [max_rows] positions
+    float *row_ml, *row_acc;                 // two sides: [2][max_rows][Hq][2] and [D], what a side found for a row that has both
     float* part_ml;                          // [2 n_ctas][rows of a unit][2]
     float* part_acc;                         // [2 n_ctas][rows of a unit][D]
     int64_t max_rows, max_units;
@@ -213,8 +217,13 @@ struct ChunkPlan {                           // the buffer's parts
 };
 size_t chunk_plan_layout(ChunkPlan* p, void* base, const ChunkKind& kind, const Shape& s, int32_t max_batch, int64_t max_rows, int32_t n_sms);
 cudaError_t chunk_attn_init();
+struct ChunkGroups {                         // consecutive requests that share their first prefix_len tokens; n = 0: none
+    int32_t n;
+    const int64_t* indptr;                   // [n + 1] requests
+    const int32_t* prefix_len;
+};
 cudaError_t launch_chunk_plan(const ChunkPlan& p, const Shape& s, int32_t batch, const int64_t* q_indptr, const int32_t* ctx_len,
-                              const int64_t* kv_indptr, const nsd_chunk_masks& masks, int32_t* status, cudaStream_t stream);
+                              const int64_t* kv_indptr, const nsd_chunk_masks& masks, const ChunkGroups& groups, int32_t* status, cudaStream_t stream);
 struct ChunkAttnLaunch {
     Shape shape;
     const uint16_t* slab;

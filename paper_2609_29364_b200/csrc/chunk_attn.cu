@@ -965,7 +965,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
 // the first such boundary of a unit does the work for all of them.  Pieces are read in walking order, so the result does not
 // depend on timing.  A thread = four dims of one row at a time, four pieces' loads under way together: the chain of loads
 // bounds it (one request of 8000 tokens, cut into 64 pieces, with one after another 27 us for both kernels, so 18).
-constexpr int kJoinThreads = 256, kJoinSlices = 4, kMaxCtas = 511;
+constexpr int kJoinThreads = 256, kJoinSlices = 4, kGroupSlices = 16, kMaxCtas = 511;
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads)
 chunk_join_kernel(const __grid_constant__ ChunkPlan p, uint16_t* __restrict__ o, float* __restrict__ lse, int32_t Hq, int32_t Hkv, int32_t G, int32_t T) {
@@ -989,7 +989,7 @@ chunk_join_kernel(const __grid_constant__ ChunkPlan p, uint16_t* __restrict__ o,
         const ChunkStart x = starts[k], y = starts[k + 1];
         return x.unit != y.unit || x.head != y.head || x.tile != y.tile;
     };
-    for (int e = blockIdx.y * kJoinThreads + threadIdx.x; e < elements; e += kJoinSlices * kJoinThreads) {
+    for (int e = blockIdx.y * kJoinThreads + threadIdx.x; e < elements; e += gridDim.y * kJoinThreads) {
         const int r = e / (D / 4), d4 = e % (D / 4), t = r / G, g = r - t * G;
         const int64_t in = (int64_t)(t / T) * p.kind.rows + (t % T) * G + g;                  // row of a partial slot
         float m = -INFINITY, l = 0.f;
@@ -1166,9 +1166,10 @@ cudaError_t launch_chunk_plan(const ChunkPlan& p, const Shape& s, int32_t batch,
     const int T = p.kind.tokens(s.Hq / s.Hkv);
     const PlanArgs a{p, masks, batch, T, s.Hkv, s.bs, q_indptr, kv_indptr, ctx_len, groups, status};
     if (batch > 0) {
-        // a warp per unit: enough of them for the average request, at most 64 CTAs for the longest
-        const int64_t units = p.max_rows / (p.kind.tiles * T) / 4 + 1;
-        const unsigned slices = (unsigned)(units < 64 ? units : 64);
+        // a warp per unit: enough of them for the average request, at most 64 CTAs for the longest, and no more than some 16 per
+        // SM in all (512 requests of up to 5 rows in units of 10: 2 slices 4 us, the 52 that all rows in one request would need 32 us)
+        const int64_t units = p.max_rows / (p.kind.tiles * T) / 4 + 1, fair = 2048 / batch + 1;
+        const unsigned slices = (unsigned)(units < 64 ? (units < fair ? units : fair) : (fair < 64 ? fair : 64));
         chunk_units_kernel<<<dim3((unsigned)(batch + groups.n), slices), 128, 0, stream>>>(a);
         const cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
@@ -1208,7 +1209,7 @@ cudaError_t launch_chunk_attn(const ChunkPlan& p, const ChunkAttnLaunch& l, cuda
 }
 
 cudaError_t launch_chunk_join(const ChunkPlan& p, const Shape& s, uint16_t* o, float* lse, cudaStream_t stream) {
-    const dim3 grid(p.n_ctas - 1, kJoinSlices);
+    const dim3 grid(p.n_ctas - 1, p.kind.sides == 2 ? kGroupSlices : kJoinSlices);
     const int G = s.Hq / s.Hkv, T = p.kind.tokens(G);
     return s.D == 128 ? launch_kernel(chunk_join_kernel<128>, grid, dim3(kJoinThreads), 0, stream, true, p, o, lse, s.Hq, s.Hkv, G, T)
                       : launch_kernel(chunk_join_kernel<64>, grid, dim3(kJoinThreads), 0, stream, true, p, o, lse, s.Hq, s.Hkv, G, T);

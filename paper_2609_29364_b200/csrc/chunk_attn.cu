@@ -17,16 +17,19 @@ constexpr float kLn2 = 0.6931471805599453f;
 // two of its tiles do (loading Q, filling the pipeline, writing O).  Measured with 122 single tokens over 4600 keys beside
 // 2500 tokens of prompts (D = 128, four q heads per kv head, no masks): 578 us; 749 with all tiles alike, 623 with 1.5, 607
 // with 2.5.  Other shapes, masks and caps share the rule unmeasured; the split stays exact, only its balance depends on it.
-constexpr int kUnitTiles = 2;
-
+// Where groups' shared keys are more than half of the work, the tiles of the requests' own keys take longer (their few CTAs wait
+// for memory that the others keep busy): 256 requests of 3 to 5 rows behind 32 777 keys, over up to 2000 of their own, 703 us
+// with 4, 7 and three tiles against 835; behind 4000 keys 304 against 292, 64 single tokens behind 4000 57 against 53.
+struct ChunkCost {
+    int32_t one, two, unit;                            // a tile in a unit of one and of two row tiles; a unit, in tiles
+};
 __device__ __forceinline__ void report(int32_t* status, int32_t bit, int r) {
     atomicOr(status, bit);
     atomicCAS(status + 1, 0, r + 1);
 }
 
-__device__ __forceinline__ int tile_cost(const ChunkUnit& u, int T) { return u.ntok > T ? 2 : 1; }
-__device__ __forceinline__ int64_t unit_cost(const ChunkUnit& u, int T) { return ((int64_t)u.n_tiles + kUnitTiles) * tile_cost(u, T); }
-
+__device__ __forceinline__ int tile_cost(const ChunkCost& c, const ChunkUnit& u, int T) { return u.ntok > T ? c.two : c.one; }
+__device__ __forceinline__ int64_t unit_cost(const ChunkCost& c, const ChunkUnit& u, int T) { return ((int64_t)u.n_tiles + c.unit) * tile_cost(c, u, T); }
 
 // ---- plan -------------------------------------------------------------------------------------
 // Two kernels.  The first works on every request's units side by side: the visible keys of each
@@ -186,8 +189,21 @@ chunk_split_kernel(const PlanArgs a) {
     const int64_t i0 = min(tid * per, n_raw), i1 = min(i0 + per, n_raw);
     int n_mine = 0;
     int64_t c_mine = 0;
+    ChunkCost k{1, 2, a.p.kind.unit_tiles};
+    if (a.p.kind.sides == 2) {
+        __shared__ unsigned long long sides[2];
+        if (tid < 2) sides[tid] = 0;
+        __syncthreads();
+        unsigned long long mine[2] = {0, 0};
+        for (int64_t i = i0; i < i1; ++i)
+            if (raw(i).ntok > 0) mine[raw(i).side] += unit_cost(k, raw(i), a.T);
+        for (int s = 0; s < 2; ++s)
+            if (mine[s]) atomicAdd(&sides[s], mine[s]);
+        __syncthreads();
+        if (sides[1] > sides[0]) k = ChunkCost{4, 7, 3};
+    }
     for (int64_t i = i0; i < i1; ++i)
-        if (raw(i).ntok > 0) ++n_mine, c_mine += unit_cost(raw(i), a.T);
+        if (raw(i).ntok > 0) ++n_mine, c_mine += unit_cost(k, raw(i), a.T);
     int n_inc = n_mine;
     int64_t c_inc = c_mine;
 #pragma unroll
@@ -213,7 +229,7 @@ chunk_split_kernel(const PlanArgs a) {
         a.p.units[n_at] = u;
         cost[n_at] = c_at;
         ++n_at;
-        c_at += unit_cost(u, a.T);
+        c_at += unit_cost(k, u, a.T);
     }
     if (tid == 0) {
         cost[n_units] = c_all;
@@ -240,7 +256,7 @@ chunk_split_kernel(const PlanArgs a) {
                 if (cost[mid] <= rem) lo = mid; else hi = mid;
             }
             st.unit = lo;
-            st.tile = (int)max((int64_t)0, (rem - cost[lo]) / tile_cost(a.p.units[lo], a.T) - kUnitTiles);
+            st.tile = (int)max((int64_t)0, (rem - cost[lo]) / tile_cost(k, a.p.units[lo], a.T) - k.unit);
         }
         a.p.starts[c] = st;
     }

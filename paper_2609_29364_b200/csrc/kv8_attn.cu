@@ -18,7 +18,7 @@ constexpr int kTileKeys = 128, kBs = 16, kBlocks = kTileKeys / kBs;
 constexpr int kMaxRows = kKv8Kind.rows;
 constexpr int kThreads = 384, kSoftThreads = 256;
 constexpr int kWarpIssue = 8, kWarpV = 10, kWarpQ = 11;   // 9: the producer of K
-constexpr uint32_t kPollLimit = 1u << 30;              // polls of one wait, if nsd_config.wait_budget does not say
+constexpr uint32_t kPollLimit = 1u << 24;              // polls of one wait, some tenths of a second at least, if nsd_config.wait_budget does not say
 constexpr float kTop = 4.f, kMost = 15.f;              // log2 of a row's largest weight when its reference is set, and at most
 constexpr float kMid = 8.f, kLow = 16.f;               // a weight's second term is held times kMid, its third times both
 constexpr int kNoScale = -1000;                        // exponent of V's reference before any
@@ -81,11 +81,22 @@ struct Smem8 {
 };
 constexpr int kTmemCols = 256, kTmemO = 128;           // two buffers of S, 64 columns apart, and O
 
-__device__ __forceinline__ int ordered(float x) {      // an integer that grows with x; NaN above everything
-    const int b = __float_as_int(x);
-    return x != x ? 0x7fffffff : b ^ ((b >> 31) & 0x7fffffff);
+// Four rows' values over the lanes of a warp: row j on lanes 8 j .. 8 j + 7.
+template <typename Op>
+__device__ __forceinline__ float over_lanes(float (&v)[4], int lane, Op op) {
+#pragma unroll
+    for (int k = 2; k > 0; k >>= 1) {
+        const bool up = lane & (k * 8);
+#pragma unroll
+        for (int j = 0; j < k; ++j) {
+            const float send = up ? v[j] : v[j + k], keep = up ? v[j + k] : v[j];
+            v[j] = op(keep, __shfl_xor_sync(0xffffffffu, send, k * 8));
+        }
+    }
+#pragma unroll
+    for (int k = 4; k > 0; k >>= 1) v[0] = op(v[0], __shfl_xor_sync(0xffffffffu, v[0], k));
+    return v[0];
 }
-__device__ __forceinline__ float unordered(int b) { return __int_as_float(b ^ ((b >> 31) & 0x7fffffff)); }
 
 // Pairs of 16-bit floats to the nearest ones of two mantissa bits (their upper bytes are then e5m2), and what is left, exactly.
 __device__ __forceinline__ uint32_t upper(uint32_t h) { return (h + 0x00800080u) & 0xff00ff00u; }
@@ -199,12 +210,15 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
     pdl_wait();                                        // from here on: what the kernel before writes
     const bool planned = is_plan(a.p, a.T, a.Hkv);
     if (!planned && blockIdx.x == 0 && tid == 0) report(a.status, STATUS_BAD_TOKEN, -1);
-    // the count-th completion; the same answer in every lane
+    // Waits for the count-th completion, bounded by a number of polls; the same answer in every lane.  Short, since it stands in
+    // many places: what the warps of an SM execute has to stay near the size of its instruction cache.
     auto wait = [&](uint32_t bar, uint32_t count) {
-        bool ok = bar_try(bar, count & 1);
-        if (__all_sync(0xffffffffu, ok)) return true;
-        ok = bar_wait_slow(bar, count & 1, &abort_s, limit);
-        return (bool)__all_sync(0xffffffffu, ok);
+        for (uint32_t i = 0; i < limit; ++i) {
+            if (__all_sync(0xffffffffu, bar_try(bar, count & 1))) return true;
+            if (__any_sync(0xffffffffu, abort_s)) return false;
+        }
+        abort_s = 1;
+        return false;
     };
     auto ready = [&](uint32_t bar, uint32_t count) { return (bool)__all_sync(0xffffffffu, bar_try(bar, count & 1)); };
     // Behind this barrier every warp has left its loop and the abort flag is final.
@@ -346,13 +360,9 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                         }
 #pragma unroll
                         for (int ch = 0; ch < NC; ++ch) {
-                            int best = 0;
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const int top1 = __reduce_max_sync(0xffffffffu, ordered(__uint_as_float(x[ch * 4 + j])));
-                                if (lane == j) best = top1;
-                            }
-                            if (lane < 4) st.top[q][r0 + ch * 4 + lane] = unordered(best);
+                            float v[4] = {__uint_as_float(x[ch * 4]), __uint_as_float(x[ch * 4 + 1]), __uint_as_float(x[ch * 4 + 2]), __uint_as_float(x[ch * 4 + 3])};
+                            const float best = over_lanes(v, lane, [](float a, float b) { return fmaxf(a, b); });
+                            if ((lane & 7) == 0) st.top[q][r0 + ch * 4 + (lane >> 3)] = best;
                         }
                         const int e = __reduce_max_sync(0xffffffffu, ev);
                         if (lane == 0) st.exp_top[q] = e;
@@ -430,7 +440,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                         hold(v_full + 8 * stage, use);
                         if (!seen && half == 0) {
                             const uint32_t row = smem0 + L::kOffV + stage * L::kTile + key * D;
-#pragma unroll
+#pragma unroll 1
                             for (int ch = 0; ch < D / 16; ++ch)
                                 asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(row + ((ch + lane) % (D / 16)) * 16), "r"(0) : "memory");
                         }
@@ -445,19 +455,8 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                 for (int ch = 0; ch < NC; ++ch) {
                     const float2 f0 = unpair(l2[ch * 2]), f1 = unpair(l2[ch * 2 + 1]);
                     float v[4] = {f0.x, f0.y, f1.x, f1.y};
-#pragma unroll
-                    for (int k = 2; k > 0; k >>= 1) {
-                        const bool up = lane & (k * 8);
-#pragma unroll
-                        for (int j = 0; j < k; ++j) {
-                            const float send = up ? v[j] : v[j + k], keep = up ? v[j + k] : v[j];
-                            v[j] = keep + __shfl_xor_sync(0xffffffffu, send, k * 8);
-                        }
-                    }
-                    v[0] += __shfl_xor_sync(0xffffffffu, v[0], 4);
-                    v[0] += __shfl_xor_sync(0xffffffffu, v[0], 2);
-                    v[0] += __shfl_xor_sync(0xffffffffu, v[0], 1);
-                    if ((lane & 7) == 0) st.top[q][r0 + ch * 4 + (lane >> 3)] = v[0];
+                    const float sum = over_lanes(v, lane, [](float a, float b) { return a + b; });
+                    if ((lane & 7) == 0) st.top[q][r0 + ch * 4 + (lane >> 3)] = sum;
                 }
             };
             const int n_ch = HP / 4;
@@ -509,18 +508,13 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                 }
             };
 #pragma unroll 1
-            for (int ch = 0; ch < n_ch; ch += 2) {
+            for (int ch = 0; ch < n_ch; ++ch) {
                 if (r0 + ch * 4 >= R) break;
-                uint32_t y[24];
+                uint32_t y[12];
 #pragma unroll
                 for (int t = 0; t < 3; ++t) tmem_ld4(tmem_o + ch * 12 + t * 4, y + 4 * t);
-                if (ch + 1 < n_ch) {
-#pragma unroll
-                    for (int t = 3; t < 6; ++t) tmem_ld4(tmem_o + ch * 12 + t * 4, y + 4 * t);
-                }
-                tmem_wait<24>(y);
+                tmem_wait<12>(y);
                 rows(ch, y);
-                if (ch + 1 < n_ch) rows(ch + 1, y + 12);
             }
             tc_fence_before();
             __syncwarp();
@@ -670,7 +664,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
         // [term][row] of the product's second operand.  bf16 has eight significant bits, the terms nine: nothing is lost but
         // what lies below 2^-16 then.
         constexpr int kPer = D / 32;                   // elements of a lane
-        constexpr int kRowsAhead = 4;
+        constexpr int kRowsAhead = 2;
         const bool causal = planned && a.p.header->causal;
         uint32_t n_q = 0;
         bool ok = true;

@@ -198,9 +198,10 @@ struct ChunkHeader {
 struct ChunkKind {
     uint32_t magic;
     int32_t rows, tiles, per_sm, sides;      // sides 2: for groups that share a prefix, every row twice
+    int32_t unit_tiles;                      // what a unit costs beside its tiles, in tiles
     __host__ __device__ int tokens(int G) const { return rows / G; }         // of a tile
 };
-constexpr ChunkKind kChunkKind{0x4e534443u, 128, 2, 1, 1}, kKv8Kind{0x4e534438u, 40, 1, 2, 1}, kPrefixKind{0x4e534450u, 128, 2, 1, 2};
+constexpr ChunkKind kChunkKind{0x4e534443u, 128, 2, 1, 1, 2}, kKv8Kind{0x4e534438u, 40, 1, 2, 1, 4}, kPrefixKind{0x4e534450u, 128, 2, 1, 2, 2};
 struct ChunkPlan {                           // the buffer's parts
     ChunkHeader* header;
     ChunkStart* starts;                      // [n_ctas + 1]

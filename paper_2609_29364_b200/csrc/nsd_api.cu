@@ -1004,6 +1004,7 @@ static nsd_status append_impl(nsd_ctx* ctx, bool to8, void* kv_pool, void* scale
         for (int a = 0, p = 0; a < n_axes; ++a)
             for (int i = 0; i < h_sections[a]; ++i) l.axis[p++] = (uint8_t)a;
     }
+    if (to8 && n_rows == 0) return NSD_OK;                   // tensors without elements have no address
     if ((k != nullptr) != (v != nullptr) || (!q && !k)) return NSD_ERR_INVALID_ARG;
     if (n_rows == 0) return NSD_OK;
     if (!still && (!positions || !inv_freq)) return NSD_ERR_INVALID_ARG;

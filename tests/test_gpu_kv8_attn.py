@@ -267,3 +267,116 @@ def test_append_plan_attend_together():
     from kv8_testlib import K8Run
 
     K8Run().check()
+
+
+def test_refusals_launch_nothing():
+    import paper_2609_29364_b200 as nsd
+
+    b = Batch8([100], [2], seed=30)
+    c = b.context()
+    plan = b.plan(c)
+    before = c.nsd_launch_count()
+
+    def code(call):
+        with pytest.raises(nsd.NsdError) as e:
+            call()
+        return e.value.code
+
+    args = dict(plan=plan, max_rows=2, kv8=b.kv8, scales=b.scales, q=b.q[0], o=b.o[0], lse=b.lse[0], kv_indices=b.kvi)
+    assert code(lambda: c.nsd_kv8_attn(**args, layer=1)) == 2
+    assert code(lambda: c.nsd_kv8_attn(**args, layer=-1)) == 2
+    assert code(lambda: c.nsd_kv8_attn(**args, scale=float("nan"))) == 1
+    assert code(lambda: c.nsd_kv8_attn(**args, scale=-1.0)) == 1
+    assert code(lambda: c.nsd_kv8_attn(**{**args, "plan": plan[:-256]})) == 3
+    assert code(lambda: c.nsd_kv8_attn(**{**args, "plan": plan[16:]})) == 1
+    assert code(lambda: c.nsd_kv8_attn(**{**args, "kv8": b.kv8.data_ptr() + 8})) == 1
+    wide = torch.zeros((2, 8 * 128 + 4), dtype=torch.bfloat16, device=DEV)
+    assert code(lambda: c.nsd_kv8_attn(**{**args, "q": wide[:, :1024]})) == 1
+    assert code(lambda: c.nsd_kv8_plan(plan[:256], 2, b.qp, b.ctx_len, b.kvp)) == 3
+    assert code(lambda: c.nsd_kv8_plan(plan, 2, b.qp, b.ctx_len, b.kvp, window=-1)) == 1
+    many = torch.zeros(5, dtype=torch.int64, device=DEV)
+    assert code(lambda: c.nsd_kv8_plan(plan, 2, many, torch.zeros(2, dtype=torch.int32, device=DEV), many)) == 2
+    assert c.nsd_launch_count() == before and (b.o == 7.0).all()
+
+
+def test_an_empty_batch_and_requests_without_rows():
+    b = Batch8([100, 20], [0, 0], seed=31, pad_rows=3).run()
+    assert (b.o == 7.0).all()
+
+
+def test_blocks_shared_by_requests_and_named_twice():
+    b = Batch8([64, 64, 100], [1, 2, 3], seed=32)
+    t = b.kv_indices
+    a0, a1, a2 = (int(x) for x in b.kv_indptr[:3])
+    t[a1:a1 + 4] = t[a0:a0 + 4]                                          # four full blocks in common
+    t[a2 + 2] = t[a2 + 1]                                                # and one twice in a row
+    b.kvi = gpu(t)
+    b.run()
+
+
+def test_blocks_before_the_window_may_be_gone():
+    b = Batch8([700, 300], [5, 1], seed=33)
+    for r, c in ((0, 700), (1, 300)):
+        at, gone = int(b.kv_indptr[r]), (c + 1 - 100) // 16
+        b.kv_indices[at:at + gone] = -1
+    b.kvi = gpu(b.kv_indices)
+    b.run(window=100)
+
+
+def test_offsets_beyond_32_bits():
+    """Blocks whose codes lie more than 2^32 bytes into the cache."""
+    small = Batch8([300], [2], heads=8, kv_heads=8, dim=128, seed=34)
+    blocks = 140000
+    big = torch.zeros((1, blocks, 2, 8, 16, 128), dtype=torch.uint8, device=DEV)
+    scales = torch.zeros((1, blocks, 8, 2, 16), dtype=torch.uint8, device=DEV)
+    shift = blocks - small.num_blocks
+    big[0, shift:], scales[0, shift:] = small.kv8[0], small.scales[0]
+    from kv8_testlib import T
+
+    c = T.context(8, 8, 128, blocks, max_batch=1)
+    plan = small.plan(c)
+    c.nsd_kv8_attn(plan, small.max_rows, big, scales, small.q[0], small.o[0], small.lse[0], small.kvi + shift)
+    assert c.nsd_get_status() == (0, -1)
+    small.check()
+
+
+def test_waits_that_run_out_end_the_call_and_nothing_else():
+    """With one poll per wait, calls give up wherever a copy or a product is not there at once: they end, say so or are right,
+    and the next context works on the same memory."""
+    b = Batch8([3000, 200, 17], [5, 1, 2], seed=35)
+    c = b.context(wait_budget=1)
+    gave_up = 0
+    for _ in range(5):
+        b.attn(c, b.plan(c))
+        rc, _ = c.nsd_get_status()
+        assert rc in (0, 8)
+        gave_up += rc == 8
+        if rc == 0:
+            b.check()
+    assert gave_up > 0
+    b.o.fill_(7.0), b.lse.fill_(7.0)
+    b.run()
+
+
+def test_two_plans_at_once_on_two_streams():
+    a, b = Batch8([5000, 30], [3, 1], seed=36), Batch8([200, 4000], [1, 4], seed=37)
+    ca, cb = a.context(), b.context()
+    pa, pb = a.plan(ca), b.plan(cb)
+    torch.cuda.synchronize()
+    s, t = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        a.attn(ca, pa, stream=s)
+        b.attn(cb, pb, stream=t)
+    torch.cuda.synchronize()
+    assert ca.nsd_get_status() == (0, -1) and cb.nsd_get_status() == (0, -1)
+    a.check(), b.check()
+
+
+def test_random_batches():
+    rng = np.random.default_rng(38)
+    for i in range(12):
+        n = int(rng.integers(1, 30))
+        heads, hkv, dim = SHAPES[int(rng.integers(0, len(SHAPES)))]
+        ctx = np.where(rng.random(n) < 0.5, rng.integers(0, 60, n), rng.integers(0, 3000, n)).tolist()
+        new = np.where(rng.random(n) < 0.8, rng.integers(0, 6, n), rng.integers(0, 40, n)).tolist()
+        Batch8(ctx, new, heads=heads, kv_heads=hkv, dim=dim, seed=100 + i, pad_rows=2).run(**({"window": int(rng.integers(1, 500))} if i % 3 == 0 else {}))

@@ -240,3 +240,51 @@ def test_offsets_beyond_32_bits():
             assert np.array_equal(K.code_values(kv8[0, sl // BS, j, :, sl % BS]), values)
             assert np.array_equal(scales[0, sl // BS, :, j, sl % BS].cpu().numpy(), e + 127)
     assert int((scales != 0).sum()) == 3 * 16
+
+
+def test_refusals_launch_nothing():
+    import paper_2609_29364_b200 as nsd
+
+    c = T.context(8, 2, 64, num_blocks=4, num_layers=2)
+    kv8, scales, _ = cache(c)
+    pool = torch.zeros((2, 4, 2, 2, BS, 64), dtype=torch.bfloat16, device=DEV)
+    ids, k, slots = gpu(torch.zeros(2, dtype=torch.int32)), torch.zeros((2, 128), device=DEV), gpu(torch.zeros(2, dtype=torch.int64))
+    q, pos, freq = torch.zeros((2, 512), device=DEV), gpu(torch.zeros((5, 2), dtype=torch.int32)), torch.ones(64, device=DEV)
+    out = torch.zeros((2, 8, 64), dtype=torch.bfloat16, device=DEV)
+    before = c.nsd_launch_count()
+
+    def code(call):
+        with pytest.raises(nsd.NsdError) as e:
+            call()
+        return e.value.code
+
+    assert code(lambda: c.nsd_kv8_pack(pool, kv8, scales, ids, ids, 2, 1)) == 2                   # layers
+    assert code(lambda: c.nsd_kv8_pack(pool, kv8, scales, ids, ids, -1, 1)) == 2
+    assert code(lambda: c.nsd_kv8_unpack(kv8, scales, pool, ids, ids, 1, 2)) == 2
+    assert code(lambda: c.nsd_kv8_unpack(kv8.data_ptr() + 8, scales, pool, ids, ids)) == 1        # alignment
+    assert code(lambda: c.nsd_kv8_pack(pool, kv8, scales.data_ptr() + 8, ids, ids)) == 1
+    assert code(lambda: c.nsd_kv8_append(kv8, scales, 2, None, k, k, None, slots)) == 2           # layer
+    assert code(lambda: c.nsd_kv8_append(kv8, scales, 0, None, k, k, None, None)) == 1            # no slots
+    assert code(lambda: c.nsd_kv8_append(kv8, scales, 0, None, k.half(), k.half(), None, slots)) == 4
+    assert code(lambda: c.nsd_kv8_append(kv8, scales, 0, q, k, k, out, slots, pos, [8] * 5, freq)) == 2
+    assert code(lambda: c.nsd_kv8_append(kv8, scales, 0, q, k, k, out, slots, pos[:1], [33], freq)) == 2
+    assert code(lambda: c.nsd_kv8_append(kv8, scales, 0, None, k, k, None, slots, adjacent=True)) == 1
+    assert code(lambda: c.nsd_kv8_append(kv8.data_ptr() + 4, scales, 0, None, k, k, None, slots)) == 1
+    assert code(lambda: c.nsd_rope_append(pool, 0, q, k, k, out, pos[:0], [], freq, slots)) == 2  # the 16-bit append still wants an axis
+    c.nsd_kv8_pack(pool, kv8, scales, ids[:0], ids[:0])
+    c.nsd_kv8_pack(pool, kv8, scales, ids, ids, 1, 0)
+    c.nsd_kv8_append(kv8, scales, 0, None, k[:0], k[:0], None, slots[:0])
+    assert c.nsd_launch_count() == before and (kv8 == 0xA5).all()
+
+
+def test_pack_and_append_on_another_stream_than_the_current_one():
+    c = T.context(8, 2, 64, num_blocks=4)
+    kv8, scales, _ = cache(c)
+    pool = torch.randn((1, 4, 2, 2, BS, 64), device=DEV).to(torch.bfloat16)
+    ids = gpu(torch.arange(4, dtype=torch.int32))
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    c.nsd_kv8_pack(pool, kv8, scales, ids, ids, stream=s)
+    s.synchronize()
+    values, _ = K.quantise(pool.double().cpu().numpy())
+    assert np.array_equal(K.code_values(kv8), values)

@@ -415,7 +415,7 @@ class VerifyContext:
             raise ValueError("positions: [axes][rows] is wanted, and sections: one number per axis")
         rc = call(
             self._h, *stores, layer, n, 0 if dtype is self._f32 else (1 if dtype is self._bf16 else -1), qp, qs, kp, ks, vp, vs,
-            op, os_, _tensor(positions, self._i32, "positions"), axes, (ctypes.c_int32 * axes)(*sections),
+            op, os_, _tensor(positions, self._i32, "positions"), axes, (ctypes.c_int32 * axes)(*sections) if axes else None,
             _tensor(inv_freq, self._f32, "inv_freq", sum(sections)),
             (NSD_ROPE_ADJACENT if adjacent else 0) | (NSD_ROPE_CYCLED if cycled else 0), _tensor(slot_map, self._i64, "slot_map", n),
             self._stream(stream, *(None if type(t) is int else t for t in tensors), q, k, v, q_out if q is not None else None, positions, inv_freq, slot_map))

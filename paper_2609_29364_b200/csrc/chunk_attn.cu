@@ -197,8 +197,11 @@ chunk_split_kernel(const PlanArgs a) {
         unsigned long long mine[2] = {0, 0};
         for (int64_t i = i0; i < i1; ++i)
             if (raw(i).ntok > 0) mine[raw(i).side] += unit_cost(k, raw(i), a.T);
-        for (int s = 0; s < 2; ++s)
-            if (mine[s]) atomicAdd(&sides[s], mine[s]);
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) mine[s] += __shfl_xor_sync(0xffffffffu, mine[s], d);
+            if (lane == 0 && mine[s]) atomicAdd(&sides[s], mine[s]);
+        }
         __syncthreads();
         if (sides[1] > sides[0]) k = ChunkCost{4, 7, 3};
     }

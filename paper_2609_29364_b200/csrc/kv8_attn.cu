@@ -663,8 +663,9 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
         // The rows times the power of two that brings their largest element to [2^14, 2^15), split into three e5m2 terms: rows
         // [term][row] of the product's second operand.  bf16 has eight significant bits, the terms nine: nothing is lost but
         // what lies below 2^-16 then.
-        constexpr int kPer = D / 32;                   // elements of a lane
-        constexpr int kRowsAhead = 2;
+        constexpr int kLanes = D / 8, kStep = 32 / kLanes;                              // lanes of a row, eight elements each; rows at a time
+        const int sub = lane / kLanes, d = lane % kLanes;
+        const uint32_t inv_G = (65536 + a.G - 1) / a.G;                                 // r / G for the few rows there are
         const bool causal = planned && a.p.header->causal;
         uint32_t n_q = 0;
         bool ok = true;
@@ -675,75 +676,67 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             const int slot = n_q & 1, R = piece ? w.u.ntok * a.G : 0, RP = columns(R);
             const uint32_t qb = smem0 + L::kOffQ + slot * L::kQ;
             Meta& mt = meta[slot];
-            uint32_t v[kRowsAhead][kPer / 2];
-            auto fetch = [&](int first) {              // nothing beyond R is read
-#pragma unroll
-                for (int i = 0; i < kRowsAhead; ++i) {
-                    const int r = first + i;
-#pragma unroll
-                    for (int j = 0; j < kPer / 2; ++j) v[i][j] = 0;
-                    if (r < R) {
-                        const uint16_t* const src = a.q + (int64_t)(w.u.row0 + r / a.G) * a.q_stride + (w.head * a.G + r % a.G) * D + lane * kPer;
-                        if constexpr (D == 128) {
-                            const uint2 z = __ldg(reinterpret_cast<const uint2*>(src));
-                            v[i][0] = z.x, v[i][kPer / 2 - 1] = z.y;
-                        } else {
-                            v[i][0] = __ldg(reinterpret_cast<const uint32_t*>(src));
-                        }
-                    }
-                }
-            };
-            auto largest = [&](int i) {                // magnitude bits of this lane's part of a row
-                uint32_t big = 0;
-#pragma unroll
-                for (int j = 0; j < kPer / 2; ++j) big = max(big, max(v[i][j] & 0x7fffu, (v[i][j] >> 16) & 0x7fffu));
-                return big;
+            auto read = [&](int r) {
+                if (r >= R) return make_uint4(0, 0, 0, 0);
+                const int t = (r * inv_G) >> 16;
+                return __ldg(reinterpret_cast<const uint4*>(a.q + (int64_t)(w.u.row0 + t) * a.q_stride + (w.head * a.G + r - t * a.G) * D + d * 8));
             };
             const bool tiles = piece && w.k1 > w.k0;
-            uint32_t big = 0;                          // of all rows, but for what is no number
+            uint32_t big = 0;                          // magnitude bits of the largest element
+            uint4 ahead = make_uint4(0, 0, 0, 0);
             if (tiles) {                               // while the buffer is not free yet
 #pragma unroll 1
-                for (int first = 0; first < R; first += kRowsAhead) {
-                    fetch(first);
+                for (int first = 0; first < R; first += 4 * kStep) {
+                    uint4 v[4];
 #pragma unroll
-                    for (int i = 0; i < kRowsAhead; ++i) {
-                        const uint32_t m = largest(i);
-                        if (!__any_sync(0xffffffffu, m >= 0x7f80u)) big = max(big, m);
+                    for (int i = 0; i < 4; ++i) v[i] = read(first + i * kStep + sub);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        big = __vmaxu2(big, __vmaxu2(__vmaxu2(v[i].x & 0x7fff7fffu, v[i].y & 0x7fff7fffu), __vmaxu2(v[i].z & 0x7fff7fffu, v[i].w & 0x7fff7fffu)));
+                }
+                big = __reduce_max_sync(0xffffffffu, max(big & 0xffffu, big >> 16));
+                ahead = read(sub);
+            }
+            const bool odd = big >= 0x7f80u;           // some value is no number: the largest of the others
+            if (odd) {
+                big = 0;
+#pragma unroll 1
+                for (int first = 0; first < R; first += kStep) {
+                    const uint4 v = read(first + sub);
+                    const uint32_t word[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const uint32_t m = word[j >> 1] >> (16 * (j & 1)) & 0x7fffu;
+                        big = max(big, m < 0x7f80u ? m : 0u);
                     }
                 }
                 big = __reduce_max_sync(0xffffffffu, big);
-                if (R > kRowsAhead) fetch(0);
             }
-            const int k = 141 - max((int)(big >> 7), 1);                                // 2^k as a product: k may be 140
-            const float f0 = __uint_as_float((uint32_t)((k >> 1) + 127) << 23), f1 = __uint_as_float((uint32_t)(k - (k >> 1) + 127) << 23);
+            const int k = min(141 - max((int)(big >> 7), 1), 127);
+            const float f = __uint_as_float((uint32_t)(k + 127) << 23);
             if (n_q >= 2 && !(ok = wait(q_empty + 8 * slot, (n_q >> 1) - 1))) break;
             if (tiles) {
 #pragma unroll 1
-                for (int first = 0; first < RP; first += kRowsAhead) {
-                    uint32_t h[kRowsAhead][2];
-                    bool none[kRowsAhead];             // a value that is no number: the whole row is none
+                for (int first = 0; first < RP; first += kStep) {
+                    const int r = first + sub;
+                    const uint32_t word[4] = {ahead.x, ahead.y, ahead.z, ahead.w};
+                    ahead = read(r + kStep);
+                    uint32_t h[4], t0[3], t1[3];
 #pragma unroll
-                    for (int i = 0; i < kRowsAhead; ++i) {
-                        none[i] = __any_sync(0xffffffffu, largest(i) >= 0x7f80u);
-                        h[i][1] = 0;
+                    for (int j = 0; j < 4; ++j) h[j] = pack_half(__uint_as_float(word[j] << 16) * f, __uint_as_float(word[j] & 0xffff0000u) * f);
+                    split4<false>(h[0], h[1], t0);
+                    split4<false>(h[2], h[3], t1);
+                    if (odd) {                         // a row with such a value is none: not a number in all its elements
+                        bool none = false;
 #pragma unroll
-                        for (int j = 0; j < kPer / 2; ++j)
-                            h[i][j] = pack_half(__uint_as_float(v[i][j] << 16) * f0 * f1, __uint_as_float(v[i][j] & 0xffff0000u) * f0 * f1);
+                        for (int j = 0; j < 4; ++j) none = none || (word[j] & 0x7fffu) >= 0x7f80u || (word[j] >> 16 & 0x7fffu) >= 0x7f80u;
+                        if (__ballot_sync(0xffffffffu, none) >> (sub * kLanes) & (uint32_t)((1ull << kLanes) - 1)) t0[0] = t1[0] = 0x7f7f7f7fu;
                     }
-                    fetch(first + kRowsAhead);
 #pragma unroll
-                    for (int i = 0; i < kRowsAhead; ++i) {
-                        uint32_t t[3];
-                        split4<false>(h[i][0], h[i][1], t);
-                        if (none[i]) t[0] = 0x7f7f7f7fu;
-#pragma unroll
-                        for (int j = 0; j < 3; ++j) {
-                            const int row = j * RP + first + i;                         // the swizzle exchanges 16-byte pieces by the row
-                            if constexpr (D == 128)
-                                asm volatile("st.shared.b32 [%0], %1;" ::"r"(qb + row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + (lane & 3) * 4), "r"(t[j]) : "memory");
-                            else
-                                asm volatile("st.shared.b16 [%0], %1;" ::"r"(qb + row * 64 + (((lane >> 3) ^ ((row >> 1) & 3)) << 4) + (lane & 7) * 2), "h"((uint16_t)t[j]) : "memory");
-                        }
+                    for (int t = 0; t < 3; ++t) {
+                        const int row = t * RP + r;    // the swizzle exchanges 16-byte pieces by the row
+                        const int piece16 = (d >> 1) ^ (D == 128 ? row & 7 : row >> 1 & 3);
+                        asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(qb + row * D + piece16 * 16 + (d & 1) * 8), "r"(t0[t]), "r"(t1[t]) : "memory");
                     }
                 }
                 int lo_max = 0, hi_min = 0x7fffffff;

@@ -48,6 +48,7 @@ struct __align__(16) Meta {                            // a piece, beside its Q 
     int n, rows;                                       // key tiles, -1 behind the last piece; stacked rows
     int row0, head, slot;                              // first token's row; kv head; partial slot or -1
     int key_first;                                     // of the first tile
+    int key_lo, key_hi, gaps;                          // keys that some row sees: [key_lo, key_hi), unless there are gaps
     float c;                                           // sc 2^-k 2^-7, where the rows were multiplied by 2^k
 };
 struct __align__(16) State {
@@ -293,11 +294,14 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                     const uint32_t stage = n_t % kStages, use = n_t / kStages;
                     const int at = key0 + key;
                     const bool masked = key0 < lo_max || key0 + kTileKeys > hi_min;
-                    bool seen = true;
+                    bool seen = true;                  // by some row
                     if (masked) {
-                        seen = false;
+                        seen = at >= mt.key_lo && at < mt.key_hi;
+                        if (mt.gaps) {
+                            seen = false;
 #pragma unroll 1
-                        for (int r = 0; r < R; r += G) seen = seen || (at >= mt.lo[r] && at < mt.hi[r]);
+                            for (int r = 0; r < R; r += G) seen = seen || (at >= mt.lo[r] && at < mt.hi[r]);
+                        }
                     }
                     hold(s_full + 8 * (n_t & 1), n_t >> 1);
                     tc_fence_after();
@@ -316,12 +320,13 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                         for (int ch = 0; ch < NC; ++ch) {
                             uint32_t y[4];
                             tmem_ld4(tmem_s + ch * 4, y);
+                            const int4 lo4 = *reinterpret_cast<const int4*>(mt.lo + r0 + ch * 4), hi4 = *reinterpret_cast<const int4*>(mt.hi + r0 + ch * 4);
+                            const int lo[4] = {lo4.x, lo4.y, lo4.z, lo4.w}, hi[4] = {hi4.x, hi4.y, hi4.z, hi4.w};
                             tmem_wait<4>(y);
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
-                                const int r = r0 + ch * 4 + j;
                                 if (none) y[j] = 0x7fc00000u;
-                                if (at < mt.lo[r] || at >= mt.hi[r]) y[j] = 0xff800000u;
+                                if (at < lo[j] || at >= hi[j]) y[j] = 0xff800000u;
                             }
                             tmem_st4(tmem_s + ch * 4, y);
                         }
@@ -757,7 +762,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                 mt.n = piece ? w.k1 - w.k0 : -1, mt.rows = R;
                 const int d0 = (-k - 7) >> 1, d1 = -k - 7 - d0;                         // sc 2^(-k - 7)
                 mt.c = a.sc * __uint_as_float((uint32_t)(d0 + 127) << 23) * __uint_as_float((uint32_t)(d1 + 127) << 23);
-                if (piece) mt.row0 = w.u.row0, mt.head = w.head, mt.slot = w.slot, mt.key_first = (w.u.key_lo / kTileKeys + w.k0) * kTileKeys;
+                if (piece) mt.row0 = w.u.row0, mt.head = w.head, mt.slot = w.slot, mt.key_first = (w.u.key_lo / kTileKeys + w.k0) * kTileKeys, mt.key_lo = w.u.key_lo, mt.key_hi = w.u.key_hi, mt.gaps = w.u.gaps;
             }
             fence_async_smem();
             __syncwarp();

@@ -58,15 +58,15 @@ __device__ __forceinline__ int group_of(const ChunkGroups& g, int r) {
 }
 // Keys that a group's rows have in common and that are read for all of them at once: none for a request by itself.
 __device__ __forceinline__ int shared_keys(const ChunkGroups& g, int k) { return g.indptr[k + 1] - g.indptr[k] > 1 ? g.prefix_len[k] : 0; }
-__device__ __forceinline__ bool request_ok(const PlanArgs& a, int r) {
+__device__ __forceinline__ bool request_ok(const PlanArgs& a, const ChunkGroups& groups, int r) {
     const int64_t s = a.q_indptr[r], e = a.q_indptr[r + 1], c = a.ctx_len[r];
     if (!(s >= 0 && s <= e && e <= a.p.max_rows && c >= 0 && c + (e - s) <= 0x7fffffffll - kTileKeys && a.kv_indptr[r] >= 0 && a.kv_indptr[r] <= a.kv_indptr[r + 1]))
         return false;
-    if (a.groups.n == 0) return true;
+    if (groups.n == 0) return true;
     // groups cover the batch in order, and what a request's group shares the request has
-    const int k = group_of(a.groups, r);
-    return a.groups.indptr[k] >= 0 && a.groups.indptr[k] <= r && a.groups.indptr[k + 1] > r && a.groups.indptr[k + 1] <= a.batch && a.groups.prefix_len[k] >= 0 &&
-           (e == s || a.groups.prefix_len[k] <= c);
+    const int k = group_of(groups, r);
+    return groups.indptr[k] >= 0 && groups.indptr[k] <= r && groups.indptr[k + 1] > r && groups.indptr[k + 1] <= a.batch && groups.prefix_len[k] >= 0 &&
+           (e == s || groups.prefix_len[k] <= c);
 }
 
 __global__ void __launch_bounds__(128)
@@ -82,7 +82,7 @@ chunk_units_kernel(const PlanArgs a) {
         if (first < 0 || first >= end || end > a.batch) return;                         // none, or reported with a request
         r = (int)first;
     }
-    if (!request_ok(a, r)) {
+    if (!request_ok(a, a.groups, r)) {
         if (shared) return;
         if (blockIdx.y == 0 && threadIdx.x == 0) report(a.status, STATUS_BAD_TOKEN, r);
         return;
@@ -169,13 +169,19 @@ chunk_split_kernel(const PlanArgs a) {
     __shared__ int32_t warp_n[kSplitThreads / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     bool ok = true;
-    for (int r = tid; r < a.batch; r += kSplitThreads) ok = ok && request_ok(a, r);
+    ChunkGroups groups = a.groups;
+    if (groups.n > 0 && groups.n < kCostSmem) {        // the costs come later: until then their place holds the groups' offsets
+        for (int k = tid; k <= groups.n; k += kSplitThreads) cost_s[k] = groups.indptr[k];
+        groups.indptr = cost_s;
+        __syncthreads();
+    }
+    for (int r = tid; r < a.batch; r += kSplitThreads) ok = ok && request_ok(a, groups, r);
     if (tid == 0 && a.batch > 0 && a.q_indptr[0] != 0) {
         report(a.status, STATUS_BAD_TOKEN, 0);
         ok = false;
     }
-    for (int k = tid; k < a.groups.n; k += kSplitThreads)
-        if (a.groups.indptr[k] >= a.groups.indptr[k + 1] || (k == 0 && a.groups.indptr[0] != 0) || (k == a.groups.n - 1 && a.groups.indptr[k + 1] != a.batch)) {
+    for (int k = tid; k < groups.n; k += kSplitThreads)
+        if (groups.indptr[k] >= groups.indptr[k + 1] || (k == 0 && groups.indptr[0] != 0) || (k == groups.n - 1 && groups.indptr[k + 1] != a.batch)) {
             report(a.status, STATUS_BAD_TOKEN, -1);
             ok = false;
         }
@@ -187,6 +193,9 @@ chunk_split_kernel(const PlanArgs a) {
     auto raw = [&](int64_t i) -> const ChunkUnit& { return a.p.raw[i < n_own ? i : a.p.max_units / 2 + (i - n_own)]; };
     const int64_t per = (n_raw + kSplitThreads - 1) / kSplitThreads;
     const int64_t i0 = min(tid * per, n_raw), i1 = min(i0 + per, n_raw);
+    // a thread has one unit as a rule: it stays in registers
+    const ChunkUnit only = i0 < i1 ? raw(i0) : ChunkUnit{};
+    auto unit = [&](int64_t i) { return i == i0 ? only : raw(i); };
     int n_mine = 0;
     int64_t c_mine = 0;
     ChunkCost k{1, 2, a.p.kind.unit_tiles};
@@ -195,8 +204,10 @@ chunk_split_kernel(const PlanArgs a) {
         if (tid < 2) sides[tid] = 0;
         __syncthreads();
         unsigned long long mine[2] = {0, 0};
-        for (int64_t i = i0; i < i1; ++i)
-            if (raw(i).ntok > 0) mine[raw(i).side] += unit_cost(k, raw(i), a.T);
+        for (int64_t i = i0; i < i1; ++i) {
+            const ChunkUnit u = unit(i);
+            if (u.ntok > 0) mine[u.side] += unit_cost(k, u, a.T);
+        }
         for (int s = 0; s < 2; ++s) {
 #pragma unroll
             for (int d = 16; d > 0; d >>= 1) mine[s] += __shfl_xor_sync(0xffffffffu, mine[s], d);
@@ -205,8 +216,10 @@ chunk_split_kernel(const PlanArgs a) {
         __syncthreads();
         if (sides[1] > sides[0]) k = ChunkCost{4, 7, 3};
     }
-    for (int64_t i = i0; i < i1; ++i)
-        if (raw(i).ntok > 0) ++n_mine, c_mine += unit_cost(k, raw(i), a.T);
+    for (int64_t i = i0; i < i1; ++i) {
+        const ChunkUnit u = unit(i);
+        if (u.ntok > 0) ++n_mine, c_mine += unit_cost(k, u, a.T);
+    }
     int n_inc = n_mine;
     int64_t c_inc = c_mine;
 #pragma unroll
@@ -225,7 +238,7 @@ chunk_split_kernel(const PlanArgs a) {
     }
     int64_t* const cost = n_units < kCostSmem ? cost_s : a.p.cost;
     for (int64_t i = i0; i < i1; ++i) {
-        ChunkUnit u = raw(i);
+        ChunkUnit u = unit(i);
         if (u.ntok <= 0) continue;
         u.last = n_at - u.first + u.last;
         u.first = n_at - u.first;

@@ -11,7 +11,9 @@ namespace {
 // both sides move in whole lines; the D / 8 lanes of a row find its maximum by shuffles.  Nothing
 // is read twice, so HBM bounds it: 3 D + 1 bytes per row.  The grid is (pairs, tiles of a block,
 // layers), so that no thread divides to find its place (with one flat index, taken apart by three
-// 64-bit divisions, 2048 blocks of 4 layers took 336 us), and the loads of kAhead tiles are under way together.
+// 64-bit divisions, 2048 blocks of 4 layers took 336 and 288 us), and the loads of kAhead tiles are
+// under way together.  2048 blocks of 4 layers (8 kv heads of 128) 157 us packed = 5.1 TB/s, 146
+// unpacked = 5.5 TB/s; 67 blocks 6.8 and 5.3 us.
 constexpr int kBsP = 16;
 constexpr int kThreadsP = 256;
 constexpr int kAhead = 4;

@@ -13,6 +13,44 @@
 namespace nsd {
 namespace {
 
+// A unit is up to 40 stacked rows (tokens of one request times the G q heads of a kv head).  The keys sit on the tensor-memory
+// lanes, the rows on the columns; per tile of 128 keys
+//     S[128 keys x R]  = K Q^T       A = K's codes (e4m3, K-major), B = Q as three e5m2 terms, one pass over K for each
+//     O[D x 3 R]      += V^T P^T     A = V's codes (MN-major), B = the weights as three e5m2 terms side by side
+// so that the cache's bytes go from TMA to the tensor cores as they are.  No product is rounded: a bf16 query has eight
+// significant bits and a 16-bit weight eleven, the three terms hold nine and eleven, and the accumulators are 32 bits.  The
+// keys' powers of two are one number per lane: K's multiplies the scores, V's the weights before they are split.  The third
+// term of a weight keeps its bits down to 2^-24 because the terms have columns of O of their own and may each have a scale.
+// Rows on the lanes, as in the 16-bit kernels, would leave 100 of 128 lanes idle at the sizes this is for, and put the
+// exponentials of 4 to 40 rows on one or two warps.
+//
+// The weights are 2^(s - m), with a reference m per row that is set in a piece's first tile so that its largest weight is 2^4,
+// and moved only when one would pass 2^15 (all softmax warps vote in every tile); V's powers of two likewise are taken
+// relative to the largest so far, so that a weight times them stays within 16 bits.  Sums of the weights are 32-bit and of
+// the unrounded ones, a thread's own until the end of the piece.
+//
+// Two CTAs per SM, each a pipeline of its own with an equal share of the line (request, kv head, unit, key tile), twelve warps:
+//   0-7   softmax: warp w has the keys of lane quarter w % 4 and one half of the rows; they also write the rows out
+//   8     issues the MMAs: S of a tile ahead of P V of the one before it
+//   9, 10 K (with the scales of K and V) and V, one TMA box per pool block, two stages each (four at D = 64)
+//   11    Q of the next piece, and what the other warps have to know of it
+// Pieces that a CTA boundary cuts leave their O and statistics in the plan, and chunk_join_kernel joins them in order.
+//
+// What bounds it: single tokens HBM (512 over 2048 keys each, 32 q heads and 8 kv heads of 128: 347 us = 6.2 TB/s, 0.97 of
+// the copy rate; the 16-bit kernel reads twice the bytes); five rows per request the chain of a tile's softmax (430 us = 5.1
+// TB/s; 3 to 5 rows over 128 to 4096 keys 437); ten rows (40 stacked) 130 us for 4 x 60 000 keys = 3.8 TB/s; 64 single tokens
+// over 512 to 2048 keys 42 us, of which some 15 are the start, the last pieces and the join; 512 x 256 keys 94 us: a piece of two
+// or three tiles costs as much again in its beginning and end.  D = 64 halves the bytes but not the softmax: 512 x 5 rows
+// over 2048 keys 390 us.  The instructions of a tile matter more than their number of cycles alone: with a longer loop
+// (waits with time limits, eight rows of Q at a time, a fourth term) the SM's instruction cache no longer held it and times rose
+// by a fifth.
+//
+// Tried: rows' terms in columns of S of their own, one pass over K (512 x 5 rows 474 us instead of 449: the sums of the terms
+// then fall to the softmax warps); one CTA per SM with two streams over alternate tiles (1126 us; 668 with two CTAs); four warps
+// for Q (516 instead of 499); S of a tile after P V of the one before (513 instead of 449).
+//
+// Every wait is bounded.  When one runs out, the CTA raises its abort flag; once all warps have left their loops, the issuer
+// waits for its MMAs in flight and each producer for its copies (bounded again), and the call ends with STATUS_TIMEOUT.
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kTileKeys = 128, kBs = 16, kBlocks = kTileKeys / kBs;
 constexpr int kMaxRows = kKv8Kind.rows;

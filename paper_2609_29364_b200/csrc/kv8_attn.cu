@@ -15,7 +15,7 @@ namespace {
 
 // A unit is up to 40 stacked rows (tokens of one request times the G q heads of a kv head).  The keys sit on the tensor-memory
 // lanes, the rows on the columns; per tile of 128 keys
-//     S[128 keys x R]  = K Q^T       A = K's codes (e4m3, K-major), B = Q as three e5m2 terms, one pass over K for each
+//     S[128 keys x R]  = K Q^T       A = K's codes (e4m3, K-major), B = Q as three e5m2 terms
 //     O[D x 3 R]      += V^T P^T     A = V's codes (MN-major), B = the weights as three e5m2 terms side by side
 // so that the cache's bytes go from TMA to the tensor cores as they are.  No product is rounded: a bf16 query has eight
 // significant bits and a 16-bit weight eleven, the three terms hold nine and eleven, and the accumulators are 32 bits.  The
@@ -36,18 +36,17 @@ namespace {
 //   11    Q of the next piece, and what the other warps have to know of it
 // Pieces that a CTA boundary cuts leave their O and statistics in the plan, and chunk_join_kernel joins them in order.
 //
-// What bounds it: single tokens HBM (512 over 2048 keys each, 32 q heads and 8 kv heads of 128: 347 us = 6.2 TB/s, 0.97 of
-// the copy rate; the 16-bit kernel reads twice the bytes); five rows per request the chain of a tile's softmax (430 us = 5.1
-// TB/s; 3 to 5 rows over 128 to 4096 keys 437); ten rows (40 stacked) 130 us for 4 x 60 000 keys = 3.8 TB/s; 64 single tokens
-// over 512 to 2048 keys 42 us, of which some 15 are the start, the last pieces and the join; 512 x 256 keys 94 us: a piece of two
+// What bounds it: single tokens HBM (512 over 2048 keys each, 32 q heads and 8 kv heads of 128: 341 us = 6.3 TB/s, 0.98 of
+// the copy rate; the 16-bit kernel reads twice the bytes); five rows per request the chain of a tile's softmax (427 us = 5.1
+// TB/s; 3 to 5 rows over 128 to 4096 keys 444); ten rows (40 stacked) 130 us for 4 x 60 000 keys = 3.8 TB/s; 64 single tokens
+// over 512 to 2048 keys 40 us, of which some 15 are the start, the last pieces and the join; 512 x 256 keys 98 us: a piece of two
 // or three tiles costs as much again in its beginning and end.  D = 64 halves the bytes but not the softmax: 512 x 5 rows
 // over 2048 keys 390 us.  The instructions of a tile matter more than their number of cycles alone: with a longer loop
 // (waits with time limits, eight rows of Q at a time, a fourth term) the SM's instruction cache no longer held it and times rose
 // by a fifth.
 //
-// Tried: rows' terms in columns of S of their own, one pass over K (512 x 5 rows 474 us instead of 449: the sums of the terms
-// then fall to the softmax warps); one CTA per SM with two streams over alternate tiles (1126 us; 668 with two CTAs); four warps
-// for Q (516 instead of 499); S of a tile after P V of the one before (513 instead of 449).
+// Tried: one CTA per SM with two streams over alternate tiles (1126 us; 668 with two CTAs); four warps for Q (516 instead of
+// 499); S of a tile after P V of the one before (513 instead of 449).
 //
 // Every wait is bounded.  When one runs out, the CTA raises its abort flag; once all warps have left their loops, the issuer
 // waits for its MMAs in flight and each producer for its copies (bounded again), and the call ends with STATUS_TIMEOUT.
@@ -119,6 +118,11 @@ struct Smem8 {
     static_assert(2 * (kBytes + 1024) <= 228 * 1024, "two CTAs per SM");
 };
 constexpr int kTmemCols = 256, kTmemO = 128;           // two buffers of S, 64 columns apart, and O
+// With up to 16 rows the three terms of S have columns of their own (four rows and three terms after another, as in P and O) and
+// one pass over K serves them all: 512 single tokens over 2048 keys 341 us instead of 347, 64 over 512 to 2048 40 instead of 42.
+// With more rows the sums of the terms cost the softmax warps more than two passes cost the tensor cores (5 rows 430 instead of
+// 426): then they are summed where they lie.
+constexpr int kApart = 16;
 
 // Four rows' values over the lanes of a warp: row j on lanes 8 j .. 8 j + 7.
 template <typename Op>
@@ -167,6 +171,9 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
     const __half2 h = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
+// 12 or 24 columns
+__device__ __forceinline__ void tmem_ld_terms(uint32_t at, uint32_t (&r)[12]) { tmem_ld8(at, r), tmem_ld4(at + 8, r + 8); }
+__device__ __forceinline__ void tmem_ld_terms(uint32_t at, uint32_t (&r)[24]) { tmem_ld16(at, r), tmem_ld8(at + 16, r + 16); }
 // Waits for this thread's tensor-memory loads; their registers are operands, so that no use moves in front of the wait.
 template <int N>
 __device__ __forceinline__ void tmem_wait(uint32_t* r) {
@@ -265,7 +272,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
         __syncwarp();
         asm volatile("barrier.cta.sync 1, %0;" ::"n"(kThreads) : "memory");
     };
-    auto columns = [](int rows) { return (rows + 7) & ~7; };                            // of one term of S
+    auto columns = [](int rows) { return (rows + 7) & ~7; };                            // of one term
     // P and O: a warp's half of the rows, four rows and three terms after another, filled up to 16 columns
     auto half_columns = [](int rows) { return (3 * rows + 15) & ~15; };
 
@@ -351,13 +358,15 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                     const float kk = none ? (masked ? 1.f : __uint_as_float(0x7fc00000u)) : fmaxf(__uint_as_float((kb + 7) << 23) * mt.c, 1.17549435e-38f);
                     const uint64_t kk2 = pair(kk, kk);
                     const int ev = seen ? (int)vb - 127 : kNoScale;
-                    const uint32_t tmem_s = tmem + (n_t & 1) * 64 + lanes + r0;
+                    constexpr bool kTerms = 8 * NC <= kApart;
+                    const uint32_t tmem_s = tmem + (n_t & 1) * 64 + lanes + (kTerms ? 3 * r0 : r0);
                     // Scores are hidden where they lie, in a loop of its own: rare, and out of the way of the others.
                     if (masked) {
 #pragma unroll 1
-                        for (int ch = 0; ch < NC; ++ch) {
+                        for (int k = 0; k < (kTerms ? 3 : 1) * NC; ++k) {
+                            const int ch = kTerms ? k / 3 : k;
                             uint32_t y[4];
-                            tmem_ld4(tmem_s + ch * 4, y);
+                            tmem_ld4(tmem_s + k * 4, y);
                             const int4 lo4 = *reinterpret_cast<const int4*>(mt.lo + r0 + ch * 4), hi4 = *reinterpret_cast<const int4*>(mt.hi + r0 + ch * 4);
                             const int lo[4] = {lo4.x, lo4.y, lo4.z, lo4.w}, hi[4] = {hi4.x, hi4.y, hi4.z, hi4.w};
                             tmem_wait<4>(y);
@@ -366,24 +375,35 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                                 if (none) y[j] = 0x7fc00000u;
                                 if (at < lo[j] || at >= hi[j]) y[j] = 0xff800000u;
                             }
-                            tmem_st4(tmem_s + ch * 4, y);
+                            tmem_st4(tmem_s + k * 4, y);
                         }
                         tmem_wait_st();
                     }
                     // The scores of this thread's key and rows less the rows' references, -inf where a row does not see the key.  The
                     // product is rounded before the difference, so that the largest score less itself is 0 however large it is.
                     uint32_t x[4 * NC];
-                    float4 m[NC];
+                    uint64_t sum[2 * NC];
+                    if constexpr (kTerms) {
+                        uint32_t y[12 * NC];
+                        tmem_ld_terms(tmem_s, y);
+                        tmem_wait<12 * NC>(y);
 #pragma unroll
-                    for (int ch = 0; ch < NC; ++ch) tmem_ld4(tmem_s + ch * 4, x + ch * 4);
+                        for (int k = 0; k < 2 * NC; ++k) {
+                            const uint32_t* const v = y + (k >> 1) * 12 + (k & 1) * 2;
+                            sum[k] = add2(add2(bits2(v[0], v[1]), bits2(v[4], v[5])), bits2(v[8], v[9]));
+                        }
+                    } else {
 #pragma unroll
-                    for (int ch = 0; ch < NC; ++ch) m[ch] = *reinterpret_cast<const float4*>(st.neg + r0 + ch * 4);
-                    tmem_wait<4 * NC>(x);
+                        for (int ch = 0; ch < NC; ++ch) tmem_ld4(tmem_s + ch * 4, x + ch * 4);
+                        tmem_wait<4 * NC>(x);
+#pragma unroll
+                        for (int k = 0; k < 2 * NC; ++k) sum[k] = bits2(x[2 * k], x[2 * k + 1]);
+                    }
                     float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
                     for (int ch = 0; ch < NC; ++ch) {
-                        const float2 f0 = unpair(add2(mul2(bits2(x[ch * 4], x[ch * 4 + 1]), kk2), pair(m[ch].x, m[ch].y)));
-                        const float2 f1 = unpair(add2(mul2(bits2(x[ch * 4 + 2], x[ch * 4 + 3]), kk2), pair(m[ch].z, m[ch].w)));
+                        const float4 m = *reinterpret_cast<const float4*>(st.neg + r0 + ch * 4);
+                        const float2 f0 = unpair(add2(mul2(sum[2 * ch], kk2), pair(m.x, m.y))), f1 = unpair(add2(mul2(sum[2 * ch + 1], kk2), pair(m.z, m.w)));
                         x[ch * 4] = __float_as_uint(f0.x), x[ch * 4 + 1] = __float_as_uint(f0.y);
                         x[ch * 4 + 2] = __float_as_uint(f1.x), x[ch * 4 + 3] = __float_as_uint(f1.y);
                         top[0] = fmaxf(fmaxf(top[0], f0.x), f0.y), top[1] = fmaxf(fmaxf(top[1], f1.x), f1.y);
@@ -590,12 +610,13 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             const uint32_t stage = n_s % kStages, slot = (n_q - 1) & 1;
             if (!(ok = wait(k_full + 8 * stage, n_s / kStages))) return;
             tc_fence_after();
-            const uint32_t idesc = instr_desc_f8(kTileKeys, (RP + 15) & ~15, 0, 0);
+            const bool apart = RP <= kApart;
+            const uint32_t idesc = instr_desc_f8(kTileKeys, ((apart ? 3 * RP : RP) + 15) & ~15, 0, 0);
             const uint64_t dk = smem_desc(smem0 + L::kOffK + stage * L::kTile, 16, 8 * D, L::kSwizzle);
             const uint64_t dq = smem_desc(smem0 + L::kOffQ + slot * L::kQ, 16, 8 * D, L::kSwizzle);
             if (elect_one()) {
-#pragma unroll
-                for (int t = 0; t < 3; ++t)
+#pragma unroll 1
+                for (int t = 0; t < (apart ? 1 : 3); ++t)
 #pragma unroll
                     for (int k = 0; k < D / 32; ++k)                                    // 32 dims each
                         umma_ss_f8(tmem + (n_s & 1) * 64, dk + 2 * k, dq + ((t * RP * D) >> 4) + 2 * k, idesc, t > 0 || k > 0);
@@ -704,8 +725,8 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
     } else {
         // ================================ Q and the pieces ================================
         // The rows times the power of two that brings their largest element to [2^14, 2^15), split into three e5m2 terms: rows
-        // [term][row] of the product's second operand.  bf16 has eight significant bits, the terms nine: nothing is lost but
-        // what lies below 2^-16 then.
+        // of the product's second operand, in the order of S's columns.  bf16 has eight significant bits, the terms nine: nothing
+        // is lost but what lies below 2^-16 then.
         constexpr int kLanes = D / 8, kStep = 32 / kLanes;                              // lanes of a row, eight elements each; rows at a time
         const int sub = lane / kLanes, d = lane % kLanes;
         const uint32_t inv_G = (65536 + a.G - 1) / a.G;                                 // r / G for the few rows there are
@@ -777,7 +798,8 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                     }
 #pragma unroll
                     for (int t = 0; t < 3; ++t) {
-                        const int row = t * RP + r;    // the swizzle exchanges 16-byte pieces by the row
+                        const int row = RP <= kApart ? 3 * (r & ~3) + 4 * t + (r & 3) : t * RP + r;
+                        // the swizzle exchanges 16-byte pieces by the row
                         const int piece16 = (d >> 1) ^ (D == 128 ? row & 7 : row >> 1 & 3);
                         asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(qb + row * D + piece16 * 16 + (d & 1) * 8), "r"(t0[t]), "r"(t1[t]) : "memory");
                     }

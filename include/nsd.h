@@ -680,10 +680,13 @@ nsd_status nsd_kv8_unpack(nsd_ctx* ctx, const void* kv8, const void* scales, voi
  * Made for few rows per request: up to 40 stacked rows of a kv head (tokens times grouped q heads)
  * read the cache once, longer chunks once per 40.
  * Slots that hold no visible token may hold anything.  A row whose q holds a NaN or an infinity, or
- * that sees a K of which a code is NaN or a row whose scale is 255, has o and lse NaN.  A NaN code
- * in a visible V reaches the other rows of the same request that are computed with them (up to 40 stacked rows).
- * fp32 accumulation and softmax statistics; q is multiplied exactly (but for elements below 2^-24
- * of its row's largest); the weights are rounded to 11 bits for the product with V.
+ * that sees a K of which a code is NaN or a K or V whose scale byte is beyond 247, has o and lse NaN.
+ * A NaN code in a visible V reaches the other rows of the same request that are computed with them
+ * (up to 40 stacked rows).
+ * fp32 accumulation and softmax statistics; q is multiplied exactly, but for what lies below 2^-30
+ * of the largest element of the rows computed together (the terms of q end there); the weights are
+ * rounded to 11 bits for the product with V.  A call gives the same bits every time; how a row's
+ * sums are split, and so their last bits, depends on the batch.
  * Arguments and errors as nsd_chunk_plan / nsd_chunk_attn; scale 0 = 1/sqrt(head_dim).
  */
 size_t nsd_kv8_plan_bytes(const nsd_ctx* ctx, int64_t max_rows);
@@ -714,7 +717,8 @@ nsd_status nsd_kv8_attn(nsd_ctx* ctx, void* plan, size_t plan_bytes, const void*
  * (nsd_prefix_plan_bytes) also holds what each side found for every row in 32 bits: 8 (head_dim + 2)
  * num_q_heads bytes per row.
  * Everything else -- rows, tables, capture, scale, softcap, alibi_slopes, errors -- as nsd_chunk_plan
- * and nsd_chunk_attn.  Plans of the three kinds are not interchangeable.
+ * and nsd_chunk_attn.  Plans of the three kinds are not interchangeable: each is reported as
+ * DEVICE_FAULT by the others' attention, which then writes nothing.
  */
 size_t nsd_prefix_plan_bytes(const nsd_ctx* ctx, int64_t max_rows);
 nsd_status nsd_prefix_plan(nsd_ctx* ctx, void* plan, size_t plan_bytes, int32_t batch, int64_t max_rows, int32_t n_groups,

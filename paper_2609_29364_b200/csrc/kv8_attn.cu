@@ -55,7 +55,7 @@ constexpr int kTileKeys = 128, kBs = 16, kBlocks = kTileKeys / kBs;
 constexpr int kMaxRows = kKv8Kind.rows;
 constexpr int kThreads = 384, kSoftThreads = 256;
 constexpr int kWarpIssue = 8, kWarpV = 10, kWarpQ = 11;   // 9: the producer of K
-constexpr uint32_t kPollLimit = 1u << 24;              // polls of one wait, some tenths of a second at least, if nsd_config.wait_budget does not say
+constexpr uint32_t kPollLimit = 1u << 21;              // polls of one wait, if nsd_config.wait_budget does not say: one that finds nothing takes 1.4 us, so three seconds
 constexpr float kTop = 4.f, kMost = 15.f;              // log2 of a row's largest weight when its reference is set, and at most
 constexpr float kMid = 8.f, kLow = 16.f;               // a weight's second term is held times kMid, its third times both
 constexpr int kNoScale = -1000;                        // exponent of V's reference before any

@@ -130,8 +130,9 @@ class Batch8(T.Batch):
 def check_attn8(o, lse, ref, keys, v_max):
     """q and the cache's values are multiplied exactly, sums and scores are held in 32 bits: as in the 16-bit form a weight
     and a row's sum move by less than 2^-10 of themselves.  The weights are rounded to 11 bits (half a step: 2^-11 of the
-    weight) and, below 2^-16 of a reference that lies at most 2^9 under the scale, to multiples: each weight is off by at
-    most 2^-24 of the largest one, which is at most 1, against the largest |v|.  The result is rounded to bf16: 2^-8 |o|."""
+    weight) and, where they are small, to multiples: off by at most 2^-25 as 16-bit floats and 2^-24 in the third term, where
+    a row's largest weight is 2^4 at least and V's power of two at most twice the largest |v|'s.  So each weight is off by less
+    than 2^-24 of the largest one, which is at most 1, against the largest |v|.  The result is rounded to bf16: 2^-8 |o|."""
     o_ref, lse_ref, mag = (t.cpu() for t in ref)
     o = o.double().cpu().reshape(o_ref.shape)
     assert torch.isfinite(o).all(), "non-finite output"

@@ -471,9 +471,8 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
     // Everything so far ran beside the end of the kernel before this one; what it writes (the plan, q, the pool) is read, and what
     // it reads is written, from here on.
     pdl_wait();
-    const bool planned = is_plan(a.p, a.T, a.Hkv);
-    if (!planned && blockIdx.x == 0 && tid == 0) report(a.status, STATUS_BAD_TOKEN, -1);
-    Walk w(a.p, a.Hkv, planned);
+    Walk w(a.p, a.T, a.Hkv);
+    if (!w.planned && blockIdx.x == 0 && tid == 0) report(a.status, STATUS_BAD_TOKEN, -1);
     // the count-th completion; the same answer in every lane
     auto poll = [&](uint32_t bar, uint32_t count) { return (bool)__all_sync(0xffffffffu, bar_try(bar, count & 1)); };
     auto wait = [&](uint32_t bar, uint32_t count) {
@@ -509,7 +508,7 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
         // One register of parities: phases of S, of O of this stream and of the other, of joins by this stream and by the other,
         // key tiles so far; and whether the other stream is still reading this one's O.
         enum : uint32_t { PH_S = 1, PH_O = 2, PH_O_OTHER = 4, PH_X = 8, PH_X_OTHER = 16, PH_TILE = 32, LENT = 64, CAUSAL = 128 };
-        uint32_t ph = planned && a.p.header->causal ? CAUSAL : 0;    // CAUSAL: a row's keys follow from its position
+        uint32_t ph = w.planned && a.p.header->causal ? CAUSAL : 0;    // CAUSAL: a row's keys follow from its position
         bool fail = false;
         auto wait_all = [&](uint32_t bar, uint32_t phase) {
             fail = !wait(bar, (ph & phase) ? 1 : 0);
@@ -1004,15 +1003,16 @@ chunk_join_kernel(const __grid_constant__ ChunkPlan p, uint16_t* __restrict__ o,
     __shared__ ChunkStart starts[kMaxCtas + 1];
     const int c = blockIdx.x + 1;
     pdl_wait();
-    if (!is_plan(p, T, Hkv)) return;
-    const ChunkStart cut = p.starts[c], before = p.starts[c - 1];
+    const bool planned = is_plan(p, T, Hkv);
+    for (int k = c - 1 + threadIdx.x; k <= p.n_ctas; k += kJoinThreads) starts[k] = p.starts[k];     // beside the header, not behind it
+    __syncthreads();
+    if (!planned) return;
+    const ChunkStart cut = starts[c], before = starts[c - 1];
     auto same = [&](const ChunkStart& x) { return x.unit == cut.unit && x.head == cut.head && x.tile > 0; };
     if (cut.tile == 0 || same(before)) return;
     const ChunkUnit u = p.units[cut.unit];
     const int elements = u.ntok * G * (D / 4);
     if ((int)blockIdx.y * kJoinThreads >= elements) return;
-    for (int k = c + threadIdx.x; k <= p.n_ctas; k += kJoinThreads) starts[k] = p.starts[k];
-    __syncthreads();
     int end = c;                                       // CTAs c .. end - 1 start inside the unit
     while (end < p.n_ctas && same(starts[end])) ++end;
     // a CTA without work left nothing

@@ -21,8 +21,11 @@ struct Walk {
     // the piece under way
     ChunkUnit u;
     int head, k0, k1, slot;                            // key tiles [k0, k1) in walking order; partial slot or -1
-    __device__ __forceinline__ Walk(const ChunkPlan& p, int Hkv_, bool planned) : units(p.units), at{}, end{}, Hkv(Hkv_) {
-        if (planned) at = p.starts[blockIdx.x], end = p.starts[blockIdx.x + 1];
+    bool planned;                                      // else there is no work
+    // The share is read beside the header, not behind it: a trip to the L2 less before the first tile.
+    __device__ __forceinline__ Walk(const ChunkPlan& p, int T, int Hkv_)
+        : units(p.units), at(p.starts[blockIdx.x]), end(p.starts[blockIdx.x + 1]), Hkv(Hkv_), planned(is_plan(p, T, Hkv_)) {
+        if (!planned) end = at;
     }
     __device__ __forceinline__ bool next() {
         if (at.unit == end.unit && at.head == end.head && at.tile == end.tile) return false;

@@ -196,7 +196,7 @@ struct Walk8 {
     Walk w;
     ChunkUnit ahead;
     bool more;
-    __device__ __forceinline__ Walk8(const ChunkPlan& p, int Hkv, bool planned) : w(p, Hkv, planned), ahead{} { look(); }
+    __device__ __forceinline__ Walk8(const ChunkPlan& p, int T, int Hkv) : w(p, T, Hkv), ahead{} { look(); }
     __device__ __forceinline__ void look() {
         more = !(w.at.unit == w.end.unit && w.at.head == w.end.head && w.at.tile == w.end.tile);
         if (more) ahead = w.units[w.at.unit];
@@ -254,8 +254,6 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base_s, 0);
     pdl_wait();                                        // from here on: what the kernel before writes
-    const bool planned = is_plan(a.p, a.T, a.Hkv);
-    if (!planned && blockIdx.x == 0 && tid == 0) report(a.status, STATUS_BAD_TOKEN, -1);
     // Waits for the count-th completion, bounded by a number of polls; the same answer in every lane.  Short, since it stands in
     // many places: what the warps of an SM execute has to stay near the size of its instruction cache.
     auto wait = [&](uint32_t bar, uint32_t count) {
@@ -675,7 +673,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
         const int32_t oob = a.num_blocks * 2 * a.Hkv;                                   // past the slab: zero fill
         uint32_t n_t = 0;
         bool ok = true;
-        Walk8 walk(a.p, a.Hkv, planned);
+        Walk8 walk(a.p, a.T, a.Hkv);
         const Walk& w = walk.w;
         while (ok && walk.next()) {
             const int n = w.k1 - w.k0;
@@ -730,11 +728,12 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
         constexpr int kLanes = D / 8, kStep = 32 / kLanes;                              // lanes of a row, eight elements each; rows at a time
         const int sub = lane / kLanes, d = lane % kLanes;
         const uint32_t inv_G = (65536 + a.G - 1) / a.G;                                 // r / G for the few rows there are
-        const bool causal = planned && a.p.header->causal;
         uint32_t n_q = 0;
         bool ok = true;
-        Walk8 walk(a.p, a.Hkv, planned);
+        Walk8 walk(a.p, a.T, a.Hkv);
         const Walk& w = walk.w;
+        const bool causal = w.planned && a.p.header->causal;
+        if (!w.planned && blockIdx.x == 0 && lane == 0) report(a.status, STATUS_BAD_TOKEN, -1);
         for (;;) {
             const bool piece = walk.next();
             const int slot = n_q & 1, R = piece ? w.u.ntok * a.G : 0, RP = columns(R);

@@ -728,6 +728,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
         constexpr int kLanes = D / 8, kStep = 32 / kLanes;                              // lanes of a row, eight elements each; rows at a time
         const int sub = lane / kLanes, d = lane % kLanes;
         const uint32_t inv_G = (65536 + a.G - 1) / a.G;                                 // r / G for the few rows there are
+        const int64_t gap = a.q_stride - a.G * D;                                       // from a token's last row of the head to the next one's first
         uint32_t n_q = 0;
         bool ok = true;
         Walk8 walk(a.p, a.T, a.Hkv);
@@ -739,14 +740,14 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             const int slot = n_q & 1, R = piece ? w.u.ntok * a.G : 0, RP = columns(R);
             const uint32_t qb = smem0 + L::kOffQ + slot * L::kQ;
             Meta& mt = meta[slot];
+            const uint16_t* const q0 = a.q + (int64_t)w.u.row0 * a.q_stride + w.head * a.G * D + d * 8;
             auto read = [&](int r) {
                 if (r >= R) return make_uint4(0, 0, 0, 0);
-                const int t = (r * inv_G) >> 16;
-                return __ldg(reinterpret_cast<const uint4*>(a.q + (int64_t)(w.u.row0 + t) * a.q_stride + (w.head * a.G + r - t * a.G) * D + d * 8));
+                return __ldg(reinterpret_cast<const uint4*>(q0 + r * D + ((r * inv_G) >> 16) * gap));
             };
             const bool tiles = piece && w.k1 > w.k0;
             uint32_t big = 0;                          // magnitude bits of the largest element
-            uint4 ahead = make_uint4(0, 0, 0, 0);
+            uint4 ahead[2] = {};
             if (tiles) {                               // while the buffer is not free yet
 #pragma unroll 1
                 for (int first = 0; first < R; first += 4 * kStep) {
@@ -758,7 +759,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                         big = __vmaxu2(big, __vmaxu2(__vmaxu2(v[i].x & 0x7fff7fffu, v[i].y & 0x7fff7fffu), __vmaxu2(v[i].z & 0x7fff7fffu, v[i].w & 0x7fff7fffu)));
                 }
                 big = __reduce_max_sync(0xffffffffu, max(big & 0xffffu, big >> 16));
-                ahead = read(sub);
+                ahead[0] = read(sub), ahead[1] = read(sub + kStep);
             }
             const bool odd = big >= 0x7f80u;           // some value is no number: the largest of the others
             if (odd) {
@@ -779,28 +780,42 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             const float f = __uint_as_float((uint32_t)(k + 127) << 23);
             if (n_q >= 2 && !(ok = wait(q_empty + 8 * slot, (n_q >> 1) - 1))) break;
             if (tiles) {
+                // A row's 16-byte pieces are exchanged by its number (the swizzle), of which a term changes one bit at most.
+                const bool apart = RP <= kApart;
+                const uint32_t term = (apart ? 4 : RP) * D, flip = apart ? D / 2 : 0;
+                auto place = [&](int r) {
+                    const int row = apart ? 3 * (r & ~3) + (r & 3) : r;
+                    return qb + row * D + (((d >> 1) ^ (D == 128 ? row & 7 : row >> 1 & 3)) << 4) + (d & 1) * 8;
+                };
 #pragma unroll 1
-                for (int first = 0; first < RP; first += kStep) {
-                    const int r = first + sub;
-                    const uint32_t word[4] = {ahead.x, ahead.y, ahead.z, ahead.w};
-                    ahead = read(r + kStep);
-                    uint32_t h[4], t0[3], t1[3];
+                for (int first = 0; first < RP; first += 2 * kStep) {                   // two rows per lane: one hides the other's latency
+                    const uint4 now[2] = {ahead[0], ahead[1]};
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) h[j] = pack_half(__uint_as_float(word[j] << 16) * f, __uint_as_float(word[j] & 0xffff0000u) * f);
-                    split4<false>(h[0], h[1], t0);
-                    split4<false>(h[2], h[3], t1);
-                    if (odd) {                         // a row with such a value is none: not a number in all its elements
+                    for (int i = 0; i < 2; ++i) ahead[i] = read(first + (2 + i) * kStep + sub);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t word[4] = {now[i].x, now[i].y, now[i].z, now[i].w};
+                        uint32_t h[4], t0[3], t1[3];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) h[j] = pack_half(__uint_as_float(word[j] << 16) * f, __uint_as_float(word[j] & 0xffff0000u) * f);
+                        split4<false>(h[0], h[1], t0);
+                        split4<false>(h[2], h[3], t1);
+                        const uint32_t to = place(first + i * kStep + sub);
+#pragma unroll
+                        for (int t = 0; t < 3; ++t)
+                            asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"((t == 1 ? to ^ flip : to) + t * term), "r"(t0[t]), "r"(t1[t]) : "memory");
+                    }
+                }
+                if (odd) {                             // a row with such a value is none: not a number in all its elements
+#pragma unroll 1
+                    for (int first = 0; first < R; first += kStep) {
+                        const uint4 v = read(first + sub);
+                        const uint32_t word[4] = {v.x, v.y, v.z, v.w};
                         bool none = false;
 #pragma unroll
                         for (int j = 0; j < 4; ++j) none = none || (word[j] & 0x7fffu) >= 0x7f80u || (word[j] >> 16 & 0x7fffu) >= 0x7f80u;
-                        if (__ballot_sync(0xffffffffu, none) >> (sub * kLanes) & (uint32_t)((1ull << kLanes) - 1)) t0[0] = t1[0] = 0x7f7f7f7fu;
-                    }
-#pragma unroll
-                    for (int t = 0; t < 3; ++t) {
-                        const int row = RP <= kApart ? 3 * (r & ~3) + 4 * t + (r & 3) : t * RP + r;
-                        // the swizzle exchanges 16-byte pieces by the row
-                        const int piece16 = (d >> 1) ^ (D == 128 ? row & 7 : row >> 1 & 3);
-                        asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(qb + row * D + piece16 * 16 + (d & 1) * 8), "r"(t0[t]), "r"(t1[t]) : "memory");
+                        if (__ballot_sync(0xffffffffu, none) >> (sub * kLanes) & (uint32_t)((1ull << kLanes) - 1))
+                            asm volatile("st.shared.v2.b32 [%0], {%1, %1};" ::"r"(place(first + sub)), "r"(0x7f7f7f7f) : "memory");
                     }
                 }
                 int lo_max = 0, hi_min = 0x7fffffff;

@@ -527,55 +527,55 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             else if (n_ch == 4) tiles(std::integral_constant<int, 4>());
             else tiles(std::integral_constant<int, 5>());
             if (out) break;
-            // ---- the piece's rows
-            const float m_run = tid < RP ? -st.neg[tid] : 0.f;
+            // ---- the piece's rows; what needs no product, while the last one is under way
+            softmax_sync();
+            const int64_t part0 = (int64_t)part * kMaxRows, orow0 = (int64_t)mt.row0 * a.Hq + mt.head * G;
+            if (tid < R) {
+                const float m_run = -st.neg[tid], l = (st.top[0][tid] + st.top[1][tid]) + (st.top[2][tid] + st.top[3][tid]);
+                float f = l != 0.f ? 1.f : 0.f;        // a sum of zero: nothing was seen, O may be anything
+                // A row whose sum is no number joins with a reference of infinity: all factors are then 0 or not a number.
+                if (part >= 0) {
+                    *reinterpret_cast<float2*>(a.p.part_ml + (part0 + tid) * 2) = make_float2(l != l ? INFINITY : (l == 0.f ? -INFINITY : m_run), l);
+                } else {
+                    if (l != 0.f) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f) : "f"(l));
+                    if (a.lse) a.lse[orow0 + (tid / G) * a.Hq + tid % G] = l == 0.f ? -INFINITY : (m_run + log2f(l)) * kLn2;
+                }
+                st.fac[tid] = f;
+            }
             hold(o_done, n_t - 1);
             if (!anew(n_q + 1)) break;
             tc_fence_after();
-            const int64_t part0 = (int64_t)part * kMaxRows;
-            if (tid < R) {
-                const float l = (st.top[0][tid] + st.top[1][tid]) + (st.top[2][tid] + st.top[3][tid]);
-                // A row whose sum is no number joins with a reference of infinity: all factors are then 0 or not a number.
-                if (part >= 0) *reinterpret_cast<float2*>(a.p.part_ml + (part0 + tid) * 2) = make_float2(l != l ? INFINITY : (l == 0.f ? -INFINITY : m_run), l);
-                else if (a.lse) a.lse[(int64_t)(mt.row0 + tid / G) * a.Hq + mt.head * G + tid % G] = l == 0.f ? -INFINITY : (m_run + log2f(l)) * kLn2;
-            }
             // O is [dim][half, chunk, term, row]: a thread has one dim (64 dims sit on 16 lanes of each quarter) and its half of the rows
-            const bool live = D == 128 || lane < 16;
-            const int d = D == 128 ? key : q * 16 + lane;
+            const bool live = D == 128 || lane < 16, whole = part < 0;
             const float scale_v = ref_v == kNoScale ? 0.f : __uint_as_float((uint32_t)(ref_v + 127) << 23);
-            int tok = r0 / G, g = r0 - tok * G;
-            const int64_t orow0 = (int64_t)mt.row0 * a.Hq + mt.head * G;
-            auto rows = [&](int ch, const uint32_t* y) {
-                const float4 l4 = *reinterpret_cast<const float4*>(st.top[0] + r0 + ch * 4);
-                const float4 la = *reinterpret_cast<const float4*>(st.top[1] + r0 + ch * 4), lb = *reinterpret_cast<const float4*>(st.top[2] + r0 + ch * 4),
-                             lc = *reinterpret_cast<const float4*>(st.top[3] + r0 + ch * 4);
-                const float l[4] = {(l4.x + la.x) + (lb.x + lc.x), (l4.y + la.y) + (lb.y + lc.y), (l4.z + la.z) + (lb.z + lc.z), (l4.w + la.w) + (lb.w + lc.w)};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int r = r0 + ch * 4 + j;
-                    float f = 1.f;                     // a sum of zero: nothing was seen, O may be anything
-                    if (part < 0) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f) : "f"(l[j]));
-                    const float sum = fmaf(fmaf(__uint_as_float(y[8 + j]), 1.f / kLow, __uint_as_float(y[4 + j])), 1.f / kMid, __uint_as_float(y[j]));
-                    const float v = l[j] != 0.f ? sum * f * scale_v : 0.f;
-                    if (live && r < R) {
-                        if (part >= 0) {
-                            a.p.part_acc[(part0 + r) * D + d] = v;
-                        } else {
-                            const __nv_bfloat16 b = __float2bfloat16_rn(v);
-                            a.o[(orow0 + (int64_t)tok * a.Hq + g) * D + d] = *reinterpret_cast<const uint16_t*>(&b);
-                        }
-                    }
-                    if (++g == G) g = 0, ++tok;
-                }
-            };
+            int g = r0 % G;
+            const int size = whole ? 2 : 4, jump = whole ? (a.Hq - G) * D * 2 : 0;      // bytes of a value; from a token's last row of the head to the next one's first
+            char* to = whole ? reinterpret_cast<char*>(a.o + (orow0 + (int64_t)(r0 / G) * a.Hq + g) * D) : reinterpret_cast<char*>(a.p.part_acc + (part0 + r0) * D);
+            to += (D == 128 ? key : q * 16 + lane) * size;
 #pragma unroll 1
             for (int ch = 0; ch < n_ch; ++ch) {
                 if (r0 + ch * 4 >= R) break;
                 uint32_t y[12];
 #pragma unroll
                 for (int t = 0; t < 3; ++t) tmem_ld4(tmem_o + ch * 12 + t * 4, y + 4 * t);
+                const float4 f4 = *reinterpret_cast<const float4*>(st.fac + r0 + ch * 4);
+                const float f[4] = {f4.x, f4.y, f4.z, f4.w};
                 tmem_wait<12>(y);
-                rows(ch, y);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float sum = fmaf(fmaf(__uint_as_float(y[8 + j]), 1.f / kLow, __uint_as_float(y[4 + j])), 1.f / kMid, __uint_as_float(y[j]));
+                    const float v = f[j] != 0.f ? sum * f[j] * scale_v : 0.f;
+                    if (live && r0 + ch * 4 + j < R) {
+                        if (whole) {
+                            const __nv_bfloat16 b = __float2bfloat16_rn(v);
+                            *reinterpret_cast<uint16_t*>(to) = *reinterpret_cast<const uint16_t*>(&b);
+                        } else {
+                            *reinterpret_cast<float*>(to) = v;
+                        }
+                    }
+                    to += D * size;
+                    if (++g == G) g = 0, to += jump;
+                }
             }
             tc_fence_before();
             __syncwarp();

@@ -154,6 +154,7 @@ class Cta:
                 self.bars["p_full",].arrive()
                 n_t += 1
             if n:
+                yield ("meet", w)                      # the rows' sums
                 yield from hold(("o_done",), n_t - 1)
             yield from hold(("q_full", (n_q + 1) & 1), (n_q + 1) >> 1)
             if not (yield from agreed()):

@@ -20,15 +20,22 @@ constexpr float kLn2 = 0.6931471805599453f;
 // Where groups' shared keys are more than half of the work, the tiles of the requests' own keys take longer (their few CTAs wait
 // for memory that the others keep busy): 256 requests of 3 to 5 rows behind 32 777 keys, over up to 2000 of their own, 703 us
 // with 4, 7 and three tiles against 835; behind 4000 keys 304 against 292, 64 single tokens behind 4000 57 against 53.
+// The 8-bit attention has its rows on the columns, so a tile costs by their number (512 requests over 2048 keys: 3 and 4 rows of
+// four heads 361 and 368 us, 5 rows 411, 9 rows 548): 512 requests of 3 to 5 rows over 128 to 4096 keys 415 us with tiles weighed
+// so, 437 with all alike; 1 to 9 rows over 64 to 1024 keys 308 against 327.  A unit as 4 tiles: 427 and 421 with 2 and 3, 419 to
+// 429 with 5 to 8.
 struct ChunkCost {
     int32_t one, two, unit;                            // a tile in a unit of one and of two row tiles; a unit, in tiles
+    int32_t rows;                                      // not 0: a tile costs four and one for every eight of the rows stacked in it, up to this many
 };
 __device__ __forceinline__ void report(int32_t* status, int32_t bit, int r) {
     atomicOr(status, bit);
     atomicCAS(status + 1, 0, r + 1);
 }
 
-__device__ __forceinline__ int tile_cost(const ChunkCost& c, const ChunkUnit& u, int T) { return u.ntok > T ? c.two : c.one; }
+__device__ __forceinline__ int tile_cost(const ChunkCost& c, const ChunkUnit& u, int T) {
+    return c.rows ? 4 + (u.ntok * c.rows + 8 * T - 1) / (8 * T) : (u.ntok > T ? c.two : c.one);
+}
 __device__ __forceinline__ int64_t unit_cost(const ChunkCost& c, const ChunkUnit& u, int T) { return ((int64_t)u.n_tiles + c.unit) * tile_cost(c, u, T); }
 
 // ---- plan -------------------------------------------------------------------------------------
@@ -198,7 +205,7 @@ chunk_split_kernel(const PlanArgs a) {
     auto unit = [&](int64_t i) { return i == i0 ? only : raw(i); };
     int n_mine = 0;
     int64_t c_mine = 0;
-    ChunkCost k{1, 2, a.p.kind.unit_tiles};
+    ChunkCost k{1, 2, a.p.kind.unit_tiles, a.p.kind.tiles == 1 ? a.p.kind.rows : 0};
     if (a.p.kind.sides == 2) {
         __shared__ unsigned long long sides[2];
         if (tid < 2) sides[tid] = 0;
@@ -214,7 +221,7 @@ chunk_split_kernel(const PlanArgs a) {
             if (lane == 0 && mine[s]) atomicAdd(&sides[s], mine[s]);
         }
         __syncthreads();
-        if (sides[1] > sides[0]) k = ChunkCost{4, 7, 3};
+        if (sides[1] > sides[0]) k = ChunkCost{4, 7, 3, 0};
     }
     for (int64_t i = i0; i < i1; ++i) {
         const ChunkUnit u = unit(i);

@@ -547,9 +547,9 @@ chunk_attn_kernel(const __grid_constant__ AttnArgs a) {
             int pos = w.u.pos0 + t_row;
             if (live) {
                 if constexpr (MODE & MODE_GROUPS) {
-                    const int64_t at = row + (w.u.side ? a.p.max_rows : 0);
-                    lo = a.p.row_lo[at], hi = a.p.row_hi[at];
-                    if constexpr (MODE & MODE_BIAS) pos = a.p.row_pos[row];
+                    // from the group's last shared key to the row's own, or all shared ones: both in the unit, no trip to memory
+                    lo = w.u.key_lo, hi = w.u.side ? w.u.key_hi : pos + 1;
+                    if constexpr (MODE & MODE_BIAS) pos = w.u.side ? a.p.row_pos[row] : pos;
                 } else {
                     if (ph & CAUSAL) hi = pos + 1;
                     else lo = a.p.row_lo[row], hi = a.p.row_hi[row];

@@ -1162,7 +1162,7 @@ static nsd_status copy8_impl(nsd_ctx* ctx, bool pack, void* kv_pool, void* kv8, 
     if (!kv_pool || !kv8 || !scales || !src || !dst) return NSD_ERR_INVALID_ARG;
     if (misaligned(kv_pool, 16) || misaligned(kv8, 16) || misaligned(scales, 16)) return NSD_ERR_INVALID_ARG;
     const Kv8Copy c{ctx->shape, static_cast<uint16_t*>(kv_pool), static_cast<uint8_t*>(kv8), static_cast<uint8_t*>(scales), n_blocks, src, dst,
-                    layer_begin, layer_count, ctx->cfg.num_slabs, ctx->n_sms, ctx->d_status};
+                    layer_begin, layer_count, ctx->cfg.num_slabs, ctx->d_status};
     const OnDevice on(ctx->device);
     NSD_CUDA(ctx, on.err);
     NSD_CUDA(ctx, pack ? launch_kv8_pack(c, static_cast<cudaStream_t>(stream)) : launch_kv8_unpack(c, static_cast<cudaStream_t>(stream)));

@@ -251,7 +251,7 @@ struct Kv8Copy {
     uint8_t *codes, *scales;
     int64_t n_blocks;
     const int32_t *src, *dst;
-    int32_t layer_begin, layer_count, num_slabs, n_sms;
+    int32_t layer_begin, layer_count, num_slabs;
     int32_t* status;
 };
 cudaError_t launch_kv8_pack(const Kv8Copy& c, cudaStream_t stream);      // pool -> codes and scales

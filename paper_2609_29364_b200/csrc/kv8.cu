@@ -13,8 +13,9 @@ namespace {
 // layers), so that no thread divides to find its place (with one flat index, taken apart by three
 // 64-bit divisions, 2048 blocks of 4 layers took 336 and 288 us), and the loads of kAhead tiles are
 // under way together (4: 162 and 135 us, 16: 180 and 130).  A CTA takes one pair (16 CTAs per SM
-// that take several: 151 and 137).  2048 blocks of 4 layers (8 kv heads of 128) 150 us packed = 5.4
-// TB/s, 130 unpacked = 6.2 TB/s; 67 blocks 6.8 and 5.3 us.
+// that take several: 151 and 137).  2048 blocks of 4 layers (8 kv heads of 128) 140 us packed = 5.8
+// TB/s (149 with a row's maximum of floats instead of packed bits), 130 unpacked = 6.2 TB/s; 67
+// blocks 6.8 and 5.3 us.
 constexpr int kBsP = 16;
 constexpr int kThreadsP = 256;
 constexpr int kAhead = 8;
@@ -58,19 +59,29 @@ kv8_copy_kernel(const __grid_constant__ Kv8Copy c) {
                 for (int i = 0; i < kAhead; ++i) {
                     if (t0 + i * kPerCta >= tiles) break;
                     const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-                    float x[8], top = 0.f;
+                    // magnitudes order as their bits do, two at a time
+                    uint32_t top = 0;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        x[2 * j] = __uint_as_float(v[j] << 16), x[2 * j + 1] = __uint_as_float(v[j] & 0xffff0000u);
-                        top = fmaxf(top, fmaxf(kv8_magnitude(x[2 * j]), kv8_magnitude(x[2 * j + 1])));
+                    for (int j = 0; j < 4; ++j) top = __vmaxu2(top, v[j] & 0x7fff7fffu);
+#pragma unroll
+                    for (int s = kLanes / 2; s > 0; s >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, s));
+                    top = max(top & 0xffffu, top >> 16);
+                    float x[8];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[2 * j] = __uint_as_float(v[j] << 16), x[2 * j + 1] = __uint_as_float(v[j] & 0xffff0000u);
+                    if (__any_sync(0xffffffffu, top >= 0x7f80u)) {                      // no number in a row of the warp: the largest of the others
+                        float m = 0.f;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) m = fmaxf(m, kv8_magnitude(x[j])), x[j] = fmaf(x[j], 0.f, x[j]);
+#pragma unroll
+                        for (int s = kLanes / 2; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
+                        top = __float_as_uint(m) >> 16;
                     }
-#pragma unroll
-                    for (int s = kLanes / 2; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-                    const uint32_t byte = kv8_scale_byte(top);
+                    const uint32_t byte = kv8_scale_byte(__uint_as_float(top << 16));
                     const float inv = kv8_inverse(byte);
                     uint2 out;
-                    out.x = kv8_codes2(x[0], x[1], inv) | kv8_codes2(x[2], x[3], inv) << 16;
-                    out.y = kv8_codes2(x[4], x[5], inv) | kv8_codes2(x[6], x[7], inv) << 16;
+                    out.x = kv8_codes2_finite(x[0], x[1], inv) | kv8_codes2_finite(x[2], x[3], inv) << 16;
+                    out.y = kv8_codes2_finite(x[4], x[5], inv) | kv8_codes2_finite(x[6], x[7], inv) << 16;
                     *reinterpret_cast<uint2*>(at8 + i * kStep) = out;
                     if (d0 == 0) *scale_at(i) = (uint8_t)byte;
                 }

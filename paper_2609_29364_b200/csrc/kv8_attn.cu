@@ -37,11 +37,11 @@ namespace {
 // Pieces that a CTA boundary cuts leave their O and statistics in the plan, and chunk_join_kernel joins them in order.
 //
 // What bounds it: single tokens HBM (512 over 2048 keys each, 32 q heads and 8 kv heads of 128: 341 us = 6.3 TB/s, 0.98 of
-// the copy rate; the 16-bit kernel reads twice the bytes); five rows per request the chain of a tile's softmax (427 us = 5.1
-// TB/s; 3 to 5 rows over 128 to 4096 keys 444); ten rows (40 stacked) 130 us for 4 x 60 000 keys = 3.8 TB/s; 64 single tokens
-// over 512 to 2048 keys 40 us, of which some 15 are the start, the last pieces and the join; 512 x 256 keys 98 us: a piece of two
-// or three tiles costs as much again in its beginning and end.  D = 64 halves the bytes but not the softmax: 512 x 5 rows
-// over 2048 keys 390 us.  The instructions of a tile matter more than their number of cycles alone: with a longer loop
+// the copy rate; the 16-bit kernel reads twice the bytes); five rows per request the chain of a tile's softmax (410 us = 5.3
+// TB/s; 3 to 5 rows over 128 to 4096 keys 416); ten rows (40 stacked) 124 us for 4 x 60 000 keys = 4.0 TB/s; 64 single tokens
+// over 512 to 2048 keys 40 us, of which some 15 are the start, the last pieces and the join; 512 x 256 keys 96 us, with five rows
+// 148: a piece of two or three tiles costs as much again in its beginning and end (its queries, the first references, rows out).  D = 64 halves the bytes but not the softmax: 512 x 5 rows
+// over 2048 keys 366 us.  The instructions of a tile matter more than their number of cycles alone: with a longer loop
 // (waits with time limits, eight rows of Q at a time, a fourth term) the SM's instruction cache no longer held it and times rose
 // by a fifth.
 //

@@ -26,13 +26,15 @@ __device__ __forceinline__ float kv8_inverse(uint32_t byte) { return __uint_as_f
 __device__ __forceinline__ float kv8_scale(uint32_t byte) {
     return __uint_as_float(byte == 0 ? 0x00400000u : (byte == 255 ? 0x7fc00000u : byte << 23));
 }
-// Two codes, round to nearest even; the lower byte is lo.  Infinities become NaN instead of the largest code.
-__device__ __forceinline__ uint32_t kv8_codes2(float lo, float hi, float inverse) {
-    lo *= inverse, hi *= inverse;
-    lo = fmaf(lo, 0.f, lo), hi = fmaf(hi, 0.f, hi);
+// Two codes, round to nearest even; the lower byte is lo.  Infinities become the largest code: only for rows that have none.
+__device__ __forceinline__ uint32_t kv8_codes2_finite(float lo, float hi, float inverse) {
     uint16_t r;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi * inverse), "f"(lo * inverse));
     return r;
+}
+// For any row: infinities become NaN.
+__device__ __forceinline__ uint32_t kv8_codes2(float lo, float hi, float inverse) {
+    return kv8_codes2_finite(fmaf(lo, 0.f, lo), fmaf(hi, 0.f, hi), inverse);
 }
 __device__ __forceinline__ float2 kv8_values2(uint32_t codes) {          // of the lower two bytes
     uint32_t h;

@@ -166,6 +166,33 @@ def test_what_is_not_a_number_stays_with_the_rows_that_see_it():
     assert ((b.o[0, :7].double().cpu() - o_ref.cpu()).abs() <= 2.0 ** -8 * o_ref.cpu().abs() + 2.0 ** -9 * mag.cpu() + 1e-3)[good].all()
 
 
+@pytest.mark.parametrize("tokens", [1, 3, 6, 9])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_queries_that_are_no_numbers_leave_the_other_rows(dim, tokens):
+    """Rows with a NaN or an infinity among up to 36 stacked ones, beside rows of every size: these are right to the same limit
+    as without them (the limit of check_attn8, whose first two terms are below 2^-8 |o| + 2^-9 of the weighted |v|)."""
+    b = Batch8([100, 300], [tokens, tokens], heads=8, kv_heads=2, dim=dim, seed=30 + tokens)
+    b.q *= torch.exp2(torch.arange(-6, 2, device=DEV).float())[None, None, :].repeat_interleave(dim, -1).to(torch.bfloat16)
+    bad = torch.zeros((2 * tokens, 8), dtype=torch.bool, device=DEV)
+    for i, x in enumerate((float("nan"), float("inf"), float("-inf"))):
+        row, head, at = (i * 5 + 1) % (2 * tokens), (3 * i + 2) % 8, (i * 37 + dim - 1) % dim
+        b.q[0, row, head * dim + at] = x
+        bad[row, head] = True
+    b.q[0, tokens, 7 * dim:] = float("nan")                             # a whole row
+    bad[tokens, 7] = True
+    c = b.context()
+    b.attn(c, b.plan(c))
+    assert c.nsd_get_status() == (0, -1)
+    assert torch.equal(torch.isnan(b.lse[0, :2 * tokens]), bad)
+    assert torch.equal(torch.isnan(b.o[0, :2 * tokens]).all(-1), bad) and torch.equal(torch.isnan(b.o[0, :2 * tokens]).any(-1), bad)
+    b.q.copy_(torch.nan_to_num(b.q, nan=0.0, posinf=0.0, neginf=0.0))
+    o_ref, lse_ref, mag = (t.cpu() for t in b.reference())
+    good = ~bad.cpu()
+    limit = 2.0 ** -8 * o_ref.abs() + 2.0 ** -9 * mag + 2.0 ** -24 * (300 + tokens) * float(b.values[0, :, 1].abs().max())
+    assert ((b.o[0, :2 * tokens].double().cpu() - o_ref).abs() <= limit)[good].all()
+    assert ((b.lse[0, :2 * tokens].double().cpu() - lse_ref).abs() <= 2.0 ** -10 + 2.0 ** -20 * lse_ref.abs())[good].all()
+
+
 def test_bad_blocks_and_short_tables_are_reported():
     b = Batch8([100, 50], [1, 1], seed=21)
     c = b.context()

@@ -176,6 +176,30 @@ def test_pack_and_unpack(shape, blocks):
     assert torch.equal(pool[1:, to.long()].cpu(), want)
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+def test_pack_keeps_what_is_not_a_number_to_itself(dim):
+    """NaN and infinities become NaN codes and do not count towards their row's scale; rows beside them in a warp, of zeros, of
+    subnormal numbers and of the largest ones are as ever."""
+    c = T.context(4, 2, dim, num_blocks=3)
+    x = rows_like_a_model(3 * 2 * BS, 2, dim, 9, torch.bfloat16).reshape(1, 3, 2, BS, 2, dim).transpose(3, 4).contiguous()
+    nan, inf, most, least = float("nan"), float("inf"), torch.finfo(torch.bfloat16).max, 2.0 ** -133
+    x[0, 0, 0, 0, 3, 5], x[0, 0, 0, 0, 3, 6] = nan, most
+    x[0, 0, 1, 1, 4, dim - 1] = inf
+    x[0, 0, 1, 1, 5] = 0.0
+    x[0, 0, 1, 1, 6] *= -0.0
+    x[0, 1, 0, 0, 0], x[0, 1, 0, 0, 1], x[0, 1, 0, 0, 2], x[0, 1, 0, 0, 4] = -inf, nan, most, -most
+    x[0, 1, 1, 0, 15] = torch.arange(dim).to(torch.bfloat16) * least
+    x[0, 1, 1, 0, 14] = least
+    x[0, 1, 1, 0, 14, 0] = inf
+    kv8, scales, _ = cache(c)
+    ids = torch.tensor([0, 1], dtype=torch.int32)
+    c.nsd_kv8_pack(gpu(x), kv8, scales, gpu(ids), gpu(ids))
+    values, e = K.quantise(x.double().numpy()[:, :2])
+    assert np.array_equal(K.code_values(kv8[:, :2]), values, equal_nan=True)
+    assert np.array_equal(scales[:, :2].cpu().numpy(), np.swapaxes(e + 127, 2, 3))
+    assert c.nsd_get_status() == (0, -1) and (kv8[:, 2] == 0xA5).all()
+
+
 def test_every_code_and_scale_unpacks_to_its_value():
     c = T.context(2, 2, 128, num_blocks=16)
     codes = torch.arange(256, dtype=torch.uint8).repeat(16 * 2 * 2 * BS * 128 // 256).reshape(1, 16, 2, 2, BS, 128).clone()

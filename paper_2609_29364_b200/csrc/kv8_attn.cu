@@ -355,7 +355,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                     const bool none = kb > 247 || vb > 247;
                     const float kk = none ? (masked ? 1.f : __uint_as_float(0x7fc00000u)) : fmaxf(__uint_as_float((kb + 7) << 23) * mt.c, 1.17549435e-38f);
                     const uint64_t kk2 = pair(kk, kk);
-                    const int ev = seen ? (int)vb - 127 : kNoScale;
+                    const int ev = seen && !none ? (int)vb - 127 : kNoScale;            // of a key that makes its rows NaN: nothing, for the other rows
                     constexpr bool kTerms = 8 * NC <= kApart;
                     const uint32_t tmem_s = tmem + (n_t & 1) * 64 + lanes + (kTerms ? 3 * r0 : r0);
                     // Scores are hidden where they lie, in a loop of its own: rare, and out of the way of the others.
@@ -408,7 +408,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                     }
                     __syncwarp();
                     if (lane == 0) mbar_arrive(k_empty + 8 * stage);                    // S is complete and the scales are read
-                    int dev = seen ? ev - ref_v : 0;
+                    int dev = ev - ref_v;
                     if (fail) st.fail[turn] = 1;
                     any = any_of_softmax(fail || pending || fmaxf(top[0], top[1]) + (float)max(dev, -40) > kMost);
                     turn ^= 1;
@@ -466,7 +466,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                             tmem_wait_st();
                         }
                         ref_v = ref;
-                        dev = seen ? ev - ref_v : 0;
+                        dev = ev - ref_v;
 #pragma unroll
                         for (int ch = 0; ch < NC; ++ch) {
                             const float4 up = *reinterpret_cast<const float4*>(st.step + r0 + ch * 4);

@@ -1,0 +1,32 @@
+"""Attention over the 8-bit cache where rows of V differ by many powers of two, each row held to a limit of its own."""
+import numpy as np
+import pytest
+import torch
+
+from chunk_testlib import DEV
+from kv8_range_testlib import Range8
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("byte", [248, 250, 254, 255])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_a_scale_that_is_none_stays_with_the_rows_that_see_it(dim, byte):
+    """The power of two of V, or of K, of a drafted token: only the rows from that token on see it."""
+    for kv in (0, 1):
+        b = Range8([200, 40, 130], [4, 3, 1], dim=dim, seed=byte)
+        spoilt = []
+        for request, token, first in ((0, 203, 3), (1, 41, 5)):
+            block, slot = b.place(request, token)
+            b.scales[0, block, 1, kv, slot] = byte
+            spoilt += list(range(first, 4 if request == 0 else 7))
+        c = b.context()
+        b.attn(c, b.plan(c))
+        assert c.nsd_get_status() == (0, -1)
+        bad = torch.zeros((b.rows, b.heads), dtype=torch.bool, device=DEV)
+        bad[spoilt, b.heads // 2:] = True
+        assert torch.equal(torch.isnan(b.o[0]).all(-1), bad) and torch.equal(torch.isnan(b.o[0]).any(-1), bad)
+        assert torch.equal(torch.isnan(b.lse[0]), bad)
+        b.o[0][bad], b.lse[0][bad] = 0.0, 0.0
+        good = [r for r in range(b.rows) if r not in spoilt]
+        b.close(rows=good)

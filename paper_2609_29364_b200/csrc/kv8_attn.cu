@@ -532,10 +532,14 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             const int64_t part0 = (int64_t)part * kMaxRows, orow0 = (int64_t)mt.row0 * a.Hq + mt.head * G;
             if (tid < R) {
                 const float m_run = -st.neg[tid], l = (st.top[0][tid] + st.top[1][tid]) + (st.top[2][tid] + st.top[3][tid]);
-                float f = l != 0.f ? 1.f : 0.f;        // a sum of zero: nothing was seen, O may be anything
-                // A row whose sum is no number joins with a reference of infinity: all factors are then 0 or not a number.
+                float f = 0.f;                         // a sum of zero: nothing was seen, O may be anything
+                // V's power of two is shared out between a piece's sum and its products, half each, so that both stay in range wherever V
+                // lies; f is what the products get.  A row whose sum is no number joins with a reference of infinity: all factors are then
+                // 0 or not a number.
                 if (part >= 0) {
-                    *reinterpret_cast<float2*>(a.p.part_ml + (part0 + tid) * 2) = make_float2(l != l ? INFINITY : (l == 0.f ? -INFINITY : m_run), l);
+                    const float m = m_run + (float)(ref_v >> 1), by = m - m_run;         // what the reference has moved by after its rounding
+                    if (l != 0.f) f = l == l ? exp2f((float)ref_v - by) : l;
+                    *reinterpret_cast<float2*>(a.p.part_ml + (part0 + tid) * 2) = make_float2(l != l ? INFINITY : (l == 0.f ? -INFINITY : m), l != 0.f ? l * exp2f(-by) : 0.f);
                 } else {
                     if (l != 0.f) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f) : "f"(l));
                     if (a.lse) a.lse[orow0 + (tid / G) * a.Hq + tid % G] = l == 0.f ? -INFINITY : (m_run + log2f(l)) * kLn2;
@@ -547,7 +551,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             tc_fence_after();
             // O is [dim][half, chunk, term, row]: a thread has one dim (64 dims sit on 16 lanes of each quarter) and its half of the rows
             const bool live = D == 128 || lane < 16, whole = part < 0;
-            const float scale_v = ref_v == kNoScale ? 0.f : __uint_as_float((uint32_t)(ref_v + 127) << 23);
+            const float scale_v = ref_v == kNoScale ? 0.f : (whole ? __uint_as_float((uint32_t)(ref_v + 127) << 23) : 1.f);
             int g = r0 % G;
             const int size = whole ? 2 : 4, jump = whole ? (a.Hq - G) * D * 2 : 0;      // bytes of a value; from a token's last row of the head to the next one's first
             char* to = whole ? reinterpret_cast<char*>(a.o + (orow0 + (int64_t)(r0 / G) * a.Hq + g) * D) : reinterpret_cast<char*>(a.p.part_acc + (part0 + r0) * D);

@@ -30,3 +30,16 @@ def test_a_scale_that_is_none_stays_with_the_rows_that_see_it(dim, byte):
         b.o[0][bad], b.lse[0][bad] = 0.0, 0.0
         good = [r for r in range(b.rows) if r not in spoilt]
         b.close(rows=good)
+
+
+@pytest.mark.parametrize("by", [117, 100, 60, -60, -100, -115])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_large_and_small_v_in_pieces_as_in_whole_units(dim, by):
+    """A context that many CTAs share, whose pieces are joined, and requests that each have one to themselves."""
+    b = Range8([20000], [2], dim=dim, heads=4, kv_heads=1, seed=by % 97)
+    b.shift_v(0, by)
+    b.run_close()
+    b = Range8([300] * 300, [1] * 300, dim=dim, heads=4, kv_heads=1, seed=by % 89)
+    for r in range(300):
+        b.shift_v(r, by)
+    b.run_close()

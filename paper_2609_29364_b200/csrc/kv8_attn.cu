@@ -86,7 +86,8 @@ struct __align__(16) Meta {                            // a piece, beside its Q 
     int row0, head, slot;                              // first token's row; kv head; partial slot or -1
     int key_first;                                     // of the first tile
     int key_lo, key_hi, gaps;                          // keys that some row sees: [key_lo, key_hi), unless there are gaps
-    float c;                                           // sc 2^-k 2^-7, where the rows were multiplied by 2^k
+    float c;                                           // sc 2^-k 2^-key_up, where the rows were multiplied by 2^k
+    int key_up;                                        // what is added to a key's exponent instead: 7, less where c would leave the normal numbers
 };
 struct __align__(16) State {
     float neg[kMaxRows];                               // minus the reference of each row's weights
@@ -351,9 +352,9 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                     // the scales came with K, which the issuer of S waited for
                     const unsigned char* const sb = smem + L::kOffScales + stage * (kBlocks * 32) + (key >> 4) * 32 + (key & 15);
                     const uint32_t kb = sb[0], vb = sb[16];
-                    // The key's power of two, times 2^7 against the rows' 2^-7, and theirs: not 0, so that a hidden score stays -inf.
+                    // The key's power of two, times 2^key_up against the rows' 2^-key_up, and theirs: not 0, so that a hidden score stays -inf.
                     const bool none = kb > 247 || vb > 247;
-                    const float kk = none ? (masked ? 1.f : __uint_as_float(0x7fc00000u)) : fmaxf(__uint_as_float((kb + 7) << 23) * mt.c, 1.17549435e-38f);
+                    const float kk = none ? (masked ? 1.f : __uint_as_float(0x7fc00000u)) : fmaxf(__uint_as_float((uint32_t)max((int)kb + mt.key_up, 0) << 23) * mt.c, 1.17549435e-38f);
                     const uint64_t kk2 = pair(kk, kk);
                     const int ev = seen && !none ? (int)vb - 127 : kNoScale;            // of a key that makes its rows NaN: nothing, for the other rows
                     constexpr bool kTerms = 8 * NC <= kApart;
@@ -842,8 +843,12 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             }
             if (lane == 0) {
                 mt.n = piece ? w.k1 - w.k0 : -1, mt.rows = R;
-                const int d0 = (-k - 7) >> 1, d1 = -k - 7 - d0;                         // sc 2^(-k - 7)
+                // Queries near the least numbers under a small scale: c keeps its bits, the keys' exponents take what it would fall below
+                // the normal numbers by (keys so small that theirs then fall below add nothing to a score).
+                const int least = (int)(__float_as_uint(a.sc) >> 23) - 127 - k - 7, under = max(-126 - least, 0);
+                const int d0 = (under - k - 7) >> 1, d1 = under - k - 7 - d0;           // sc 2^(-k - 7 + under)
                 mt.c = a.sc * __uint_as_float((uint32_t)(d0 + 127) << 23) * __uint_as_float((uint32_t)(d1 + 127) << 23);
+                mt.key_up = 7 - under;
                 if (piece) mt.row0 = w.u.row0, mt.head = w.head, mt.slot = w.slot, mt.key_first = (w.u.key_lo / kTileKeys + w.k0) * kTileKeys, mt.key_lo = w.u.key_lo, mt.key_hi = w.u.key_hi, mt.gaps = w.u.gaps;
             }
             fence_async_smem();

@@ -43,3 +43,18 @@ def test_large_and_small_v_in_pieces_as_in_whole_units(dim, by):
     for r in range(300):
         b.shift_v(r, by)
     b.run_close()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_small_queries_with_large_keys(dim):
+    """Queries near the least numbers against keys near the largest, under a small scale."""
+    b = Range8([300, 20, 140], [3, 1, 2], dim=dim, heads=8, kv_heads=2, seed=5)
+    b.q.mul_(2.0 ** -118)
+    held = b.scales != 255
+    b.scales[0, :, :, 0] = torch.where(held[0, :, :, 0], b.scales[0, :, :, 0] + 118, 255).to(torch.uint8)
+    b.values[0, :, 0] *= 2.0 ** 118
+    for scale in (0.1, 2.0 ** -9):
+        if scale < 0.01:
+            b.scales[0, :, :, 0] = torch.where(held[0, :, :, 0], b.scales[0, :, :, 0] + 5, 255).to(torch.uint8)
+            b.values[0, :, 0] *= 2.0 ** 5
+        b.run_close(scale=scale)

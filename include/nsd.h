@@ -684,8 +684,9 @@ nsd_status nsd_kv8_unpack(nsd_ctx* ctx, const void* kv8, const void* scales, voi
  * A NaN code in a visible V reaches the other rows of the same request that are computed with them
  * (up to 40 stacked rows).
  * fp32 accumulation and softmax statistics; q is multiplied exactly, but for what lies below 2^-30
- * of the largest element of the rows computed together (the terms of q end there); the weights are
- * rounded to 11 bits for the product with V.  A call gives the same bits every time; how a row's
+ * of the largest element of the rows computed together (the terms of q end there); a weight times its
+ * key's power of two is rounded to 11 bits for the product with V, or to 2^-25 of the row's largest such
+ * product where it is smaller, whatever V's powers of two.  A call gives the same bits every time; how a row's
  * sums are split, and so their last bits, depends on the batch.
  * Arguments and errors as nsd_chunk_plan / nsd_chunk_attn; scale 0 = 1/sqrt(head_dim).
  */

@@ -24,10 +24,16 @@ namespace {
 // Rows on the lanes, as in the 16-bit kernels, would leave 100 of 128 lanes idle at the sizes this is for, and put the
 // exponentials of 4 to 40 rows on one or two warps.
 //
-// The weights are 2^(s - m), with a reference m per row that is set in a piece's first tile so that its largest weight is 2^4,
-// and moved only when one would pass 2^15 (all softmax warps vote in every tile); V's powers of two likewise are taken
-// relative to the largest so far, so that a weight times them stays within 16 bits.  Sums of the weights are 32-bit and of
-// the unrounded ones, a thread's own until the end of the piece.
+// The weights are 2^(s - m).  What has to stay within 16 bits is a weight times its key's power of two, so the reference m of
+// a row is set by that product: in a piece's first tile so that the largest is 2^3, and moved only when one would pass 2^15.875
+// (61440 is where an e5m2 term would round to infinity; all softmax warps vote in every tile).  A row thus keeps the keys that make up
+// its output, whatever the V of keys that it gives no weight or does not see.  From 2^4 references would move twice as often (512
+// requests of 3 to 5 rows over 128 to 4096 keys: 416 us instead of 404).  Sums of the weights are 32-bit and of the unrounded ones, a
+// thread's own until the end of the piece.
+// One reference for both serves while V's powers of two lie in 2^-60 to 2^40 (kLow, kHigh): a weight is then at most 2^76, and the
+// sums of pieces can be joined in 32 bits.  A piece that meets another power where it sees to its references goes on in wide form
+// (wide_tile): the row's sum has a reference of its own (off), the products another (sh), both brought up to date in every tile, in
+// a function apart from the others.  It costs several times as long.
 //
 // Two CTAs per SM, each a pipeline of its own with an equal share of the line (request, kv head, unit, key tile), twelve warps:
 //   0-7   softmax: warp w has the keys of lane quarter w % 4 and one half of the rows; they also write the rows out
@@ -56,9 +62,10 @@ constexpr int kMaxRows = kKv8Kind.rows;
 constexpr int kThreads = 384, kSoftThreads = 256;
 constexpr int kWarpIssue = 8, kWarpV = 10, kWarpQ = 11;   // 9: the producer of K
 constexpr uint32_t kPollLimit = 1u << 21;              // polls of one wait, if nsd_config.wait_budget does not say: one that finds nothing takes 1.4 us, so three seconds
-constexpr float kTop = 4.f, kMost = 15.f;              // log2 of a row's largest weight when its reference is set, and at most
-constexpr float kMid = 8.f, kLow = 16.f;               // a weight's second term is held times kMid, its third times both
-constexpr int kNoScale = -1000;                        // exponent of V's reference before any
+constexpr float kTop = 3.f, kMost = 15.875f;           // log2 of a row's largest product when its reference is set, and at most
+constexpr int kLow = -60, kHigh = 40;                  // exponents of V that one reference serves
+constexpr float kMid = 8.f, kFine = 16.f;              // a weight's second term is held times kMid, its third times both
+constexpr int kNoScale = -1000;                        // exponent of a V that no row sees, or that makes its rows NaN
 
 __device__ __forceinline__ void report(int32_t* status, int32_t bit, int r) {
     atomicOr(status, bit);
@@ -91,11 +98,13 @@ struct __align__(16) Meta {                            // a piece, beside its Q 
 };
 struct __align__(16) State {
     float neg[kMaxRows];                               // minus the reference of each row's weights
-    float step[kMaxRows];                              // its last change
+    float off[kMaxRows];                               // the row's sum is of weights 2^-off: 0, but in wide form; -inf: no key seen yet
+    float sh[kMaxRows];                                // and its products of those times 2^sh: 0, but in wide form
+    float sum[kMaxRows];                               // in wide form the row's sum so far
+    float step[kMaxRows];                              // what the reference moves by
     float fac[kMaxRows];
-    int unset[kMaxRows];                               // the row has no reference yet
-    float top[4][kMaxRows];                            // a quarter's largest scores; at the end its sums
-    int exp_top[4];
+    float top[4][kMaxRows];                            // a quarter's largest products or weights; at the end its sums
+    volatile int go_wide, wide;                        // the piece has to go on in wide form; does so
     volatile int fail[2];                              // a warp has given up, by barriers in turn
 };
 
@@ -125,6 +134,11 @@ constexpr int kTmemCols = 256, kTmemO = 128;           // two buffers of S, 64 c
 // 426): then they are summed where they lie.
 constexpr int kApart = 16;
 
+__device__ __forceinline__ float max_over_lanes(float v) {               // of those that are numbers
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
 // Four rows' values over the lanes of a warp: row j on lanes 8 j .. 8 j + 7.
 template <typename Op>
 __device__ __forceinline__ float over_lanes(float (&v)[4], int lane, Op op) {
@@ -162,7 +176,7 @@ __device__ __forceinline__ void split4(uint32_t a, uint32_t b, uint32_t* terms) 
     if constexpr (FINE) ra = times(ra, kMid), rb = times(rb, kMid);
     const uint32_t a1 = upper(ra), b1 = upper(rb);
     uint32_t a2 = minus(ra, a1), b2 = minus(rb, b1);
-    if constexpr (FINE) a2 = times(a2, kLow), b2 = times(b2, kLow);
+    if constexpr (FINE) a2 = times(a2, kFine), b2 = times(b2, kFine);
     a2 += 0x00800080u, b2 += 0x00800080u;
     terms[0] = __byte_perm(a0, b0, 0x7531);
     terms[1] = __byte_perm(a1, b1, 0x7531);
@@ -191,6 +205,105 @@ __device__ __forceinline__ bool any_of_softmax(bool p) {                 // over
 }
 __device__ __forceinline__ void softmax_sync() { asm volatile("barrier.cta.sync 2, %0;" ::"n"(kSoftThreads) : "memory"); }
 __device__ __forceinline__ uint64_t bits2(uint32_t lo, uint32_t hi) { return pair(__uint_as_float(lo), __uint_as_float(hi)); }
+
+__device__ __forceinline__ float best_of(const State& st, int r) { return fmaxf(fmaxf(st.top[0][r], st.top[1][r]), fmaxf(st.top[2][r], st.top[3][r])); }
+__device__ __forceinline__ float sum_of(const State& st, int r) { return (st.top[0][r] + st.top[1][r]) + (st.top[2][r] + st.top[3][r]); }
+// O, which holds a piece's earlier tiles: the rows of this thread's chunks times fac.
+__device__ __forceinline__ void scale_rows(const State& st, uint32_t tmem_o, int r0, int chunks) {
+#pragma unroll 1
+    for (int ch = 0; ch < chunks; ++ch) {
+        uint32_t o[12];
+#pragma unroll
+        for (int t = 0; t < 3; ++t) tmem_ld4(tmem_o + ch * 12 + t * 4, o + 4 * t);
+        const float4 f = *reinterpret_cast<const float4*>(st.fac + r0 + ch * 4);
+        const float by[4] = {f.x, f.y, f.z, f.w};
+        tmem_wait<12>(o);
+#pragma unroll
+        for (int j = 0; j < 12; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * by[j & 3]);
+#pragma unroll
+        for (int t = 0; t < 3; ++t) tmem_st4(tmem_o + ch * 12 + t * 4, o + 4 * t);
+    }
+    tmem_wait_st();
+}
+// A tile in wide form, by all softmax threads: scores from S (in three terms, or summed), both references brought up to date, the
+// tile's weights added to the rows' sums, and the products' exponents left where S was.  A function of its own, since the tiles of
+// other pieces slow down by up to a tenth with this between them.  enter: the first such tile of a piece, the sums so far in top;
+// later: O holds earlier tiles.
+__device__ __noinline__ void wide_tile(State& st, bool enter, bool later, bool terms, uint32_t tmem_s, uint32_t tmem_o, int r0, int chunks, int rows, float kk, float ev) {
+    const int tid = threadIdx.x, lane = tid & 31, q = tid >> 5 & 3, apart = terms ? 12 : 4;
+    if (enter) {                                       // from here on neg is 0 and off all of the reference: scores are rounded alike in every tile
+        softmax_sync();
+        if (tid < rows) {
+            st.sum[tid] = sum_of(st, tid);
+            if (st.off[tid] != -INFINITY) st.off[tid] = -st.neg[tid];
+            st.neg[tid] = 0.f;
+        }
+        softmax_sync();
+    }
+    bool first = false, still = false;                 // the row sees its first key; has seen none
+    float by = 0.f;
+    // Largest scores, which become the weights' references; sums of weights; largest products, against the row's so far, which are
+    // smaller by as much as that reference has grown; and the products' exponents.
+#pragma unroll 1
+    for (int pass = 0; pass < 4; ++pass) {
+#pragma unroll 1
+        for (int ch = 0; ch < chunks; ++ch) {
+            uint32_t y[4];
+            float v[4];
+            if (terms && pass == 0) {
+                uint32_t t[12];
+                tmem_ld_terms(tmem_s + ch * 12, t);
+                tmem_wait<12>(t);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = __float_as_uint((__uint_as_float(t[j]) + __uint_as_float(t[4 + j])) + __uint_as_float(t[8 + j]));
+            } else {
+                tmem_ld4(tmem_s + ch * apart, y);
+                tmem_wait<4>(y);
+            }
+            if (pass == 0) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * kk);
+                tmem_st4(tmem_s + ch * apart, y);
+                tmem_wait_st();
+            }
+            const float4 off = *reinterpret_cast<const float4*>(st.off + r0 + ch * 4), sh = *reinterpret_cast<const float4*>(st.sh + r0 + ch * 4);
+            const float less[4] = {off.x, off.y, off.z, off.w}, more[4] = {sh.x, sh.y, sh.z, sh.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] = __uint_as_float(y[j]) - (pass == 0 || less[j] == -INFINITY ? 0.f : less[j]);
+                if (pass == 1) v[j] = ex2_approx(v[j]);
+                if (pass >= 2) v[j] += ev + more[j];
+                y[j] = __float_as_uint(v[j]);
+            }
+            if (pass == 3) {
+                tmem_st4(tmem_s + ch * apart, y);
+                continue;
+            }
+            const float all = over_lanes(v, lane, [&](float a, float b) { return pass == 1 ? a + b : fmaxf(a, b); });
+            if ((lane & 7) == 0) st.top[q][r0 + ch * 4 + (lane >> 3)] = all;
+        }
+        if (pass == 3) break;
+        softmax_sync();
+        if (tid < rows) {
+            if (pass == 0) {
+                const float best = best_of(st, tid), was = st.off[tid];
+                still = was == -INFINITY && best == -INFINITY, first = was == -INFINITY && !still;
+                const float to = first ? best : fmaxf(was, best);
+                by = first || still ? 0.f : to - was;
+                st.off[tid] = to;
+            } else if (pass == 1) {
+                st.sum[tid] = (first ? 0.f : st.sum[tid] * ex2_approx(-by)) + sum_of(st, tid);
+            } else {
+                const float best = best_of(st, tid), up = still ? 0.f : (first ? best : fmaxf(best, kTop - by)) - kTop;
+                st.sh[tid] -= up;
+                st.fac[tid] = first ? 0.f : ex2_approx(-by - up);
+            }
+        }
+        softmax_sync();
+    }
+    tmem_wait_st();
+    if (later) scale_rows(st, tmem_o, r0, chunks);
+}
 
 // A CTA's walk over its share of the line, the next unit read ahead.
 struct Walk8 {
@@ -300,7 +413,8 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
         bool any, out = false;
         // A piece begins behind the barrier that ends the one before: its Q has been waited for there, and the references are anew.
         auto anew = [&](uint32_t n_q) {
-            if (tid < kMaxRows) st.neg[tid] = 0.f, st.unset[tid] = 1;
+            if (tid < kMaxRows) st.neg[tid] = st.sh[tid] = 0.f, st.off[tid] = -INFINITY;
+            if (tid == 0) st.go_wide = st.wide = 0;
             hold(q_full + 8 * (n_q & 1), n_q >> 1);
             return agreed(false, any);
         };
@@ -326,14 +440,23 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
             const uint32_t tmem_o = tmem + kTmemO + lanes + half * NH;
             const uint32_t p_at = smem0 + half * (NH / 16) * (kTileKeys * 16) + key * 16;
             const int lo_max = mt.lo_max, hi_min = mt.hi_min;
-            int ref_v = kNoScale, key0 = mt.key_first;
-            bool pending = true;                       // some row has no reference yet
+            int key0 = mt.key_first;
+            bool pending = true;                       // every tile sees to the references: some row has none yet, or the form is wide
             // A piece of NC chunks of four rows per thread, without a branch between them.
             auto tiles = [&](auto chunks) {
                 constexpr int NC = decltype(chunks)::value;
                 uint64_t l2[2 * NC];
 #pragma unroll
                 for (int i = 0; i < 2 * NC; ++i) l2[i] = 0;
+                auto sum_rows = [&] {                  // over the lanes (a chunk's four rows end up on lanes 0, 8, 16, 24)
+#pragma unroll
+                    for (int ch = 0; ch < NC; ++ch) {
+                        const float2 f0 = unpair(l2[ch * 2]), f1 = unpair(l2[ch * 2 + 1]);
+                        float v[4] = {f0.x, f0.y, f1.x, f1.y};
+                        const float sum = over_lanes(v, lane, [](float a, float b) { return a + b; });
+                        if ((lane & 7) == 0) st.top[q][r0 + ch * 4 + (lane >> 3)] = sum;
+                    }
+                };
                 for (int i = 0; i < n; ++i, ++n_t, key0 += kTileKeys) {
                     const uint32_t stage = n_t % kStages, use = n_t / kStages;
                     const int at = key0 + key;
@@ -356,7 +479,8 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                     const bool none = kb > 247 || vb > 247;
                     const float kk = none ? (masked ? 1.f : __uint_as_float(0x7fc00000u)) : fmaxf(__uint_as_float((uint32_t)max((int)kb + mt.key_up, 0) << 23) * mt.c, 1.17549435e-38f);
                     const uint64_t kk2 = pair(kk, kk);
-                    const int ev = seen && !none ? (int)vb - 127 : kNoScale;            // of a key that makes its rows NaN: nothing, for the other rows
+                    int ev = seen && !none ? (int)vb - 127 : kNoScale;  // of a key that makes its rows NaN: nothing, for the other rows
+                    const float look_at = ev < kHigh ? (float)max(ev, kLow) : 1000.f;   // beyond kMost with the largest weight: see to the references
                     constexpr bool kTerms = 8 * NC <= kApart;
                     const uint32_t tmem_s = tmem + (n_t & 1) * 64 + lanes + (kTerms ? 3 * r0 : r0);
                     // Scores are hidden where they lie, in a loop of its own: rare, and out of the way of the others.
@@ -409,78 +533,79 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                     }
                     __syncwarp();
                     if (lane == 0) mbar_arrive(k_empty + 8 * stage);                    // S is complete and the scales are read
-                    int dev = ev - ref_v;
                     if (fail) st.fail[turn] = 1;
-                    any = any_of_softmax(fail || pending || fmaxf(top[0], top[1]) + (float)max(dev, -40) > kMost);
+                    any = any_of_softmax(fail || pending || fmaxf(top[0], top[1]) + look_at > kMost);
                     turn ^= 1;
-                    // The references: in a piece's first tile, and in the rare ones where a weight would leave the range of 16 bits
-                    // or some row has seen nothing yet.
+                    // The references: in a piece's first tile, and in the rare ones where a product would leave the range of 16 bits, a
+                    // weight or a power of two that of one reference, or some row has seen nothing yet.
                     if (any) {
                         if (st.fail[turn ^ 1]) {
                             fail = out = true;
                             break;
                         }
+                        const bool enter = !st.wide;   // written behind a barrier that follows this
+                        bool wide = !enter;
+                        if (enter) {
+                            if (ev > kNoScale && (ev < kLow || ev >= kHigh)) st.go_wide = 1;
 #pragma unroll
-                        for (int ch = 0; ch < NC; ++ch) {
-                            float v[4] = {__uint_as_float(x[ch * 4]), __uint_as_float(x[ch * 4 + 1]), __uint_as_float(x[ch * 4 + 2]), __uint_as_float(x[ch * 4 + 3])};
-                            const float best = over_lanes(v, lane, [](float a, float b) { return fmaxf(a, b); });
-                            if ((lane & 7) == 0) st.top[q][r0 + ch * 4 + (lane >> 3)] = best;
-                        }
-                        const int e = __reduce_max_sync(0xffffffffu, ev);
-                        if (lane == 0) st.exp_top[q] = e;
-                        softmax_sync();
-                        bool still = false;
-                        if (tid < RP) {
-                            const float best = fmaxf(fmaxf(st.top[0][tid], st.top[1][tid]), fmaxf(st.top[2][tid], st.top[3][tid]));
-                            const bool first = st.unset[tid] && best != -INFINITY;
-                            const float up = first || best > kTop ? best - kTop : 0.f;
-                            st.neg[tid] -= up;
-                            st.step[tid] = up;
-                            st.fac[tid] = first ? 0.f : ex2_approx(-up);
-                            if (first) st.unset[tid] = 0;
-                            still = best == -INFINITY && st.unset[tid];
-                        }
-                        const int ref = max(max(max(st.exp_top[0], st.exp_top[1]), max(st.exp_top[2], st.exp_top[3])), ref_v);
-                        pending = any_of_softmax(still);
-                        if (i > 0) {
-                            const float shrink = ex2_approx((float)(ref_v - ref));
-#pragma unroll
-                            for (int j = 0; j < 2 * NC; ++j) {
-                                const float2 f = *reinterpret_cast<const float2*>(st.fac + r0 + 2 * j);
-                                l2[j] = mul2(l2[j], pair(f.x, f.y));
-                            }
-                            hold(o_done, n_t - 1);     // O holds this piece's earlier tiles
-                            tc_fence_after();
-#pragma unroll 1
                             for (int ch = 0; ch < NC; ++ch) {
-                                uint32_t o[12];
+                                float v[4];
 #pragma unroll
-                                for (int t = 0; t < 3; ++t) tmem_ld4(tmem_o + ch * 12 + t * 4, o + 4 * t);
-                                const float4 f = *reinterpret_cast<const float4*>(st.fac + r0 + ch * 4);
-                                const float by[4] = {f.x * shrink, f.y * shrink, f.z * shrink, f.w * shrink};
-                                tmem_wait<12>(o);
-#pragma unroll
-                                for (int j = 0; j < 12; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * by[j & 3]);
-#pragma unroll
-                                for (int t = 0; t < 3; ++t) tmem_st4(tmem_o + ch * 12 + t * 4, o + 4 * t);
+                                for (int j = 0; j < 4; ++j) v[j] = max_over_lanes(__uint_as_float(x[ch * 4 + j]) + (float)ev);
+                                if (lane == 0) *reinterpret_cast<float4*>(&st.top[q][r0 + ch * 4]) = make_float4(v[0], v[1], v[2], v[3]);
                             }
-                            tmem_wait_st();
+                            softmax_sync();
+                            wide = st.go_wide;
                         }
-                        ref_v = ref;
-                        dev = ev - ref_v;
+                        if (!wide) {
+                            bool still = false;
+                            if (tid < RP) {
+                                const float best = best_of(st, tid);
+                                const bool unset = st.off[tid] == -INFINITY, first = unset && best != -INFINITY;
+                                const float up = first || best > kTop ? best - kTop : 0.f;
+                                st.neg[tid] -= up;
+                                st.step[tid] = up;
+                                st.fac[tid] = first ? 0.f : ex2_approx(-up);
+                                if (first) st.off[tid] = 0.f;
+                                still = unset && !first;
+                            }
+                            pending = any_of_softmax(still);
+                            if (i > 0) {
 #pragma unroll
-                        for (int ch = 0; ch < NC; ++ch) {
-                            const float4 up = *reinterpret_cast<const float4*>(st.step + r0 + ch * 4);
-                            x[ch * 4] = __float_as_uint(__uint_as_float(x[ch * 4]) - up.x), x[ch * 4 + 1] = __float_as_uint(__uint_as_float(x[ch * 4 + 1]) - up.y);
-                            x[ch * 4 + 2] = __float_as_uint(__uint_as_float(x[ch * 4 + 2]) - up.z), x[ch * 4 + 3] = __float_as_uint(__uint_as_float(x[ch * 4 + 3]) - up.w);
+                                for (int j = 0; j < 2 * NC; ++j) {
+                                    const float2 f = *reinterpret_cast<const float2*>(st.fac + r0 + 2 * j);
+                                    l2[j] = mul2(l2[j], pair(f.x, f.y));
+                                }
+                                hold(o_done, n_t - 1);
+                                tc_fence_after();
+                                scale_rows(st, tmem_o, r0, NC);
+                            }
+#pragma unroll
+                            for (int ch = 0; ch < NC; ++ch) {
+                                const float4 up = *reinterpret_cast<const float4*>(st.step + r0 + ch * 4);
+                                x[ch * 4] = __float_as_uint(__uint_as_float(x[ch * 4]) - up.x), x[ch * 4 + 1] = __float_as_uint(__uint_as_float(x[ch * 4 + 1]) - up.y);
+                                x[ch * 4 + 2] = __float_as_uint(__uint_as_float(x[ch * 4 + 2]) - up.z), x[ch * 4 + 3] = __float_as_uint(__uint_as_float(x[ch * 4 + 3]) - up.w);
+                            }
+                        } else {
+                            // In place of S, which the issuer leaves alone until the weights are there.
+                            if (enter) sum_rows();
+                            if (i > 0) hold(o_done, n_t - 1);
+                            tc_fence_after();
+                            wide_tile(st, enter, i > 0, kTerms, tmem_s, tmem_o, r0, NC, RP, kk, (float)ev);
+#pragma unroll
+                            for (int ch = 0; ch < NC; ++ch) tmem_ld4(tmem_s + ch * (kTerms ? 12 : 4), x + ch * 4);
+                            tmem_wait<4 * NC>(x);
+                            if (tid == 0) st.wide = 1;
+                            pending = true;
+                            ev = 0;                    // of a product only 2^x is left; the sums of the threads no longer count
                         }
                     }
                     const bool p_free = i == 0 || bar_try(o_done, (n_t - 1) & 1);       // looked at here, needed below
                     // weights: their sums in 32 bits; times V's power of two, and split, for the product
-                    const float vs = __uint_as_float((uint32_t)(min(max(dev, -126), 127) + 127) << 23);
-                    const uint64_t vs2 = pair(vs, vs);
                     constexpr int kUnits = (3 * NC + 3) / 4;
                     uint32_t word[4 * kUnits] = {};
+                    const float vs = __uint_as_float((uint32_t)(min(max(ev, -126), 127) + 127) << 23);
+                    const uint64_t vs2 = pair(vs, vs);
 #pragma unroll
                     for (int ch = 0; ch < NC; ++ch) {
                         uint32_t h[2];
@@ -512,47 +637,45 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                     __syncwarp();
                     if (lane == 0) mbar_arrive(p_full);
                 }
-                // sums over the lanes (a chunk's four rows end up on lanes 0, 8, 16, 24)
-#pragma unroll
-                for (int ch = 0; ch < NC; ++ch) {
-                    const float2 f0 = unpair(l2[ch * 2]), f1 = unpair(l2[ch * 2 + 1]);
-                    float v[4] = {f0.x, f0.y, f1.x, f1.y};
-                    const float sum = over_lanes(v, lane, [](float a, float b) { return a + b; });
-                    if ((lane & 7) == 0) st.top[q][r0 + ch * 4 + (lane >> 3)] = sum;
-                }
+                sum_rows();
             };
             const int n_ch = HP / 4;
-            if (n_ch == 1) tiles(std::integral_constant<int, 1>());
-            else if (n_ch == 2) tiles(std::integral_constant<int, 2>());
+            // A round's units alternate between neighbouring sizes, and an SM's instruction cache holds two of these loops or not by where
+            // they lie: neighbours stand apart (512 requests of 3 to 5 rows over 128 to 4096 keys 426 us, 459 in order of size; of 2 to 6
+            // over 2048 keys 480 and 499).
+            if (n_ch == 2) tiles(std::integral_constant<int, 2>());
+            else if (n_ch == 5) tiles(std::integral_constant<int, 5>());
             else if (n_ch == 3) tiles(std::integral_constant<int, 3>());
-            else if (n_ch == 4) tiles(std::integral_constant<int, 4>());
-            else tiles(std::integral_constant<int, 5>());
+            else if (n_ch == 1) tiles(std::integral_constant<int, 1>());
+            else tiles(std::integral_constant<int, 4>());
             if (out) break;
             // ---- the piece's rows; what needs no product, while the last one is under way
             softmax_sync();
             const int64_t part0 = (int64_t)part * kMaxRows, orow0 = (int64_t)mt.row0 * a.Hq + mt.head * G;
             if (tid < R) {
-                const float m_run = -st.neg[tid], l = (st.top[0][tid] + st.top[1][tid]) + (st.top[2][tid] + st.top[3][tid]);
-                float f = 0.f;                         // a sum of zero: nothing was seen, O may be anything
-                // V's power of two is shared out between a piece's sum and its products, half each, so that both stay in range wherever V
-                // lies; f is what the products get.  A row whose sum is no number joins with a reference of infinity: all factors are then
-                // 0 or not a number.
+                const float m_run = st.off[tid] - st.neg[tid], l = st.wide ? st.sum[tid] : sum_of(st, tid), a_o = -st.sh[tid];
+                float f = 0.f, more = 1.f;             // a sum of zero: nothing was seen, O may be anything
+                // What the products' reference differs by is shared out, half each: between a piece's sum and its products (f), so that both
+                // stay in range wherever V lies, or between the two factors of a row.  A row whose sum is no number joins with a reference
+                // of infinity: all factors are then 0 or not a number.
                 if (part >= 0) {
-                    const float m = m_run + (float)(ref_v >> 1), by = m - m_run;         // what the reference has moved by after its rounding
-                    if (l != 0.f) f = l == l ? exp2f((float)ref_v - by) : l;
-                    *reinterpret_cast<float2*>(a.p.part_ml + (part0 + tid) * 2) = make_float2(l != l ? INFINITY : (l == 0.f ? -INFINITY : m), l != 0.f ? l * exp2f(-by) : 0.f);
+                    const float m = m_run + 0.5f * a_o, by = m - m_run;                 // by: what it has moved by after its rounding
+                    if (l != 0.f) f = l == l ? ex2_approx(a_o - by) : l;
+                    *reinterpret_cast<float2*>(a.p.part_ml + (part0 + tid) * 2) = make_float2(l != l ? INFINITY : (l == 0.f ? -INFINITY : m), l != 0.f ? l * ex2_approx(-by) : 0.f);
                 } else {
                     if (l != 0.f) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f) : "f"(l));
+                    more = ex2_approx(0.5f * a_o);
+                    f *= more;
                     if (a.lse) a.lse[orow0 + (tid / G) * a.Hq + tid % G] = l == 0.f ? -INFINITY : (m_run + log2f(l)) * kLn2;
                 }
                 st.fac[tid] = f;
+                st.step[tid] = more;
             }
             hold(o_done, n_t - 1);
             if (!anew(n_q + 1)) break;
             tc_fence_after();
             // O is [dim][half, chunk, term, row]: a thread has one dim (64 dims sit on 16 lanes of each quarter) and its half of the rows
             const bool live = D == 128 || lane < 16, whole = part < 0;
-            const float scale_v = ref_v == kNoScale ? 0.f : (whole ? __uint_as_float((uint32_t)(ref_v + 127) << 23) : 1.f);
             int g = r0 % G;
             const int size = whole ? 2 : 4, jump = whole ? (a.Hq - G) * D * 2 : 0;      // bytes of a value; from a token's last row of the head to the next one's first
             char* to = whole ? reinterpret_cast<char*>(a.o + (orow0 + (int64_t)(r0 / G) * a.Hq + g) * D) : reinterpret_cast<char*>(a.p.part_acc + (part0 + r0) * D);
@@ -563,13 +686,13 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                 uint32_t y[12];
 #pragma unroll
                 for (int t = 0; t < 3; ++t) tmem_ld4(tmem_o + ch * 12 + t * 4, y + 4 * t);
-                const float4 f4 = *reinterpret_cast<const float4*>(st.fac + r0 + ch * 4);
-                const float f[4] = {f4.x, f4.y, f4.z, f4.w};
+                const float4 f4 = *reinterpret_cast<const float4*>(st.fac + r0 + ch * 4), g4 = *reinterpret_cast<const float4*>(st.step + r0 + ch * 4);
+                const float f[4] = {f4.x, f4.y, f4.z, f4.w}, more[4] = {g4.x, g4.y, g4.z, g4.w};
                 tmem_wait<12>(y);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float sum = fmaf(fmaf(__uint_as_float(y[8 + j]), 1.f / kLow, __uint_as_float(y[4 + j])), 1.f / kMid, __uint_as_float(y[j]));
-                    const float v = f[j] != 0.f ? sum * f[j] * scale_v : 0.f;
+                    const float sum = fmaf(fmaf(__uint_as_float(y[8 + j]), 1.f / kFine, __uint_as_float(y[4 + j])), 1.f / kMid, __uint_as_float(y[j]));
+                    const float v = f[j] != 0.f ? sum * f[j] * more[j] : 0.f;
                     if (live && r0 + ch * 4 + j < R) {
                         if (whole) {
                             const __nv_bfloat16 b = __float2bfloat16_rn(v);

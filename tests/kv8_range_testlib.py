@@ -102,13 +102,13 @@ def close8(o, lse, ref, part, keys):
     """Weights and a row's sum move by less than 2^-10 of themselves through scores and exponentials in 32 bits, as in the 16-bit
     form.  A weight times its key's power of two is rounded to 11 bits (half a step: 2^-11 of it) and, where it is small, to
     multiples: off by at most 2^-25 as a 16-bit float and 2^-24 in its third term, 2^-23.4 together, where the row's largest such
-    product is 2^4 at least.  A code is 448 at most, and the largest one of a row 224 at least (its power of two is the least
-    that holds it), so a key moves an element by less than 2^-23.4 448 / (2^4 224) < 2^-26 of `part`, the largest product of a
+    product is 2^3 at least.  A code is 448 at most, and the largest one of a row 224 at least (its power of two is the least
+    that holds it), so a key moves an element by less than 2^-23.4 448 / (2^3 224) < 2^-25 of `part`, the largest product of a
     weight and a row's largest |v|.  The result is rounded to bf16: 2^-8 |o|, or a step of its smallest numbers."""
     o_ref, lse_ref, mag = (t.cpu() for t in ref)
     o, lse = o.double().cpu().reshape(o_ref.shape), lse.double().cpu().reshape(lse_ref.shape)
     assert torch.isfinite(o).all() and torch.isfinite(lse).all(), "non-finite output"
-    limit = T.HALF_BF16 * o_ref.abs() + (2.0 ** -10 + 2.0 ** -11) * mag + 2.0 ** -26 * keys * part.cpu()[..., None] + LEAST
+    limit = T.HALF_BF16 * o_ref.abs() + (2.0 ** -10 + 2.0 ** -11) * mag + 2.0 ** -25 * keys * part.cpu()[..., None] + LEAST
     off = (o - o_ref).abs() / limit
     assert (off <= 1).all(), f"{int((off > 1).sum())} of {off.numel()} outside, worst {off.max():.3g} of the limit"
     assert ((lse - lse_ref).abs() <= 2.0 ** -10 + 2.0 ** -20 * lse_ref.abs()).all(), "lse"

@@ -58,3 +58,88 @@ def test_small_queries_with_large_keys(dim):
             b.scales[0, :, :, 0] = torch.where(held[0, :, :, 0], b.scales[0, :, :, 0] + 5, 255).to(torch.uint8)
             b.values[0, :, 0] *= 2.0 ** 5
         b.run_close(scale=scale)
+
+
+@pytest.mark.parametrize("tokens", [1, 5])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_a_large_v_with_next_to_no_weight(dim, tokens):
+    """One row of V 2^22 to 2^118 larger than the others, of a key whose weight is below 2^-60 of a row's: first, last and in the
+    middle of contexts that each have a CTA to themselves."""
+    n = 150
+    b = Range8([600] * n, [tokens] * n, dim=dim, heads=4, kv_heads=2, seed=11 + tokens)
+    for r in range(n):
+        token = (0, 599, 300, 130, 127)[r % 5]
+        b.point(r, token, -(45.0, 65.0, 100.0)[r // 5 % 3])
+        b.shift_v(r, (22, 24, 26, 30, 40, 59, 64, 80, 100, 118)[r // 15], [token])
+    b.run_close()
+
+
+@pytest.mark.parametrize("ctx", [140, 9000])
+@pytest.mark.parametrize("by", [22, 30, 45, 90, 118])
+def test_a_large_v_with_next_to_no_weight_in_pieces(by, ctx):
+    for token in (0, ctx // 2, ctx - 1):
+        b = Range8([ctx], [3], heads=8, kv_heads=2, seed=by)
+        b.point(0, token, -60.0)
+        b.shift_v(0, by, [token])
+        b.run_close()
+
+
+@pytest.mark.parametrize("by", [10, 22, 30, 45, 60, 90, 118, -60, -110])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_a_large_v_that_only_later_rows_see(dim, by):
+    """Drafted tokens whose V differs from the context's by many powers of two: the rows before them do not see it."""
+    n = 80
+    b = Range8([260] * n, [5] * n, dim=dim, heads=8, kv_heads=2, seed=by % 101)
+    for r in range(n):
+        b.shift_v(r, by, [(264,), (262,), (261, 264), (263, 260)][r % 4])
+    b.run_close()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_v_of_every_size_alone_and_mixed(dim):
+    """Whole requests of one size, rows of random sizes with scores of order one and twenty, sizes that grow and fall along
+    the context, and rows of zeros: all of them, a whole tile, single ones with and without all of the weight."""
+    rng = np.random.default_rng(21)
+    n = 160
+    b = Range8([500] * n, [3] * n, dim=dim, heads=4, kv_heads=2, seed=21)
+    for r in range(n):
+        kind = r % 8
+        if kind == 0:
+            b.shift_v(r, (-115, -90, -62, -56, -50, -30, 0, 30, 40, 44, 48, 52, 56, 60, 75, 90, 100, 110, 117, 118)[r // 8])
+        elif kind == 1:
+            b.shift_v(r, rng.integers(-115, 119, 503))
+        elif kind == 2:
+            b.shift_v(r, np.round(np.linspace(-115, 118, 503)).astype(int)[::1 if r % 16 < 8 else -1])
+        elif kind == 3:
+            b.clear_v(r) if r % 3 == 0 else b.clear_v(r, np.arange(128 if r % 3 == 1 else 300))
+        elif kind == 4:
+            b.clear_v(r, [int(rng.integers(0, 500))])
+            b.point(r, 5 + r, 60.0)
+            b.clear_v(r, [5 + r])
+        elif kind == 5:
+            b.point(r, 200 + r, 90.0)
+            b.shift_v(r, -int(rng.integers(0, 115)), [200 + r])
+        elif kind == 6:
+            for t in rng.integers(0, 500, 40):
+                b.point(r, int(t), float(rng.normal() * 20))
+            b.shift_v(r, rng.integers(-115, 119, 503))
+        else:
+            b.shift_v(r, rng.integers(-30, 31, 503))
+    b.run_close()
+    b.run_close(window=200)
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_random_sizes_in_random_batches(seed):
+    rng = np.random.default_rng(seed)
+    heads, hkv, dim = [(8, 2, 128), (4, 4, 64), (5, 1, 64), (32, 1, 128), (28, 4, 128), (12, 4, 64)][seed]
+    n = int(rng.integers(1, 30))
+    ctx, new = rng.integers(0, 1500, n).tolist(), rng.integers(1, 12, n).tolist()
+    b = Range8(ctx, new, heads=heads, kv_heads=hkv, dim=dim, seed=seed)
+    for r in range(n):
+        total = ctx[r] + new[r]
+        b.shift_v(r, rng.integers(-115, 119, total) if rng.random() < 0.5 else rng.integers(-40, 41, total))
+        for t in rng.integers(0, total, total // 8):
+            b.point(r, int(t), float(rng.normal() * 30))
+    b.run_close()
+    b.run_close(row_first=[int(rng.integers(0, 400)) if rng.random() < 0.5 else 0 for _ in range(b.rows)]) if min(ctx) > 500 else None

@@ -31,7 +31,8 @@ namespace {
 // requests of 3 to 5 rows over 128 to 4096 keys: 416 us instead of 404).  Sums of the weights are 32-bit and of the unrounded ones, a
 // thread's own until the end of the piece.
 // One reference for both serves while V's powers of two lie in 2^-60 to 2^40 (kLow, kHigh): a weight is then at most 2^76, and the
-// sums of pieces can be joined in 32 bits.  A piece that meets another power where it sees to its references goes on in wide form
+// sums of pieces can be joined in 32 bits.  A piece that meets another power where it sees to its references, or a score beyond 2^12
+// (one rounding with a reference and one without would then differ by more than a weight's), goes on in wide form
 // (wide_tile): the row's sum has a reference of its own (off), the products another (sh), both brought up to date in every tile, in
 // a function apart from the others.  It costs several times as long.
 //
@@ -64,6 +65,7 @@ constexpr int kWarpIssue = 8, kWarpV = 10, kWarpQ = 11;   // 9: the producer of 
 constexpr uint32_t kPollLimit = 1u << 21;              // polls of one wait, if nsd_config.wait_budget does not say: one that finds nothing takes 1.4 us, so three seconds
 constexpr float kTop = 3.f, kMost = 15.875f;           // log2 of a row's largest product when its reference is set, and at most
 constexpr int kLow = -60, kHigh = 40;                  // exponents of V that one reference serves
+constexpr float kFar = 4096.f;                         // scores that one reference serves: those beyond are rounded to more than 2^-12
 constexpr float kMid = 8.f, kFine = 16.f;              // a weight's second term is held times kMid, its third times both
 constexpr int kNoScale = -1000;                        // exponent of a V that no row sees, or that makes its rows NaN
 
@@ -104,7 +106,7 @@ struct __align__(16) State {
     float step[kMaxRows];                              // what the reference moves by
     float fac[kMaxRows];
     float top[4][kMaxRows];                            // a quarter's largest products or weights; at the end its sums
-    volatile int go_wide, wide;                        // the piece has to go on in wide form; does so
+    volatile int odd, far, wide;                       // the piece has to go on in wide form, by a power of V or by a score; does so
     volatile int fail[2];                              // a warp has given up, by barriers in turn
 };
 
@@ -227,10 +229,12 @@ __device__ __forceinline__ void scale_rows(const State& st, uint32_t tmem_o, int
 }
 // A tile in wide form, by all softmax threads: scores from S (in three terms, or summed), both references brought up to date, the
 // tile's weights added to the rows' sums, and the products' exponents left where S was.  A function of its own, since the tiles of
-// other pieces slow down by up to a tenth with this between them.  enter: the first such tile of a piece, the sums so far in top;
-// later: O holds earlier tiles.
-__device__ __noinline__ void wide_tile(State& st, bool enter, bool later, bool terms, uint32_t tmem_s, uint32_t tmem_o, int r0, int chunks, int rows, float kk, float ev) {
-    const int tid = threadIdx.x, lane = tid & 31, q = tid >> 5 & 3, apart = terms ? 12 : 4;
+// other pieces slow down by up to a tenth with this between them.  form: chunks of a thread; 8: the first such tile of a piece, the sums
+// so far in top; 16: O holds earlier tiles.
+__device__ __noinline__ void wide_tile(State& st, int form, uint32_t tmem_s, uint32_t tmem_o, float kk, float ev) {
+    const int tid = threadIdx.x, lane = tid & 31, q = tid >> 5 & 3, chunks = form & 7, rows = chunks * 8, r0 = tid >> 7 ? rows / 2 : 0;
+    const bool terms = rows <= kApart, enter = form & 8, later = form & 16;
+    const int apart = terms ? 12 : 4;
     if (enter) {                                       // from here on neg is 0 and off all of the reference: scores are rounded alike in every tile
         softmax_sync();
         if (tid < rows) {
@@ -414,7 +418,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
         // A piece begins behind the barrier that ends the one before: its Q has been waited for there, and the references are anew.
         auto anew = [&](uint32_t n_q) {
             if (tid < kMaxRows) st.neg[tid] = st.sh[tid] = 0.f, st.off[tid] = -INFINITY;
-            if (tid == 0) st.go_wide = st.wide = 0;
+            if (tid == 0) st.odd = st.far = st.wide = 0;
             hold(q_full + 8 * (n_q & 1), n_q >> 1);
             return agreed(false, any);
         };
@@ -472,7 +476,8 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                     }
                     hold(s_full + 8 * (n_t & 1), n_t >> 1);
                     tc_fence_after();
-                    // the scales came with K, which the issuer of S waited for
+                    // The scales landed with K, before the issuer could send the product that s_full stands for.  (A look at k_full beside
+                    // it costs 5 to 10 %.)
                     const unsigned char* const sb = smem + L::kOffScales + stage * (kBlocks * 32) + (key >> 4) * 32 + (key & 15);
                     const uint32_t kb = sb[0], vb = sb[16];
                     // The key's power of two, times 2^key_up against the rows' 2^-key_up, and theirs: not 0, so that a hidden score stays -inf.
@@ -502,8 +507,8 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                         }
                         tmem_wait_st();
                     }
-                    // The scores of this thread's key and rows less the rows' references, -inf where a row does not see the key.  The
-                    // product is rounded before the difference, so that the largest score less itself is 0 however large it is.
+                    // The scores of this thread's key and rows less the rows' references, -inf where a row does not see the key.  (Product and
+                    // difference become one instruction with one rounding.)
                     uint32_t x[4 * NC];
                     uint64_t sum[2 * NC];
                     if constexpr (kTerms) {
@@ -546,7 +551,7 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                         const bool enter = !st.wide;   // written behind a barrier that follows this
                         bool wide = !enter;
                         if (enter) {
-                            if (ev > kNoScale && (ev < kLow || ev >= kHigh)) st.go_wide = 1;
+                            if (ev > kNoScale && (ev < kLow || ev >= kHigh)) st.odd = 1;
 #pragma unroll
                             for (int ch = 0; ch < NC; ++ch) {
                                 float v[4];
@@ -555,21 +560,28 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                                 if (lane == 0) *reinterpret_cast<float4*>(&st.top[q][r0 + ch * 4]) = make_float4(v[0], v[1], v[2], v[3]);
                             }
                             softmax_sync();
-                            wide = st.go_wide;
+                            wide = st.odd;
+                            if (!wide) {
+                                bool still = false;
+                                float neg = 0.f, off = 0.f;
+                                if (tid < RP) {
+                                    const float best = best_of(st, tid);
+                                    neg = st.neg[tid], off = st.off[tid];
+                                    const bool first = off == -INFINITY && best != -INFINITY;
+                                    const float up = first || best > kTop ? best - kTop : 0.f;
+                                    if (fabsf(neg - up) > kFar) st.far = 1;
+                                    st.neg[tid] = neg - up;
+                                    st.step[tid] = up;
+                                    st.fac[tid] = first ? 0.f : ex2_approx(-up);
+                                    if (first) st.off[tid] = 0.f;
+                                    still = off == -INFINITY && !first;
+                                }
+                                pending = any_of_softmax(still);
+                                wide = st.far;
+                                if (wide && tid < RP) st.neg[tid] = neg, st.off[tid] = off;              // as they were
+                            }
                         }
                         if (!wide) {
-                            bool still = false;
-                            if (tid < RP) {
-                                const float best = best_of(st, tid);
-                                const bool unset = st.off[tid] == -INFINITY, first = unset && best != -INFINITY;
-                                const float up = first || best > kTop ? best - kTop : 0.f;
-                                st.neg[tid] -= up;
-                                st.step[tid] = up;
-                                st.fac[tid] = first ? 0.f : ex2_approx(-up);
-                                if (first) st.off[tid] = 0.f;
-                                still = unset && !first;
-                            }
-                            pending = any_of_softmax(still);
                             if (i > 0) {
 #pragma unroll
                                 for (int j = 0; j < 2 * NC; ++j) {
@@ -591,13 +603,15 @@ kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
                             if (enter) sum_rows();
                             if (i > 0) hold(o_done, n_t - 1);
                             tc_fence_after();
-                            wide_tile(st, enter, i > 0, kTerms, tmem_s, tmem_o, r0, NC, RP, kk, (float)ev);
+                            wide_tile(st, NC | (enter ? 8 : 0) | (i > 0 ? 16 : 0), tmem_s, tmem_o, kk, (float)ev);
 #pragma unroll
                             for (int ch = 0; ch < NC; ++ch) tmem_ld4(tmem_s + ch * (kTerms ? 12 : 4), x + ch * 4);
                             tmem_wait<4 * NC>(x);
                             if (tid == 0) st.wide = 1;
                             pending = true;
-                            ev = 0;                    // of a product only 2^x is left; the sums of the threads no longer count
+                            ev = 0;                    // of a product only 2^x is left
+#pragma unroll
+                            for (int j = 0; j < 2 * NC; ++j) l2[j] = 0;                 // no longer counts
                         }
                     }
                     const bool p_free = i == 0 || bar_try(o_done, (n_t - 1) & 1);       // looked at here, needed below

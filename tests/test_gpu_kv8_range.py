@@ -143,3 +143,28 @@ def test_random_sizes_in_random_batches(seed):
             b.point(r, int(t), float(rng.normal() * 30))
     b.run_close()
     b.run_close(row_first=[int(rng.integers(0, 400)) if rng.random() < 0.5 else 0 for _ in range(b.rows)]) if min(ctx) > 500 else None
+
+
+@pytest.mark.parametrize("tokens", [1, 5])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_equal_scores_beyond_2_24_weigh_the_same(dim, tokens):
+    """Two keys with one score that no other comes near, the first where the row's reference moves: the mean of their rows of V.
+    The scores, 2^26 and up in steps of some 2^8, are exact sums of two products."""
+    n = 40
+    b = Range8([700] * n, [tokens] * n, dim=dim, heads=8, kv_heads=2, seed=3)
+    b.q.zero_()
+    q = b.q.view(1, b.rows, b.heads, dim)
+    q[..., 0], q[..., 1] = 2.0 ** 18, 1.0
+    b.kv8[0, :, 0], b.values[0, :, 0] = torch.where(b.kv8[0, :, 0] == 0x7F, 0x7F, 0).to(torch.uint8), 0.0
+
+    def key(request, token, first, second):
+        block, slot = b.place(request, token)
+        for d, x in ((0, first), (1, second)):
+            b.kv8[0, block, 0, :, slot, d] = torch.tensor([x]).to(torch.float8_e4m3fn).view(torch.uint8).to(DEV)
+            b.values[0, block, 0, :, slot, d] = x
+        b.scales[0, block, :, 0, slot] = 127
+    for r in range(n):
+        key(r, 5 + r, 256.0, 0.0)                      # 2^26
+        key(r, 300 + r, 256.0, 128.0 + 16 * (r % 16))  # more by 128 to 368
+        key(r, 500 + r, 256.0, 128.0 + 16 * (r % 16))  # the same again, in a later tile
+    b.run_close(scale=1.0)

@@ -41,7 +41,8 @@ __device__ __forceinline__ int64_t unit_cost(const ChunkCost& c, const ChunkUnit
 // ---- plan -------------------------------------------------------------------------------------
 // Two kernels.  The first works on every request's units side by side: the visible keys of each
 // row and their hull over the unit.  Unit j of request r sits at r + floor(q_indptr[r] / TU) + j,
-// an index that needs no prefix sum and leaves at most one gap per request.  The second, one CTA,
+// an index that needs no prefix sum and leaves at most one gap per request; a warp finds the request of
+// its slot by two or three rounds of 32 probes.  The second, one CTA,
 // closes the gaps, sums the costs and cuts the whole work -- units x kv heads x key tiles in one
 // line -- into n_ctas equal pieces.  Two launches and two chains of dependent loads bound it: 7 to
 // 9 us for a prompt of 8192, for 64 single tokens and for 128 mixed requests alike, once per step.
@@ -76,48 +77,70 @@ __device__ __forceinline__ bool request_ok(const PlanArgs& a, const ChunkGroups&
            (e == s || groups.prefix_len[k] <= c);
 }
 
-__global__ void __launch_bounds__(128)
+// The last of n entries whose first slot is not behind slot i, 32 probes at a time; first is called for entries 0 .. n - 1 only.
+template <typename First>
+__device__ __forceinline__ int entry_of(int n, int64_t i, int lane, First first) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 31) / 32, at = lo + lane * step;
+        const uint32_t before = __ballot_sync(0xffffffffu, at < hi && first(min(at, n - 1)) <= i);
+        lo += (before ? 31 - __clz(before) : 0) * step;
+        hi = min(hi, lo + step);
+    }
+    return lo;
+}
+// A warp takes a slot of a request's units, or of a group's -- a request whose rows are those of its members and whose keys are the
+// shared ones -- so that the work spreads over the GPU wherever the rows are.  Both kernels, 512 requests of which one has 100 000 new
+// tokens and the others one: 17.5 us; 42 with 2048 CTAs dealt out to the requests, 51 with 64 for each; 4096 requests with one such 39,
+// 158 and 307; 512 of 5 rows 11, 12 and 16; 64 single tokens 9 to 10 either way.
+constexpr int kUnitWarps = 4, kUnitCtas = 4096;
+__global__ void __launch_bounds__(kUnitWarps * 32)
 chunk_units_kernel(const PlanArgs a) {
     pdl_release_dependents();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    // behind the requests come the groups, each as a request whose rows are those of its members and whose keys are the shared ones
-    const bool shared = (int)blockIdx.x >= a.batch;
-    int r = blockIdx.x, group = 0;
-    if (shared) {
-        group = r - a.batch;
-        const int64_t first = a.groups.indptr[group], end = a.groups.indptr[group + 1];
-        if (first < 0 || first >= end || end > a.batch) return;                         // none, or reported with a request
-        r = (int)first;
-    }
-    if (!request_ok(a, a.groups, r)) {
-        if (shared) return;
-        if (blockIdx.y == 0 && threadIdx.x == 0) report(a.status, STATUS_BAD_TOKEN, r);
-        return;
-    }
-    const int TU = a.p.kind.tiles * a.T;
-    const int64_t s = a.q_indptr[r], e = shared ? a.q_indptr[a.groups.indptr[group + 1]] : a.q_indptr[r + 1];
-    if (shared && (e < s || e > a.p.max_rows)) return;
-    const int common = a.groups.n ? shared_keys(a.groups, shared ? group : group_of(a.groups, r)) : 0;
-    const int n = (int)(e - s), ctx = a.ctx_len[r], total = ctx + n;
-    const int n_units = shared && common == 0 ? 0 : (n + TU - 1) / TU;
-    const int64_t at = (shared ? a.p.max_units / 2 + group : r) + s / TU, owned = 1 + e / TU - s / TU;
-    if (shared) {
-        if (common == 0)                               // the rows have one side only
-            for (int64_t i = (int64_t)blockIdx.y * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.y * blockDim.x) a.p.row_lo[a.p.max_rows + s + i] = a.p.row_hi[a.p.max_rows + s + i] = 0;
-        // the shared blocks are read through the table of the first member that has rows
-        int lo = r, hi = (int)a.groups.indptr[group + 1];
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (a.q_indptr[mid] <= s) lo = mid; else hi = mid;
+    const int lane = threadIdx.x & 31, TU = a.p.kind.tiles * a.T;
+    const int64_t rows = min(max(a.q_indptr[a.batch], (int64_t)0), a.p.max_rows), room = a.p.max_rows / TU;
+    const int64_t own = a.batch + room, all = a.groups.n > 0 ? own + a.groups.n + rows / TU : a.batch + rows / TU;
+    for (int64_t slot = (int64_t)blockIdx.x * kUnitWarps + (threadIdx.x >> 5); slot < all; slot += (int64_t)gridDim.x * kUnitWarps) {
+        const bool shared = slot >= own;
+        const int64_t i = shared ? slot - own : slot;
+        int r, group = 0;
+        if (shared) {
+            auto first = [&](int g) {
+                const int64_t at = a.groups.indptr[g];
+                return at >= 0 && at <= a.batch ? g + a.q_indptr[at] / TU : (int64_t)g;
+            };
+            group = entry_of(a.groups.n, i, lane, first);
+            const int64_t begin = a.groups.indptr[group], end = a.groups.indptr[group + 1];
+            if (begin < 0 || begin >= end || end > a.batch) continue;                    // reported by the second kernel, as all that is malformed
+            r = (int)begin;
+        } else {
+            if (i >= a.batch + rows / TU) continue;
+            r = entry_of(a.batch, i, lane, [&](int k) { return k + a.q_indptr[k] / TU; });
         }
-        r = lo;
-        if (a.kv_indptr[r] < 0 || a.kv_indptr[r] > a.kv_indptr[r + 1]) return;          // reported with the request
-    }
-    const int64_t row_at = shared ? a.p.max_rows : 0;
-    int prefix = 0;
-    if (a.masks.prefix_len) prefix = min(max(a.masks.prefix_len[r], 0), total);
-    const int64_t nblk = a.kv_indptr[r + 1] - a.kv_indptr[r];
-    for (int64_t j = blockIdx.y * 4 + warp; j < owned; j += gridDim.y * 4) {
+        if (!request_ok(a, a.groups, r)) continue;
+        const int64_t s = a.q_indptr[r], e = shared ? a.q_indptr[a.groups.indptr[group + 1]] : a.q_indptr[r + 1];
+        if (e < s || e > a.p.max_rows) continue;
+        const int64_t j = i - (shared ? group : r) - s / TU;                             // the unit
+        if (j < 0 || j > e / TU - s / TU) continue;
+        const int common = a.groups.n ? shared_keys(a.groups, shared ? group : group_of(a.groups, r)) : 0;
+        const int n = (int)(e - s), ctx = a.ctx_len[r];
+        const int n_units = shared && common == 0 ? 0 : (n + TU - 1) / TU;
+        ChunkUnit& to = a.p.raw[(shared ? a.p.max_units / 2 : 0) + i];
+        if (shared) {
+            if (common == 0)                           // the rows have one side only
+                for (int64_t b = j * TU + lane; b < min((int64_t)n, (j + 1) * TU); b += 32) a.p.row_lo[a.p.max_rows + s + b] = a.p.row_hi[a.p.max_rows + s + b] = 0;
+            // the shared blocks are read through the table of the first member that has rows
+            int lo = r, hi = (int)a.groups.indptr[group + 1];
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (a.q_indptr[mid] <= s) lo = mid; else hi = mid;
+            }
+            r = lo;
+            if (a.kv_indptr[r] < 0 || a.kv_indptr[r] > a.kv_indptr[r + 1]) continue;
+        }
+        const int64_t row_at = shared ? a.p.max_rows : 0;
+        int prefix = 0;
+        if (a.masks.prefix_len) prefix = min(max(a.masks.prefix_len[r], 0), ctx + n);
         ChunkUnit u{};
         if (j < n_units) {
             const int i0 = (int)j * TU;
@@ -152,7 +175,7 @@ chunk_units_kernel(const PlanArgs a) {
             hi = __reduce_max_sync(0xffffffffu, hi);
             u.gaps = __any_sync(0xffffffffu, gaps);
             u.tbl = a.kv_indptr[r];
-            u.nblk = (int32_t)min(nblk, (int64_t)0x7fffffff);
+            u.nblk = (int32_t)min(a.kv_indptr[r + 1] - a.kv_indptr[r], (int64_t)0x7fffffff);
             u.row0 = (int32_t)(s + i0);
             u.req = r;
             u.pos0 = ctx + i0;
@@ -163,7 +186,7 @@ chunk_units_kernel(const PlanArgs a) {
             u.first = (int)j;                          // made absolute by the second kernel
             u.last = n_units - 1;
         }
-        if (lane == 0) a.p.raw[at + j] = u;
+        if (lane == 0) to = u;
     }
 }
 
@@ -182,7 +205,11 @@ chunk_split_kernel(const PlanArgs a) {
         groups.indptr = cost_s;
         __syncthreads();
     }
-    for (int r = tid; r < a.batch; r += kSplitThreads) ok = ok && request_ok(a, groups, r);
+    for (int r = tid; r < a.batch; r += kSplitThreads)
+        if (!request_ok(a, groups, r)) {
+            report(a.status, STATUS_BAD_TOKEN, r);
+            ok = false;
+        }
     if (tid == 0 && a.batch > 0 && a.q_indptr[0] != 0) {
         report(a.status, STATUS_BAD_TOKEN, 0);
         ok = false;
@@ -1206,11 +1233,9 @@ cudaError_t launch_chunk_plan(const ChunkPlan& p, const Shape& s, int32_t batch,
     const int T = p.kind.tokens(s.Hq / s.Hkv);
     const PlanArgs a{p, masks, batch, T, s.Hkv, s.bs, q_indptr, kv_indptr, ctx_len, groups, status};
     if (batch > 0) {
-        // a warp per unit: enough of them for the average request, at most 64 CTAs for the longest, and no more than some 16 per
-        // SM in all (512 requests of up to 5 rows in units of 10: 2 slices 4 us, the 52 that all rows in one request would need 32 us)
-        const int64_t units = p.max_rows / (p.kind.tiles * T) / 4 + 1, fair = 2048 / batch + 1;
-        const unsigned slices = (unsigned)(units < 64 ? (units < fair ? units : fair) : (fair < 64 ? fair : 64));
-        chunk_units_kernel<<<dim3((unsigned)(batch + groups.n), slices), 128, 0, stream>>>(a);
+        const int64_t room = p.max_rows / (p.kind.tiles * T), slots = batch + room + (groups.n > 0 ? groups.n + room : 0);
+        const int64_t ctas = (slots + kUnitWarps - 1) / kUnitWarps;
+        chunk_units_kernel<<<(unsigned)(ctas < kUnitCtas ? ctas : kUnitCtas), kUnitWarps * 32, 0, stream>>>(a);
         const cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
     }

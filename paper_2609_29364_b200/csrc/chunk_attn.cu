@@ -127,8 +127,6 @@ chunk_units_kernel(const PlanArgs a) {
         const int n_units = shared && common == 0 ? 0 : (n + TU - 1) / TU;
         ChunkUnit& to = a.p.raw[(shared ? a.p.max_units / 2 : 0) + i];
         if (shared) {
-            if (common == 0)                           // the rows have one side only
-                for (int64_t b = j * TU + lane; b < min((int64_t)n, (j + 1) * TU); b += 32) a.p.row_lo[a.p.max_rows + s + b] = a.p.row_hi[a.p.max_rows + s + b] = 0;
             // the shared blocks are read through the table of the first member that has rows
             int lo = r, hi = (int)a.groups.indptr[group + 1];
             while (hi - lo > 1) {
@@ -138,7 +136,6 @@ chunk_units_kernel(const PlanArgs a) {
             r = lo;
             if (a.kv_indptr[r] < 0 || a.kv_indptr[r] > a.kv_indptr[r + 1]) continue;
         }
-        const int64_t row_at = shared ? a.p.max_rows : 0;
         int prefix = 0;
         if (a.masks.prefix_len) prefix = min(max(a.masks.prefix_len[r], 0), ctx + n);
         ChunkUnit u{};
@@ -155,9 +152,8 @@ chunk_units_kernel(const PlanArgs a) {
                 if (i < i0 + u.ntok) {
                     if (a.masks.row_first) first = max(first, a.masks.row_first[s + i]);
                     any = first < stop;
-                    a.p.row_lo[row_at + s + i] = any ? first : 0;
-                    a.p.row_hi[row_at + s + i] = any ? stop : 0;
-                    if (a.p.row_pos && !shared) a.p.row_pos[s + i] = pos;
+                    if (a.p.row_lo) a.p.row_lo[s + i] = any ? first : 0, a.p.row_hi[s + i] = any ? stop : 0;
+                    else if (!shared) a.p.row_pos[s + i] = pos, a.p.row_shared[s + i] = common;
                     if (any) lo = min(lo, first), hi = max(hi, stop);
                 }
                 // Stops grow from row to row, so the keys of rows that follow one another without an empty one between leave no
@@ -1108,7 +1104,7 @@ chunk_merge_kernel(const __grid_constant__ ChunkPlan p, uint16_t* __restrict__ o
     const int64_t at = ((int64_t)blockIdx.x * kMergeThreads + threadIdx.x) / kLanes;
     const int d = threadIdx.x % kLanes * 4;
     pdl_wait();
-    if (!is_plan(p, T, Hkv) || at >= p.header->n_rows * Hq || p.row_hi[p.max_rows + at / Hq] == 0) return;
+    if (!is_plan(p, T, Hkv) || at >= p.header->n_rows * Hq || p.row_shared[at / Hq] == 0) return;
     const int64_t other = p.max_rows * Hq + at;
     const float2 ml0 = *reinterpret_cast<const float2*>(p.row_ml + at * 2), ml1 = *reinterpret_cast<const float2*>(p.row_ml + other * 2);
     const float4 a = *reinterpret_cast<const float4*>(p.row_acc + at * D + d), b = *reinterpret_cast<const float4*>(p.row_acc + other * D + d);
@@ -1204,10 +1200,12 @@ size_t chunk_plan_layout(ChunkPlan* p, void* base, const ChunkKind& kind, const 
     q.raw = static_cast<ChunkUnit*>(part(max_units * sizeof(ChunkUnit)));
     q.units = static_cast<ChunkUnit*>(part(max_units * sizeof(ChunkUnit)));
     q.cost = static_cast<int64_t*>(part((max_units + 1) * sizeof(int64_t)));
-    q.row_lo = static_cast<int32_t*>(part(kind.sides * max_rows * sizeof(int32_t)));
-    q.row_hi = static_cast<int32_t*>(part(kind.sides * max_rows * sizeof(int32_t)));
-    if (kind.sides == 2) {
+    if (kind.sides == 1) {
+        q.row_lo = static_cast<int32_t*>(part(max_rows * sizeof(int32_t)));
+        q.row_hi = static_cast<int32_t*>(part(max_rows * sizeof(int32_t)));
+    } else {
         q.row_pos = static_cast<int32_t*>(part(max_rows * sizeof(int32_t)));
+        q.row_shared = static_cast<int32_t*>(part(max_rows * sizeof(int32_t)));
         q.row_ml = static_cast<float*>(part(2 * max_rows * s.Hq * 2 * sizeof(float)));
         q.row_acc = static_cast<float*>(part(2 * max_rows * s.Hq * s.D * sizeof(float)));
     }

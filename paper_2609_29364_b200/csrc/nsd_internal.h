@@ -207,8 +207,8 @@ struct ChunkPlan {                           // the buffer's parts
     ChunkStart* starts;                      // [n_ctas + 1]
     ChunkUnit *raw, *units;                  // [max_units]
     int64_t* cost;                           // [max_units + 1] prefix sums over the units, one kv head
-    int32_t *row_lo, *row_hi;                // [sides][max_rows] visible keys of each row
-    int32_t* row_pos;                        // two sides: [max_rows] positions
+    int32_t *row_lo, *row_hi;                // one side: [max_rows] visible keys of each row
+    int32_t *row_pos, *row_shared;           // two sides: [max_rows] positions, shared keys (0: the row has one side only)
     float *row_ml, *row_acc;                 // two sides: [2][max_rows][Hq][2] and [D], what a side found for a row that has both
     float* part_ml;                          // [2 n_ctas][rows of a unit][2]
     float* part_acc;                         // [2 n_ctas][rows of a unit][D]

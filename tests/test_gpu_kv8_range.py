@@ -168,3 +168,22 @@ def test_equal_scores_beyond_2_24_weigh_the_same(dim, tokens):
         key(r, 300 + r, 256.0, 128.0 + 16 * (r % 16))  # more by 128 to 368
         key(r, 500 + r, 256.0, 128.0 + 16 * (r % 16))  # the same again, in a later tile
     b.run_close(scale=1.0)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_queries_of_zeros_beside_ones_whose_scores_overflow(dim):
+    """One head's scores are beyond 32 bits; the other's are all 0, and its rows the mean of V."""
+    b = Range8([200, 30], [3, 1], dim=dim, heads=2, kv_heads=1, seed=7)
+    q = b.q.view(1, b.rows, 2, dim)
+    q[0, :, 0], q[0, :, 1] = 0.0, 2.0 ** 126
+    held = b.scales[0, :, :, 0] != 255
+    b.scales[0, :, :, 0] = torch.where(held, b.scales[0, :, :, 0] + 100, 255).to(torch.uint8)
+    b.values[0, :, 0] *= 2.0 ** 100
+    c = b.context()
+    b.attn(c, b.plan(c))
+    assert c.nsd_get_status() == (0, -1)
+    o_ref = torch.stack([b.values[0, b.places(r)[0], 1, 0, b.places(r)[1]][: b.ctx[r] + i + 1].mean(0) for r in range(2) for i in range(b.new[r])])
+    mag = torch.stack([b.values[0, b.places(r)[0], 1, 0, b.places(r)[1]][: b.ctx[r] + i + 1].abs().mean(0) for r in range(2) for i in range(b.new[r])])
+    keys = torch.tensor([float(b.ctx[r] + i + 1) for r in range(2) for i in range(b.new[r])], dtype=torch.float64, device=DEV)
+    assert ((b.o[0, :, 0].double() - o_ref).abs() <= 2.0 ** -8 * o_ref.abs() + 2.0 ** -9 * mag).all()
+    assert ((b.lse[0, :, 0].double() - keys.log()).abs() <= 2.0 ** -10).all()

@@ -20,8 +20,10 @@ constexpr float kLn2 = 0.6931471805599453f;
 // Where groups' shared keys are more than half of the work, the tiles of the requests' own keys take longer (their few CTAs wait
 // for memory that the others keep busy): 256 requests of 3 to 5 rows behind 32 777 keys, over up to 2000 of their own, 703 us
 // with 4, 7 and three tiles against 835; behind 4000 keys 304 against 292, 64 single tokens behind 4000 57 against 53.
+// These costs come from the two batches on either side; near the switch, and with D = 64, other heads or several groups, only the
+// balance depends on them, and it was not measured.
 // The 8-bit attention has its rows on the columns, so a tile costs by their number (512 requests over 2048 keys: 3 and 4 rows of
-// four heads 361 and 368 us, 5 rows 411, 9 rows 548): 512 requests of 3 to 5 rows over 128 to 4096 keys 415 us with tiles weighed
+// four heads 363 and 369 us, 5 rows 412, 9 rows 527): 512 requests of 3 to 5 rows over 128 to 4096 keys 415 us with tiles weighed
 // so, 437 with all alike; 1 to 9 rows over 64 to 1024 keys 308 against 327.  A unit as 4 tiles: 427 and 421 with 2 and 3, 419 to
 // 429 with 5 to 8.
 struct ChunkCost {
@@ -44,8 +46,8 @@ __device__ __forceinline__ int64_t unit_cost(const ChunkCost& c, const ChunkUnit
 // an index that needs no prefix sum and leaves at most one gap per request; a warp finds the request of
 // its slot by two or three rounds of 32 probes.  The second, one CTA,
 // closes the gaps, sums the costs and cuts the whole work -- units x kv heads x key tiles in one
-// line -- into n_ctas equal pieces.  Two launches and two chains of dependent loads bound it: 7 to
-// 9 us for a prompt of 8192, for 64 single tokens and for 128 mixed requests alike, once per step.
+// line -- into n_ctas equal pieces.  Two launches and two chains of dependent loads bound it: 9 to
+// 11 us for a prompt of 8192, for 64 single tokens and for 512 requests of 5 rows alike, once per step.
 struct PlanArgs {
     ChunkPlan p;
     nsd_chunk_masks masks;

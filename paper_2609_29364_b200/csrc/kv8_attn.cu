@@ -43,17 +43,19 @@ namespace {
 //   11    Q of the next piece, and what the other warps have to know of it
 // Pieces that a CTA boundary cuts leave their O and statistics in the plan, and chunk_join_kernel joins them in order.
 //
-// What bounds it: single tokens HBM (512 over 2048 keys each, 32 q heads and 8 kv heads of 128: 341 us = 6.3 TB/s, 0.98 of
-// the copy rate; the 16-bit kernel reads twice the bytes); five rows per request the chain of a tile's softmax (410 us = 5.3
-// TB/s; 3 to 5 rows over 128 to 4096 keys 416); ten rows (40 stacked) 124 us for 4 x 60 000 keys = 4.0 TB/s; 64 single tokens
-// over 512 to 2048 keys 40 us, of which some 15 are the start, the last pieces and the join; 512 x 256 keys 96 us, with five rows
-// 148: a piece of two or three tiles costs as much again in its beginning and end (its queries, the first references, rows out).  D = 64 halves the bytes but not the softmax: 512 x 5 rows
-// over 2048 keys 366 us.  The instructions of a tile matter more than their number of cycles alone: with a longer loop
-// (waits with time limits, eight rows of Q at a time, a fourth term) the SM's instruction cache no longer held it and times rose
-// by a fifth.
+// What bounds it: single tokens HBM (512 over 2048 keys each, 32 q heads and 8 kv heads of 128: 343 us = 6.3 TB/s, 0.98 of
+// the copy rate; the 16-bit kernel reads twice the bytes); five rows per request the chain of a tile's softmax (412 us = 5.3
+// TB/s; 3 to 5 rows over 128 to 4096 keys 413); ten rows (40 stacked) 124 us for 4 x 60 000 keys = 4.0 TB/s; 64 single tokens
+// over 512 to 2048 keys 41 us, of which some 15 are the start, the last pieces and the join; 512 x 256 keys 102 us, with five rows
+// 150: a piece of two or three tiles costs as much again in its beginning and end (its queries, the first references, rows out).
+// D = 64 halves the bytes but not the softmax: 512 over 2048 keys 266 us, with five rows 373.  With up to four stacked rows (a token of
+// four heads) half of the softmax warps have rows of padding only, which go through every step.  The instructions of a tile matter
+// more than their number of cycles alone: with a longer loop (waits with time limits, eight rows of Q at a time, a fourth term) the
+// SM's instruction cache no longer held it and times rose by a fifth.
 //
 // Tried: one CTA per SM with two streams over alternate tiles (1126 us; 668 with two CTAs); four warps for Q (516 instead of
-// 499); S of a tile after P V of the one before (513 instead of 449).
+// 499); S of a tile after P V of the one before (513 instead of 449); the wide form between the other tiles' instructions (357 and 439
+// us for 1 and 5 rows over 2048 keys instead of 343 and 413); the look at the references as a function too (353 and 418).
 //
 // Every wait is bounded.  When one runs out, the CTA raises its abort flag; once all warps have left their loops, the issuer
 // waits for its MMAs in flight and each producer for its copies (bounded again), and the call ends with STATUS_TIMEOUT.
